@@ -329,6 +329,68 @@ litevggt_status litevggt_timer_samples(litevggt_ctx* ctx, int which, float* ms, 
 /* Number of kernels this library has launched on behalf of ctx since creation. */
 litevggt_status litevggt_launch_count(const litevggt_ctx* ctx, int64_t* launches);
 
+/* ------------------------------------------------------------------ paged K/V cache
+ * For frames that keep arriving: the keys and values of their (merged) tokens stay in pages of a pool, and the tokens of
+ * every new chunk attend to all that their sequence holds.  (The paper has no counterpart: its sequences are complete
+ * before their first layer.)  Independent of litevggt_ctx; any K/V head count, head dimension 64 or 128.
+ *
+ * A batch is what the calls of one step have in common: for each sequence how many rows of the packed tensors belong to
+ * it, how many tokens it holds, in which pages.  A sequence's rows are its last tokens: the call that appends a chunk
+ * and those that attend from it take the same batch, whose lengths already count the chunk; a reader that wants a whole
+ * sequence names as many rows as it has tokens.  Batches are made on the host and serve every layer of a step. */
+enum {
+  LITEVGGT_KV_BF16 = 0,
+  LITEVGGT_KV_E4M3 = 1 /* a row of a head as E4M3 codes x and an exponent byte e + 127, standing for x 2^e: the least
+                          e >= -118 with max|row| <= 448 * 2^e; a row that is not finite is held as byte 255 and reads as NaN */
+};
+typedef struct {
+  int32_t pages;     /* in the pool */
+  int32_t page_size; /* tokens of a page: 16, 32, 64 or 128 */
+  int32_t kv_heads;
+  int32_t head_dim;  /* 64 or 128 */
+  int32_t dtype;     /* LITEVGGT_KV_BF16, LITEVGGT_KV_E4M3 */
+} litevggt_kv_config;  /* pages * kv_heads * page_size < 2^31 */
+typedef struct litevggt_kv_cache litevggt_kv_cache;
+typedef struct litevggt_kv_batch litevggt_kv_batch;
+
+/* A cache over the caller's pool.  k, v: dev [pages, kv_heads, page_size, head_dim], bf16 or codes; k_exp, v_exp: dev bytes
+ * [pages, kv_heads, page_size], E4M3 only; status: dev, one 32-bit word that holds zero.  All of it outlives the cache,
+ * pages need not be initialised. */
+litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, void* k, void* v, uint8_t* k_exp, uint8_t* v_exp,
+                                   uint32_t* status, litevggt_kv_cache** out);
+litevggt_status litevggt_kv_destroy(litevggt_kv_cache* cache);
+
+/* Plans a batch of n_seq sequences (host only, no GPU work).  rows, lengths: host [n_seq], not negative; pages: host, the
+ * ceil(length / page_size) pages of every sequence one after the other, each below cfg.pages (sequences may share pages
+ * that they only read).  q_heads: a multiple of kv_heads; query head h reads K/V head h / (q_heads / kv_heads).
+ * causal_block = c > 0: row i of a sequence sees the tokens before its rows, and of its rows those of the blocks of c up
+ * to i's own, so c = 1 is causal by tokens, c = tokens of a frame causal by frames; 0: all rows see all tokens.
+ * *bytes receives the device memory that the batch needs. */
+litevggt_status litevggt_kv_batch_create(const litevggt_kv_cache* cache, int32_t n_seq, const int32_t* rows, const int32_t* lengths,
+                                         const int32_t* pages, int32_t q_heads, int32_t causal_block, litevggt_kv_batch** out,
+                                         size_t* bytes);
+/* Gives the batch its memory (dev, 256-byte aligned; the caller's, in use until the last call with this batch has run) and
+ * copies its arrays there on `stream`.  Calls with one batch follow one another in stream order: they share its workspace. */
+litevggt_status litevggt_kv_batch_place(litevggt_kv_batch* batch, void* memory, size_t bytes, void* stream);
+litevggt_status litevggt_kv_batch_destroy(litevggt_kv_batch* batch);
+
+/* Writes K and V of the batch's rows into their sequences' pages.  k, v: dev bf16 [rows, kv_heads, head_dim], 16-byte
+ * aligned, head_dim contiguous, the other strides in elements (multiples of 8, not negative).
+ * LITEVGGT_ERR_SHAPE if a sequence has more rows than tokens. */
+litevggt_status litevggt_kv_append(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* k, int64_t k_row_stride,
+                                   int64_t k_head_stride, const void* v, int64_t v_row_stride, int64_t v_head_stride, void* stream);
+/* The reverse: K and V of the batch's rows as bf16 [rows, kv_heads, head_dim], contiguous (what codes stand for is exact in bf16). */
+litevggt_status litevggt_kv_gather(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, void* k, void* v, void* stream);
+/* out[i] = sum_j softmax_j(scale q[i] . k[j]) v[j] over the tokens j that row i sees; zero for a row that sees none (a
+ * sequence without tokens, or causal rows ahead of its first token).  A token that a row does not see has no influence
+ * on it, whatever it holds.  q: dev bf16 [rows, q_heads, head_dim] with strides as above; out: dev bf16, contiguous;
+ * scale: positive, finite. */
+litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
+                                   int64_t q_head_stride, float scale, void* out, void* stream);
+/* As litevggt_poll_device_status, and the number of kernels launched on behalf of the cache. */
+litevggt_status litevggt_kv_poll(litevggt_kv_cache* cache, void* stream);
+litevggt_status litevggt_kv_launch_count(const litevggt_kv_cache* cache, int64_t* launches);
+
 const char* litevggt_status_string(litevggt_status s);
 
 #ifdef __cplusplus

@@ -18,3 +18,4 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
+from .kv_cache import KVBatch, KVCache  # noqa: E402,F401

@@ -45,6 +45,12 @@ class AttnExt(C.Structure):
                 ("k_norm_beta", C.c_void_p), ("norm_eps", C.c_float), ("rope", C.c_int32), ("rope_base", C.c_float)]
 
 
+class KVConfig(C.Structure):
+    """Mirror of litevggt_kv_config."""
+    _fields_ = [("pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
 def load_library():
     """Load liblitevggt.so (once).  Raises if it has not been built: there is no fallback."""
     global _LIB
@@ -87,6 +93,16 @@ def load_library():
         "litevggt_poll_device_status": [vp, vp],
         "litevggt_selftest_bounded_wait": [vp, i64, P(C.c_uint32), vp],
         "litevggt_launch_count": [vp, P(i64)],
+        "litevggt_kv_create": [P(KVConfig), C.c_int, vp, vp, vp, vp, vp, P(vp)],
+        "litevggt_kv_destroy": [vp],
+        "litevggt_kv_batch_create": [vp, i32, vp, vp, vp, i32, i32, P(vp), P(C.c_size_t)],
+        "litevggt_kv_batch_place": [vp, vp, C.c_size_t, vp],
+        "litevggt_kv_batch_destroy": [vp],
+        "litevggt_kv_append": [vp, vp, vp, i64, i64, vp, i64, i64, vp],
+        "litevggt_kv_gather": [vp, vp, vp, vp, vp],
+        "litevggt_kv_attend": [vp, vp, vp, i64, i64, C.c_float, vp, vp],
+        "litevggt_kv_poll": [vp, vp],
+        "litevggt_kv_launch_count": [vp, P(i64)],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)

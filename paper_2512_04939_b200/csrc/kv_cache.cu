@@ -1,0 +1,415 @@
+// The paged K/V cache: its entry points, and the kernels that write it and read it back.
+//
+// Writing and reading move every byte once and compute next to nothing, so HBM bounds both.  A unit of work is one
+// row of one K/V head, K and V alike: 16 bytes of bf16 a lane, the 8 (or 16) lanes of a row side by side in the warp, so
+// that a row's largest magnitude takes three (four) shuffles and its codes leave as 64 (128) bytes in a row.
+#include <string.h>
+
+#include <new>
+
+#include "kv_cache.h"
+#include "kv_quant.cuh"
+
+namespace lv {
+
+namespace {
+
+constexpr int kMoveThreads = 256;
+
+// The sequence that a row of the packed tensors belongs to.
+__device__ __forceinline__ KvSeq seq_of_row(const KvArrays& a, int row) {
+  int lo = 0, hi = a.n_seq - 1;
+  while (lo < hi) {  // the last one that begins at or before the row; ones without rows share their successor's start
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.seqs[mid].row0 <= row) lo = mid;
+    else hi = mid - 1;
+  }
+  return a.seqs[lo];
+}
+// Index of a row's token and head among the pool's rows.
+__device__ __forceinline__ long long pool_row(const KvPool& pool, const KvArrays& a, int row, int head) {
+  const KvSeq q = seq_of_row(a, row);
+  const int token = q.len - q.rows + (row - q.row0);
+  const long long page = a.pages[q.page0 + (token >> pool.page_shift)];
+  return (page * pool.kv_heads + head) * pool.page_size + (token & (pool.page_size - 1));
+}
+
+// Largest magnitude of a row, as the bits of a bf16.
+template <int kLanes>
+__device__ __forceinline__ uint32_t row_top(const uint4& x) {
+  uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+#pragma unroll
+  for (int d = 1; d < kLanes; d *= 2) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, d));
+  return max(m & 0xffffu, m >> 16);
+}
+__device__ __forceinline__ uint2 row_codes(const uint4& x, uint32_t byte) {
+  if (byte == kKvNanByte) return make_uint2(0u, 0u);
+  const float f = kv_inverse_scale(byte);
+  return make_uint2(pack_e4m3x4(bf16_lo(x.x) * f, bf16_hi(x.x) * f, bf16_lo(x.y) * f, bf16_hi(x.y) * f),
+                    pack_e4m3x4(bf16_lo(x.z) * f, bf16_hi(x.z) * f, bf16_lo(x.w) * f, bf16_hi(x.w) * f));
+}
+// Eight codes to eight bf16.
+__device__ __forceinline__ uint4 row_values(const uint2& codes, uint32_t byte) {
+  const KvFactor f = kv_factor(byte);
+  const uint32_t w[2] = {codes.x, codes.y};
+  uint32_t r[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    r[2 * i] = mul_bf16x2(kv_code_bits(__byte_perm(w[i], 0u, 0x1404)), f.first * 0x10001u);
+    r[2 * i + 1] = mul_bf16x2(kv_code_bits(__byte_perm(w[i], 0u, 0x3424)), f.first * 0x10001u);
+  }
+  if (kv_needs_second(byte)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = mul_bf16x2(r[i], f.second * 0x10001u);
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+template <int kHd, bool kNarrow>
+__global__ void __launch_bounds__(kMoveThreads)
+kv_append_kernel(KvPool pool, KvArrays arrays, const __nv_bfloat16* __restrict__ k, KvStride ks, const __nv_bfloat16* __restrict__ v,
+                 KvStride vs, long long units) {
+  constexpr int kLanes = kHd / 8;
+  wait_for_previous_kernel();
+  const int part = threadIdx.x % kLanes;
+  const long long unit = (long long)blockIdx.x * (kMoveThreads / kLanes) + threadIdx.x / kLanes;
+  const bool live = unit < units;
+  const int row = live ? (int)(unit / pool.kv_heads) : 0, head = live ? (int)(unit % pool.kv_heads) : 0;
+  uint4 xk = make_uint4(0u, 0u, 0u, 0u), xv = xk;
+  if (live) {
+    xk = ldg16(k + row * ks.row + head * ks.head + part * 8);
+    xv = ldg16(v + row * vs.row + head * vs.head + part * 8);
+  }
+  const long long at = live ? pool_row(pool, arrays, row, head) : 0;
+  if constexpr (kNarrow) {
+    const uint32_t bk = kv_exponent_byte(row_top<kLanes>(xk)), bv = kv_exponent_byte(row_top<kLanes>(xv));
+    if (live) {
+      *reinterpret_cast<uint2*>(pool.k + at * kHd + part * 8) = row_codes(xk, bk);
+      *reinterpret_cast<uint2*>(pool.v + at * kHd + part * 8) = row_codes(xv, bv);
+      if (part == 0) pool.k_exp[at] = (uint8_t)bk;
+      if (part == 1) pool.v_exp[at] = (uint8_t)bv;
+    }
+  } else if (live) {
+    stg16(pool.k + (at * kHd + part * 8) * 2, xk);
+    stg16(pool.v + (at * kHd + part * 8) * 2, xv);
+  }
+}
+
+template <int kHd, bool kNarrow>
+__global__ void __launch_bounds__(kMoveThreads)
+kv_gather_kernel(KvPool pool, KvArrays arrays, __nv_bfloat16* __restrict__ k, __nv_bfloat16* __restrict__ v, long long units) {
+  constexpr int kLanes = kHd / 8;
+  wait_for_previous_kernel();
+  const int part = threadIdx.x % kLanes;
+  const long long unit = (long long)blockIdx.x * (kMoveThreads / kLanes) + threadIdx.x / kLanes;
+  if (unit >= units) return;
+  const long long at = pool_row(pool, arrays, (int)(unit / pool.kv_heads), (int)(unit % pool.kv_heads));
+  uint4 xk, xv;
+  if constexpr (kNarrow) {
+    const uint2 ck = *reinterpret_cast<const uint2*>(pool.k + at * kHd + part * 8);
+    const uint2 cv = *reinterpret_cast<const uint2*>(pool.v + at * kHd + part * 8);
+    const uint32_t bk = pool.k_exp[at], bv = pool.v_exp[at];
+    xk = row_values(ck, bk);
+    xv = row_values(cv, bv);
+  } else {
+    xk = ldg16(pool.k + (at * kHd + part * 8) * 2);
+    xv = ldg16(pool.v + (at * kHd + part * 8) * 2);
+  }
+  stg16(k + unit * kHd + part * 8, xk);
+  stg16(v + unit * kHd + part * 8, xv);
+}
+
+// Calls f with the head dimension and the pool's type as constants.
+template <class F>
+void by_kind(const litevggt_kv_cache& c, const F& f) {
+  using std::integral_constant;
+  const bool narrow = c.cfg.dtype == LITEVGGT_KV_E4M3;
+  if (c.cfg.head_dim == 64) {
+    if (narrow) f(integral_constant<int, 64>{}, integral_constant<bool, true>{});
+    else f(integral_constant<int, 64>{}, integral_constant<bool, false>{});
+  } else {
+    if (narrow) f(integral_constant<int, 128>{}, integral_constant<bool, true>{});
+    else f(integral_constant<int, 128>{}, integral_constant<bool, false>{});
+  }
+}
+
+unsigned move_blocks(const litevggt_kv_cache& c, long long units) {
+  const long long per_block = kMoveThreads / (c.cfg.head_dim / 8);
+  return (unsigned)((units + per_block - 1) / per_block);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_append(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const __nv_bfloat16* k, KvStride k_stride,
+                             const __nv_bfloat16* v, KvStride v_stride, cudaStream_t s, int* launches) {
+  const long long units = b.rows * c.cfg.kv_heads;
+  cudaError_t e = cudaSuccess;
+  by_kind(c, [&](auto hd, auto narrow) {
+    e = launch(kv_append_kernel<decltype(hd)::value, decltype(narrow)::value>, dim3(move_blocks(c, units)), kMoveThreads, 0, s, c.pool,
+               kv_arrays(b), k, k_stride, v, v_stride, units);
+  });
+  ++*launches;
+  return e;
+}
+
+cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch& b, __nv_bfloat16* k, __nv_bfloat16* v, cudaStream_t s,
+                             int* launches) {
+  const long long units = b.rows * c.cfg.kv_heads;
+  cudaError_t e = cudaSuccess;
+  by_kind(c, [&](auto hd, auto narrow) {
+    e = launch(kv_gather_kernel<decltype(hd)::value, decltype(narrow)::value>, dim3(move_blocks(c, units)), kMoveThreads, 0, s, c.pool,
+               kv_arrays(b), k, v, units);
+  });
+  ++*launches;
+  return e;
+}
+
+namespace {
+
+bool cache_ok(const litevggt_kv_cache* c) { return c != nullptr && c->magic == kKvCacheMagic; }
+bool batch_ok(const litevggt_kv_batch* b) { return b != nullptr && b->magic == kKvBatchMagic; }
+
+// A batch of this cache whose arrays are on the device.
+litevggt_status usable(const litevggt_kv_cache* c, const litevggt_kv_batch* b) {
+  if (!cache_ok(c) || b == nullptr) return LITEVGGT_ERR_NULL;
+  if (!batch_ok(b) || b->owner != c || b->base == nullptr) return LITEVGGT_ERR_STALE_PLAN;
+  return LITEVGGT_OK;
+}
+
+// Rows of heads that may be read 16 bytes at a time.
+litevggt_status stride_ok(int64_t row, int64_t head) {
+  if (row < 0 || head < 0 || row > UINT32_MAX || head > UINT32_MAX) return LITEVGGT_ERR_SHAPE;
+  return row % 8 != 0 || head % 8 != 0 ? LITEVGGT_ERR_ALIGN : LITEVGGT_OK;
+}
+
+// Lays out a batch's device memory: first what the host writes (`image`), then what only kernels use.
+void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int head_dim) {
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (size_t)round_up((long long)(bytes > 0 ? bytes : 1), 256);
+    return here;
+  };
+  const KvWork& few = b->few;
+  b->o_seqs = take(b->seqs.size() * sizeof(KvSeq));
+  b->o_pages = take(n_pages * sizeof(int));
+  b->o_few_pieces = take(few.pieces.size() * sizeof(KvPiece));
+  b->o_few_first = take(few.first.size() * sizeof(int));
+  b->o_joins = take((size_t)few.joins * sizeof(int));
+  b->image.assign(at, 0);  // the counters start at zero
+  b->o_few_rows = take((size_t)few.slots * kKvFewRows * head_dim * sizeof(float));
+  b->o_few_sums = take((size_t)few.slots * kKvFewRows * 2 * sizeof(float));
+  b->bytes = at;
+  auto put = [&](size_t to, const void* from, size_t bytes) {
+    if (bytes > 0) memcpy(b->image.data() + to, from, bytes);
+  };
+  put(b->o_seqs, b->seqs.data(), b->seqs.size() * sizeof(KvSeq));
+  put(b->o_pages, pages, n_pages * sizeof(int));
+  put(b->o_few_pieces, few.pieces.data(), few.pieces.size() * sizeof(KvPiece));
+  put(b->o_few_first, few.first.data(), few.first.size() * sizeof(int));
+}
+
+litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int32_t* rows, const int32_t* lengths, const int32_t* pages,
+                           int32_t q_heads, int32_t causal_block, litevggt_kv_batch* b) {
+  long long row0 = 0, page0 = 0;
+  b->rows_held = true;
+  for (int i = 0; i < n_seq; ++i) {
+    if (rows[i] < 0 || lengths[i] < 0) return LITEVGGT_ERR_SHAPE;
+    if (rows[i] > lengths[i]) b->rows_held = false;
+    b->seqs.push_back(KvSeq{(int)row0, rows[i], lengths[i], (int)page0});
+    row0 += rows[i];
+    page0 += ((long long)lengths[i] + c->cfg.page_size - 1) / c->cfg.page_size;
+    if (row0 * q_heads > INT32_MAX || page0 > INT32_MAX) return LITEVGGT_ERR_SHAPE;
+  }
+  if (page0 > 0 && pages == nullptr) return LITEVGGT_ERR_NULL;
+  for (long long i = 0; i < page0; ++i)
+    if (pages[i] < 0 || pages[i] >= c->cfg.pages) return LITEVGGT_ERR_SHAPE;
+  b->magic = kKvBatchMagic;
+  b->owner = c;
+  b->q_heads = q_heads;
+  b->group = q_heads / c->cfg.kv_heads;
+  b->causal_block = causal_block;
+  b->rows = row0;
+  std::vector<int> few;
+  int most = 0;
+  for (int i = 0; i < n_seq; ++i)
+    if (rows[i] > 0) {
+      few.push_back(i);
+      most = std::max(most, rows[i] * b->group);
+    }
+  const int per_sm = c->cfg.head_dim == 128 && most > 8 ? 1 : 2;  // CTAs, by their registers
+  b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
+                  KvCut{kKvFewRows, kKvFewUnit, c->num_sms * per_sm, 1, INT32_MAX, 1.0});
+  lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
+  return LITEVGGT_OK;
+}
+
+}  // namespace
+}  // namespace lv
+
+using namespace lv;
+
+extern "C" {
+
+litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, void* k, void* v, uint8_t* k_exp, uint8_t* v_exp,
+                                   uint32_t* status, litevggt_kv_cache** out) {
+  if (cfg == nullptr || out == nullptr) return LITEVGGT_ERR_NULL;
+  *out = nullptr;
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) return LITEVGGT_ERR_BAD_CONFIG;
+  if (cfg->page_size != 16 && cfg->page_size != 32 && cfg->page_size != 64 && cfg->page_size != 128) return LITEVGGT_ERR_BAD_CONFIG;
+  if (cfg->dtype != LITEVGGT_KV_BF16 && cfg->dtype != LITEVGGT_KV_E4M3) return LITEVGGT_ERR_BAD_CONFIG;
+  if (cfg->kv_heads < 1 || cfg->pages < 1) return LITEVGGT_ERR_BAD_CONFIG;
+  // a row of a head is addressed by one 32-bit coordinate
+  if ((long long)cfg->pages * cfg->kv_heads > INT32_MAX / cfg->page_size) return LITEVGGT_ERR_BAD_CONFIG;
+  if (k == nullptr || v == nullptr || status == nullptr) return LITEVGGT_ERR_NULL;
+  const bool narrow = cfg->dtype == LITEVGGT_KV_E4M3;
+  if (narrow && (k_exp == nullptr || v_exp == nullptr)) return LITEVGGT_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v) || (narrow && (!aligned16(k_exp) || !aligned16(v_exp)))) return LITEVGGT_ERR_ALIGN;
+  int count = 0, major = 0, sms = 0;
+  if (cudaGetDeviceCount(&count) != cudaSuccess || device < 0 || device >= count) {
+    (void)cudaGetLastError();
+    return LITEVGGT_ERR_CUDA;
+  }
+  cudaError_t e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  if (e != cudaSuccess) return cuda_status(e);
+  if (major != 10) return LITEVGGT_ERR_ARCH;
+  litevggt_kv_cache* c = new (std::nothrow) litevggt_kv_cache();
+  if (c == nullptr) return LITEVGGT_ERR_ALLOC;
+  c->magic = kKvCacheMagic;
+  c->cfg = *cfg;
+  c->device = device;
+  c->num_sms = sms;
+  int shift = 4;
+  while ((1 << shift) < cfg->page_size) ++shift;
+  c->pool = KvPool{static_cast<uint8_t*>(k), static_cast<uint8_t*>(v), narrow ? k_exp : nullptr, narrow ? v_exp : nullptr,
+                   cfg->kv_heads, cfg->page_size, shift};
+  c->status = status;
+  c->launches = 0;
+  *out = c;
+  return LITEVGGT_OK;
+}
+
+litevggt_status litevggt_kv_destroy(litevggt_kv_cache* cache) {
+  if (cache == nullptr) return LITEVGGT_OK;
+  if (!cache_ok(cache)) return LITEVGGT_ERR_NULL;
+  cache->magic = 0;
+  delete cache;
+  return LITEVGGT_OK;
+}
+
+litevggt_status litevggt_kv_batch_create(const litevggt_kv_cache* cache, int32_t n_seq, const int32_t* rows, const int32_t* lengths,
+                                         const int32_t* pages, int32_t q_heads, int32_t causal_block, litevggt_kv_batch** out,
+                                         size_t* bytes) {
+  if (!cache_ok(cache) || rows == nullptr || lengths == nullptr || out == nullptr || bytes == nullptr) return LITEVGGT_ERR_NULL;
+  *out = nullptr;
+  if (n_seq < 1 || q_heads < 1 || q_heads % cache->cfg.kv_heads != 0 || causal_block < 0) return LITEVGGT_ERR_SHAPE;
+  litevggt_kv_batch* b = new (std::nothrow) litevggt_kv_batch();
+  if (b == nullptr) return LITEVGGT_ERR_ALLOC;
+  litevggt_status st = LITEVGGT_ERR_ALLOC;
+  try {
+    st = plan_batch(cache, n_seq, rows, lengths, pages, q_heads, causal_block, b);
+  } catch (...) {  // no memory on the host
+  }
+  if (st != LITEVGGT_OK) {
+    delete b;
+    return st;
+  }
+  *bytes = b->bytes;
+  *out = b;
+  return LITEVGGT_OK;
+}
+
+litevggt_status litevggt_kv_batch_place(litevggt_kv_batch* batch, void* memory, size_t bytes, void* stream) {
+  if (!batch_ok(batch) || memory == nullptr) return LITEVGGT_ERR_NULL;
+  if (bytes < batch->bytes) return LITEVGGT_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(memory) & 255u) != 0) return LITEVGGT_ERR_ALIGN;
+  // (from pageable memory: the call has taken the bytes when it returns)
+  const cudaError_t e = cudaMemcpyAsync(memory, batch->image.data(), batch->image.size(), cudaMemcpyHostToDevice, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_status(e);
+  batch->base = static_cast<uint8_t*>(memory);
+  return LITEVGGT_OK;
+}
+
+litevggt_status litevggt_kv_batch_destroy(litevggt_kv_batch* batch) {
+  if (batch == nullptr) return LITEVGGT_OK;
+  if (!batch_ok(batch)) return LITEVGGT_ERR_STALE_PLAN;
+  batch->magic = 0;
+  delete batch;
+  return LITEVGGT_OK;
+}
+
+litevggt_status litevggt_kv_append(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* k, int64_t k_row_stride,
+                                   int64_t k_head_stride, const void* v, int64_t v_row_stride, int64_t v_head_stride, void* stream) {
+  litevggt_status st = usable(cache, batch);
+  if (st != LITEVGGT_OK) return st;
+  if (!batch->rows_held) return LITEVGGT_ERR_SHAPE;
+  if (batch->rows == 0) return LITEVGGT_OK;
+  if (k == nullptr || v == nullptr) return LITEVGGT_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v)) return LITEVGGT_ERR_ALIGN;
+  if ((st = stride_ok(k_row_stride, k_head_stride)) != LITEVGGT_OK) return st;
+  if ((st = stride_ok(v_row_stride, v_head_stride)) != LITEVGGT_OK) return st;
+  DeviceGuard g(cache->device);
+  if (!g.ok) return LITEVGGT_ERR_CUDA;
+  int n = 0;
+  const cudaError_t e = launch_kv_append(*cache, *batch, static_cast<const __nv_bfloat16*>(k), KvStride{k_row_stride, k_head_stride},
+                                         static_cast<const __nv_bfloat16*>(v), KvStride{v_row_stride, v_head_stride},
+                                         (cudaStream_t)stream, &n);
+  cache->launches += n;
+  return cuda_status(e);
+}
+
+litevggt_status litevggt_kv_gather(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, void* k, void* v, void* stream) {
+  const litevggt_status st = usable(cache, batch);
+  if (st != LITEVGGT_OK) return st;
+  if (!batch->rows_held) return LITEVGGT_ERR_SHAPE;
+  if (batch->rows == 0) return LITEVGGT_OK;
+  if (k == nullptr || v == nullptr) return LITEVGGT_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v)) return LITEVGGT_ERR_ALIGN;
+  DeviceGuard g(cache->device);
+  if (!g.ok) return LITEVGGT_ERR_CUDA;
+  int n = 0;
+  const cudaError_t e =
+      launch_kv_gather(*cache, *batch, static_cast<__nv_bfloat16*>(k), static_cast<__nv_bfloat16*>(v), (cudaStream_t)stream, &n);
+  cache->launches += n;
+  return cuda_status(e);
+}
+
+litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
+                                   int64_t q_head_stride, float scale, void* out, void* stream) {
+  litevggt_status st = usable(cache, batch);
+  if (st != LITEVGGT_OK) return st;
+  if (!(scale > 0.0f) || !(scale < 1e30f)) return LITEVGGT_ERR_SHAPE;
+  if (batch->rows == 0) return LITEVGGT_OK;
+  if (q == nullptr || out == nullptr) return LITEVGGT_ERR_NULL;
+  if (!aligned16(q) || !aligned16(out)) return LITEVGGT_ERR_ALIGN;
+  if ((st = stride_ok(q_row_stride, q_head_stride)) != LITEVGGT_OK) return st;
+  DeviceGuard g(cache->device);
+  if (!g.ok) return LITEVGGT_ERR_CUDA;
+  const KvAttend a{static_cast<const __nv_bfloat16*>(q), KvStride{q_row_stride, q_head_stride}, static_cast<__nv_bfloat16*>(out),
+                   batch->q_heads, batch->group, batch->causal_block, scale * 1.4426950408889634f};
+  int n = 0;
+  cudaError_t e = cudaSuccess;
+  if (!batch->few.pieces.empty()) e = launch_kv_attn_few(*cache, *batch, a, (cudaStream_t)stream, &n);
+  cache->launches += n;
+  return cuda_status(e);
+}
+
+litevggt_status litevggt_kv_poll(litevggt_kv_cache* cache, void* stream) {
+  if (!cache_ok(cache)) return LITEVGGT_ERR_NULL;
+  cudaStream_t s = (cudaStream_t)stream;
+  uint32_t word = 0;
+  cudaError_t e = cudaMemcpyAsync(&word, cache->status, sizeof(word), cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaMemsetAsync(cache->status, 0, sizeof(word), s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess) return cuda_status(e);
+  return word & kStatusTimeout ? LITEVGGT_ERR_DEVICE_TIMEOUT : LITEVGGT_OK;
+}
+
+litevggt_status litevggt_kv_launch_count(const litevggt_kv_cache* cache, int64_t* launches) {
+  if (!cache_ok(cache) || launches == nullptr) return LITEVGGT_ERR_NULL;
+  *launches = cache->launches;
+  return LITEVGGT_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,94 @@
+// The objects behind the paged K/V cache's entry points, and what its kernels are launched with.
+#pragma once
+
+#include <vector>
+
+#include "host_common.h"
+#include "kv_plan.h"
+
+namespace lv {
+
+constexpr uint32_t kKvCacheMagic = 0x4c564b43u;
+constexpr uint32_t kKvBatchMagic = 0x4c564b42u;
+
+// The pools as a kernel sees them: [pages, kv_heads, page_size, head_dim] of bf16 or E4M3 codes, the codes' exponents
+// [pages, kv_heads, page_size].
+struct KvPool {
+  uint8_t *k, *v;
+  uint8_t *k_exp, *v_exp;  // null for bf16
+  int kv_heads, page_size, page_shift;
+};
+
+// A batch's arrays on the device.
+struct KvArrays {
+  const KvSeq* seqs;
+  const int* pages;
+  int n_seq;
+};
+struct KvLaunch {
+  const KvPiece* pieces;
+  const int* first;
+  int workers;
+  int* joins;   // counters, zero between launches
+  float* rows;  // partial rows, as the kernel lays them out
+  float* sums;  // their {reference, sum}
+};
+
+// Rows of a tensor [rows, heads, head_dim]: elements from one row to the next, from one head to the next.
+struct KvStride {
+  long long row, head;
+};
+
+struct KvAttend {
+  const __nv_bfloat16* q;
+  KvStride q_stride;
+  __nv_bfloat16* out;  // [rows, q_heads, head_dim]
+  int q_heads, group, causal_block;
+  float scale_log2;    // softmax scale in base-2 units
+};
+
+}  // namespace lv
+
+struct litevggt_kv_cache {
+  uint32_t magic;
+  litevggt_kv_config cfg;
+  int device, num_sms;
+  lv::KvPool pool;
+  uint32_t* status;
+  CUtensorMap k_map, v_map;  // bf16 pools, boxes of one page of a head and 64 channels
+  long long launches;
+};
+
+struct litevggt_kv_batch {
+  uint32_t magic;
+  const litevggt_kv_cache* owner;
+  int q_heads, group, causal_block;
+  long long rows;
+  bool rows_held;  // no sequence has more rows than tokens
+  std::vector<lv::KvSeq> seqs;
+  lv::KvWork few;
+  std::vector<uint8_t> image;  // what the device gets
+  size_t bytes;                // of device memory
+  size_t o_seqs, o_pages, o_few_pieces, o_few_first, o_joins, o_few_rows, o_few_sums;
+  uint8_t* base = nullptr;     // the caller's device memory
+};
+
+namespace lv {
+
+inline KvArrays kv_arrays(const litevggt_kv_batch& b) {
+  return KvArrays{reinterpret_cast<const KvSeq*>(b.base + b.o_seqs), reinterpret_cast<const int*>(b.base + b.o_pages), (int)b.seqs.size()};
+}
+
+// kv_cache.cu
+cudaError_t launch_kv_append(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const __nv_bfloat16* k, KvStride k_stride,
+                             const __nv_bfloat16* v, KvStride v_stride, cudaStream_t s, int* launches);
+cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch& b, __nv_bfloat16* k, __nv_bfloat16* v, cudaStream_t s,
+                             int* launches);
+
+// kv_attn_few.cu
+constexpr int kKvFewRows = 16;    // rows of a piece at most
+constexpr int kKvFewWarps = 8;
+constexpr int kKvFewUnit = 128;   // keys
+cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
+
+}  // namespace lv

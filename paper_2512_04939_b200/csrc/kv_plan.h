@@ -1,0 +1,130 @@
+// How the work of a batch over a paged K/V cache is cut: which rows of which sequence meet which keys in which CTA.  Host
+// arithmetic only; the batch's arrays are made here once and serve every layer that works on the same lengths and pages.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+#include <vector>
+
+namespace lv {
+
+// A sequence of a batch: its rows in the packed tensors, the tokens that it holds, where its pages begin in the batch's list.
+struct KvSeq {
+  int row0, rows, len, page0;
+};
+
+// Keys [key0, key1) of rows [row0, row0 + rows) of one sequence and K/V head.  The `group` query heads that share the head
+// are rows of their own, side by side: row = token * group + head within the group.
+struct alignas(16) KvPiece {
+  int seq, kv_head, row0, rows;
+  int key0, key1;
+  int slot;        // where its partial rows go, -1: the rows have no other piece
+  int first_slot;  // of all pieces of the same rows
+  int parts, join; // how many they are, and the counter of those that have come
+  int pad[2];
+};
+
+// Tokens that row `token` of a sequence's chunk sees; none if it is negative.
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+inline int kv_seen(int len, int rows, int causal_block, int token) {
+  if (causal_block == 0) return len;
+  const long long end = (long long)len - rows + (long long)(token / causal_block + 1) * causal_block;
+  return end < len ? (int)end : len;
+}
+
+struct KvWork {
+  std::vector<KvPiece> pieces;
+  std::vector<int> first;  // [workers + 1] a worker's pieces; every worker that is launched has one
+  int slots = 0, joins = 0;
+};
+
+// What a kernel needs from the cutting.
+struct KvCut {
+  int row_block;   // rows of one piece at most
+  int unit;        // keys: pieces begin at multiples of it
+  int workers;     // at most
+  int min_units;   // of a piece where rows are cut
+  int max_units;
+  double overhead; // of a piece, in units
+};
+
+// Cuts the rows of the sequences in `which` into pieces.  All pieces in a row, every worker takes an equal share of what
+// they cost, so a launch ends at the same time everywhere whatever the lengths; a share's border cuts the keys of the
+// rows that it falls into.
+inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& which, int group, int kv_heads, int causal_block,
+                     const KvCut& cut) {
+  KvWork work;
+  // cost of a unit of `rows` rows: what fills less than half of the rows takes less than the full block, but not half
+  auto unit_cost = [&](int rows) { return 2 * rows <= cut.row_block ? 0.65 : 1.0; };
+  auto units_of = [&](const KvSeq& q, int row0, int rows) {
+    const int seen = kv_seen(q.len, q.rows, causal_block, (row0 + rows - 1) / group);
+    return seen > 0 ? (seen - 1) / cut.unit + 1 : 0;
+  };
+  double total = 0.0;
+  for (int s : which) {
+    const KvSeq& q = seqs[(size_t)s];
+    const int rows = q.rows * group;
+    double one_head = 0.0;
+    for (int r = 0; r < rows; r += cut.row_block) {
+      const int n = std::min(cut.row_block, rows - r);
+      one_head += units_of(q, r, n) * unit_cost(n) + cut.overhead;
+    }
+    total += one_head * kv_heads;
+  }
+  if (total <= 0.0) return work;
+  const double share = std::max(total / cut.workers, cut.min_units + cut.overhead);
+  double spent = 0.0;
+  int worker = 0;
+  work.first.push_back(0);
+  auto next_worker = [&]() {
+    if (worker + 1 >= cut.workers || (size_t)work.first.back() == work.pieces.size()) return false;
+    work.first.push_back((int)work.pieces.size());
+    ++worker;
+    return true;
+  };
+  for (int s : which) {
+    const KvSeq& q = seqs[(size_t)s];
+    for (int h = 0; h < kv_heads; ++h)
+      for (int r = 0; r < q.rows * group; r += cut.row_block) {
+        const int n = std::min(cut.row_block, q.rows * group - r);
+        const int units = units_of(q, r, n), seen = units > 0 ? kv_seen(q.len, q.rows, causal_block, (r + n - 1) / group) : 0;
+        const double cost = unit_cost(n);
+        const size_t begin = work.pieces.size();
+        int done = 0;
+        do {
+          const double left = (worker + 1) * share - spent - cut.overhead;
+          int take = left > 0.0 ? (int)(left / cost) : 0;
+          if (worker + 1 >= cut.workers) take = units;
+          if (take < std::min(cut.min_units, units - done) && next_worker()) continue;
+          if (units - done - take < cut.min_units) take = units - done;  // no crumbs
+          take = std::min(std::max(take, std::min(cut.min_units, units - done)), std::min(units - done, cut.max_units));
+          KvPiece p{};
+          p.seq = s; p.kv_head = h; p.row0 = r; p.rows = n;
+          p.key0 = done * cut.unit;
+          p.key1 = std::min((done + take) * (long long)cut.unit, (long long)seen);
+          p.slot = -1;
+          work.pieces.push_back(p);
+          done += take;
+          spent += take * cost + cut.overhead;
+        } while (done < units);
+        const int parts = (int)(work.pieces.size() - begin);
+        if (parts > 1) {
+          for (size_t i = begin; i < work.pieces.size(); ++i) {
+            work.pieces[i].slot = work.slots + (int)(i - begin);
+            work.pieces[i].first_slot = work.slots;
+            work.pieces[i].parts = parts;
+            work.pieces[i].join = work.joins;
+          }
+          work.slots += parts;
+          ++work.joins;
+        }
+      }
+  }
+  work.first.push_back((int)work.pieces.size());
+  return work;
+}
+
+}  // namespace lv

@@ -1,0 +1,191 @@
+"""A paged K/V cache and the attention that reads it, for frames that keep arriving.
+
+    cache = KVCache.empty(pages, page_size, kv_heads, head_dim, dtype="e4m3")
+    batch = cache.batch(rows=[1041], lengths=[52050], pages=[page_ids])    # once per step, for every layer's cache alike
+    cache.append(batch, k, v)                                              # the last 1041 tokens of the sequence
+    out = cache.attend(batch, q)                                           # over all 52050
+
+Which pages a sequence owns is the caller's business; the library checks that they exist.  Shapes, types, strides and
+devices are checked here, everything else in the C library.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+
+import numpy as np
+import torch
+
+from .binding import KVConfig, _check, load_library
+
+_DTYPES = {"bf16": (0, torch.bfloat16), "e4m3": (1, torch.float8_e4m3fn)}
+
+
+def _strides(t: torch.Tensor) -> tuple[int, int]:
+    """Elements from row to row and from head to head; the stride of a dimension of one says nothing."""
+    return (t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+class KVBatch:
+    """Rows, lengths and pages of a step's sequences, planned for one cache (see :meth:`KVCache.batch`)."""
+
+    def __init__(self, owner: "KVCache", handle, memory: torch.Tensor, rows: int, q_heads: int, stream: int):
+        self.owner = owner
+        self.handle = handle
+        self.memory = memory
+        self.rows = rows
+        self.q_heads = q_heads
+        self._stream = stream
+
+    def __del__(self):
+        if self.handle is not None:
+            self.owner.lib.litevggt_kv_batch_destroy(self.handle)
+            self.handle = None
+
+
+class KVCache:
+    """A cache over pools of the caller's: ``k``, ``v`` [pages, kv_heads, page_size, head_dim], bfloat16, or float8_e4m3fn
+    with the exponents ``k_exp``, ``v_exp`` uint8 [pages, kv_heads, page_size]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None):
+        self.lib = load_library()
+        if k.dim() != 4 or v.shape != k.shape:
+            raise ValueError(f"k and v must both be [pages, kv_heads, page_size, head_dim], got {tuple(k.shape)} and {tuple(v.shape)}")
+        narrow = k.dtype == torch.float8_e4m3fn
+        if not narrow and k.dtype != torch.bfloat16 or v.dtype != k.dtype:
+            raise ValueError(f"k and v must both be bfloat16 or both float8_e4m3fn, got {k.dtype} and {v.dtype}")
+        tensors = {"k": k, "v": v}
+        if narrow:
+            for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+                if t is None or t.dtype != torch.uint8 or t.shape != k.shape[:3]:
+                    raise ValueError(f"{name} must be uint8 {tuple(k.shape[:3])} beside float8_e4m3fn pools")
+                tensors[name] = t
+        elif k_exp is not None or v_exp is not None:
+            raise ValueError("bfloat16 pools have no exponents")
+        for name, t in tensors.items():
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            if not t.is_cuda or t.device != k.device:
+                raise ValueError("every pool must live on the same CUDA device")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.device = k.device
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.status = torch.zeros(64, dtype=torch.int32, device=k.device)
+        cfg = KVConfig(self.pages, self.page_size, self.kv_heads, self.head_dim, 1 if narrow else 0)
+        self.handle = C.c_void_p()
+        _check(self.lib.litevggt_kv_create(C.byref(cfg), self.device.index, *(C.c_void_p(t.data_ptr()) if t is not None else None
+                                                                             for t in (k, v, k_exp, v_exp, self.status)),
+                                           C.byref(self.handle)), "kv_create")
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype: str = "bf16", device: int = 0) -> "KVCache":
+        """A cache with pools of its own, not initialised."""
+        if dtype not in _DTYPES:
+            raise ValueError(f"dtype must be one of {sorted(_DTYPES)}, got {dtype!r}")
+        where = torch.device("cuda", device)
+        shape = (pages, kv_heads, page_size, head_dim)
+        pools = [torch.empty(shape, dtype=_DTYPES[dtype][1], device=where) for _ in range(2)]
+        if dtype == "e4m3":
+            pools += [torch.empty(shape[:3], dtype=torch.uint8, device=where) for _ in range(2)]
+        return cls(*pools)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None and self.handle.value:
+            self.lib.litevggt_kv_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # ------------------------------------------------------------------ a step
+    def batch(self, rows, lengths, pages, q_heads: int | None = None, causal_block: int = 0) -> KVBatch:
+        """Plans a step: ``rows[i]`` rows of the packed tensors belong to sequence i, which holds ``lengths[i]`` tokens (those
+        rows included, as its last) in the pages ``pages[i]`` (more than it needs may be named).  ``causal_block`` = c: a
+        row sees the tokens before its sequence's rows and the blocks of c rows up to its own; 0: all of them."""
+        if len(rows) != len(lengths) or len(rows) != len(pages) or len(rows) == 0:
+            raise ValueError(f"rows, lengths and pages name {len(rows)}, {len(lengths)} and {len(pages)} sequences")
+        n_rows, n_tokens = np.asarray(rows, np.int64), np.asarray(lengths, np.int64)
+        if min(n_rows.min(), n_tokens.min()) < 0 or max(n_rows.max(), n_tokens.max()) >= 2 ** 31:
+            raise ValueError("rows and lengths must lie in [0, 2^31)")
+        lists = []
+        for n, ids in zip(n_tokens.tolist(), pages):
+            need = -(-n // self.page_size)
+            if len(ids) < need:
+                raise ValueError(f"a sequence of {n} tokens needs {need} pages, got {len(ids)}")
+            lists.append(np.asarray(ids[:need], np.int64))
+        flat = np.concatenate(lists)
+        if flat.size and (flat.min() < 0 or flat.max() >= self.pages):
+            raise ValueError(f"pages must lie in [0, {self.pages})")
+        r32, n32, p32 = (np.ascontiguousarray(a, np.int32) for a in (n_rows, n_tokens, flat))
+        q_heads = self.kv_heads if q_heads is None else q_heads
+        handle, n_bytes = C.c_void_p(), C.c_size_t()
+        _check(self.lib.litevggt_kv_batch_create(self.handle, len(rows), r32.ctypes.data, n32.ctypes.data, p32.ctypes.data, q_heads,
+                                                 causal_block, C.byref(handle), C.byref(n_bytes)), "kv_batch_create")
+        with torch.cuda.device(self.device):
+            memory = torch.empty(n_bytes.value, dtype=torch.uint8, device=self.device)
+        stream = self._stream()
+        made = KVBatch(self, handle, memory, int(n_rows.sum()), q_heads, stream)
+        _check(self.lib.litevggt_kv_batch_place(handle, memory.data_ptr(), n_bytes.value, stream), "kv_batch_place")
+        return made
+
+    def append(self, batch: KVBatch, k: torch.Tensor, v: torch.Tensor) -> None:
+        """Writes ``k``, ``v`` [batch.rows, kv_heads, head_dim] (bfloat16; slices of a fused projection will do) into the
+        batch's sequences as their last tokens."""
+        for name, t in (("k", k), ("v", v)):
+            self._check_rows(name, t, batch.rows, self.kv_heads)
+        _check(self.lib.litevggt_kv_append(self.handle, batch.handle, k.data_ptr(), *_strides(k), v.data_ptr(), *_strides(v),
+                                           self._use(batch)), "kv_append")
+
+    def gather(self, batch: KVBatch) -> tuple[torch.Tensor, torch.Tensor]:
+        """K and V of the batch's rows, bfloat16 [batch.rows, kv_heads, head_dim]."""
+        k = torch.empty(batch.rows, self.kv_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+        v = torch.empty_like(k)
+        _check(self.lib.litevggt_kv_gather(self.handle, batch.handle, k.data_ptr(), v.data_ptr(), self._use(batch)), "kv_gather")
+        return k, v
+
+    def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+        """softmax(scale q K^T) V of the batch's rows over the tokens that they see; ``q`` bfloat16 [batch.rows, q_heads, head_dim].
+        ``scale`` is 1 / sqrt(head_dim) unless given.  A row that sees no token comes out as zero."""
+        self._check_rows("q", q, batch.rows, batch.q_heads)
+        if out is None:
+            out = torch.empty(batch.rows, batch.q_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+        else:
+            self._check_rows("out", out, batch.rows, batch.q_heads)
+            if not out.is_contiguous():
+                raise ValueError("out must be contiguous")
+        scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
+        _check(self.lib.litevggt_kv_attend(self.handle, batch.handle, q.data_ptr(), *_strides(q), scale, out.data_ptr(),
+                                           self._use(batch)), "kv_attend")
+        return out
+
+    # ------------------------------------------------------------------ checks
+    def poll(self):
+        """Synchronise the current stream; raise if a kernel gave up on a wait."""
+        _check(self.lib.litevggt_kv_poll(self.handle, self._stream()), "kv_poll")
+
+    def launch_count(self) -> int:
+        n = C.c_int64()
+        _check(self.lib.litevggt_kv_launch_count(self.handle, C.byref(n)), "kv_launch_count")
+        return n.value
+
+    def _stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
+
+    def _use(self, batch: KVBatch) -> int:
+        """The current stream, to which the batch's memory now belongs as well."""
+        stream = self._stream()
+        if stream != batch._stream:
+            batch.memory.record_stream(torch.cuda.current_stream(self.device))
+            self.status.record_stream(torch.cuda.current_stream(self.device))
+        return stream
+
+    def _check_rows(self, name: str, t: torch.Tensor, rows: int, heads: int):
+        if t.shape != (rows, heads, self.head_dim):
+            raise ValueError(f"{name} must be [{rows}, {heads}, {self.head_dim}], got {tuple(t.shape)}")
+        if t.dtype != torch.bfloat16 or t.device != self.device:
+            raise ValueError(f"{name} must be bfloat16 on {self.device}, got {t.dtype} on {t.device}")
+        if t.stride(2) != 1 or any(n % 8 for n in _strides(t)) or t.data_ptr() % 16:
+            raise ValueError(f"{name}'s head_dim must be contiguous, its rows and heads 16-byte aligned, got strides {t.stride()}")
