@@ -75,7 +75,8 @@ inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& whi
     total += one_head * kv_heads;
   }
   if (total <= 0.0) return work;
-  const double share = std::max(total / cut.workers, cut.min_units + cut.overhead);
+  // (nearly every worker's border cuts some rows in two, which makes one more piece)
+  const double share = std::max(total / cut.workers + cut.overhead, cut.min_units + cut.overhead);
   double spent = 0.0;
   int worker = 0;
   work.first.push_back(0);
