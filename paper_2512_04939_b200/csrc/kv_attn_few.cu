@@ -437,9 +437,7 @@ cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const 
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = set_max_dynamic_smem_once(reinterpret_cast<const void*>(kernel), Shape::kSmemBytes, done);
   if (e != cudaSuccess) return e;
-  const KvLaunch work{reinterpret_cast<const KvPiece*>(b.base + b.o_few_pieces), reinterpret_cast<const int*>(b.base + b.o_few_first),
-                      (int)b.few.first.size() - 1, reinterpret_cast<int*>(b.base + b.o_joins),
-                      reinterpret_cast<float*>(b.base + b.o_few_rows), reinterpret_cast<float*>(b.base + b.o_few_sums)};
+  const KvLaunch work = kv_launch(b, b.few, b.at_few);
   return launch(kernel, dim3((unsigned)work.workers), kKvFewWarps * 32, (size_t)Shape::kSmemBytes, s, c.pool, kv_arrays(b), work, a);
 }
 

@@ -190,23 +190,33 @@ void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int hea
     at += (size_t)round_up((long long)(bytes > 0 ? bytes : 1), 256);
     return here;
   };
-  const KvWork& few = b->few;
+  auto take_lists = [&](const KvWork& w, litevggt_kv_batch::Places* p) {
+    p->pieces = take(w.pieces.size() * sizeof(KvPiece));
+    p->first = take(w.first.size() * sizeof(int));
+    p->joins = take((size_t)w.joins * sizeof(int));
+  };
   b->o_seqs = take(b->seqs.size() * sizeof(KvSeq));
   b->o_pages = take(n_pages * sizeof(int));
-  b->o_few_pieces = take(few.pieces.size() * sizeof(KvPiece));
-  b->o_few_first = take(few.first.size() * sizeof(int));
-  b->o_joins = take((size_t)few.joins * sizeof(int));
+  take_lists(b->few, &b->at_few);
+  take_lists(b->tiles, &b->at_tiles);
   b->image.assign(at, 0);  // the counters start at zero
-  b->o_few_rows = take((size_t)few.slots * kKvFewRows * head_dim * sizeof(float));
-  b->o_few_sums = take((size_t)few.slots * kKvFewRows * 2 * sizeof(float));
+  // the two launches follow one another, and so use the same memory
+  const size_t parts[2] = {(size_t)b->few.slots * kKvFewRows, (size_t)b->tiles.slots * kKvTileRows};
+  const size_t most = std::max(parts[0], parts[1]);
+  b->at_few.rows = b->at_tiles.rows = take(most * head_dim * sizeof(float));
+  b->at_few.sums = b->at_tiles.sums = take(most * 2 * sizeof(float));
   b->bytes = at;
   auto put = [&](size_t to, const void* from, size_t bytes) {
     if (bytes > 0) memcpy(b->image.data() + to, from, bytes);
   };
   put(b->o_seqs, b->seqs.data(), b->seqs.size() * sizeof(KvSeq));
   put(b->o_pages, pages, n_pages * sizeof(int));
-  put(b->o_few_pieces, few.pieces.data(), few.pieces.size() * sizeof(KvPiece));
-  put(b->o_few_first, few.first.data(), few.first.size() * sizeof(int));
+  auto put_lists = [&](const KvWork& w, const litevggt_kv_batch::Places& p) {
+    put(p.pieces, w.pieces.data(), w.pieces.size() * sizeof(KvPiece));
+    put(p.first, w.first.data(), w.first.size() * sizeof(int));
+  };
+  put_lists(b->few, b->at_few);
+  put_lists(b->tiles, b->at_tiles);
 }
 
 litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int32_t* rows, const int32_t* lengths, const int32_t* pages,
@@ -230,16 +240,17 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
   b->group = q_heads / c->cfg.kv_heads;
   b->causal_block = causal_block;
   b->rows = row0;
-  std::vector<int> few;
+  std::vector<int> few, many;
   int most = 0;
-  for (int i = 0; i < n_seq; ++i)
-    if (rows[i] > 0) {
-      few.push_back(i);
-      most = std::max(most, rows[i] * b->group);
-    }
+  for (int i = 0; i < n_seq; ++i) {
+    const long long r = (long long)rows[i] * b->group;
+    if (r > kKvFewRows) many.push_back(i);
+    else if (r > 0) few.push_back(i), most = std::max(most, (int)r);
+  }
   const int per_sm = c->cfg.head_dim == 128 && most > 8 ? 1 : 2;  // CTAs, by their registers
   b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
                   KvCut{kKvFewRows, kKvFewUnit, c->num_sms * per_sm, 1, INT32_MAX, 1.0});
+  b->tiles = kv_cut(b->seqs, many, b->group, c->cfg.kv_heads, causal_block, KvCut{kKvTileRows, kKvTileUnit, c->num_sms, 4, 512, 4.0});
   lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
   return LITEVGGT_OK;
 }
@@ -286,6 +297,19 @@ litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, vo
                    cfg->kv_heads, cfg->page_size, shift};
   c->status = status;
   c->launches = 0;
+  if (!narrow) {  // rows of heads as one matrix; a box is a page of a head and 64 channels
+    static std::atomic<void*> encode{nullptr};
+    void* fn = encode.load(std::memory_order_acquire);
+    bool ok = fn != nullptr || resolve_encode_tiled(&fn);
+    if (ok) encode.store(fn, std::memory_order_release);
+    const uint64_t rows = (uint64_t)cfg->pages * cfg->kv_heads * cfg->page_size, hd = (uint64_t)cfg->head_dim;
+    ok = ok && make_tmap_bf16_2d(fn, &c->k_map, k, hd, rows, hd, 64, (uint32_t)cfg->page_size, true) &&
+         make_tmap_bf16_2d(fn, &c->v_map, v, hd, rows, hd, 64, (uint32_t)cfg->page_size, true);
+    if (!ok) {
+      delete c;
+      return LITEVGGT_ERR_CUDA;
+    }
+  }
   *out = c;
   return LITEVGGT_OK;
 }
@@ -391,6 +415,7 @@ litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_b
   int n = 0;
   cudaError_t e = cudaSuccess;
   if (!batch->few.pieces.empty()) e = launch_kv_attn_few(*cache, *batch, a, (cudaStream_t)stream, &n);
+  if (e == cudaSuccess && !batch->tiles.pieces.empty()) e = launch_kv_attn_tiles(*cache, *batch, a, (cudaStream_t)stream, &n);
   cache->launches += n;
   return cuda_status(e);
 }

@@ -46,7 +46,6 @@ struct KvAttend {
   int q_heads, group, causal_block;
   float scale_log2;    // softmax scale in base-2 units
 };
-
 }  // namespace lv
 
 struct litevggt_kv_cache {
@@ -66,10 +65,13 @@ struct litevggt_kv_batch {
   long long rows;
   bool rows_held;  // no sequence has more rows than tokens
   std::vector<lv::KvSeq> seqs;
-  lv::KvWork few;
+  lv::KvWork few, tiles;       // sequences of few rows, and the others
   std::vector<uint8_t> image;  // what the device gets
   size_t bytes;                // of device memory
-  size_t o_seqs, o_pages, o_few_pieces, o_few_first, o_joins, o_few_rows, o_few_sums;
+  size_t o_seqs, o_pages;
+  struct Places {
+    size_t pieces, first, joins, rows, sums;
+  } at_few, at_tiles;
   uint8_t* base = nullptr;     // the caller's device memory
 };
 
@@ -77,6 +79,12 @@ namespace lv {
 
 inline KvArrays kv_arrays(const litevggt_kv_batch& b) {
   return KvArrays{reinterpret_cast<const KvSeq*>(b.base + b.o_seqs), reinterpret_cast<const int*>(b.base + b.o_pages), (int)b.seqs.size()};
+}
+
+inline KvLaunch kv_launch(const litevggt_kv_batch& b, const KvWork& work, const litevggt_kv_batch::Places& at) {
+  return KvLaunch{reinterpret_cast<const KvPiece*>(b.base + at.pieces), reinterpret_cast<const int*>(b.base + at.first),
+                  (int)work.first.size() - 1, reinterpret_cast<int*>(b.base + at.joins), reinterpret_cast<float*>(b.base + at.rows),
+                  reinterpret_cast<float*>(b.base + at.sums)};
 }
 
 // kv_cache.cu
@@ -90,5 +98,9 @@ constexpr int kKvFewRows = 16;    // rows of a piece at most
 constexpr int kKvFewWarps = 8;
 constexpr int kKvFewUnit = 128;   // keys
 cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
+// kv_attn_tiles.cu
+constexpr int kKvTileRows = 256;
+constexpr int kKvTileUnit = 128;
+cudaError_t launch_kv_attn_tiles(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
 
 }  // namespace lv
