@@ -10,6 +10,7 @@
 //               channels of those four keys and pairs them up with byte permutations; its accumulators' keys in S are the same
 //               ones, so P goes from accumulator to operand without leaving the lane
 // The warps of a CTA take turns on a piece's keys, each with a softmax reference of its own; they meet once at its end.
+#include "exp2.cuh"
 #include "kv_cache.h"
 #include "kv_quant.cuh"
 
@@ -22,11 +23,6 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 __device__ __forceinline__ uint4 load16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
 
@@ -225,7 +221,7 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
           if (m > top[half]) {
-            const float factor = top[half] == -INFINITY ? 0.0f : exp2_fast(ref[half] - m);
+            const float factor = top[half] == -INFINITY ? 0.0f : fast_exp2(ref[half] - m);
             top[half] = m;
             ref[half] = m;
             sum[half] *= factor;
@@ -241,7 +237,7 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int half = 0; half < (kHalf ? 1 : 2); ++half) {
-            const float a = exp2_fast(sc[s][t][2 * half] - ref[half]), b = exp2_fast(sc[s][t][2 * half + 1] - ref[half]);
+            const float a = fast_exp2(sc[s][t][2 * half] - ref[half]), b = fast_exp2(sc[s][t][2 * half + 1] - ref[half]);
             // operands of the second product, each off by up to 2^-8; the sum is that of the rounded ones, so what the rounding
             // changes is how much a key weighs among the others and not the whole row's size
             p[s][t][half] = pack_bf16(a, b);
@@ -385,7 +381,7 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
       const float m_use = m == -INFINITY ? 0.0f : m;
 #pragma unroll
       for (int w = 0; w < kKvFewWarps; ++w) {
-        const float mw = smem_ml[(w * Shape::kRows + r) * 2], weight = mw == -INFINITY ? 1.0f : exp2_fast(mw - m_use);
+        const float mw = smem_ml[(w * Shape::kRows + r) * 2], weight = mw == -INFINITY ? 1.0f : fast_exp2(mw - m_use);
         l += smem_ml[(w * Shape::kRows + r) * 2 + 1] * weight;
         acc += smem_o[(w * Shape::kRows + r) * kHd + ch] * weight;
       }
@@ -418,7 +414,7 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
           const float m_use = m == -INFINITY ? 0.0f : m;
           for (int w = 0; w < piece.parts; ++w) {
             const float2 x = __ldcg(ml + (size_t)w * kKvFewRows);
-            const float weight = x.x == -INFINITY ? 1.0f : exp2_fast(x.x - m_use);
+            const float weight = x.x == -INFINITY ? 1.0f : fast_exp2(x.x - m_use);
             l += x.y * weight;
             acc += __ldcg(part + (size_t)w * kKvFewRows * kHd) * weight;
           }

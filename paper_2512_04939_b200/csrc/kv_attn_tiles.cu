@@ -18,6 +18,7 @@
 //         the V warp: what no row sees becomes zero (a page's tail may hold anything, and 0 * NaN is NaN), and values that
 //         are not finite are taken out; the softmax adds them to the rows that see them.
 //   E4M3  codes and exponents come by bulk copies into a ring of their own; the four warps widen them to the same tiles, exactly.
+#include "exp2.cuh"
 #include "kv_cache.h"
 #include "kv_quant.cuh"
 
@@ -26,6 +27,9 @@ namespace lv {
 namespace {
 
 constexpr int kTileKeys = 128;
+#ifndef LV_KV_POLY
+#define LV_KV_POLY 0
+#endif
 
 template <int kHd, bool kNarrow>
 struct TiShape {
@@ -40,6 +44,7 @@ struct TiShape {
   static constexpr int kTileBytes = kSubBytes * kHd / 64; // of Q, K or V
   static constexpr int kRawBytes = kTileKeys * kHd + kTileKeys;
   static constexpr uint32_t kColO = 256;
+  static constexpr int kPolyPairs = LV_KV_POLY;  // of the 16 pairs of 32 scores, on the FMA pipes
   static constexpr int kSmemBytes = 2 * kTileBytes + 2 * kStages * kTileBytes + 2 * kRaw * kRawBytes + (kStreams == 2 ? 8192 : 0) + 512 + 1024;
 };
 
@@ -47,17 +52,12 @@ template <int kStages, int kRaw>
 struct TiBarriers {
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], v_land[kStages];
   uint64_t raw_full[2][kRaw > 0 ? kRaw : 1], raw_empty[2][kRaw > 0 ? kRaw : 1];  // [K, V]
-  uint64_t q_ready[2], s_full[2], p_ready[2][2], o_done[2], teardown[2];
+  uint64_t q_ready[2], s_full[2][2], p_ready[2][2], o_done[2], teardown[2];
   uint32_t tmem_base, abort_flag;
   int taken_out[2];  // a piece (its number + 1, by its parity) whose V held values that are not finite where not all rows see them
   int last_of_join;
 };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem_dst)),
                "l"(src), "r"(bytes), "r"(smem_u32(bar))
@@ -65,9 +65,10 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
 }
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// The reference may lag this far behind a row's maximum (base-2 units) before the row is scaled anew: with it the
-// probabilities stay below 2^8 and their sums far inside 32 bits.
-constexpr float kSlack = 8.0f;
+// A row's reference moves to its maximum when a step's probabilities add up to more than kLate, and then if that maximum lies
+// more than kSlack above it (base-2 units).  So no probability is over 2^20, which bf16 and sums in 32 bits hold as well
+// as 1; what a maximum 2^20 above the reference takes from the other end is keys under 2^-106 of it.
+constexpr float kLate = 1048576.0f, kSlack = 4.0f;
 
 // Of `from`, the latest loads (up to one a slot) have landed; they must before the shared memory is given up.
 template <int kSlots>
@@ -149,7 +150,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       }
     for (int t = 0; t < 2; ++t) {
       mbar_init(&bars->q_ready[t], 4 * kStreams);
-      mbar_init(&bars->s_full[t], 1);
+      mbar_init(&bars->s_full[t][0], 1);
+      mbar_init(&bars->s_full[t][1], 1);
       mbar_init(&bars->p_ready[t][0], 4);
       mbar_init(&bars->p_ready[t][1], 4);
       mbar_init(&bars->o_done[t], 1);
@@ -235,54 +237,65 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     // ------------------------------------------------------------------ MMA issuer of row tile t
     if (elect_one()) {
       const int t = warp - kIssuer;
-      constexpr uint32_t idesc_qk = umma_idesc_bf16(128, 128, false, false);
+      constexpr uint32_t idesc_qk = umma_idesc_bf16(128, Shape::kKeys, false, false);
       constexpr uint32_t idesc_pv = umma_idesc_bf16(128, kHd, false, true);
       const uint32_t s_col = tmem_base + t * 128;
       const uint32_t o_col = tmem_base + Shape::kColO + t * kStreams * kHd;
       const uint64_t q_desc = smem_desc_sw128(smem_u32(smem_q + t * kTileBytes), 16, 1024);
       const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem_k), 16, 1024);
       const uint64_t v_desc0 = smem_desc_sw128(smem_u32(smem_v), kSubBytes, 1024);  // 64 channels further on: the next sub-tile
+      auto slot_at = [&](int slot) { return (uint64_t)((slot * kTileBytes) >> 4); };
+      auto issue_qk = [&](int c, int slot) {
+#pragma unroll
+        for (int k = 0; k < kHd / 16; ++k) {
+          const uint64_t in_tile = (uint64_t)(((k >> 2) * kSubBytes + (k & 3) * 32) >> 4);
+          umma_ss(s_col + c * 64, q_desc + in_tile, k_desc0 + slot_at(slot) + (uint64_t)(c * 512) + in_tile, idesc_qk, k != 0 ? 1u : 0u);
+        }
+        umma_commit(&bars->s_full[t][c]);
+      };
       Ring ring;
       uint32_t step = 0, round = 0;
       bool ok = true;
       for (int id = id0; id < id_end && ok; ++id) {
         const Job job = job_of(work, arrays, at, id);
         const int mine = tiles_of(job, at, t);
-        if (mine > 0) ok = mbar_wait(&bars->q_ready[t], round & 1u, ctl);
-        for (int j = 0; j < job.tiles && ok; ++j) {
-          const uint64_t at_slot = (uint64_t)((ring.slot * kTileBytes) >> 4);
-          if (!mbar_wait(&bars->k_full[ring.slot], ring.phase, ctl)) { ok = false; break; }
-          if (j < mine) {
-            tc_fence_after();
+        if (mine > 0) {
+          ok = mbar_wait(&bars->q_ready[t], round & 1u, ctl) && mbar_wait(&bars->k_full[ring.slot], ring.phase, ctl);
+          if (!ok) break;
+          tc_fence_after();
 #pragma unroll
-            for (int k = 0; k < kHd / 16; ++k) {
-              const uint64_t in_tile = (uint64_t)(((k >> 2) * kSubBytes + (k & 3) * 32) >> 4);
-              umma_ss(s_col, q_desc + in_tile, k_desc0 + at_slot + in_tile, idesc_qk, k != 0 ? 1u : 0u);
-            }
-            umma_commit(&bars->s_full[t]);
-            umma_commit(&bars->k_empty[ring.slot]);
-          } else {
-            mbar_arrive(&bars->k_empty[ring.slot]);
-          }
-          if (!mbar_wait(&bars->v_full[ring.slot], ring.phase, ctl)) { ok = false; break; }
+          for (int c = 0; c < kStreams; ++c) issue_qk(c, ring.slot);
+          umma_commit(&bars->k_empty[ring.slot]);
+        }
+        for (int j = 0; j < job.tiles && ok; ++j) {
+          Ring next = ring;
+          next.next<kStages>();
           if (j < mine) {
+            ok = mbar_wait(&bars->v_full[ring.slot], ring.phase, ctl);
+            if (ok && j + 1 < mine) ok = mbar_wait(&bars->k_full[next.slot], next.phase, ctl);
 #pragma unroll
             for (int c = 0; c < kStreams; ++c) {
-              if (!mbar_wait(&bars->p_ready[t][c], step & 1u, ctl)) { ok = false; break; }
+              ok = ok && mbar_wait(&bars->p_ready[t][c], step & 1u, ctl);
+              if (!ok) break;
               tc_fence_after();
 #pragma unroll
               for (int k = 0; k < Shape::kKeys / 16; ++k)
-                umma_ts(o_col + c * kHd, s_col + c * 64 + k * 8, v_desc0 + at_slot + (uint64_t)(((c * 64 + k * 16) * 128) >> 4), idesc_pv,
-                        (j | k) != 0 ? 1u : 0u);
+                umma_ts(o_col + c * kHd, s_col + c * 64 + k * 8, v_desc0 + slot_at(ring.slot) + (uint64_t)(((c * 64 + k * 16) * 128) >> 4),
+                        idesc_pv, (j | k) != 0 ? 1u : 0u);
+              if (j + 1 < mine) issue_qk(c, next.slot);  // where these probabilities were
             }
             if (!ok) break;
             umma_commit(&bars->v_empty[ring.slot]);
-            if (j + 1 == mine) umma_commit(&bars->o_done[t]);
+            if (j + 1 < mine) umma_commit(&bars->k_empty[next.slot]);
+            else umma_commit(&bars->o_done[t]);
             ++step;
-          } else {
+          } else {  // tiles that the other rows see
+            ok = mbar_wait(&bars->k_full[ring.slot], ring.phase, ctl) && mbar_wait(&bars->v_full[ring.slot], ring.phase, ctl);
+            if (!ok) break;
+            mbar_arrive(&bars->k_empty[ring.slot]);
             mbar_arrive(&bars->v_empty[ring.slot]);
           }
-          ring.next<kStages>();
+          ring = next;
         }
         round += mine > 0 ? 1u : 0u;
       }
@@ -426,74 +439,100 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       float2 sum = make_float2(0.0f, 0.0f);
       const int first_seen = __shfl_sync(0xffffffffu, live ? seen : 0x7fffffff, 0);  // rows of a warp see ever more
 
-      for (int j = 0; j < mine && ok; ++j, ++step) {
-        ok = mbar_wait_warp(&bars->s_full[t], step & 1u, ctl);
-        if (!ok) break;
-        tc_fence_after();
-        const int key = (job.tile0 + j) * kTileKeys + c * 64;
-        const bool edge = key + Shape::kKeys > first_seen;
-        constexpr int kGroups = Shape::kKeys / 32;
-        auto scores = [&](int g, uint32_t (&s)[32]) {
+      // One step: 64 or 128 scores of the row.  With kEdge some rows of the warp do not see all of its keys.
+      constexpr int kGroups = Shape::kKeys / 32;
+      bool unset = true;  // a row of the warp has no reference yet
+      auto take_step = [&](auto edge_constant, int key, bool first) {
+        constexpr bool kEdge = decltype(edge_constant)::value;
+        auto load = [&](int g, uint32_t (&s)[32]) {
           tmem_ld32(s_addr + g * 32, s);
           tmem_ld_wait();
-          if (edge) {
+          if constexpr (kEdge) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (key + g * 32 + i >= seen) s[i] = 0xff800000u;
           }
         };
-        float most = -INFINITY;
+        // The row's maximum becomes its reference where it lies far above the present one.
+        auto refer = [&]() {
+          float most = -INFINITY;
+#pragma unroll 1
+          for (int g = 0; g < kGroups; ++g) {
+            uint32_t s[32];
+            load(g, s);
+            float m[4];
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          uint32_t s[32];
-          scores(g, s);
-          float m[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            m[i] = fmax3(__uint_as_float(s[8 * i]), __uint_as_float(s[8 * i + 1]), __uint_as_float(s[8 * i + 2]));
-            m[i] = fmax3(m[i], __uint_as_float(s[8 * i + 3]), __uint_as_float(s[8 * i + 4]));
-            m[i] = fmax3(m[i], __uint_as_float(s[8 * i + 5]), __uint_as_float(s[8 * i + 6]));
-            m[i] = fmaxf(m[i], __uint_as_float(s[8 * i + 7]));
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t* x = &s[8 * i];
+              m[i] = fmax3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
+              m[i] = fmax3(m[i], __uint_as_float(x[3]), __uint_as_float(x[4]));
+              m[i] = fmax3(m[i], __uint_as_float(x[5]), __uint_as_float(x[6]));
+            }
+            most = fmax3(most, fmax3(m[0], m[1], __uint_as_float(s[7])), fmax3(m[2], m[3], __uint_as_float(s[15])));
+            most = fmax3(most, __uint_as_float(s[23]), __uint_as_float(s[31]));
           }
-          most = fmax3(most, fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-        }
-        most *= at.scale_log2;
-        const bool move = most > top + kSlack;
-        if (__any_sync(0xffffffffu, move)) {
-          const float factor = move ? (top == -INFINITY ? 0.0f : exp2_fast(ref - most)) : 1.0f;
+          most *= at.scale_log2;
+          const bool move = most > top + kSlack;
+          const float factor = move ? (top == -INFINITY ? 0.0f : fast_exp2(ref - most)) : 1.0f;
           if (move) {
             top = ref = most;
             sum.x *= factor;
             sum.y *= factor;
           }
-          if (j > 0) {
+          unset = __any_sync(0xffffffffu, top == -INFINITY);
+          if (!first) {
 #pragma unroll 1
-            for (int g = 0; g < kHd / 32; ++g) {
-              uint32_t o[32];
-              tmem_ld32(o_addr + g * 32, o);
+            for (int g = 0; g < kHd / 16; ++g) {
+              uint32_t o[16];
+              tmem_ld16(o_addr + g * 16, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
-              tmem_st32(o_addr + g * 32, o);
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
+              tmem_st16(o_addr + g * 16, o);
             }
           }
-        }
-        const float2 scale2 = make_float2(at.scale_log2, at.scale_log2), ref2 = make_float2(-ref, -ref);
+        };
+        // Only a row's first keys are asked for their maximum.  After that its probabilities are taken under the reference
+        // that it has; they tell by themselves when it has fallen too far behind, before anything has been put in the place of
+        // the scores: then the reference moves and they are taken again.
+        uint32_t p[kGroups][16];
+        float2 more;
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+          if (unset || again) refer();
+          const float2 scale2 = make_float2(at.scale_log2, at.scale_log2), ref2 = make_float2(-ref, -ref);
+          more = make_float2(0.0f, 0.0f);
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          uint32_t s[32], p[16];
-          scores(g, s);
+          for (int g = 0; g < kGroups; ++g) {
+            uint32_t s[32];
+            load(g, s);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, ref2);
-            const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-            p[i] = pack_bf16(e.x, e.y);
-            // Where a row may see few keys, the sum is that of the rounded probabilities, so that their rounding changes only
-            // what a key weighs among the others; elsewhere it averages out.
-            sum = __fadd2_rn(sum, edge ? make_float2(bf16_lo(p[i]), bf16_hi(p[i])) : e);
+            for (int i = 0; i < 16; ++i) {
+              float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, ref2);
+              if (i < Shape::kPolyPairs) {
+                x = poly_exp2_pair(make_float2(fminf(fmax_nan(x.x, -126.0f), 120.0f), fminf(fmax_nan(x.y, -126.0f), 120.0f)));
+              } else {
+                x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+              }
+              p[g][i] = pack_bf16(x.x, x.y);
+              // Where a row may see few keys, the sum is that of the rounded probabilities, so that their rounding changes only
+              // what a key weighs among the others; elsewhere it averages out.
+              more = __fadd2_rn(more, kEdge ? make_float2(bf16_lo(p[g][i]), bf16_hi(p[g][i])) : x);
+            }
           }
-          tmem_st16(s_addr + g * 16, p);
+          if (again || !__any_sync(0xffffffffu, !(more.x + more.y <= kLate))) break;
         }
+        sum = __fadd2_rn(sum, more);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) tmem_st16(s_addr + g * 16, p[g]);
+      };
+      for (int j = 0; j < mine && ok; ++j, ++step) {
+        ok = mbar_wait_warp(&bars->s_full[t][c], step & 1u, ctl);
+        if (!ok) break;
+        tc_fence_after();
+        const int key = (job.tile0 + j) * kTileKeys + c * 64;
+        if (key + Shape::kKeys > first_seen) take_step(std::true_type{}, key, j == 0);
+        else take_step(std::false_type{}, key, j == 0);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -515,8 +554,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         const float2 a = ml[r], b = ml[128 + r];
         m = fmaxf(a.x, b.x);
         const float m_use = m == -INFINITY ? 0.0f : m;
-        weight[0] = a.x == -INFINITY ? 1.0f : exp2_fast(a.x - m_use);  // without a key so far: its sum and rows are zero
-        weight[1] = b.x == -INFINITY ? 1.0f : exp2_fast(b.x - m_use);
+        weight[0] = a.x == -INFINITY ? 1.0f : fast_exp2(a.x - m_use);  // without a key so far: its sum and rows are zero
+        weight[1] = b.x == -INFINITY ? 1.0f : fast_exp2(b.x - m_use);
         row_sum = a.y * weight[0] + b.y * weight[1];
       }
       const bool bad = *reinterpret_cast<volatile int*>(&bars->taken_out[id & 1]) == id + 1;
@@ -603,7 +642,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           float joint = -INFINITY, l = 0.0f;
           for (int w = 0; w < job.p.parts; ++w) joint = fmaxf(joint, __ldcg(ml + (size_t)w * 256).x);
           const float use = joint == -INFINITY ? 0.0f : joint;
-          auto weight_of = [&](float x) { return x == -INFINITY ? 1.0f : exp2_fast(x - use); };
+          auto weight_of = [&](float x) { return x == -INFINITY ? 1.0f : fast_exp2(x - use); };
           for (int w = 0; w < job.p.parts; ++w) {
             const float2 x = __ldcg(ml + (size_t)w * 256);
             l += x.y * weight_of(x.x);
