@@ -3,21 +3,25 @@
 // A piece is up to 256 rows (two tiles of 128) of one sequence and K/V head against a range of keys in tiles of 128; heads
 // that share K and V are rows side by side, so their keys come once.  One CTA per SM works off the pieces of its share.
 //
-// Tensor memory (512 columns): S of both tiles, 128 columns each; the rest is output.
-//   head dim 64:  a tile's 128 keys are two streams of 64, each with four softmax warps of its own (one thread = one row), its
-//                 own reference and its own 64 columns of output: the two halves of a row never speak to each other until
-//                 the end of the piece, where they are weighed against one another.  16 softmax warps.
-//   head dim 128: one stream of 128 keys a tile, 128 columns of output.  8 softmax warps; here the tensor cores are the bound.
-// P (bf16 pairs) goes over the start of the stream's own columns of S and is the second product's A operand.  The instructions
-// of a tile retire in order: Q K^T of the next key tile is issued behind the P V that reads the columns it writes, and when
-// its scores are reported, that P V has retired as well.  So a softmax warp that finds a row's maximum far above its reference
-// may scale the row's output right there.  While one tile waits for its products, the other's softmax runs.
+// Two threads share a row, 64 of a key tile's 128 keys each (streams; 16 softmax warps).  At head dim 64 the special-function unit
+// is the bound (16 exponentials a clock against 256 tensor operations for each), so all else is kept away from it and from
+// the issue slots: Q is an operand from tensor memory, and the second product's B operand carries a column of ones, so that
+// the tensor core adds up the bf16 probabilities that it multiplies.  At head dim 128 the tensor cores are the bound, and their
+// memory is full with S and O: Q comes from shared memory, the threads add up their own probabilities.
+// A row's reference is its maximum in the piece's first key tile, and it stays: p may grow to 2^60 in bf16 and 32-bit sums as
+// well as stay below 1.  Where it grows more (the row's sum tells, at the end of the piece), the piece is done again when
+// all others are through, with one sweep for the maxima first.
+// Tensor memory (512 columns): S of both tiles, 128 columns each; O of both, 80 columns (64 channels, the sum, 15 unused) or 128;
+// at head dim 64 Q of both, 32 columns.  P (bf16 pairs) goes over the start of the stream's own columns of S and is the second
+// product's A operand.  The instructions of a tile retire in order: a stream's next Q K^T is issued behind the P V that reads the
+// columns it writes.
 //
-// Warps: softmax; two MMA issuers (one per tile); one TMA producer; one that looks after V, or four that widen codes:
-//   bf16  K comes by TMA straight into its swizzled tile, V too; a tile of V that holds keys which some rows do not see passes
+// Warps: softmax; two MMA issuers (one per tile), a TMA producer, one that looks after V; for codes eight that widen them:
+//   bf16  K and V come by TMA straight into their swizzled tiles; a tile of V that holds keys which some rows do not see passes
 //         the V warp: what no row sees becomes zero (a page's tail may hold anything, and 0 * NaN is NaN), and values that
 //         are not finite are taken out; the softmax adds them to the rows that see them.
-//   E4M3  codes and exponents come by bulk copies into a ring of their own; the four warps widen them to the same tiles, exactly.
+//   E4M3  codes and exponents come by bulk copies into a ring of their own; the eight warps widen them to the same tiles,
+//         exactly, and look after V on the way.
 #include "exp2.cuh"
 #include "kv_cache.h"
 #include "kv_quant.cuh"
@@ -27,25 +31,29 @@ namespace lv {
 namespace {
 
 constexpr int kTileKeys = 128;
+// Head dim 64: of the 16 pairs of 32 scores, this many take their exponentials on the FMA pipes.
 #ifndef LV_KV_POLY
-#define LV_KV_POLY 0
+#define LV_KV_POLY 4
 #endif
+constexpr int kPolyPairs = LV_KV_POLY;
+constexpr int kStreams = 2;                  // of a tile: a row's two threads
+constexpr int kSoftmaxWarps = 8 * kStreams;
+constexpr int kKeys = kTileKeys / kStreams;  // of a stream's step
 
 template <int kHd, bool kNarrow>
 struct TiShape {
-  static constexpr int kStreams = kHd == 64 ? 2 : 1;  // of a tile
-  static constexpr int kKeys = kTileKeys / kStreams;  // of a stream's step
-  static constexpr int kSoftmaxWarps = 8 * kStreams;
-  static constexpr int kHelpers = kNarrow ? 4 : 1;
-  static constexpr int kThreads = (kSoftmaxWarps + 3 + kHelpers) * 32;
+  static constexpr bool kOnes = kHd == 64;    // the tensor core adds up the rows, and Q is in its memory
+  static constexpr int kHelpers = kNarrow ? 8 : 1;
+  static constexpr int kThreads = (kSoftmaxWarps + 4 + (kNarrow ? 8 : 0)) * 32;
   static constexpr int kStages = kHd == 64 ? (kNarrow ? 3 : 4) : 2;
   static constexpr int kRaw = kNarrow ? (kHd == 64 ? 3 : 1) : 0;
   static constexpr int kSubBytes = 128 * 128;             // 128 rows of 64 channels
   static constexpr int kTileBytes = kSubBytes * kHd / 64; // of Q, K or V
   static constexpr int kRawBytes = kTileKeys * kHd + kTileKeys;
-  static constexpr uint32_t kColO = 256;
-  static constexpr int kPolyPairs = LV_KV_POLY;  // of the 16 pairs of 32 scores, on the FMA pipes
-  static constexpr int kSmemBytes = 2 * kTileBytes + 2 * kStages * kTileBytes + 2 * kRaw * kRawBytes + (kStreams == 2 ? 8192 : 0) + 512 + 1024;
+  static constexpr int kOnesBytes = kOnes ? 16 * 128 : 0;
+  static constexpr uint32_t kColO = 256, kOCols = kOnes ? 80 : 128, kColQ = 416;
+  static constexpr int kQBytes = kOnes ? 0 : 2 * kTileBytes;
+  static constexpr int kSmemBytes = kQBytes + 2 * kStages * kTileBytes + kOnesBytes + 2 * kRaw * kRawBytes + 512 + 1024;
 };
 
 template <int kStages, int kRaw>
@@ -54,9 +62,30 @@ struct TiBarriers {
   uint64_t raw_full[2][kRaw > 0 ? kRaw : 1], raw_empty[2][kRaw > 0 ? kRaw : 1];  // [K, V]
   uint64_t q_ready[2], s_full[2][2], p_ready[2][2], o_done[2], teardown[2];
   uint32_t tmem_base, abort_flag;
-  int taken_out[2];  // a piece (its number + 1, by its parity) whose V held values that are not finite where not all rows see them
-  int last_of_join;
+  int taken_out[2];  // a piece (its number + 1, by the turn's parity) whose V held values that are not finite where not all rows see them
+  int again[2];      // a piece (likewise) that has to be done again
+  int any_again, last_of_join;
 };
+
+// 2^x for a pair of arguments on the FMA pipes: the nearest whole number n goes into the exponent field, a cubic gives the
+// power of the rest (relative error 7.5e-5, far below the rounding to bf16).  n is held to [-125, 125] by one integer
+// instruction, so what lies far outside comes out as next to nothing or as a number that no row's sum overlooks; the
+// polynomial carries the factor 2^-125 that the exponent is counted from.  x = -infinity does not come here (NaN).
+__device__ __forceinline__ float2 poly_exp2_clamped(float2 x) {
+  const float2 t = __fadd2_rn(x, make_float2(12582912.0f, 12582912.0f));
+  const float2 n = __fadd2_rn(t, make_float2(-12582912.0f, -12582912.0f));
+  const float2 f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
+  constexpr float k = 2.350988701644575e-38f;  // 2^-125
+  auto horner = [&](float2 p, float c) { return __ffma2_rn(p, f, make_float2(c, c)); };
+  float2 p = horner(make_float2(0.0551716648f * k, 0.0551716648f * k), 0.2426111251f * k);
+  p = horner(p, 0.6932609677f * k);
+  p = horner(p, 0.9999280572f * k);
+  constexpr int kBias = 0x4b400000 - 125;  // of t's bits
+  const int nx = __viaddmin_s32_relu(__float_as_int(t.x), -kBias, 250), ny = __viaddmin_s32_relu(__float_as_int(t.y), -kBias, 250);
+  return make_float2(__int_as_float(__float_as_int(p.x) + (nx << 23)), __int_as_float(__float_as_int(p.y) + (ny << 23)));
+}
+// What a row's sum has to stay below.
+constexpr float kSumLimit = 1.152921504606847e18f;  // 2^60
 
 __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(smem_dst)),
@@ -64,11 +93,6 @@ __device__ __forceinline__ void bulk_load(void* smem_dst, const void* src, uint3
                : "memory");
 }
 __device__ __forceinline__ void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-
-// A row's reference moves to its maximum when a step's probabilities add up to more than kLate, and then if that maximum lies
-// more than kSlack above it (base-2 units).  So no probability is over 2^20, which bf16 and sums in 32 bits hold as well
-// as 1; what a maximum 2^20 above the reference takes from the other end is keys under 2^-106 of it.
-constexpr float kLate = 1048576.0f, kSlack = 4.0f;
 
 // Of `from`, the latest loads (up to one a slot) have landed; they must before the shared memory is given up.
 template <int kSlots>
@@ -122,16 +146,17 @@ __global__ void __launch_bounds__(TiShape<kHd, kNarrow>::kThreads, 1)
 kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, KvPool pool, KvArrays arrays,
                      KvLaunch work, KvAttend at, uint32_t* status) {
   using Shape = TiShape<kHd, kNarrow>;
-  constexpr int kStreams = Shape::kStreams, kStages = Shape::kStages, kRaw = Shape::kRaw, kRawSlots = kRaw > 0 ? kRaw : 1, kSubs = kHd / 64;
+  constexpr bool kOnes = Shape::kOnes;
+  constexpr int kStages = Shape::kStages, kRaw = Shape::kRaw, kRawSlots = kRaw > 0 ? kRaw : 1, kSubs = kHd / 64;
   constexpr int kTileBytes = Shape::kTileBytes, kSubBytes = Shape::kSubBytes;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem_q = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* smem_k = smem_q + 2 * kTileBytes;
+  uint8_t* smem_k = smem_q + Shape::kQBytes;
   uint8_t* smem_v = smem_k + kStages * kTileBytes;
-  uint8_t* smem_codes = smem_v + kStages * kTileBytes;  // [K, V][slot] codes, then exponents
-  float2* smem_ml = reinterpret_cast<float2*>(smem_codes + 2 * kRaw * Shape::kRawBytes);  // [parity][tile][stream][row]
+  uint8_t* smem_ones = smem_v + kStages * kTileBytes;
+  uint8_t* smem_codes = smem_ones + Shape::kOnesBytes;  // [K, V][slot] codes, then exponents
   using Barriers = TiBarriers<kStages, kRaw>;
-  Barriers* bars = reinterpret_cast<Barriers*>(smem_ml + (kStreams == 2 ? 1024 : 0));
+  Barriers* bars = reinterpret_cast<Barriers*>(smem_codes + 2 * kRaw * Shape::kRawBytes);
   static_assert(sizeof(Barriers) <= 512, "");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -157,15 +182,24 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       mbar_init(&bars->o_done[t], 1);
       mbar_init(&bars->teardown[t], 1);
       bars->taken_out[t] = 0;
+      bars->again[t] = 0;
     }
     mbar_fence_init();
     bars->abort_flag = 0;
+    bars->any_again = 0;
     if constexpr (!kNarrow) {
       tma_prefetch_desc(&k_map);
       tma_prefetch_desc(&v_map);
     }
   }
-  constexpr int kIssuer = Shape::kSoftmaxWarps, kProducer = kIssuer + 2, kHelper = kIssuer + 3;
+  // The block behind V whose first column is 1 and whose other columns are 0: 16 key rows laid out like a V tile, the last 16
+  // of the second product's 80 columns.  Every instruction's descriptor carries the stride from its own V rows to it.
+  if (kOnes && threadIdx.x < Shape::kOnesBytes / 16) {
+    const int r = threadIdx.x >> 3, chunk = threadIdx.x & 7;
+    reinterpret_cast<uint4*>(smem_ones)[threadIdx.x] = make_uint4(chunk == (r & 7) ? 0x00003f80u : 0u, 0u, 0u, 0u);
+    fence_proxy_async_shared();
+  }
+  constexpr int kIssuer = kSoftmaxWarps, kProducer = kIssuer + 2, kHelper = kNarrow ? kIssuer + 4 : kIssuer + 3;
   if (warp == kIssuer) {
     tmem_alloc(&bars->tmem_base, 512);
     tmem_relinquish();
@@ -178,13 +212,32 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
   wait_for_previous_kernel();
   const int id0 = work.first[blockIdx.x], id_end = work.first[blockIdx.x + 1];
 
+  // Every role goes over the CTA's pieces; and a second time over those whose reference did not do, twice each: once for the
+  // maxima, once for the rows.
+  enum Mode { kFast = 0, kMaxima = 1, kCareful = 2 };
+  auto pieces = [&](auto run) {
+    for (int id = id0; id < id_end; ++id) {
+      run(id, kFast);
+      __syncwarp();
+    }
+    named_barrier(10, Shape::kThreads);
+    if (*reinterpret_cast<volatile int*>(&bars->any_again) == 0) return;
+    for (int id = id0; id < id_end; ++id)
+      if (__ldcg(work.again + id) != 0) {
+        run(id, kMaxima);
+        __syncwarp();
+        run(id, kCareful);
+        __syncwarp();
+      }
+  };
+
   if (warp == kProducer) {
     // ------------------------------------------------------------------ TMA producer: lane i fetches a tile's i-th page
     Ring ring;
     uint32_t issued[2] = {0, 0};
     bool ok = true;
     const int per_tile = kTileKeys >> pool.page_shift;
-    for (int id = id0; id < id_end && ok; ++id) {
+    pieces([&](int id, int) {
       const Job job = job_of(work, arrays, at, id);
       for (int j = 0; j < job.tiles && ok; ++j) {
         const int key = (job.tile0 + j) * kTileKeys;
@@ -227,62 +280,72 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         if constexpr (kNarrow) ring.next<kRawSlots>();
         else ring.next<kStages>();
       }
-    }
+    });
     if (lane == 0) {  // every load has landed before the CTA may go
       drain<kNarrow ? kRawSlots : kStages>(kNarrow ? bars->raw_full[0] : bars->k_full, issued[0], status);
       drain<kNarrow ? kRawSlots : kStages>(kNarrow ? bars->raw_full[1] : bars->v_land, issued[1], status);
     }
     __syncwarp();
   } else if (warp == kIssuer || warp == kIssuer + 1) {
-    // ------------------------------------------------------------------ MMA issuer of row tile t
-    if (elect_one()) {
-      const int t = warp - kIssuer;
-      constexpr uint32_t idesc_qk = umma_idesc_bf16(128, Shape::kKeys, false, false);
-      constexpr uint32_t idesc_pv = umma_idesc_bf16(128, kHd, false, true);
-      const uint32_t s_col = tmem_base + t * 128;
-      const uint32_t o_col = tmem_base + Shape::kColO + t * kStreams * kHd;
-      const uint64_t q_desc = smem_desc_sw128(smem_u32(smem_q + t * kTileBytes), 16, 1024);
-      const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem_k), 16, 1024);
-      const uint64_t v_desc0 = smem_desc_sw128(smem_u32(smem_v), kSubBytes, 1024);  // 64 channels further on: the next sub-tile
-      auto slot_at = [&](int slot) { return (uint64_t)((slot * kTileBytes) >> 4); };
-      auto issue_qk = [&](int c, int slot) {
+    // ------------------------------------------------------------------ MMA issuer of row tile t: one lane
+    const int t = warp - kIssuer;
+    constexpr uint32_t idesc_qk = umma_idesc_bf16(128, kKeys, false, false);
+    constexpr uint32_t idesc_pv = umma_idesc_bf16(128, Shape::kOCols, false, true);
+    const uint32_t s_col = tmem_base + t * 128, o_col = tmem_base + Shape::kColO + t * Shape::kOCols, q_col = tmem_base + Shape::kColQ + t * 32;
+    const uint64_t q_desc = smem_desc_sw128(smem_u32(smem_q + t * kTileBytes), 16, 1024);
+    const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem_k), 16, 1024);
+    // V's next 64 columns: the ones, behind the ring, or the next sub-tile.  x 16-byte units into the ring the stride to the
+    // ones (bits 16-29) shrinks by what the address grows.
+    const uint64_t v_desc0 = smem_desc_sw128(smem_u32(smem_v), kOnes ? kStages * kTileBytes : kSubBytes, 1024);
+    auto v_desc_at = [&](uint32_t x) { return kOnes ? v_desc0 + x - ((uint64_t)x << 16) : v_desc0 + x; };
+    auto issue_qk = [&](int c, int slot) {
 #pragma unroll
-        for (int k = 0; k < kHd / 16; ++k) {
-          const uint64_t in_tile = (uint64_t)(((k >> 2) * kSubBytes + (k & 3) * 32) >> 4);
-          umma_ss(s_col + c * 64, q_desc + in_tile, k_desc0 + slot_at(slot) + (uint64_t)(c * 512) + in_tile, idesc_qk, k != 0 ? 1u : 0u);
-        }
-        umma_commit(&bars->s_full[t][c]);
-      };
-      Ring ring;
-      uint32_t step = 0, round = 0;
-      bool ok = true;
-      for (int id = id0; id < id_end && ok; ++id) {
+      for (int k = 0; k < kHd / 16; ++k) {
+        const uint64_t in_tile = (uint64_t)(((k >> 2) * kSubBytes + (k & 3) * 32) >> 4);
+        const uint64_t k_desc = k_desc0 + (uint64_t)((slot * kTileBytes) >> 4) + (uint64_t)(c * 512) + in_tile;
+        if constexpr (kOnes) umma_ts(s_col + c * 64, q_col + k * 8, k_desc, idesc_qk, k != 0 ? 1u : 0u);
+        else umma_ss(s_col + c * 64, q_desc + in_tile, k_desc, idesc_qk, k != 0 ? 1u : 0u);
+      }
+      umma_commit(&bars->s_full[t][c]);
+    };
+    Ring ring;
+    uint32_t step = 0, round = 0;
+    bool ok = true;
+    pieces([&](int id, int mode) {
+      if (elect_one()) {  // the same lane every time
+        if (!ok) return;
         const Job job = job_of(work, arrays, at, id);
         const int mine = tiles_of(job, at, t);
         if (mine > 0) {
           ok = mbar_wait(&bars->q_ready[t], round & 1u, ctl) && mbar_wait(&bars->k_full[ring.slot], ring.phase, ctl);
-          if (!ok) break;
-          tc_fence_after();
+          if (ok) {
+            tc_fence_after();
 #pragma unroll
-          for (int c = 0; c < kStreams; ++c) issue_qk(c, ring.slot);
-          umma_commit(&bars->k_empty[ring.slot]);
+            for (int c = 0; c < kStreams; ++c) issue_qk(c, ring.slot);
+            umma_commit(&bars->k_empty[ring.slot]);
+          }
         }
         for (int j = 0; j < job.tiles && ok; ++j) {
           Ring next = ring;
           next.next<kStages>();
           if (j < mine) {
             ok = mbar_wait(&bars->v_full[ring.slot], ring.phase, ctl);
-            if (ok && j + 1 < mine) ok = mbar_wait(&bars->k_full[next.slot], next.phase, ctl);
 #pragma unroll
             for (int c = 0; c < kStreams; ++c) {
               ok = ok && mbar_wait(&bars->p_ready[t][c], step & 1u, ctl);
               if (!ok) break;
               tc_fence_after();
+              if (mode != kMaxima) {
 #pragma unroll
-              for (int k = 0; k < Shape::kKeys / 16; ++k)
-                umma_ts(o_col + c * kHd, s_col + c * 64 + k * 8, v_desc0 + slot_at(ring.slot) + (uint64_t)(((c * 64 + k * 16) * 128) >> 4),
-                        idesc_pv, (j | k) != 0 ? 1u : 0u);
-              if (j + 1 < mine) issue_qk(c, next.slot);  // where these probabilities were
+                for (int k = 0; k < kKeys / 16; ++k)
+                  umma_ts(o_col, s_col + c * 64 + k * 8, v_desc_at((uint32_t)((ring.slot * kTileBytes + (c * 64 + k * 16) * 128) >> 4)),
+                          idesc_pv, (j | c | k) != 0 ? 1u : 0u);
+              }
+              if (j + 1 < mine) {
+                if (c == 0 && !(ok = mbar_wait(&bars->k_full[next.slot], next.phase, ctl))) break;
+                tc_fence_after();
+                issue_qk(c, next.slot);  // where these probabilities were
+              }
             }
             if (!ok) break;
             umma_commit(&bars->v_empty[ring.slot]);
@@ -299,20 +362,23 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
         round += mine > 0 ? 1u : 0u;
       }
-      if (!ok) {  // what is under way must have retired before tensor memory is given up
-        umma_commit(&bars->teardown[t]);
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&bars->teardown[t], 0)) {
-          if (clock64() - t0 > kTimeoutCycles) break;
-        }
+    });
+    __syncwarp();
+    if (elect_one() && !ok) {  // what is under way must have retired before tensor memory is given up
+      umma_commit(&bars->teardown[t]);
+      const long long t0 = clock64();
+      while (!mbar_try_wait(&bars->teardown[t], 0)) {
+        if (clock64() - t0 > kTimeoutCycles) break;
       }
     }
     __syncwarp();
   } else if (warp >= kHelper) {
     // ------------------------------------------------------------------ V (and what is held in codes)
     Ring ring, raw;
+    uint32_t turn = 0;
     bool ok = true;
-    for (int id = id0; id < id_end && ok; ++id) {
+    pieces([&](int id, int) {
+      const uint32_t parity = turn++ & 1u;
       const Job job = job_of(work, arrays, at, id);
       for (int j = 0; j < job.tiles && ok; ++j) {
         const int key = (job.tile0 + j) * kTileKeys;
@@ -330,9 +396,9 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             uint8_t* tile = (x == 0 ? smem_k : smem_v) + ring.slot * kTileBytes;
             bool bad = false;
             constexpr int kPerRow = kHd / 16;  // 16 codes at a time
-#pragma unroll 4
-            for (int i = 0; i < kPerRow; ++i) {
-              const int piece = i * 128 + tid, r = piece / kPerRow, ch = piece % kPerRow;
+#pragma unroll 2
+            for (int i = 0; i < kPerRow / 2; ++i) {
+              const int piece = i * 256 + tid, r = piece / kPerRow, ch = piece % kPerRow;
               const uint4 w4 = *reinterpret_cast<const uint4*>(codes + piece * 16);
               const uint32_t byte = exps[r], w[4] = {w4.x, w4.y, w4.z, w4.w};
               const KvFactor f = kv_factor(byte);
@@ -361,7 +427,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
               *reinterpret_cast<uint4*>(row + (((2 * ch) & 7) ^ (r & 7)) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
               *reinterpret_cast<uint4*>(row + (((2 * ch + 1) & 7) ^ (r & 7)) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
             }
-            if (bad) *reinterpret_cast<volatile int*>(&bars->taken_out[id & 1]) = id + 1;
+            if (bad) *reinterpret_cast<volatile int*>(&bars->taken_out[parity]) = id + 1;
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) {
@@ -394,7 +460,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
                 if (here) *at_row = make_uint4(v[0], v[1], v[2], v[3]);
                 bad = bad || here;
               }
-            if (bad) *reinterpret_cast<volatile int*>(&bars->taken_out[id & 1]) = id + 1;
+            if (bad) *reinterpret_cast<volatile int*>(&bars->taken_out[parity]) = id + 1;
             fence_proxy_async_shared();
           }
           __syncwarp();
@@ -402,17 +468,33 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
         ring.next<kStages>();
       }
-    }
+    });
+  } else if (warp >= kIssuer) {
+    pieces([](int, int) {});  // (beside the warps that widen codes there is nothing left for the fourth)
   } else {
-    // ------------------------------------------------------------------ softmax: a thread is a row (of a stream)
+    // ------------------------------------------------------------------ softmax: a thread is a row, or the half of one
     const int t = warp / (4 * kStreams), c = (warp >> 2) % kStreams, quarter = warp & 3;
     const int r = quarter * 32 + lane;  // within the tile
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_addr = tmem_base + lane_base + t * 128 + c * 64;
-    const uint32_t o_tile = tmem_base + lane_base + Shape::kColO + t * kStreams * kHd, o_addr = o_tile + c * kHd;
-    uint32_t step = 0, round = 0;
+    const uint32_t o_addr = tmem_base + lane_base + Shape::kColO + t * Shape::kOCols;
+    uint32_t step = 0, round = 0, turn = 0;
     bool ok = true;
-    for (int id = id0; id < id_end; ++id) {
+    float kept = -INFINITY;  // the row's maximum, from one sweep to the next
+    auto largest = [](const uint32_t (&s)[32]) {
+      float m[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t* x = &s[8 * i];
+        m[i] = fmax3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
+        m[i] = fmax3(m[i], __uint_as_float(x[3]), __uint_as_float(x[4]));
+        m[i] = fmax3(m[i], __uint_as_float(x[5]), __uint_as_float(x[6]));
+        m[i] = fmaxf(m[i], __uint_as_float(x[7]));
+      }
+      return fmaxf(fmax3(m[0], m[1], m[2]), m[3]);
+    };
+    pieces([&](int id, int mode) {
+      const uint32_t parity = turn++ & 1u;
       const Job job = job_of(work, arrays, at, id);
       const int mine = tiles_of(job, at, t);
       const bool live = t * 128 + r < job.p.rows;
@@ -426,161 +508,172 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         uint4 x[kChunks];
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) x[i] = live ? ldg16(src + (c * kChunks + i) * 8) : make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (kOnes) {
+          uint32_t w[16];
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-          const int ch = c * kChunks + i;
-          *reinterpret_cast<uint4*>(smem_q + t * kTileBytes + (ch >> 3) * kSubBytes + r * 128 + ((ch & 7) ^ (r & 7)) * 16) = x[i];
+          for (int i = 0; i < 4; ++i) w[4 * i] = x[i].x, w[4 * i + 1] = x[i].y, w[4 * i + 2] = x[i].z, w[4 * i + 3] = x[i].w;
+          tmem_st16(tmem_base + lane_base + Shape::kColQ + t * 32 + c * 16, w);
+          tmem_st_wait();
+          tc_fence_before();
+        } else {
+#pragma unroll
+          for (int i = 0; i < kChunks; ++i)
+            *reinterpret_cast<uint4*>(smem_q + t * kTileBytes + c * kSubBytes + r * 128 + (i ^ (r & 7)) * 16) = x[i];
+          fence_proxy_async_shared();
         }
-        fence_proxy_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars->q_ready[t]);
       }
-      float top = -INFINITY, ref = 0.0f;  // ref: top once that is finite
-      float2 sum = make_float2(0.0f, 0.0f);
       const int first_seen = __shfl_sync(0xffffffffu, live ? seen : 0x7fffffff, 0);  // rows of a warp see ever more
+      float top = -INFINITY, ref = 0.0f;  // the row's reference; ref: what is subtracted, top where that is finite
+      float2 sum = make_float2(0.0f, 0.0f);
 
-      // One step: 64 or 128 scores of the row.  With kEdge some rows of the warp do not see all of its keys.
-      constexpr int kGroups = Shape::kKeys / 32;
-      bool unset = true;  // a row of the warp has no reference yet
-      auto take_step = [&](auto edge_constant, int key, bool first) {
-        constexpr bool kEdge = decltype(edge_constant)::value;
-        auto load = [&](int g, uint32_t (&s)[32]) {
-          tmem_ld32(s_addr + g * 32, s);
-          tmem_ld_wait();
-          if constexpr (kEdge) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (key + g * 32 + i >= seen) s[i] = 0xff800000u;
-          }
-        };
-        // The row's maximum becomes its reference where it lies far above the present one.
-        auto refer = [&]() {
-          float most = -INFINITY;
-#pragma unroll 1
-          for (int g = 0; g < kGroups; ++g) {
-            uint32_t s[32];
-            load(g, s);
-            float m[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t* x = &s[8 * i];
-              m[i] = fmax3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
-              m[i] = fmax3(m[i], __uint_as_float(x[3]), __uint_as_float(x[4]));
-              m[i] = fmax3(m[i], __uint_as_float(x[5]), __uint_as_float(x[6]));
-            }
-            most = fmax3(most, fmax3(m[0], m[1], __uint_as_float(s[7])), fmax3(m[2], m[3], __uint_as_float(s[15])));
-            most = fmax3(most, __uint_as_float(s[23]), __uint_as_float(s[31]));
-          }
-          most *= at.scale_log2;
-          const bool move = most > top + kSlack;
-          const float factor = move ? (top == -INFINITY ? 0.0f : fast_exp2(ref - most)) : 1.0f;
-          if (move) {
-            top = ref = most;
-            sum.x *= factor;
-            sum.y *= factor;
-          }
-          unset = __any_sync(0xffffffffu, top == -INFINITY);
-          if (!first) {
-#pragma unroll 1
-            for (int g = 0; g < kHd / 16; ++g) {
-              uint32_t o[16];
-              tmem_ld16(o_addr + g * 16, o);
-              tmem_ld_wait();
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
-              tmem_st16(o_addr + g * 16, o);
-            }
-          }
-        };
-        // Only a row's first keys are asked for their maximum.  After that its probabilities are taken under the reference
-        // that it has; they tell by themselves when it has fallen too far behind, before anything has been put in the place of
-        // the scores: then the reference moves and they are taken again.
-        uint32_t p[kGroups][16];
-        float2 more;
-#pragma unroll 1
-        for (bool again = false;; again = true) {
-          if (unset || again) refer();
-          const float2 scale2 = make_float2(at.scale_log2, at.scale_log2), ref2 = make_float2(-ref, -ref);
-          more = make_float2(0.0f, 0.0f);
-#pragma unroll
-          for (int g = 0; g < kGroups; ++g) {
-            uint32_t s[32];
-            load(g, s);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, ref2);
-              if (i < Shape::kPolyPairs) {
-                x = poly_exp2_pair(make_float2(fminf(fmax_nan(x.x, -126.0f), 120.0f), fminf(fmax_nan(x.y, -126.0f), 120.0f)));
-              } else {
-                x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
-              }
-              p[g][i] = pack_bf16(x.x, x.y);
-              // Where a row may see few keys, the sum is that of the rounded probabilities, so that their rounding changes only
-              // what a key weighs among the others; elsewhere it averages out.
-              more = __fadd2_rn(more, kEdge ? make_float2(bf16_lo(p[g][i]), bf16_hi(p[g][i])) : x);
-            }
-          }
-          if (again || !__any_sync(0xffffffffu, !(more.x + more.y <= kLate))) break;
-        }
-        sum = __fadd2_rn(sum, more);
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) tmem_st16(s_addr + g * 16, p[g]);
+      auto key_of = [&](int j) { return (job.tile0 + j) * kTileKeys + c * 64; };
+      auto scores_in = [&]() {
+        const bool in = mbar_wait_warp(&bars->s_full[t][c], step & 1u, ctl);
+        if (in) tc_fence_after();
+        return in;
       };
-      for (int j = 0; j < mine && ok; ++j, ++step) {
-        ok = mbar_wait_warp(&bars->s_full[t][c], step & 1u, ctl);
-        if (!ok) break;
-        tc_fence_after();
-        const int key = (job.tile0 + j) * kTileKeys + c * 64;
-        if (key + Shape::kKeys > first_seen) take_step(std::true_type{}, key, j == 0);
-        else take_step(std::false_type{}, key, j == 0);
+      auto give_p = [&]() {
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars->p_ready[t][c]);
+      };
+      // This thread's 64 scores of a step.  With kEdge some rows of the warp may not see all of its keys.
+      uint32_t s[2][32];
+      auto load = [&](bool edge, int key) {
+        tmem_ld32(s_addr, s[0]);
+        tmem_ld32(s_addr + 32, s[1]);
+        tmem_ld_wait();
+        if (edge) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (key + g * 32 + i >= seen) s[g][i] = 0xff800000u;
+        }
+      };
+      auto take_half = [&](auto edge_constant, int key) {
+        constexpr bool kEdge = decltype(edge_constant)::value;
+        load(kEdge, key);
+        const float2 scale2 = make_float2(at.scale_log2, at.scale_log2), ref2 = make_float2(-ref, -ref);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float2 x = __ffma2_rn(make_float2(__uint_as_float(s[g][2 * i]), __uint_as_float(s[g][2 * i + 1])), scale2, ref2);
+            if (!kEdge && i < kPolyPairs) x = poly_exp2_clamped(x);
+            else x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+            p[i] = pack_bf16(x.x, x.y);
+            // Where a row may see few keys, the sum is that of the rounded probabilities, so that their rounding changes only
+            // what a key weighs among the others; elsewhere it averages out.
+            if constexpr (!kOnes) sum = __fadd2_rn(sum, kEdge ? make_float2(bf16_lo(p[i]), bf16_hi(p[i])) : x);
+          }
+          tmem_st16(s_addr + g * 16, p);
+        }
+      };
+      float most = -INFINITY;
+      auto add_maximum = [&](int key) {
+        load(key + 64 > first_seen, key);
+        most = fmaxf(most, fmaxf(largest(s[0]), largest(s[1])));
+      };
+      // The two threads of a row tell each other a number, by way of two columns of tensor memory that nothing else uses just
+      // now.  Both come here whatever became of their waits.
+      auto exchange = [&](uint32_t column, uint32_t apart, float own) {
+        tmem_st1(column + c * apart, __float_as_uint(own));
+        tmem_st_wait();
+        tc_fence_before();
+        named_barrier(1 + t * 4 + quarter, 64);
+        tc_fence_after();
+        uint32_t both[2];
+        tmem_ld1(column, both[0]);
+        tmem_ld1(column + apart, both[1]);
+        tmem_ld_wait();
+        return make_float2(__uint_as_float(both[0]), __uint_as_float(both[1]));  // in the same order for both
+      };
+      // They agree on its maximum: each where its part of the output before has been read, and the next has not begun.
+      auto agree = [&]() {
+        const float2 both = exchange(o_addr, kHd / 2, most);
+        top = fmaxf(both.x, both.y) * at.scale_log2;
+      };
+      if (mine > 0) {
+        if (mode == kFast) {
+          ok = ok && scores_in();
+          if (ok) add_maximum(key_of(0));
+          agree();
+        } else if (mode == kMaxima) {
+          for (int j = 0; j < mine && ok; ++j, ++step) {
+            ok = scores_in();
+            if (!ok) break;
+            add_maximum(key_of(j));
+            give_p();
+          }
+          agree();
+          kept = top;
+        } else {
+          top = kept;
+        }
+        ref = top == -INFINITY ? 0.0f : top;
+        if (mode != kMaxima) {
+          for (int j = 0; j < mine && ok; ++j, ++step) {
+            ok = scores_in();
+            if (!ok) break;
+            if (mode == kCareful || key_of(j) + 64 > first_seen) take_half(std::true_type{}, key_of(j));
+            else take_half(std::false_type{}, key_of(j));
+            give_p();
+          }
+        }
       }
       if (mine > 0) {
         ok = ok && mbar_wait_warp(&bars->o_done[t], round & 1u, ctl);
         ++round;
         tc_fence_after();
       }
+      if (mode == kMaxima) return;
 
       // ---------------------------------------------------------------- the piece's rows
-      float row_sum = sum.x + sum.y, m = top, weight[kStreams];
-      weight[0] = 1.0f;
-      if constexpr (kStreams == 2) {
-        float2* ml = smem_ml + ((id & 1) * 2 + t) * 256;
-        ml[c * 128 + r] = make_float2(top, row_sum);
-        named_barrier(1 + t * 4 + quarter, 64);
-        const float2 a = ml[r], b = ml[128 + r];
-        m = fmaxf(a.x, b.x);
-        const float m_use = m == -INFINITY ? 0.0f : m;
-        weight[0] = a.x == -INFINITY ? 1.0f : fast_exp2(a.x - m_use);  // without a key so far: its sum and rows are zero
-        weight[1] = b.x == -INFINITY ? 1.0f : fast_exp2(b.x - m_use);
-        row_sum = a.y * weight[0] + b.y * weight[1];
+      const bool has = live && seen > job.p.key0;  // the row sees keys of this piece
+      float row_sum = sum.x + sum.y;
+      if constexpr (kOnes) {
+        if (mine > 0) {
+          uint32_t l;
+          tmem_ld1(o_addr + 64, l);
+          tmem_ld_wait();
+          row_sum = has ? __uint_as_float(l) : 0.0f;
+        }
+      } else if (mine > 0) {
+        const float2 both = exchange(s_addr - c * 64, 64, row_sum);  // where the last scores were
+        row_sum = both.x + both.y;
       }
-      const bool bad = *reinterpret_cast<volatile int*>(&bars->taken_out[id & 1]) == id + 1;
+      const bool bad = *reinterpret_cast<volatile int*>(&bars->taken_out[parity]) == id + 1;
       const bool whole = job.p.slot < 0;
-      const float inverse = whole ? (seen > 0 ? 1.0f / row_sum : 0.0f) : 1.0f;
+      const float inverse = whole && seen > 0 ? 1.0f / row_sum : 1.0f;
       constexpr int kMine = kHd / kStreams / 32;  // groups of 32 channels of this thread
 #pragma unroll 1
       for (int g = 0; g < kMine; ++g) {
-        const int ch0 = (kStreams == 2 ? c : g) * 32;
+        const int ch0 = (c * kMine + g) * 32;
         float acc[32];
         if (mine > 0) {
           uint32_t o[32];
-          tmem_ld32(o_tile + ch0, o);
+          tmem_ld32(o_addr + ch0, o);
           tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc[i] = __uint_as_float(o[i]) * weight[0];
-          if constexpr (kStreams == 2) {
-            tmem_ld32(o_tile + kHd + ch0, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) acc[i] = fmaf(__uint_as_float(o[i]), weight[kStreams - 1], acc[i]);
-          }
+          for (int i = 0; i < 32; ++i) acc[i] = __uint_as_float(o[i]);
         } else {
 #pragma unroll
           for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
+        }
+        if (mode == kFast && has) {
+          float zero = 0.0f;  // NaN where something is not finite
+#pragma unroll
+          for (int i = 0; i < 32; ++i) zero = fmaf(acc[i], 0.0f, zero);
+          if (!(row_sum > 0.0f && row_sum < kSumLimit && zero == 0.0f)) {
+            *reinterpret_cast<volatile int*>(work.again + id) = 1;
+            *reinterpret_cast<volatile int*>(&bars->again[parity]) = id + 1;
+            *reinterpret_cast<volatile int*>(&bars->any_again) = 1;
+          }
         }
         if (bad && live) {
           // values that were taken out of V, for the rows that see them
@@ -626,16 +719,19 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       }
       tc_fence_before();
       if (!whole) {
-        if (c == 0) __stcg(reinterpret_cast<float2*>(work.sums) + (size_t)job.p.slot * 256 + t * 128 + r, make_float2(m, row_sum));
-        // whoever comes last adds the parts up, in their order
+        if (c == 0) __stcg(reinterpret_cast<float2*>(work.sums) + (size_t)job.p.slot * 256 + t * 128 + r, make_float2(top, row_sum));
+        // whoever comes last adds the parts up, in their order; a piece that is to be done again has not come
         __threadfence();
-        named_barrier(9, Shape::kSoftmaxWarps * 32);
+        named_barrier(9, kSoftmaxWarps * 32);
         if (threadIdx.x == 0) {
-          const int before = atomicAdd(work.joins + job.p.join, 1);
-          bars->last_of_join = before == job.p.parts - 1;
-          if (before == job.p.parts - 1) work.joins[job.p.join] = 0;
+          int last = 0;
+          if (mode == kCareful || *reinterpret_cast<volatile int*>(&bars->again[parity]) != id + 1) {
+            last = atomicAdd(work.joins + job.p.join, 1) == job.p.parts - 1 ? 1 : 0;
+            if (last) work.joins[job.p.join] = 0;
+          }
+          *reinterpret_cast<volatile int*>(&bars->last_of_join) = last;
         }
-        named_barrier(9, Shape::kSoftmaxWarps * 32);
+        named_barrier(9, kSoftmaxWarps * 32);
         if (*reinterpret_cast<volatile int*>(&bars->last_of_join) != 0 && live) {
           __threadfence();
           const float2* ml = reinterpret_cast<const float2*>(work.sums) + (size_t)job.p.first_slot * 256 + t * 128 + r;
@@ -650,7 +746,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           const float inv = 1.0f / l;
 #pragma unroll 1
           for (int g = 0; g < kMine; ++g) {
-            const int ch0 = (kStreams == 2 ? c : g) * 32;
+            const int ch0 = (c * kMine + g) * 32;
             float acc[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
@@ -676,14 +772,17 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             }
           }
         }
-        named_barrier(9, Shape::kSoftmaxWarps * 32);  // last_of_join has been read
+        named_barrier(9, kSoftmaxWarps * 32);  // last_of_join has been read
       }
-    }
+    });
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (warp == kIssuer) tmem_dealloc(tmem_base, 512);
+  if (bars->any_again != 0) {
+    for (int id = id0 + (int)threadIdx.x; id < id_end; id += Shape::kThreads) work.again[id] = 0;
+  }
 }
 
 template <int kHd, bool kNarrow>

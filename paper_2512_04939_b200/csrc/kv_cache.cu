@@ -194,12 +194,13 @@ void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int hea
     p->pieces = take(w.pieces.size() * sizeof(KvPiece));
     p->first = take(w.first.size() * sizeof(int));
     p->joins = take((size_t)w.joins * sizeof(int));
+    p->again = take(w.pieces.size() * sizeof(int));
   };
   b->o_seqs = take(b->seqs.size() * sizeof(KvSeq));
   b->o_pages = take(n_pages * sizeof(int));
   take_lists(b->few, &b->at_few);
   take_lists(b->tiles, &b->at_tiles);
-  b->image.assign(at, 0);  // the counters start at zero
+  b->image.assign(at, 0);  // counters and marks start at zero
   // the two launches follow one another, and so use the same memory
   const size_t parts[2] = {(size_t)b->few.slots * kKvFewRows, (size_t)b->tiles.slots * kKvTileRows};
   const size_t most = std::max(parts[0], parts[1]);

@@ -51,48 +51,34 @@ struct KvCut {
   double overhead; // of a piece, in units
 };
 
-// Cuts the rows of the sequences in `which` into pieces.  All pieces in a row, every worker takes an equal share of what
-// they cost, so a launch ends at the same time everywhere whatever the lengths; a share's border cuts the keys of the
-// rows that it falls into.
-inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& which, int group, int kv_heads, int causal_block,
-                     const KvCut& cut) {
-  KvWork work;
-  // cost of a unit of `rows` rows: what fills less than half of the rows takes less than the full block, but not half
-  auto unit_cost = [&](int rows) { return 2 * rows <= cut.row_block ? 0.65 : 1.0; };
-  auto units_of = [&](const KvSeq& q, int row0, int rows) {
-    const int seen = kv_seen(q.len, q.rows, causal_block, (row0 + rows - 1) / group);
-    return seen > 0 ? (seen - 1) / cut.unit + 1 : 0;
-  };
-  double total = 0.0;
-  for (int s : which) {
-    const KvSeq& q = seqs[(size_t)s];
-    const int rows = q.rows * group;
-    double one_head = 0.0;
-    for (int r = 0; r < rows; r += cut.row_block) {
-      const int n = std::min(cut.row_block, rows - r);
-      one_head += units_of(q, r, n) * unit_cost(n) + cut.overhead;
-    }
-    total += one_head * kv_heads;
-  }
-  if (total <= 0.0) return work;
-  // (nearly every worker's border cuts some rows in two, which makes one more piece)
-  const double share = std::max(total / cut.workers + cut.overhead, cut.min_units + cut.overhead);
-  double spent = 0.0;
+// Cost of a unit of `rows` rows: what fills less than half of the rows takes less than the full block, but not half.
+inline double kv_unit_cost(const KvCut& cut, int rows) { return 2 * rows <= cut.row_block ? 0.65 : 1.0; }
+
+// What a pass over the rows found: the last worker takes what is left when the others have their shares.
+inline double kv_cut_by(double share, const std::vector<KvSeq>& seqs, const std::vector<int>& which, int group, int kv_heads,
+                        int causal_block, const KvCut& cut, KvWork* out) {
+  KvWork& work = *out;
+  work = KvWork();
+  double spent = 0.0;   // of all shares
+  double begun = 0.0;   // when the present worker began
   int worker = 0;
   work.first.push_back(0);
   auto next_worker = [&]() {
     if (worker + 1 >= cut.workers || (size_t)work.first.back() == work.pieces.size()) return false;
     work.first.push_back((int)work.pieces.size());
     ++worker;
+    begun = spent;
     return true;
   };
   for (int s : which) {
     const KvSeq& q = seqs[(size_t)s];
+    const int all = q.rows * group;
     for (int h = 0; h < kv_heads; ++h)
-      for (int r = 0; r < q.rows * group; r += cut.row_block) {
-        const int n = std::min(cut.row_block, q.rows * group - r);
-        const int units = units_of(q, r, n), seen = units > 0 ? kv_seen(q.len, q.rows, causal_block, (r + n - 1) / group) : 0;
-        const double cost = unit_cost(n);
+      for (int r = 0; r < all; r += cut.row_block) {
+        const int n = std::min(cut.row_block, all - r);
+        const int seen = std::max(kv_seen(q.len, q.rows, causal_block, (r + n - 1) / group), 0);
+        const int units = (int)(((long long)seen + cut.unit - 1) / cut.unit);
+        const double cost = kv_unit_cost(cut, n);
         const size_t begin = work.pieces.size();
         int done = 0;
         do {
@@ -105,7 +91,7 @@ inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& whi
           KvPiece p{};
           p.seq = s; p.kv_head = h; p.row0 = r; p.rows = n;
           p.key0 = done * cut.unit;
-          p.key1 = std::min((done + take) * (long long)cut.unit, (long long)seen);
+          p.key1 = (int)std::min((long long)(done + take) * cut.unit, (long long)seen);
           p.slot = -1;
           work.pieces.push_back(p);
           done += take;
@@ -125,6 +111,35 @@ inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& whi
       }
   }
   work.first.push_back((int)work.pieces.size());
+  return spent - begun;
+}
+
+// Cuts the rows of the sequences in `which` into pieces.  All pieces in a row, every worker takes an equal share of what
+// they cost, so a launch ends at the same time everywhere whatever the lengths; a share's border cuts the keys of the
+// rows that it falls into.
+inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& which, int group, int kv_heads, int causal_block,
+                     const KvCut& cut) {
+  KvWork work;
+  double total = 0.0;
+  for (int s : which) {
+    const KvSeq& q = seqs[(size_t)s];
+    const int all = q.rows * group;
+    double one_head = 0.0;
+    for (int r = 0; r < all; r += cut.row_block) {
+      const int n = std::min(cut.row_block, all - r);
+      const int seen = std::max(kv_seen(q.len, q.rows, causal_block, (r + n - 1) / group), 0);
+      one_head += (double)(((long long)seen + cut.unit - 1) / cut.unit) * kv_unit_cost(cut, n) + cut.overhead;
+    }
+    total += one_head * kv_heads;
+  }
+  if (total <= 0.0) return work;
+  // How many pieces the borders make is known only afterwards: what the last worker has too much goes to all.
+  double share = std::max(total / cut.workers + cut.overhead, cut.min_units + cut.overhead);
+  for (int pass = 0; pass < 4; ++pass) {
+    const double last = kv_cut_by(share, seqs, which, group, kv_heads, causal_block, cut, &work);
+    if (last <= 1.02 * share) break;
+    share += (last - share) / cut.workers + 0.002 * share;
+  }
   return work;
 }
 
