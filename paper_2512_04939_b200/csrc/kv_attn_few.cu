@@ -1,15 +1,21 @@
 // Attention of few rows over a paged K/V cache: single tokens, drafts of a few, heads that share K and V.
 //   o_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c q_i k_j - m_i)  for the keys j that row i sees
 // A piece is up to 16 rows of one sequence and K/V head (tokens times the query heads that share it) against a range of
-// keys.  All that counts is that K and V come from memory once and at its full rate: 4 operations a byte at one row.  A warp takes 16
-// (or 32) keys at a time straight from global memory into the fragments of mma.m16n8k16; there is no shared memory and no
-// barrier on the way.  Which lane loads which 16 bytes follows from the fragments:
-//   S = Q K^T   B holds K[key = lane / 4][channels of lane % 4]: the four lanes of a key take 16 bytes each of its row, and the
-//               contraction runs over the channels in the order in which they arrive (Q is loaded in the same order)
-//   O = P V     B holds V[keys 2q, 2q + 1, 2q + 8, 2q + 9 with q = lane % 4][channel of lane / 4]: a lane loads 8 (or 16)
+// keys.  All that counts is that K and V come from memory once and at its full rate: 4 operations a byte at one row.
+//
+// Every warp has a ring of its own in shared memory, which it fills itself (TMA boxes of 16 keys, or bulk copies of codes) and
+// which runs on from piece to piece, so that loads are under way whatever the warp is doing; the warps of a CTA take
+// turns on a piece's keys, each with a softmax reference of its own, and meet once at its end.  From the ring the keys go
+// straight into the fragments of mma.m16n8k16.  Which lane reads which bytes follows from the fragments:
+//   S = Q K^T   B holds K[key = lane / 4][channels of lane % 4]: the four lanes of a key read 16 bytes each of its row, and the
+//               contraction runs over the channels in the order in which they come (Q is loaded in the same order)
+//   O = P V     B holds V[keys 2q, 2q + 1, 2q + 8, 2q + 9 with q = lane % 4][channel of lane / 4]: a lane reads 8 (or 16)
 //               channels of those four keys and pairs them up with byte permutations; its accumulators' keys in S are the same
 //               ones, so P goes from accumulator to operand without leaving the lane
-// The warps of a CTA take turns on a piece's keys, each with a softmax reference of its own; they meet once at its end.
+// Codes are widened to f16, which takes one conversion for two of them.  Their powers of two stay outside: a key's scales its
+// scores, a value's its probability, relative to the largest that the warp has met.  Q goes to f16 under a power of two of its
+// row (exact but for elements 2^-38 under the row's largest); P has 11 bits there, not 8, down to 2^-14 of a row's largest
+// weight, and fixed steps of 2^-31 below.
 #include "exp2.cuh"
 #include "kv_cache.h"
 #include "kv_quant.cuh"
@@ -18,151 +24,226 @@ namespace lv {
 
 namespace {
 
+template <bool kHalfFloat>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  if constexpr (kHalfFloat) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  } else {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  }
 }
-__device__ __forceinline__ uint4 load16(const uint8_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+// Two codes (the low or the high half of a word) to two f16 numbers, exactly.
+__device__ __forceinline__ uint32_t widen_low(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint32_t widen_high(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint4 lds16(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_dst), "l"(src),
+               "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
 
 // The reference may lag this far behind a row's maximum (base-2 units) before the row is scaled anew.
 constexpr float kFewSlack = 8.0f;
-
-// One sub-step: 16 keys of K and V as they lie in memory.
-template <int kHd, bool kNarrow>
-struct FewKeys {
-  static constexpr int kKLoads = kHd * (kNarrow ? 1 : 2) / 64;  // of 16 bytes, for each of two keys
-  static constexpr int kVLoads = kNarrow ? 1 : kHd / 64;        // of 16 bytes (8 for 64 codes), for each of four keys
-  static constexpr int kVWords = kNarrow && kHd == 64 ? 2 : 4;
-  uint4 k[2][kKLoads];
-  uint32_t v[4][kVLoads][kVWords];
-  uint32_t k_exp[kNarrow ? 2 : 1], v_exp[kNarrow ? 4 : 1];
-};
+constexpr int kFewShift = 7;  // probabilities in f16 are taken 2^7 times as large: with the slack they stay below 2^15
 
 template <int kHd, bool kNarrow, bool kHalf>
 struct FewShape {
-  static constexpr int kSubs = !kNarrow && kHd == 128 ? 1 : 2;  // 16 keys each, of a step
-  static constexpr int kStep = 16 * kSubs;
+  static constexpr int kCtas = kNarrow && !(kHd == 128 && !kHalf) ? 2 : 1;  // per SM
+  static constexpr int kSubs = kHd == 128 && !(kNarrow && !kHalf) ? 1 : 2;  // of 16 keys, of a stage
+  static constexpr int kStages = kNarrow || (kHd == 128 && !kHalf) ? 2 : 3;
   static constexpr int kRows = kHalf ? 8 : 16;
   static constexpr int kOutTiles = kHd / 8;
-  static constexpr int kSmemBytes = kKvFewWarps * kRows * (kHd + 2) * 4;
+  static constexpr int kSubBytes = 16 * kHd * (kNarrow ? 1 : 2);           // of K or V
+  static constexpr int kStageBytes = 2 * kSubs * kSubBytes + (kNarrow ? 128 : 0);  // [K, V][sub], exponents [K, V][sub] of 16 bytes
+  static constexpr int kRingBytes = kKvFewWarps * kStages * kStageBytes;
+  static constexpr int kMergeBytes = kKvFewWarps * kRows * (kHd + 2) * 4;
+  static constexpr int kSmemBytes = kRingBytes + kMergeBytes + 1024 + 256;
 };
 
 // kHalf: at most eight rows, so the lower half of every row tile is empty and takes no registers.
 template <int kHd, bool kNarrow, bool kHalf>
-__global__ void __launch_bounds__(kKvFewWarps * 32, kHd == 128 && !kHalf ? 1 : 2)
-kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
+__global__ void __launch_bounds__(kKvFewWarps * 32, FewShape<kHd, kNarrow, kHalf>::kCtas)
+kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, KvPool pool, KvArrays arrays,
+                   KvLaunch work, KvAttend at, uint32_t* status) {
   using Shape = FewShape<kHd, kNarrow, kHalf>;
-  using Keys = FewKeys<kHd, kNarrow>;
-  constexpr int kEl = kNarrow ? 1 : 2;  // bytes of an element
-  constexpr int kSubs = Shape::kSubs;
-  extern __shared__ float smem[];
-  __shared__ int last_of_join;
-  float* smem_o = smem;                                          // [warp][row][channel]
-  float* smem_ml = smem + kKvFewWarps * Shape::kRows * kHd;      // [warp][row]{reference, sum}
-  wait_for_previous_kernel();
+  constexpr int kSubs = Shape::kSubs, kStages = Shape::kStages, kStageKeys = 16 * kSubs, kRound = kKvFewWarps * kStageKeys;
+  constexpr int kHalves = kHalf ? 1 : 2;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* smem_o = reinterpret_cast<float*>(smem + Shape::kRingBytes);  // [warp][row][channel]
+  float* smem_ml = smem_o + kKvFewWarps * Shape::kRows * kHd;          // [warp][row]{reference, sum}
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Shape::kRingBytes + Shape::kMergeBytes);  // [warp][stage]
+  uint32_t* flags = reinterpret_cast<uint32_t*>(bars + kKvFewWarps * kStages);                  // abort, last of a join
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, q4 = lane & 3;
+  if (threadIdx.x < kKvFewWarps * kStages) {
+    mbar_init(&bars[threadIdx.x], 1);
+    mbar_fence_init();
+  }
+  if (threadIdx.x == 0) flags[0] = 0;
+  __syncthreads();
+  wait_for_previous_kernel();
+  const WaitCtl ctl{flags, status};
+  uint64_t* full = bars + warp * kStages;
+  const uint32_t ring = smem_u32(smem) + warp * kStages * Shape::kStageBytes;
+  const int id0 = work.first[blockIdx.x], id_end = work.first[blockIdx.x + 1];
 
-  for (int id = work.first[blockIdx.x]; id < work.first[blockIdx.x + 1]; ++id) {
+  // ------------------------------------------------------------------ loads
+  // The stage that is fetched next, and its piece; a lane's copy is one of K or V of 16 keys (and 64 channels, or the codes or
+  // exponents).  Its page is looked up a stage ahead.
+  constexpr int kParts = kNarrow ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts;
+  const int my_part = lane % kParts, my_x = (lane / kParts) & 1, my_sub = lane / (2 * kParts);
+  int f_id = id0, f_key = 0, f_end = 0, f_head = 0, f_page0 = 0, f_page = 0;
+  uint32_t fetched = 0;
+  auto look_up = [&]() {
+    const int key = f_key + 16 * my_sub;
+    if (lane < kCopies && key < f_end) f_page = arrays.pages[f_page0 + (key >> pool.page_shift)];
+  };
+  auto enter = [&]() {  // the first piece from f_id on that has keys for this warp
+    for (; f_id < id_end; ++f_id) {
+      const KvPiece p = work.pieces[f_id];
+      f_key = p.key0 + warp * kStageKeys;
+      f_end = p.key1;
+      if (f_key >= f_end) continue;
+      f_head = p.kv_head;
+      f_page0 = arrays.seqs[p.seq].page0;
+      look_up();
+      return;
+    }
+  };
+  auto fetch = [&]() {
+    if (f_id >= id_end) return;
+    const uint32_t stage = fetched % kStages;
+    uint64_t* bar = &full[stage];
+    const int subs = min(kSubs, (f_end - f_key + 15) >> 4);
+    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(subs * (2 * Shape::kSubBytes + (kNarrow ? 32 : 0))));
+    __syncwarp();
+    if (lane < kCopies && my_sub < subs) {
+      const int key = f_key + 16 * my_sub;
+      const long long row = ((long long)f_page * pool.kv_heads + f_head) * pool.page_size + (key & (pool.page_size - 1));
+      const uint32_t base = ring + stage * Shape::kStageBytes;
+      if constexpr (kNarrow) {
+        if (my_part == 0) bulk_load(base + (my_x * kSubs + my_sub) * Shape::kSubBytes, (my_x == 0 ? pool.k : pool.v) + row * kHd, 16 * kHd, bar);
+        else bulk_load(base + 2 * kSubs * Shape::kSubBytes + (my_x * kSubs + my_sub) * 16, (my_x == 0 ? pool.k_exp : pool.v_exp) + row, 16, bar);
+      } else {
+        const uint32_t dst = base + (my_x * kSubs + my_sub) * Shape::kSubBytes + my_part * 2048;
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+                     "l"(reinterpret_cast<uint64_t>(my_x == 0 ? &k_map : &v_map)), "r"(smem_u32(bar)), "r"(my_part * 64), "r"((int)row)
+                     : "memory");
+      }
+    }
+    ++fetched;
+    f_key += kRound;
+    if (f_key < f_end) {
+      look_up();
+    } else {
+      ++f_id;
+      enter();
+    }
+  };
+  enter();
+  for (int i = 0; i < kStages; ++i) fetch();
+
+  uint32_t taken = 0;
+  bool ok = true;
+  for (int id = id0; id < id_end; ++id) {
     const KvPiece piece = work.pieces[id];
     const KvSeq seq = arrays.seqs[piece.seq];
-    const int* pages = arrays.pages + seq.page0;
-    const int last_page = (seq.len - 1) >> pool.page_shift;
 
     // ---------------------------------------------------------------- rows
-    auto q_row = [&](int r) {
-      const int at_row = piece.row0 + r;
-      return at.q + (seq.row0 + at_row / at.group) * at.q_stride.row + (piece.kv_head * at.group + at_row % at.group) * at.q_stride.head;
-    };
-    uint32_t qa[kHd / 16][kHalf ? 2 : 4];
-    {
+    uint32_t qa[kHd / 16][2 * kHalves];
+    float row_scale[kHalves];  // of the scores, in base-2 units
+#pragma unroll
+    for (int half = 0; half < kHalves; ++half) {
       // 16 bytes of a K row hold the channels of two contraction steps of 16 (bf16) or of four (codes)
-      constexpr int kRun = 16 / kEl;  // channels of a lane that lie side by side
+      constexpr int kRun = kNarrow ? 16 : 8;  // channels of a lane that lie side by side
+      const int r = g + 8 * half;
+      const bool live = r < piece.rows;
+      const int at_row = piece.row0 + (live ? r : 0);
+      const __nv_bfloat16* src =
+          at.q + (seq.row0 + at_row / at.group) * at.q_stride.row + (piece.kv_head * at.group + at_row % at.group) * at.q_stride.head;
+      uint32_t top = 0;
 #pragma unroll
-      for (int half = 0; half < (kHalf ? 1 : 2); ++half) {
-        const int r = g + 8 * half;
-        const bool live = r < piece.rows;
-        const __nv_bfloat16* src = q_row(live ? r : 0);
+      for (int i = 0; i < kHd / (4 * kRun); ++i)
 #pragma unroll
-        for (int i = 0; i < kHd / (4 * kRun); ++i)
+        for (int j = 0; j < kRun / 4; ++j) {
+          uint2 w = make_uint2(0u, 0u);
+          if (live) w = *reinterpret_cast<const uint2*>(src + (i * 4 + q4) * kRun + 4 * j);
+          qa[i * (kRun / 4) + j][half] = w.x;
+          qa[i * (kRun / 4) + j][kHalves + half] = w.y;
+          top = __vmaxu2(top, __vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu));
+        }
+      row_scale[half] = at.scale_log2;
+      if constexpr (kNarrow) {
+        top = max(top & 0xffffu, top >> 16);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // the row's largest element to [2^13, 2^14); rows of zeros or under 2^-113, and those that are not finite, as near as it goes
+        const int up = min(max(13 - ((int)(top >> 7) - 127), -126), 126);
+        const float factor = top >= 0x7f80u ? 1.0f : __int_as_float((up + 127) << 23);
+        if (top < 0x7f80u) row_scale[half] *= __int_as_float((127 - up) << 23);
 #pragma unroll
-          for (int j = 0; j < kRun / 4; ++j) {
-            uint2 w = make_uint2(0u, 0u);
-            if (live) w = *reinterpret_cast<const uint2*>(src + (i * 4 + q4) * kRun + 4 * j);
-            qa[i * (kRun / 4) + j][half] = w.x;
-            qa[i * (kRun / 4) + j][(kHalf ? 1 : 2) + half] = w.y;
+        for (int i = 0; i < kHd / 16; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t w = qa[i][j * kHalves + half];
+            qa[i][j * kHalves + half] = pack_f16(bf16_lo(w) * factor, bf16_hi(w) * factor);
           }
       }
     }
     auto seen_by = [&](int r) { return kv_seen(seq.len, seq.rows, at.causal_block, (piece.row0 + r) / at.group); };
-    const int all_see = seen_by(0);                       // keys before this one are seen by every row
-    const int seen0 = min(seen_by(g), piece.key1), seen1 = min(seen_by(g + 8), piece.key1);
+    const int all_see = min(seen_by(0), piece.key1);  // keys before this one are seen by every row
+    const int seen[2] = {min(seen_by(g), piece.key1), min(seen_by(g + 8), piece.key1)};
 
-    float o[Shape::kOutTiles][kHalf ? 2 : 4];
+    float o[Shape::kOutTiles][2 * kHalves];
 #pragma unroll
     for (int i = 0; i < Shape::kOutTiles; ++i)
 #pragma unroll
-      for (int j = 0; j < (kHalf ? 2 : 4); ++j) o[i][j] = 0.0f;
+      for (int j = 0; j < 2 * kHalves; ++j) o[i][j] = 0.0f;
     float top[2] = {-INFINITY, -INFINITY}, ref[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};  // ref: top where that is finite yet
-
-    // ---------------------------------------------------------------- loads
-    // A sub-step's base: its page's rows, from the one of its first key on.  What lies behind the sequence's end comes from its
-    // last page, whose rows exist whatever they hold.
-    auto base_of = [&](int key) -> long long {
-      const int p = min(key >> pool.page_shift, last_page);
-      const long long page = pages[p];
-      return (page * pool.kv_heads + piece.kv_head) * pool.page_size + (key & (pool.page_size - 1));
-    };
-    auto load_k = [&](Keys& d, long long row) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint8_t* src = pool.k + (row + g + 8 * t) * (kHd * kEl) + q4 * 16;
-#pragma unroll
-        for (int i = 0; i < Keys::kKLoads; ++i) d.k[t][i] = load16(src + 64 * i);
-        if constexpr (kNarrow) d.k_exp[t] = __ldg(pool.k_exp + row + g + 8 * t);
-      }
-    };
-    auto load_v = [&](Keys& d, long long row) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = 2 * q4 + (e & 1) + 8 * (e >> 1);
-        const uint8_t* src = pool.v + (row + key) * (kHd * kEl);
-#pragma unroll
-        for (int i = 0; i < Keys::kVLoads; ++i) {
-          if constexpr (Keys::kVWords == 2) {
-            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + g * 8));
-            d.v[e][i][0] = w.x, d.v[e][i][1] = w.y;
-          } else {
-            const uint4 w = load16(src + 128 * i + g * 16);
-            d.v[e][i][0] = w.x, d.v[e][i][1] = w.y, d.v[e][i][2] = w.z, d.v[e][i][3] = w.w;
-          }
-        }
-        if constexpr (kNarrow) d.v_exp[e] = __ldg(pool.v_exp + row + key);
-      }
-    };
+    uint32_t v_top = 0;  // codes: the largest exponent byte of a value so far, which the output is relative to
 
     // ---------------------------------------------------------------- sweep
-    Keys keys[kSubs];
-    int key = piece.key0 + warp * Shape::kStep;
-    long long rows[kSubs];
-    if (key < piece.key1) {
-#pragma unroll
-      for (int s = 0; s < kSubs; ++s) {
-        rows[s] = base_of(key + 16 * s);
-        load_k(keys[s], rows[s]);
-      }
-#pragma unroll
-      for (int s = 0; s < kSubs; ++s) load_v(keys[s], rows[s]);
-    }
-    for (; key < piece.key1; key += kKvFewWarps * Shape::kStep) {
-      const int next = key + kKvFewWarps * Shape::kStep;
-      const bool more = next < piece.key1;
-      if (more) {
-#pragma unroll
-        for (int s = 0; s < kSubs; ++s) rows[s] = base_of(next + 16 * s);
-      }
+    for (int key = piece.key0 + warp * kStageKeys; key < piece.key1 && ok; key += kRound) {
+      const uint32_t stage = taken % kStages;
+      ok = mbar_wait_warp(&full[stage], (taken / kStages) & 1u, ctl);
+      if (!ok) break;
+      ++taken;
+      const uint32_t base = ring + stage * Shape::kStageBytes, exps = base + 2 * kSubs * Shape::kSubBytes;
+      const bool edge = key + kStageKeys > all_see;
       // scores
       float sc[kSubs][2][4];
 #pragma unroll
@@ -171,52 +252,55 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
         for (int t = 0; t < 2; ++t) {
           float (&c)[4] = sc[s][t];
           c[0] = c[1] = c[2] = c[3] = 0.0f;
+          const int row = g + 8 * t;
+          const uint32_t at_sub = base + s * Shape::kSubBytes;
           auto step = [&](int n, uint32_t b0, uint32_t b1) {
-            if constexpr (kHalf) mma_16816(c, qa[n][0], 0u, qa[n][1], 0u, b0, b1);
-            else mma_16816(c, qa[n][0], qa[n][1], qa[n][2], qa[n][3], b0, b1);
+            if constexpr (kHalf) mma_16816<kNarrow>(c, qa[n][0], 0u, qa[n][1], 0u, b0, b1);
+            else mma_16816<kNarrow>(c, qa[n][0], qa[n][1], qa[n][2], qa[n][3], b0, b1);
           };
+          if constexpr (kNarrow) {
 #pragma unroll
-          for (int i = 0; i < Keys::kKLoads; ++i) {
-            const uint32_t w[4] = {keys[s].k[t][i].x, keys[s].k[t][i].y, keys[s].k[t][i].z, keys[s].k[t][i].w};
-            if constexpr (kNarrow) {
-              const KvFactor f = kv_factor(keys[s].k_exp[t]);
-              const uint32_t f1 = f.first * 0x10001u, f2 = f.second * 0x10001u;
-              const bool second = kv_needs_second(keys[s].k_exp[t]);
+            for (int i = 0; i < kHd / 64; ++i) {
+              const uint4 x = lds16(at_sub + row * kHd + i * 64 + q4 * 16);
+              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                uint32_t lo = mul_bf16x2(kv_code_bits(__byte_perm(w[j], 0u, 0x1404)), f1);
-                uint32_t hi = mul_bf16x2(kv_code_bits(__byte_perm(w[j], 0u, 0x3424)), f1);
-                if (second) lo = mul_bf16x2(lo, f2), hi = mul_bf16x2(hi, f2);
-                __syncwarp();
-                step(4 * i + j, lo, hi);
-              }
-            } else {
-              step(2 * i, w[0], w[1]);
-              step(2 * i + 1, w[2], w[3]);
+              for (int j = 0; j < 4; ++j) step(4 * i + j, widen_low(w[j]), widen_high(w[j]));
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < kHd / 32; ++i) {
+              const uint4 x = lds16(at_sub + (i >> 1) * 2048 + row * 128 + (((i & 1) * 4 + q4) ^ (row & 7)) * 16);
+              step(2 * i, x.x, x.y);
+              step(2 * i + 1, x.z, x.w);
             }
           }
         }
-      if (more) {
-#pragma unroll
-        for (int s = 0; s < kSubs; ++s) load_k(keys[s], rows[s]);
-      }
-      // probabilities: the reference of a row moves only when a score lies far above it
-      const bool edge = key + Shape::kStep > min(all_see, piece.key1);
+      // in base-2 units; the reference of a row moves only when a score lies far above it
       float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int s = 0; s < kSubs; ++s)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+          float k_scale[2] = {1.0f, 1.0f};
+          if constexpr (kNarrow) {
 #pragma unroll
-          for (int e = 0; e < (kHalf ? 2 : 4); ++e) {
-            float x = sc[s][t][e] * at.scale_log2;
-            if (edge && key + 16 * s + 8 * t + 2 * q4 + (e & 1) >= (e < 2 ? seen0 : seen1)) x = -INFINITY;
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t byte = lds1(exps + s * 16 + 8 * t + 2 * q4 + e);
+              k_scale[e] = __uint_as_float(byte == kKvNanByte ? 0x7fc00000u : byte << 23);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 2 * kHalves; ++e) {
+            float x = sc[s][t][e] * row_scale[e >> 1];
+            if constexpr (kNarrow) x *= k_scale[e & 1];
+            if (edge && key + 16 * s + 8 * t + 2 * q4 + (e & 1) >= seen[e >> 1]) x = -INFINITY;
             sc[s][t][e] = x;
             most[e >> 1] = fmaxf(most[e >> 1], x);
           }
+        }
       if (__any_sync(0xffffffffu, most[0] > top[0] + kFewSlack || (!kHalf && most[1] > top[1] + kFewSlack))) {
 #pragma unroll
-        for (int half = 0; half < (kHalf ? 1 : 2); ++half) {
+        for (int half = 0; half < kHalves; ++half) {
           float m = most[half];
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
@@ -230,73 +314,103 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
           }
         }
       }
-      uint32_t p[kSubs][2][kHalf ? 1 : 2];
+      // probabilities, and the weights that the values get
+      uint32_t p[kSubs][2][kHalves];
+      uint32_t v_byte[kSubs][2][2];
+      if constexpr (kNarrow) {
+        uint32_t most_byte = 0;
+#pragma unroll
+        for (int s = 0; s < kSubs; ++s)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int in_sub = 8 * t + 2 * q4 + e;
+              const uint32_t byte = lds1(exps + (kSubs + s) * 16 + in_sub);
+              v_byte[s][t][e] = byte;
+              if (byte != kKvNanByte && (!edge || key + 16 * s + in_sub < piece.key1)) most_byte = max(most_byte, byte);
+            }
+        most_byte = __reduce_max_sync(0xffffffffu, most_byte);
+        if (most_byte > v_top) {
+          const float factor = __uint_as_float((127u - min(most_byte - v_top, 126u)) << 23);  // (nothing there yet: of zeros)
+          v_top = most_byte;
+#pragma unroll
+          for (int i = 0; i < Shape::kOutTiles; ++i)
+#pragma unroll
+            for (int j = 0; j < 2 * kHalves; ++j) o[i][j] *= factor;
+        }
+      }
 #pragma unroll
       for (int s = 0; s < kSubs; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int half = 0; half < (kHalf ? 1 : 2); ++half) {
-            const float a = fast_exp2(sc[s][t][2 * half] - ref[half]), b = fast_exp2(sc[s][t][2 * half + 1] - ref[half]);
-            // operands of the second product, each off by up to 2^-8; the sum is that of the rounded ones, so what the rounding
-            // changes is how much a key weighs among the others and not the whole row's size
-            p[s][t][half] = pack_bf16(a, b);
-            sum[half] += bf16_lo(p[s][t][half]) + bf16_hi(p[s][t][half]);
+          for (int half = 0; half < kHalves; ++half) {
+            float a = fast_exp2(sc[s][t][2 * half] - ref[half]), b = fast_exp2(sc[s][t][2 * half + 1] - ref[half]);
+            if constexpr (kNarrow) {
+              sum[half] += a + b;
+              float f[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t byte = v_byte[s][t][e];
+                const int power = (int)byte - (int)v_top + kFewShift + 127;
+                f[e] = __uint_as_float(byte == kKvNanByte ? 0x7fc00000u : (uint32_t)max(power, 0) << 23);
+                // what is not seen has no weight, whatever it holds
+                if (edge && key + 16 * s + 8 * t + 2 * q4 + e >= seen[half]) f[e] = 0.0f;
+              }
+              p[s][t][half] = pack_f16(a * f[0], b * f[1]);
+            } else {
+              // operands of the second product, each off by up to 2^-8; the sum is that of the rounded ones, so what the rounding
+              // changes is how much a key weighs among the others and not the whole row's size
+              p[s][t][half] = pack_bf16(a, b);
+              sum[half] += bf16_lo(p[s][t][half]) + bf16_hi(p[s][t][half]);
+            }
           }
       // output
 #pragma unroll
       for (int s = 0; s < kSubs; ++s) {
         const int left = piece.key1 - (key + 16 * s);  // keys of the sub-step that the piece holds
-        KvFactor f[4];
-        bool second = false;
-        if constexpr (kNarrow) {
+        const uint32_t at_sub = base + (kSubs + s) * Shape::kSubBytes;
+        constexpr int kLoads = kNarrow ? 1 : kHd / 64, kWords = kNarrow && kHd == 64 ? 2 : 4;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          uint32_t v[4][kWords];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            f[e] = kv_factor(keys[s].v_exp[e]);
-            second = second || kv_needs_second(keys[s].v_exp[e]);
+            const int row = 2 * q4 + (e & 1) + 8 * (e >> 1);
+            if constexpr (kWords == 2) {
+              const uint2 x = lds8(at_sub + row * 64 + g * 8);
+              v[e][0] = x.x, v[e][1] = x.y;
+            } else {
+              const uint4 x = lds16(kNarrow ? at_sub + row * kHd + g * 16 : at_sub + i * 2048 + row * 128 + (g ^ (row & 7)) * 16);
+              v[e][0] = x.x, v[e][1] = x.y, v[e][2] = x.z, v[e][3] = x.w;
+            }
+            if (left < 16 && row >= left) {  // what lies behind the piece may be anything
+#pragma unroll
+              for (int j = 0; j < kWords; ++j) v[e][j] = 0u;
+            }
           }
-        }
-        // channels 2 j, 2 j + 1 of the lane's run, as two operands of two keys each
 #pragma unroll
-        for (int i = 0; i < Keys::kVLoads; ++i)
-#pragma unroll
-          for (int j = 0; j < Keys::kVWords; ++j) {
+          for (int j = 0; j < kWords; ++j) {
             constexpr int kPer = kNarrow ? 4 : 2;  // channels of a word
-            uint32_t w[4];
+            uint32_t b[kPer][2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = keys[s].v[e][i][j];
-            if (left < 16) {  // what lies behind the piece may be anything
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (2 * q4 + (e & 1) + 8 * (e >> 1) >= left) w[e] = 0u;
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t lo = __byte_perm(v[2 * h][j], v[2 * h + 1][j], kNarrow ? 0x5140 : 0x5410);
+              const uint32_t hi = __byte_perm(v[2 * h][j], v[2 * h + 1][j], kNarrow ? 0x7362 : 0x7632);
+              if constexpr (kNarrow) {
+                b[0][h] = widen_low(lo), b[1][h] = widen_high(lo), b[kPer - 2][h] = widen_low(hi), b[kPer - 1][h] = widen_high(hi);
+              } else {
+                b[0][h] = lo, b[1][h] = hi;
+              }
             }
 #pragma unroll
             for (int n = 0; n < kPer; ++n) {
-              uint32_t b0, b1;
-              if constexpr (kNarrow) {
-                const uint32_t pick = (uint32_t)((4 + n) << 12 | n << 4);  // bytes n of both words to the high byte of each half
-                b0 = mul_bf16x2(kv_code_bits(__byte_perm(w[0], w[1], pick)), f[0].first | f[1].first << 16);
-                b1 = mul_bf16x2(kv_code_bits(__byte_perm(w[2], w[3], pick)), f[2].first | f[3].first << 16);
-                if (second) {
-                  b0 = mul_bf16x2(b0, f[0].second | f[1].second << 16);
-                  b1 = mul_bf16x2(b1, f[2].second | f[3].second << 16);
-                }
-                if (left < 16) {
-                  // a factor behind the piece may be anything too
-                  if (2 * q4 >= left) b0 &= 0xffff0000u;
-                  if (2 * q4 + 1 >= left) b0 &= 0x0000ffffu;
-                  if (2 * q4 + 8 >= left) b1 &= 0xffff0000u;
-                  if (2 * q4 + 9 >= left) b1 &= 0x0000ffffu;
-                }
-                __syncwarp();
-              } else {
-                b0 = __byte_perm(w[0], w[1], n == 0 ? 0x5410 : 0x7632);
-                b1 = __byte_perm(w[2], w[3], n == 0 ? 0x5410 : 0x7632);
-              }
-              const int tile = (i * Keys::kVWords + j) * kPer + n;
-              if (edge) {
+              const int tile = (i * kWords + j) * kPer + n;
+              if (!kNarrow && edge) {
                 // A value that is not finite, of a key that some rows see and others do not: a probability of zero would not
                 // keep it out.  It is left out of the product and added where it is seen.
+                uint32_t b0 = b[n][0], b1 = b[n][1];
                 const bool bad = (b0 & 0x7f80u) == 0x7f80u || (b0 & 0x7f800000u) == 0x7f800000u || (b1 & 0x7f80u) == 0x7f80u ||
                                  (b1 & 0x7f800000u) == 0x7f800000u;
                 if (__any_sync(0xffffffffu, bad)) {
@@ -312,8 +426,9 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
                       const int at_key = key + 16 * s + 2 * (from & 3) + (e & 1) + 8 * (e >> 1);
                       // (selects: an accumulator is a register of a fixed name)
                       const bool odd = (from >> 2 & 1) != 0;
-                      if (at_key < seen0) o[tile][0] += odd ? 0.0f : value, o[tile][1] += odd ? value : 0.0f;
-                      if (!kHalf && at_key < seen1) o[tile][kHalf ? 0 : 2] += odd ? 0.0f : value, o[tile][kHalf ? 0 : 3] += odd ? value : 0.0f;
+#pragma unroll
+                      for (int half = 0; half < kHalves; ++half)
+                        if (at_key < seen[half]) o[tile][2 * half] += odd ? 0.0f : value, o[tile][2 * half + 1] += odd ? value : 0.0f;
                     }
                   }
                   __syncwarp();
@@ -321,32 +436,35 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
                   if ((b0 & 0x7f800000u) == 0x7f800000u) b0 &= 0x0000ffffu;
                   if ((b1 & 0x7f80u) == 0x7f80u) b1 &= 0xffff0000u;
                   if ((b1 & 0x7f800000u) == 0x7f800000u) b1 &= 0x0000ffffu;
+                  b[n][0] = b0, b[n][1] = b1;
                 }
               }
               if constexpr (kHalf) {
                 float c[4] = {o[tile][0], o[tile][1], 0.0f, 0.0f};
-                mma_16816(c, p[s][0][0], 0u, p[s][1][0], 0u, b0, b1);
+                mma_16816<kNarrow>(c, p[s][0][0], 0u, p[s][1][0], 0u, b[n][0], b[n][1]);
                 o[tile][0] = c[0], o[tile][1] = c[1];
               } else {
-                mma_16816(o[tile], p[s][0][0], p[s][0][kHalf ? 0 : 1], p[s][1][0], p[s][1][kHalf ? 0 : 1], b0, b1);
+                float (&c)[4] = *reinterpret_cast<float (*)[4]>(&o[tile][0]);
+                mma_16816<kNarrow>(c, p[s][0][0], p[s][0][kHalves - 1], p[s][1][0], p[s][1][kHalves - 1], b[n][0], b[n][1]);
               }
             }
           }
+        }
       }
-      if (more) {
-#pragma unroll
-        for (int s = 0; s < kSubs; ++s) load_v(keys[s], rows[s]);
-      }
+      __syncwarp();  // all lanes have read the stage
+      fetch();
     }
 
     // ---------------------------------------------------------------- the warps meet
-    // tile -> channel: lane g of V's loads holds a run of channels, tile n its n-th
+    // tile -> channel: lane g of V's reads holds a run of channels, tile n its n-th
     auto channel_of = [&](int tile, int n) {
       constexpr int kRun = kNarrow ? kHd / 8 : 8;
       return (tile / kRun) * (8 * kRun) + n * kRun + tile % kRun;
     };
+    // codes: back from "relative to the largest value's power of two"
+    const float v_scale = kNarrow ? __int_as_float((max((int)v_top, 9) - kFewShift) << 23) : 1.0f;
 #pragma unroll
-    for (int half = 0; half < (kHalf ? 1 : 2); ++half) {
+    for (int half = 0; half < kHalves; ++half) {
       float l = sum[half];
       l += __shfl_xor_sync(0xffffffffu, l, 1);
       l += __shfl_xor_sync(0xffffffffu, l, 2);
@@ -355,8 +473,8 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
         float* dst = smem_o + (warp * Shape::kRows + r) * kHd;
 #pragma unroll
         for (int i = 0; i < Shape::kOutTiles; ++i) {
-          dst[channel_of(i, 2 * q4)] = o[i][2 * half];
-          dst[channel_of(i, 2 * q4 + 1)] = o[i][2 * half + 1];
+          dst[channel_of(i, 2 * q4)] = o[i][2 * half] * v_scale;
+          dst[channel_of(i, 2 * q4 + 1)] = o[i][2 * half + 1] * v_scale;
         }
         if (q4 == 0) {
           float* ml = smem_ml + (warp * Shape::kRows + r) * 2;
@@ -399,11 +517,11 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
       __syncthreads();
       if (threadIdx.x == 0) {
         const int before = atomicAdd(work.joins + piece.join, 1);
-        last_of_join = before == piece.parts - 1;
-        if (last_of_join) work.joins[piece.join] = 0;
+        flags[1] = before == piece.parts - 1 ? 1u : 0u;
+        if (before == piece.parts - 1) work.joins[piece.join] = 0;
       }
       __syncthreads();
-      if (last_of_join) {
+      if (flags[1] != 0) {
         __threadfence();
         for (int i = threadIdx.x; i < piece.rows * kHd; i += kKvFewWarps * 32) {
           const int r = i / kHd, ch = i % kHd;
@@ -424,25 +542,38 @@ kv_attn_few_kernel(KvPool pool, KvArrays arrays, KvLaunch work, KvAttend at) {
     }
     __syncthreads();  // the next piece writes where this one was read
   }
+  // every load has landed before the CTA may go (all have been waited for, unless a wait was given up)
+  for (; taken < fetched; ++taken) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(&full[taken % kStages], (taken / kStages) & 1u)) {
+      if (clock64() - t0 > kTimeoutCycles) { atomicOr(status, kStatusTimeout); break; }
+    }
+  }
 }
 
 template <int kHd, bool kNarrow, bool kHalf>
 cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s) {
   using Shape = FewShape<kHd, kNarrow, kHalf>;
+  static_assert(Shape::kCtas * (Shape::kSmemBytes + 1024) <= 228 * 1024, "");
   auto kernel = kv_attn_few_kernel<kHd, kNarrow, kHalf>;
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = set_max_dynamic_smem_once(reinterpret_cast<const void*>(kernel), Shape::kSmemBytes, done);
   if (e != cudaSuccess) return e;
   const KvLaunch work = kv_launch(b, b.few, b.at_few);
-  return launch(kernel, dim3((unsigned)work.workers), kKvFewWarps * 32, (size_t)Shape::kSmemBytes, s, c.pool, kv_arrays(b), work, a);
+  return launch(kernel, dim3((unsigned)work.workers), kKvFewWarps * 32, (size_t)Shape::kSmemBytes, s, c.k_map16, c.v_map16, c.pool,
+                kv_arrays(b), work, a, c.status);
 }
 
 }  // namespace
 
+int kv_few_ctas(int head_dim, bool narrow, bool half) {
+  if (head_dim == 64) return narrow ? FewShape<64, true, true>::kCtas : FewShape<64, false, true>::kCtas;
+  if (!narrow) return FewShape<128, false, true>::kCtas;
+  return half ? FewShape<128, true, true>::kCtas : FewShape<128, true, false>::kCtas;
+}
+
 cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches) {
-  int rows = 0;
-  for (const KvPiece& p : b.few.pieces) rows = std::max(rows, p.rows);
-  const bool half = rows <= 8, narrow = c.cfg.dtype == LITEVGGT_KV_E4M3, wide = c.cfg.head_dim == 128;
+  const bool half = b.few_rows <= 8, narrow = c.cfg.dtype == LITEVGGT_KV_E4M3, wide = c.cfg.head_dim == 128;
   cudaError_t e;
   if (wide) {
     if (narrow) e = half ? start<128, true, true>(c, b, a, s) : start<128, true, false>(c, b, a, s);

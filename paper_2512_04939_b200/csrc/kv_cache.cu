@@ -248,7 +248,8 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
     if (r > kKvFewRows) many.push_back(i);
     else if (r > 0) few.push_back(i), most = std::max(most, (int)r);
   }
-  const int per_sm = c->cfg.head_dim == 128 && most > 8 ? 1 : 2;  // CTAs, by their registers
+  b->few_rows = most;
+  const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype == LITEVGGT_KV_E4M3, most <= 8);
   b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
                   KvCut{kKvFewRows, kKvFewUnit, c->num_sms * per_sm, 1, INT32_MAX, 1.0});
   b->tiles = kv_cut(b->seqs, many, b->group, c->cfg.kv_heads, causal_block, KvCut{kKvTileRows, kKvTileUnit, c->num_sms, 4, 512, 4.0});
@@ -304,8 +305,10 @@ litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, vo
     bool ok = fn != nullptr || resolve_encode_tiled(&fn);
     if (ok) encode.store(fn, std::memory_order_release);
     const uint64_t rows = (uint64_t)cfg->pages * cfg->kv_heads * cfg->page_size, hd = (uint64_t)cfg->head_dim;
-    ok = ok && make_tmap_bf16_2d(fn, &c->k_map, k, hd, rows, hd, 64, (uint32_t)cfg->page_size, true) &&
-         make_tmap_bf16_2d(fn, &c->v_map, v, hd, rows, hd, 64, (uint32_t)cfg->page_size, true);
+    auto make = [&](CUtensorMap* map, const void* base, int box) {
+      return make_tmap_bf16_2d(fn, map, base, hd, rows, hd, 64, (uint32_t)box, true);
+    };
+    ok = ok && make(&c->k_map, k, cfg->page_size) && make(&c->v_map, v, cfg->page_size) && make(&c->k_map16, k, 16) && make(&c->v_map16, v, 16);
     if (!ok) {
       delete c;
       return LITEVGGT_ERR_CUDA;

@@ -55,7 +55,8 @@ struct litevggt_kv_cache {
   int device, num_sms;
   lv::KvPool pool;
   uint32_t* status;
-  CUtensorMap k_map, v_map;  // bf16 pools, boxes of one page of a head and 64 channels
+  CUtensorMap k_map, v_map;      // bf16 pools, boxes of one page of a head and 64 channels
+  CUtensorMap k_map16, v_map16;  // the same in boxes of 16 tokens
   long long launches;
 };
 
@@ -67,6 +68,7 @@ struct litevggt_kv_batch {
   bool rows_held;  // no sequence has more rows than tokens
   std::vector<lv::KvSeq> seqs;
   lv::KvWork few, tiles;       // sequences of few rows, and the others
+  int few_rows;                // the most of the former
   std::vector<uint8_t> image;  // what the device gets
   size_t bytes;                // of device memory
   size_t o_seqs, o_pages;
@@ -98,6 +100,7 @@ cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch
 constexpr int kKvFewRows = 16;    // rows of a piece at most
 constexpr int kKvFewWarps = 8;
 constexpr int kKvFewUnit = 128;   // keys
+int kv_few_ctas(int head_dim, bool narrow, bool half);  // on an SM; half: at most eight rows
 cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
 // kv_attn_tiles.cu
 constexpr int kKvTileRows = 256;
