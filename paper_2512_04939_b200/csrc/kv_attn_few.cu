@@ -64,10 +64,12 @@ __device__ __forceinline__ uint2 lds8(uint32_t addr) {
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
   return v;
 }
-__device__ __forceinline__ uint32_t lds1(uint32_t addr) {
+// The powers of two of two neighbouring rows; infinity for one that is not finite.
+__device__ __forceinline__ void power_pair(uint32_t addr, float (&p)[2]) {
   uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
-  return v;
+  asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v) : "r"(addr));
+  p[0] = __uint_as_float(v << 23 & 0x7f800000u);
+  p[1] = __uint_as_float(v << 15 & 0x7f800000u);
 }
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_dst), "l"(src),
@@ -234,16 +236,15 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll
       for (int j = 0; j < 2 * kHalves; ++j) o[i][j] = 0.0f;
     float top[2] = {-INFINITY, -INFINITY}, ref[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};  // ref: top where that is finite yet
-    uint32_t v_top = 0;  // codes: the largest exponent byte of a value so far, which the output is relative to
+    // Codes: the largest power of two of a value so far, which the output is relative to, and the factor that makes weights of
+    // the others'; a power of infinity stands for a row that is not finite, whose codes are zero (0 * infinity = NaN).
+    float v_top = 0.0f, to_v_top = 0.0f;
 
     // ---------------------------------------------------------------- sweep
-    for (int key = piece.key0 + warp * kStageKeys; key < piece.key1 && ok; key += kRound) {
-      const uint32_t stage = taken % kStages;
-      ok = mbar_wait_warp(&full[stage], (taken / kStages) & 1u, ctl);
-      if (!ok) break;
-      ++taken;
-      const uint32_t base = ring + stage * Shape::kStageBytes, exps = base + 2 * kSubs * Shape::kSubBytes;
-      const bool edge = key + kStageKeys > all_see;
+    // One stage; with `edge` some rows do not see all of its keys, or not all of its keys are there.
+    auto take = [&](auto edge_constant, int key, uint32_t base) {
+      constexpr bool edge = decltype(edge_constant)::value;
+      const uint32_t exps = base + 2 * kSubs * Shape::kSubBytes;
       // scores
       float sc[kSubs][2][4];
 #pragma unroll
@@ -282,13 +283,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           float k_scale[2] = {1.0f, 1.0f};
-          if constexpr (kNarrow) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t byte = lds1(exps + s * 16 + 8 * t + 2 * q4 + e);
-              k_scale[e] = __uint_as_float(byte == kKvNanByte ? 0x7fc00000u : byte << 23);
-            }
-          }
+          if constexpr (kNarrow) power_pair(exps + s * 16 + 8 * t + 2 * q4, k_scale);
 #pragma unroll
           for (int e = 0; e < 2 * kHalves; ++e) {
             float x = sc[s][t][e] * row_scale[e >> 1];
@@ -316,28 +311,39 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       }
       // probabilities, and the weights that the values get
       uint32_t p[kSubs][2][kHalves];
-      uint32_t v_byte[kSubs][2][2];
+      float v_power[kSubs][2][2];
       if constexpr (kNarrow) {
-        uint32_t most_byte = 0;
+        float most_power = 0.0f;  // (positive floats order like their bits)
 #pragma unroll
         for (int s = 0; s < kSubs; ++s)
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
+          for (int t = 0; t < 2; ++t) {
+            power_pair(exps + (kSubs + s) * 16 + 8 * t + 2 * q4, v_power[s][t]);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int in_sub = 8 * t + 2 * q4 + e;
-              const uint32_t byte = lds1(exps + (kSubs + s) * 16 + in_sub);
-              v_byte[s][t][e] = byte;
-              if (byte != kKvNanByte && (!edge || key + 16 * s + in_sub < piece.key1)) most_byte = max(most_byte, byte);
+              if (edge && key + 16 * s + 8 * t + 2 * q4 + e >= piece.key1) v_power[s][t][e] = 0.0f;
+              most_power = fmaxf(most_power, v_power[s][t][e]);
             }
-        most_byte = __reduce_max_sync(0xffffffffu, most_byte);
-        if (most_byte > v_top) {
-          const float factor = __uint_as_float((127u - min(most_byte - v_top, 126u)) << 23);  // (nothing there yet: of zeros)
-          v_top = most_byte;
+          }
+        if (__any_sync(0xffffffffu, most_power > v_top)) {
+          most_power = 0.0f;
 #pragma unroll
-          for (int i = 0; i < Shape::kOutTiles; ++i)
+          for (int s = 0; s < kSubs; ++s)
 #pragma unroll
-            for (int j = 0; j < 2 * kHalves; ++j) o[i][j] *= factor;
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (v_power[s][t][e] < INFINITY) most_power = fmaxf(most_power, v_power[s][t][e]);
+          most_power = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most_power)));
+          if (most_power > v_top) {
+            const float factor = v_top / most_power;  // powers of two: exact, or zero where it is next to nothing
+            v_top = most_power;
+            to_v_top = 1.0f / most_power * (float)(1 << kFewShift);
+#pragma unroll
+            for (int i = 0; i < Shape::kOutTiles; ++i)
+#pragma unroll
+              for (int j = 0; j < 2 * kHalves; ++j) o[i][j] *= factor;
+          }
         }
       }
 #pragma unroll
@@ -352,9 +358,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               float f[2];
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const uint32_t byte = v_byte[s][t][e];
-                const int power = (int)byte - (int)v_top + kFewShift + 127;
-                f[e] = __uint_as_float(byte == kKvNanByte ? 0x7fc00000u : (uint32_t)max(power, 0) << 23);
+                f[e] = v_power[s][t][e] * to_v_top;
                 // what is not seen has no weight, whatever it holds
                 if (edge && key + 16 * s + 8 * t + 2 * q4 + e >= seen[half]) f[e] = 0.0f;
               }
@@ -451,6 +455,14 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           }
         }
       }
+    };
+    for (int key = piece.key0 + warp * kStageKeys; key < piece.key1 && ok; key += kRound) {
+      const uint32_t stage = taken % kStages;
+      ok = mbar_wait_warp(&full[stage], (taken / kStages) & 1u, ctl);
+      if (!ok) break;
+      ++taken;
+      if (key + kStageKeys > all_see) take(std::true_type{}, key, ring + stage * Shape::kStageBytes);
+      else take(std::false_type{}, key, ring + stage * Shape::kStageBytes);
       __syncwarp();  // all lanes have read the stage
       fetch();
     }
@@ -462,7 +474,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       return (tile / kRun) * (8 * kRun) + n * kRun + tile % kRun;
     };
     // codes: back from "relative to the largest value's power of two"
-    const float v_scale = kNarrow ? __int_as_float((max((int)v_top, 9) - kFewShift) << 23) : 1.0f;
+    const float v_scale = kNarrow ? v_top * (1.0f / (1 << kFewShift)) : 1.0f;
 #pragma unroll
     for (int half = 0; half < kHalves; ++half) {
       float l = sum[half];
@@ -489,30 +501,34 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       const size_t row = (size_t)(seq.row0 + at_row / at.group) * at.q_heads + piece.kv_head * at.group + at_row % at.group;
       at.out[row * kHd + ch] = __float2bfloat16_rn(value);
     };
-    // The joint reference of several parts of a row is the largest of theirs; a part without keys has none (-infinity), and
-    // weighs nothing.
-    for (int i = threadIdx.x; i < piece.rows * kHd; i += kKvFewWarps * 32) {
-      const int r = i / kHd, ch = i % kHd;
-      float m = -INFINITY, l = 0.0f, acc = 0.0f;
+    // What the warps left in shared memory, weighed against each other; the joint reference is the largest of theirs.  One that
+    // has met no key has none (-infinity), and weighs nothing.  `out` gets row, channel, output, reference and sum.
+    auto meet = [&](auto out) {
+      for (int i = threadIdx.x; i < piece.rows * kHd; i += kKvFewWarps * 32) {
+        const int r = i / kHd, ch = i % kHd;
+        float m = -INFINITY, l = 0.0f, acc = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kKvFewWarps; ++w) m = fmaxf(m, smem_ml[(w * Shape::kRows + r) * 2]);
-      const float m_use = m == -INFINITY ? 0.0f : m;
+        for (int w = 0; w < kKvFewWarps; ++w) m = fmaxf(m, smem_ml[(w * Shape::kRows + r) * 2]);
+        const float m_use = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-      for (int w = 0; w < kKvFewWarps; ++w) {
-        const float mw = smem_ml[(w * Shape::kRows + r) * 2], weight = mw == -INFINITY ? 1.0f : fast_exp2(mw - m_use);
-        l += smem_ml[(w * Shape::kRows + r) * 2 + 1] * weight;
-        acc += smem_o[(w * Shape::kRows + r) * kHd + ch] * weight;
+        for (int w = 0; w < kKvFewWarps; ++w) {
+          const float mw = smem_ml[(w * Shape::kRows + r) * 2], weight = mw == -INFINITY ? 1.0f : fast_exp2(mw - m_use);
+          l += smem_ml[(w * Shape::kRows + r) * 2 + 1] * weight;
+          acc += smem_o[(w * Shape::kRows + r) * kHd + ch] * weight;
+        }
+        out(r, ch, acc, m, l);
       }
-      if (piece.slot < 0) {
-        store(r, ch, seen_by(r) > 0 ? acc / l : 0.0f);
-      } else {
+    };
+    auto finish = [&](int r, int ch, float acc, float, float l) { store(r, ch, seen_by(r) > 0 ? acc / l : 0.0f); };
+    if (piece.slot < 0) {
+      meet(finish);
+    } else {
+      meet([&](int r, int ch, float acc, float m, float l) {
         const size_t row = (size_t)piece.slot * kKvFewRows + r;
         __stcg(work.rows + row * kHd + ch, acc);
         if (ch == 0) __stcg(reinterpret_cast<float2*>(work.sums) + row, make_float2(m, l));
-      }
-    }
-    if (piece.slot >= 0) {
-      // whoever comes last adds the parts up, in their order
+      });
+      // whoever comes last adds the parts up, in their order: every eighth goes to one warp, and the warps meet again
       __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
@@ -523,21 +539,40 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       __syncthreads();
       if (flags[1] != 0) {
         __threadfence();
-        for (int i = threadIdx.x; i < piece.rows * kHd; i += kKvFewWarps * 32) {
-          const int r = i / kHd, ch = i % kHd;
+        constexpr int kPer = kHd / 32;  // channels of a lane
+#pragma unroll 2
+        for (int r = 0; r < piece.rows; ++r) {
           const float2* ml = reinterpret_cast<const float2*>(work.sums) + (size_t)piece.first_slot * kKvFewRows + r;
-          const float* part = work.rows + ((size_t)piece.first_slot * kKvFewRows + r) * kHd + ch;
-          float m = -INFINITY, l = 0.0f, acc = 0.0f;
-          for (int w = 0; w < piece.parts; ++w) m = fmaxf(m, __ldcg(ml + (size_t)w * kKvFewRows).x);
+          const float* part = work.rows + ((size_t)piece.first_slot * kKvFewRows + r) * kHd + lane * kPer;
+          float m = -INFINITY, l = 0.0f, acc[kPer] = {};
+#pragma unroll 4
+          for (int w = warp; w < piece.parts; w += kKvFewWarps) m = fmaxf(m, __ldcg(ml + (size_t)w * kKvFewRows).x);
           const float m_use = m == -INFINITY ? 0.0f : m;
-          for (int w = 0; w < piece.parts; ++w) {
+#pragma unroll 4
+          for (int w = warp; w < piece.parts; w += kKvFewWarps) {
             const float2 x = __ldcg(ml + (size_t)w * kKvFewRows);
+            float v[kPer];
+            if constexpr (kPer == 4) {
+              const float4 y = __ldcg(reinterpret_cast<const float4*>(part + (size_t)w * kKvFewRows * kHd));
+              v[0] = y.x, v[1] = y.y, v[kPer - 2] = y.z, v[kPer - 1] = y.w;
+            } else {
+              const float2 y = __ldcg(reinterpret_cast<const float2*>(part + (size_t)w * kKvFewRows * kHd));
+              v[0] = y.x, v[1] = y.y;
+            }
             const float weight = x.x == -INFINITY ? 1.0f : fast_exp2(x.x - m_use);
             l += x.y * weight;
-            acc += __ldcg(part + (size_t)w * kKvFewRows * kHd) * weight;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) acc[i] += v[i] * weight;
           }
-          store(r, ch, seen_by(r) > 0 ? acc / l : 0.0f);
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) smem_o[(warp * Shape::kRows + r) * kHd + lane * kPer + i] = acc[i];
+          if (lane == 0) {
+            smem_ml[(warp * Shape::kRows + r) * 2] = m;
+            smem_ml[(warp * Shape::kRows + r) * 2 + 1] = l;
+          }
         }
+        __syncthreads();
+        meet(finish);
       }
     }
     __syncthreads();  // the next piece writes where this one was read
