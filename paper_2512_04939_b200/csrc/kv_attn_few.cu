@@ -83,8 +83,11 @@ constexpr int kFewShift = 7;  // probabilities in f16 are taken 2^7 times as lar
 
 template <int kHd, bool kNarrow, bool kHalf>
 struct FewShape {
-  static constexpr int kCtas = kNarrow && !(kHd == 128 && !kHalf) ? 2 : 1;  // per SM
-  static constexpr int kSubs = kHd == 128 && !(kNarrow && !kHalf) ? 1 : 2;  // of 16 keys, of a stage
+  // Rings of 17 to 25 KB a warp.  Codes of head dim 64 take so much work for a byte that sixteen warps an SM serve them
+  // better than eight with more registers (one token over 520,500: 216 us against 241 to 283); those of head dim 128 spill
+  // under 128 registers (sixteen tokens that share heads by eight: 36 us against 49).
+  static constexpr int kCtas = kNarrow && kHd == 64 ? 2 : 1;  // per SM
+  static constexpr int kSubs = kNarrow ? 2 : 128 / kHd;       // of 16 keys, of a stage
   static constexpr int kStages = kNarrow || (kHd == 128 && !kHalf) ? 2 : 3;
   static constexpr int kRows = kHalf ? 8 : 16;
   static constexpr int kOutTiles = kHd / 8;
@@ -528,7 +531,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         __stcg(work.rows + row * kHd + ch, acc);
         if (ch == 0) __stcg(reinterpret_cast<float2*>(work.sums) + row, make_float2(m, l));
       });
-      // whoever comes last adds the parts up, in their order: every eighth goes to one warp, and the warps meet again
+      // whoever comes last adds the parts up, in their order
       __threadfence();
       __syncthreads();
       if (threadIdx.x == 0) {
@@ -539,40 +542,35 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       __syncthreads();
       if (flags[1] != 0) {
         __threadfence();
-        constexpr int kPer = kHd / 32;  // channels of a lane
-#pragma unroll 2
-        for (int r = 0; r < piece.rows; ++r) {
-          const float2* ml = reinterpret_cast<const float2*>(work.sums) + (size_t)piece.first_slot * kKvFewRows + r;
-          const float* part = work.rows + ((size_t)piece.first_slot * kKvFewRows + r) * kHd + lane * kPer;
-          float m = -INFINITY, l = 0.0f, acc[kPer] = {};
-#pragma unroll 4
-          for (int w = warp; w < piece.parts; w += kKvFewWarps) m = fmaxf(m, __ldcg(ml + (size_t)w * kKvFewRows).x);
+        // first what every part weighs, [row][part], and the rows' sums behind them; then the rows
+        const float2* ml = reinterpret_cast<const float2*>(work.sums) + (size_t)piece.first_slot * kKvFewRows;
+        const float* parts = work.rows + (size_t)piece.first_slot * kKvFewRows * kHd;
+        const int n = piece.parts;
+        for (int r = warp; r < piece.rows; r += kKvFewWarps) {
+          float m = -INFINITY, l = 0.0f;
+          for (int w = lane; w < n; w += 32) m = fmaxf(m, __ldcg(ml + (size_t)w * kKvFewRows + r).x);
+#pragma unroll
+          for (int d = 1; d < 32; d *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
           const float m_use = m == -INFINITY ? 0.0f : m;
-#pragma unroll 4
-          for (int w = warp; w < piece.parts; w += kKvFewWarps) {
-            const float2 x = __ldcg(ml + (size_t)w * kKvFewRows);
-            float v[kPer];
-            if constexpr (kPer == 4) {
-              const float4 y = __ldcg(reinterpret_cast<const float4*>(part + (size_t)w * kKvFewRows * kHd));
-              v[0] = y.x, v[1] = y.y, v[kPer - 2] = y.z, v[kPer - 1] = y.w;
-            } else {
-              const float2 y = __ldcg(reinterpret_cast<const float2*>(part + (size_t)w * kKvFewRows * kHd));
-              v[0] = y.x, v[1] = y.y;
-            }
+          for (int w = lane; w < n; w += 32) {
+            const float2 x = __ldcg(ml + (size_t)w * kKvFewRows + r);
             const float weight = x.x == -INFINITY ? 1.0f : fast_exp2(x.x - m_use);
+            smem_o[r * n + w] = weight;
             l += x.y * weight;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) acc[i] += v[i] * weight;
           }
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) smem_o[(warp * Shape::kRows + r) * kHd + lane * kPer + i] = acc[i];
-          if (lane == 0) {
-            smem_ml[(warp * Shape::kRows + r) * 2] = m;
-            smem_ml[(warp * Shape::kRows + r) * 2 + 1] = l;
-          }
+          for (int d = 1; d < 32; d *= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
+          if (lane == 0) smem_ml[r] = l;
         }
         __syncthreads();
-        meet(finish);
+#pragma unroll 2
+        for (int i = threadIdx.x; i < piece.rows * kHd; i += kKvFewWarps * 32) {
+          const int r = i / kHd;
+          float acc = 0.0f;
+#pragma unroll 8
+          for (int w = 0; w < n; ++w) acc += __ldcg(parts + (size_t)w * kKvFewRows * kHd + i) * smem_o[r * n + w];
+          finish(r, i % kHd, acc, 0.0f, smem_ml[r]);
+        }
       }
     }
     __syncthreads();  // the next piece writes where this one was read
@@ -601,11 +599,7 @@ cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const 
 
 }  // namespace
 
-int kv_few_ctas(int head_dim, bool narrow, bool half) {
-  if (head_dim == 64) return narrow ? FewShape<64, true, true>::kCtas : FewShape<64, false, true>::kCtas;
-  if (!narrow) return FewShape<128, false, true>::kCtas;
-  return half ? FewShape<128, true, true>::kCtas : FewShape<128, true, false>::kCtas;
-}
+int kv_few_ctas(int head_dim, bool narrow) { return narrow && head_dim == 64 ? FewShape<64, true, true>::kCtas : 1; }
 
 cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches) {
   const bool half = b.few_rows <= 8, narrow = c.cfg.dtype == LITEVGGT_KV_E4M3, wide = c.cfg.head_dim == 128;

@@ -249,9 +249,9 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
     else if (r > 0) few.push_back(i), most = std::max(most, (int)r);
   }
   b->few_rows = most;
-  const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype == LITEVGGT_KV_E4M3, most <= 8);
+  const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype == LITEVGGT_KV_E4M3);
   b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
-                  KvCut{kKvFewRows, kKvFewUnit, c->num_sms * per_sm, 1, INT32_MAX, 1.0});
+                  KvCut{kKvFewRows, kKvFewUnit, std::min(c->num_sms * per_sm, kKvFewWorkers), 1, INT32_MAX, 1.0});
   b->tiles = kv_cut(b->seqs, many, b->group, c->cfg.kv_heads, causal_block, KvCut{kKvTileRows, kKvTileUnit, c->num_sms, 4, 512, 4.0});
   lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
   return LITEVGGT_OK;

@@ -100,7 +100,8 @@ cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch
 constexpr int kKvFewRows = 16;    // rows of a piece at most
 constexpr int kKvFewWarps = 8;
 constexpr int kKvFewUnit = 128;   // keys
-int kv_few_ctas(int head_dim, bool narrow, bool half);  // on an SM; half: at most eight rows
+constexpr int kKvFewWorkers = 512;  // CTAs of a launch at most: the weights of a row's parts lie in shared memory
+int kv_few_ctas(int head_dim, bool narrow);  // on an SM
 cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
 // kv_attn_tiles.cu
 constexpr int kKvTileRows = 256;
