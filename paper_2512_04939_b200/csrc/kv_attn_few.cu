@@ -120,37 +120,38 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   }
   if (threadIdx.x == 0) flags[0] = 0;
   __syncthreads();
-  wait_for_previous_kernel();
   const WaitCtl ctl{flags, status};
   uint64_t* full = bars + warp * kStages;
   const uint32_t ring = smem_u32(smem) + warp * kStages * Shape::kStageBytes;
-  const int id0 = work.first[blockIdx.x], id_end = work.first[blockIdx.x + 1];
 
   // ------------------------------------------------------------------ loads
   // The stage that is fetched next, and its piece; a lane's copy is one of K or V of 16 keys (and 64 channels, or the codes or
   // exponents).  Its page is looked up a stage ahead.
   constexpr int kParts = kNarrow ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts;
   const int my_part = lane % kParts, my_x = (lane / kParts) & 1, my_sub = lane / (2 * kParts);
-  int f_id = id0, f_key = 0, f_end = 0, f_head = 0, f_page0 = 0, f_page = 0;
+  int f_id = (int)blockIdx.x, f_key = 0, f_end = 0, f_head = 0, f_page0 = 0, f_page = 0, f_next = -1;
   uint32_t fetched = 0;
   auto look_up = [&]() {
     const int key = f_key + 16 * my_sub;
     if (lane < kCopies && key < f_end) f_page = arrays.pages[f_page0 + (key >> pool.page_shift)];
   };
   auto enter = [&]() {  // the first piece from f_id on that has keys for this warp
-    for (; f_id < id_end; ++f_id) {
+    while (f_id >= 0) {
       const KvPiece p = work.pieces[f_id];
       f_key = p.key0 + warp * kStageKeys;
       f_end = p.key1;
-      if (f_key >= f_end) continue;
-      f_head = p.kv_head;
-      f_page0 = arrays.seqs[p.seq].page0;
-      look_up();
-      return;
+      f_next = p.next;
+      if (f_key < f_end) {
+        f_head = p.kv_head;
+        f_page0 = p.seq.page0;
+        look_up();
+        return;
+      }
+      f_id = f_next;
     }
   };
   auto fetch = [&]() {
-    if (f_id >= id_end) return;
+    if (f_id < 0) return;
     const uint32_t stage = fetched % kStages;
     uint64_t* bar = &full[stage];
     const int subs = min(kSubs, (f_end - f_key + 15) >> 4);
@@ -175,18 +176,20 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     if (f_key < f_end) {
       look_up();
     } else {
-      ++f_id;
+      f_id = f_next;
       enter();
     }
   };
-  enter();
+  enter();  // (a batch's arrays were there before whatever kernel is still running)
+  wait_for_previous_kernel();
   for (int i = 0; i < kStages; ++i) fetch();
 
   uint32_t taken = 0;
   bool ok = true;
-  for (int id = id0; id < id_end; ++id) {
-    const KvPiece piece = work.pieces[id];
-    const KvSeq seq = arrays.seqs[piece.seq];
+  KvPiece piece;
+  for (int id = (int)blockIdx.x; id >= 0; id = piece.next) {
+    piece = work.pieces[id];
+    const KvSeq seq = piece.seq;
 
     // ---------------------------------------------------------------- rows
     uint32_t qa[kHd / 16][2 * kHalves];

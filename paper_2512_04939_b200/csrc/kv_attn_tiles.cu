@@ -17,9 +17,9 @@
 // columns it writes.
 //
 // Warps: softmax; two MMA issuers (one per tile), a TMA producer, one that looks after V; for codes eight that widen them:
-//   bf16  K and V come by TMA straight into their swizzled tiles; a tile of V that holds keys which some rows do not see passes
-//         the V warp: what no row sees becomes zero (a page's tail may hold anything, and 0 * NaN is NaN), and values that
-//         are not finite are taken out; the softmax adds them to the rows that see them.
+//   bf16  K and V come by TMA straight into their swizzled tiles; in V what no row sees becomes zero (a page's tail may
+//         hold anything, and 0 * NaN is NaN).  Values that are not finite, of keys that some rows see and others do not, make
+//         the piece come again, and then they are taken out here and added to the rows that see them.
 //   E4M3  codes and exponents come by bulk copies into a ring of their own; the eight warps widen them to the same tiles,
 //         exactly, and look after V on the way.
 #include "exp2.cuh"
@@ -123,10 +123,10 @@ struct Job {
   int min_seen;      // keys below it are seen by every row
   int max_seen;      // keys from it on by none
 };
-__device__ __forceinline__ Job job_of(const KvLaunch& work, const KvArrays& arrays, const KvAttend& at, int id) {
+__device__ __forceinline__ Job job_of(const KvLaunch& work, const KvAttend& at, int id) {
   Job j;
   j.p = work.pieces[id];
-  j.q = arrays.seqs[j.p.seq];
+  j.q = j.p.seq;
   j.tile0 = j.p.key0 / kTileKeys;
   j.tiles = (j.p.key1 - j.p.key0 + kTileKeys - 1) / kTileKeys;
   j.min_seen = kv_seen(j.q.len, j.q.rows, at.causal_block, j.p.row0 / at.group);
@@ -209,20 +209,20 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
   tc_fence_after();
   const uint32_t tmem_base = bars->tmem_base;
   const WaitCtl ctl{&bars->abort_flag, status};
+  if (threadIdx.x == 0) asm volatile("prefetch.global.L1 [%0];" ::"l"(work.pieces + blockIdx.x));
   wait_for_previous_kernel();
-  const int id0 = work.first[blockIdx.x], id_end = work.first[blockIdx.x + 1];
 
   // Every role goes over the CTA's pieces; and a second time over those whose reference did not do, twice each: once for the
   // maxima, once for the rows.
   enum Mode { kFast = 0, kMaxima = 1, kCareful = 2 };
   auto pieces = [&](auto run) {
-    for (int id = id0; id < id_end; ++id) {
-      run(id, kFast);
+    for (int id = (int)blockIdx.x; id >= 0;) {
+      id = run(id, kFast);
       __syncwarp();
     }
     named_barrier(10, Shape::kThreads);
     if (*reinterpret_cast<volatile int*>(&bars->any_again) == 0) return;
-    for (int id = id0; id < id_end; ++id)
+    for (int id = (int)blockIdx.x; id >= 0; id = work.pieces[id].next)
       if (__ldcg(work.again + id) != 0) {
         run(id, kMaxima);
         __syncwarp();
@@ -237,8 +237,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     uint32_t issued[2] = {0, 0};
     bool ok = true;
     const int per_tile = kTileKeys >> pool.page_shift;
-    pieces([&](int id, int) {
-      const Job job = job_of(work, arrays, at, id);
+    pieces([&](int id, int) -> int {
+      const Job job = job_of(work, at, id);
       for (int j = 0; j < job.tiles && ok; ++j) {
         const int key = (job.tile0 + j) * kTileKeys;
         const int n = min(per_tile, (job.q.len - key + pool.page_size - 1) >> pool.page_shift);
@@ -280,6 +280,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         if constexpr (kNarrow) ring.next<kRawSlots>();
         else ring.next<kStages>();
       }
+      return job.p.next;
     });
     if (lane == 0) {  // every load has landed before the CTA may go
       drain<kNarrow ? kRawSlots : kStages>(kNarrow ? bars->raw_full[0] : bars->k_full, issued[0], status);
@@ -311,12 +312,11 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     Ring ring;
     uint32_t step = 0, round = 0;
     bool ok = true;
-    pieces([&](int id, int mode) {
+    pieces([&](int id, int mode) -> int {
       if (elect_one()) {  // the same lane every time
-        if (!ok) return;
-        const Job job = job_of(work, arrays, at, id);
+        const Job job = job_of(work, at, id);
         const int mine = tiles_of(job, at, t);
-        if (mine > 0) {
+        if (ok && mine > 0) {
           ok = mbar_wait(&bars->q_ready[t], round & 1u, ctl) && mbar_wait(&bars->k_full[ring.slot], ring.phase, ctl);
           if (ok) {
             tc_fence_after();
@@ -362,6 +362,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
         round += mine > 0 ? 1u : 0u;
       }
+      return work.pieces[id].next;
     });
     __syncwarp();
     if (elect_one() && !ok) {  // what is under way must have retired before tensor memory is given up
@@ -377,13 +378,14 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     Ring ring, raw;
     uint32_t turn = 0;
     bool ok = true;
-    pieces([&](int id, int) {
+    pieces([&](int id, int mode) -> int {
       const uint32_t parity = turn++ & 1u;
-      const Job job = job_of(work, arrays, at, id);
+      const Job job = job_of(work, at, id);
       for (int j = 0; j < job.tiles && ok; ++j) {
         const int key = (job.tile0 + j) * kTileKeys;
         const int end = job.max_seen - key;           // rows of the tile from here on are seen by nobody
-        const int part = max(job.min_seen - key, 0);  // and from here on not by everybody
+        // and from here on not by everybody; that matters only where values are not finite, and then the piece comes again
+        const int part = mode == kCareful ? max(job.min_seen - key, 0) : end;
         if constexpr (kNarrow) {
           const int tid = threadIdx.x - kHelper * 32;
 #pragma unroll 1
@@ -411,7 +413,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
               if (kv_needs_second(byte)) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = mul_bf16x2(v[e], f.second * 0x10001u);
-                if (x == 1 && r >= part) {
+                if (x == 1 && r >= part && mode == kCareful) {
 #pragma unroll
                   for (int e = 0; e < 8; ++e) {
                     if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u, bad = bad || r < end;
@@ -439,9 +441,9 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         } else {
           ok = mbar_wait_warp(&bars->v_land[ring.slot], ring.phase, ctl);
           if (!ok) break;
-          if (part < kTileKeys) {
+          if (min(part, end) < kTileKeys) {
             bool bad = false;
-            for (int i = part * 8 + lane; i < kTileKeys * 8; i += 32)
+            for (int i = max(min(part, end), 0) * 8 + lane; i < kTileKeys * 8; i += 32)
 #pragma unroll
               for (int s = 0; s < kSubs; ++s) {
                 uint4* at_row = reinterpret_cast<uint4*>(smem_v + ring.slot * kTileBytes + s * kSubBytes) + i;
@@ -468,9 +470,10 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
         ring.next<kStages>();
       }
+      return job.p.next;
     });
   } else if (warp >= kIssuer) {
-    pieces([](int, int) {});  // (beside the warps that widen codes there is nothing left for the fourth)
+    pieces([&](int id, int) { return work.pieces[id].next; });  // (beside the warps that widen codes there is nothing left for the fourth)
   } else {
     // ------------------------------------------------------------------ softmax: a thread is a row, or the half of one
     const int t = warp / (4 * kStreams), c = (warp >> 2) % kStreams, quarter = warp & 3;
@@ -481,6 +484,34 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     uint32_t step = 0, round = 0, turn = 0;
     bool ok = true;
     float kept = -INFINITY;  // the row's maximum, from one sweep to the next
+    // The queries, this thread's half row.  Those before have been read where o_done has come: it follows their last product.
+    constexpr int kChunks = kHd / 16;  // of 16 bytes
+    int given = -1;                    // the piece whose queries are there already
+    auto read_q = [&](const Job& job, uint4 (&x)[kChunks]) {
+      const bool live = t * 128 + r < job.p.rows;
+      const int row = job.p.row0 + (live ? t * 128 + r : 0);
+      const __nv_bfloat16* src = at.q + (job.q.row0 + row / at.group) * at.q_stride.row +
+                                 (job.p.kv_head * at.group + row % at.group) * at.q_stride.head + c * (kHd / 2);
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) x[i] = live ? ldg16(src + i * 8) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    auto give_q = [&](const uint4 (&x)[kChunks]) {
+      if constexpr (kOnes) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 * i] = x[i].x, w[4 * i + 1] = x[i].y, w[4 * i + 2] = x[i].z, w[4 * i + 3] = x[i].w;
+        tmem_st16(tmem_base + lane_base + Shape::kColQ + t * 32 + c * 16, w);
+        tmem_st_wait();
+        tc_fence_before();
+      } else {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i)
+          *reinterpret_cast<uint4*>(smem_q + t * kTileBytes + c * kSubBytes + r * 128 + (i ^ (r & 7)) * 16) = x[i];
+        fence_proxy_async_shared();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->q_ready[t]);
+    };
     auto largest = [](const uint32_t (&s)[32]) {
       float m[4];
 #pragma unroll
@@ -493,37 +524,20 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       }
       return fmaxf(fmax3(m[0], m[1], m[2]), m[3]);
     };
-    pieces([&](int id, int mode) {
+    pieces([&](int id, int mode) -> int {
       const uint32_t parity = turn++ & 1u;
-      const Job job = job_of(work, arrays, at, id);
+      const Job job = job_of(work, at, id);
       const int mine = tiles_of(job, at, t);
       const bool live = t * 128 + r < job.p.rows;
       const int row = job.p.row0 + (live ? t * 128 + r : 0), token = row / at.group;
       const int seen = kv_seen(job.q.len, job.q.rows, at.causal_block, token);
       const long long out_row = (long long)(job.q.row0 + token) * at.q_heads + job.p.kv_head * at.group + row % at.group;
-      if (mine > 0) {
-        // the queries before have been read: o_done came behind their last product
-        const __nv_bfloat16* src = at.q + (job.q.row0 + token) * at.q_stride.row + (job.p.kv_head * at.group + row % at.group) * at.q_stride.head;
-        constexpr int kChunks = kHd / 8 / kStreams;  // 16 bytes each; streams share a row
+      if (mine > 0 && given != id) {
         uint4 x[kChunks];
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i) x[i] = live ? ldg16(src + (c * kChunks + i) * 8) : make_uint4(0u, 0u, 0u, 0u);
-        if constexpr (kOnes) {
-          uint32_t w[16];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[4 * i] = x[i].x, w[4 * i + 1] = x[i].y, w[4 * i + 2] = x[i].z, w[4 * i + 3] = x[i].w;
-          tmem_st16(tmem_base + lane_base + Shape::kColQ + t * 32 + c * 16, w);
-          tmem_st_wait();
-          tc_fence_before();
-        } else {
-#pragma unroll
-          for (int i = 0; i < kChunks; ++i)
-            *reinterpret_cast<uint4*>(smem_q + t * kTileBytes + c * kSubBytes + r * 128 + (i ^ (r & 7)) * 16) = x[i];
-          fence_proxy_async_shared();
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->q_ready[t]);
+        read_q(job, x);
+        give_q(x);
       }
+      given = -1;
       const int first_seen = __shfl_sync(0xffffffffu, live ? seen : 0x7fffffff, 0);  // rows of a warp see ever more
       float top = -INFINITY, ref = 0.0f;  // the row's reference; ref: what is subtracted, top where that is finite
       float2 sum = make_float2(0.0f, 0.0f);
@@ -626,26 +640,38 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           }
         }
       }
+      float row_sum = sum.x + sum.y;
       if (mine > 0) {
+        // the next piece's queries are under way while the last products are, and its first scores while the rows leave
+        Job next = job;
+        bool some = false;
+        uint4 x[kChunks];
+        if (mode == kFast && job.p.next >= 0) {
+          next = job_of(work, at, job.p.next);
+          some = tiles_of(next, at, t) > 0;
+          if (some) read_q(next, x);
+        }
         ok = ok && mbar_wait_warp(&bars->o_done[t], round & 1u, ctl);
         ++round;
         tc_fence_after();
+        if (!kOnes && mode != kMaxima) {
+          const float2 both = exchange(s_addr - c * 64, 64, row_sum);  // where the last scores were
+          row_sum = both.x + both.y;
+        }
+        if (some) {
+          give_q(x);
+          given = job.p.next;
+        }
       }
-      if (mode == kMaxima) return;
+      if (mode == kMaxima) return 0;
 
       // ---------------------------------------------------------------- the piece's rows
       const bool has = live && seen > job.p.key0;  // the row sees keys of this piece
-      float row_sum = sum.x + sum.y;
-      if constexpr (kOnes) {
-        if (mine > 0) {
-          uint32_t l;
-          tmem_ld1(o_addr + 64, l);
-          tmem_ld_wait();
-          row_sum = has ? __uint_as_float(l) : 0.0f;
-        }
-      } else if (mine > 0) {
-        const float2 both = exchange(s_addr - c * 64, 64, row_sum);  // where the last scores were
-        row_sum = both.x + both.y;
+      if (kOnes && mine > 0) {
+        uint32_t l;
+        tmem_ld1(o_addr + 64, l);
+        tmem_ld_wait();
+        row_sum = has ? __uint_as_float(l) : 0.0f;
       }
       const bool bad = *reinterpret_cast<volatile int*>(&bars->taken_out[parity]) == id + 1;
       const bool whole = job.p.slot < 0;
@@ -736,9 +762,11 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           __threadfence();
           const float2* ml = reinterpret_cast<const float2*>(work.sums) + (size_t)job.p.first_slot * 256 + t * 128 + r;
           float joint = -INFINITY, l = 0.0f;
+#pragma unroll 4
           for (int w = 0; w < job.p.parts; ++w) joint = fmaxf(joint, __ldcg(ml + (size_t)w * 256).x);
           const float use = joint == -INFINITY ? 0.0f : joint;
           auto weight_of = [&](float x) { return x == -INFINITY ? 1.0f : fast_exp2(x - use); };
+#pragma unroll 4
           for (int w = 0; w < job.p.parts; ++w) {
             const float2 x = __ldcg(ml + (size_t)w * 256);
             l += x.y * weight_of(x.x);
@@ -750,6 +778,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             float acc[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
+#pragma unroll 2
             for (int w = 0; w < job.p.parts; ++w) {
               const float wt = weight_of(__ldcg(ml + (size_t)w * 256).x);
               const float4* part = reinterpret_cast<const float4*>(work.rows) + ((size_t)(job.p.first_slot + w) * (kHd / 4) + ch0 / 4) * 256 + t * 128 + r;
@@ -774,6 +803,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
         named_barrier(9, kSoftmaxWarps * 32);  // last_of_join has been read
       }
+      return job.p.next;
     });
   }
   tc_fence_before();
@@ -781,7 +811,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
   tc_fence_after();
   if (warp == kIssuer) tmem_dealloc(tmem_base, 512);
   if (bars->any_again != 0) {
-    for (int id = id0 + (int)threadIdx.x; id < id_end; id += Shape::kThreads) work.again[id] = 0;
+    if (threadIdx.x == 0)
+      for (int id = (int)blockIdx.x; id >= 0; id = work.pieces[id].next) work.again[id] = 0;
   }
 }
 

@@ -14,6 +14,10 @@ namespace lv {
 
 namespace {
 
+#ifndef LV_MINU
+#define LV_MINU 2
+#define LV_OVH 1.5
+#endif
 constexpr int kMoveThreads = 256;
 
 // The sequence that a row of the packed tensors belongs to.
@@ -192,7 +196,6 @@ void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int hea
   };
   auto take_lists = [&](const KvWork& w, litevggt_kv_batch::Places* p) {
     p->pieces = take(w.pieces.size() * sizeof(KvPiece));
-    p->first = take(w.first.size() * sizeof(int));
     p->joins = take((size_t)w.joins * sizeof(int));
     p->again = take(w.pieces.size() * sizeof(int));
   };
@@ -213,8 +216,8 @@ void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int hea
   put(b->o_seqs, b->seqs.data(), b->seqs.size() * sizeof(KvSeq));
   put(b->o_pages, pages, n_pages * sizeof(int));
   auto put_lists = [&](const KvWork& w, const litevggt_kv_batch::Places& p) {
-    put(p.pieces, w.pieces.data(), w.pieces.size() * sizeof(KvPiece));
-    put(p.first, w.first.data(), w.first.size() * sizeof(int));
+    const std::vector<KvPiece> chain = kv_chain(w);
+    put(p.pieces, chain.data(), chain.size() * sizeof(KvPiece));
   };
   put_lists(b->few, b->at_few);
   put_lists(b->tiles, b->at_tiles);
@@ -251,7 +254,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
   b->few_rows = most;
   const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype == LITEVGGT_KV_E4M3);
   b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
-                  KvCut{kKvFewRows, kKvFewUnit, std::min(c->num_sms * per_sm, kKvFewWorkers), 1, INT32_MAX, 1.0});
+                  KvCut{kKvFewRows, kKvFewUnit, std::min(c->num_sms * per_sm, kKvFewWorkers), LV_MINU, INT32_MAX, LV_OVH});
   b->tiles = kv_cut(b->seqs, many, b->group, c->cfg.kv_heads, causal_block, KvCut{kKvTileRows, kKvTileUnit, c->num_sms, 4, 512, 4.0});
   lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
   return LITEVGGT_OK;

@@ -27,7 +27,6 @@ struct KvArrays {
 };
 struct KvLaunch {
   const KvPiece* pieces;
-  const int* first;
   int workers;
   int* joins;   // counters, zero between launches
   int* again;   // marks of the pieces, likewise
@@ -73,7 +72,7 @@ struct litevggt_kv_batch {
   size_t bytes;                // of device memory
   size_t o_seqs, o_pages;
   struct Places {
-    size_t pieces, first, joins, again, rows, sums;
+    size_t pieces, joins, again, rows, sums;
   } at_few, at_tiles;
   uint8_t* base = nullptr;     // the caller's device memory
 };
@@ -85,8 +84,7 @@ inline KvArrays kv_arrays(const litevggt_kv_batch& b) {
 }
 
 inline KvLaunch kv_launch(const litevggt_kv_batch& b, const KvWork& work, const litevggt_kv_batch::Places& at) {
-  return KvLaunch{reinterpret_cast<const KvPiece*>(b.base + at.pieces), reinterpret_cast<const int*>(b.base + at.first),
-                  (int)work.first.size() - 1, reinterpret_cast<int*>(b.base + at.joins), reinterpret_cast<int*>(b.base + at.again),
+  return KvLaunch{reinterpret_cast<const KvPiece*>(b.base + at.pieces), work.workers(), reinterpret_cast<int*>(b.base + at.joins), reinterpret_cast<int*>(b.base + at.again),
                   reinterpret_cast<float*>(b.base + at.rows), reinterpret_cast<float*>(b.base + at.sums)};
 }
 

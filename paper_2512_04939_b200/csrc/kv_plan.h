@@ -16,14 +16,20 @@ struct KvSeq {
 
 // Keys [key0, key1) of rows [row0, row0 + rows) of one sequence and K/V head.  The `group` query heads that share the head
 // are rows of their own, side by side: row = token * group + head within the group.
+// A worker is told one number, that of its first piece, which is its own, and finds everything else in the pieces: what a CTA has
+// to read before its first load of keys is this and the page.
 struct alignas(16) KvPiece {
-  int seq, kv_head, row0, rows;
-  int key0, key1;
+  KvSeq seq;
+  int kv_head, row0, rows, key0;
+  int key1;
   int slot;        // where its partial rows go, -1: the rows have no other piece
   int first_slot;  // of all pieces of the same rows
-  int parts, join; // how many they are, and the counter of those that have come
+  int parts;       // how many they are,
+  int join;        // and the counter of those that have come
+  int next;        // the worker's next piece, -1: none
   int pad[2];
 };
+static_assert(sizeof(KvPiece) == 64, "four loads of 16 bytes");
 
 // Tokens that row `token` of a sequence's chunk sees; none if it is negative.
 #ifdef __CUDACC__
@@ -39,7 +45,28 @@ struct KvWork {
   std::vector<KvPiece> pieces;
   std::vector<int> first;  // [workers + 1] a worker's pieces; every worker that is launched has one
   int slots = 0, joins = 0;
+  int workers() const { return first.empty() ? 0 : (int)first.size() - 1; }
 };
+
+// The pieces as the device gets them: worker w's first one is number w, the others lie behind.
+inline std::vector<KvPiece> kv_chain(const KvWork& work) {
+  const int workers = work.workers();
+  std::vector<KvPiece> out((size_t)workers);
+  for (int w = 0; w < workers; ++w) {
+    size_t last = (size_t)w;
+    for (int i = work.first[(size_t)w]; i < work.first[(size_t)w + 1]; ++i) {
+      if (i == work.first[(size_t)w]) {
+        out[last] = work.pieces[(size_t)i];
+      } else {
+        out[last].next = (int)out.size();
+        last = out.size();
+        out.push_back(work.pieces[(size_t)i]);
+      }
+      out[last].next = -1;
+    }
+  }
+  return out;
+}
 
 // What a kernel needs from the cutting.
 struct KvCut {
@@ -89,7 +116,7 @@ inline double kv_cut_by(double share, const std::vector<KvSeq>& seqs, const std:
           if (units - done - take < cut.min_units) take = units - done;  // no crumbs
           take = std::min(std::max(take, std::min(cut.min_units, units - done)), std::min(units - done, cut.max_units));
           KvPiece p{};
-          p.seq = s; p.kv_head = h; p.row0 = r; p.rows = n;
+          p.seq = q; p.kv_head = h; p.row0 = r; p.rows = n;
           p.key0 = done * cut.unit;
           p.key1 = (int)std::min((long long)(done + take) * cut.unit, (long long)seen);
           p.slot = -1;
