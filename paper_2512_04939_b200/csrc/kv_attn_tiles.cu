@@ -526,23 +526,27 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     };
     pieces([&](int id, int mode) -> int {
       const uint32_t parity = turn++ & 1u;
-      const Job job = job_of(work, at, id);
-      const int mine = tiles_of(job, at, t);
-      const bool live = t * 128 + r < job.p.rows;
-      const int row = job.p.row0 + (live ? t * 128 + r : 0), token = row / at.group;
-      const int seen = kv_seen(job.q.len, job.q.rows, at.causal_block, token);
-      const long long out_row = (long long)(job.q.row0 + token) * at.q_heads + job.p.kv_head * at.group + row % at.group;
-      if (mine > 0 && given != id) {
-        uint4 x[kChunks];
-        read_q(job, x);
-        give_q(x);
+      // What the sweep needs of the piece; the rest is read again behind it, where it does not hold registers.
+      int mine, key_base, seen;
+      bool live;
+      {
+        const Job job = job_of(work, at, id);
+        mine = tiles_of(job, at, t);
+        key_base = job.tile0 * kTileKeys + c * 64;
+        live = t * 128 + r < job.p.rows;
+        seen = kv_seen(job.q.len, job.q.rows, at.causal_block, (job.p.row0 + (live ? t * 128 + r : 0)) / at.group);
+        if (mine > 0 && given != id) {
+          uint4 x[kChunks];
+          read_q(job, x);
+          give_q(x);
+        }
+        given = -1;
       }
-      given = -1;
       const int first_seen = __shfl_sync(0xffffffffu, live ? seen : 0x7fffffff, 0);  // rows of a warp see ever more
       float top = -INFINITY, ref = 0.0f;  // the row's reference; ref: what is subtracted, top where that is finite
       float2 sum = make_float2(0.0f, 0.0f);
 
-      auto key_of = [&](int j) { return (job.tile0 + j) * kTileKeys + c * 64; };
+      auto key_of = [&](int j) { return key_base + j * kTileKeys; };
       auto scores_in = [&]() {
         const bool in = mbar_wait_warp(&bars->s_full[t][c], step & 1u, ctl);
         if (in) tc_fence_after();
@@ -640,13 +644,18 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           }
         }
       }
+      asm volatile("" ::: "memory");
+      const Job job = job_of(work, at, id);
+      const int row = job.p.row0 + (live ? t * 128 + r : 0), token = row / at.group;
+      const long long out_row = (long long)(job.q.row0 + token) * at.q_heads + job.p.kv_head * at.group + row % at.group;
       float row_sum = sum.x + sum.y;
       if (mine > 0) {
-        // the next piece's queries are under way while the last products are, and its first scores while the rows leave
+        // The next piece's queries are under way while the last products are, and its first scores while the rows leave.  (At
+        // head dim 64 that costs registers which the sweep has not got: 792 -> 812 us at 2048 rows over 83,280 keys.)
         Job next = job;
         bool some = false;
         uint4 x[kChunks];
-        if (mode == kFast && job.p.next >= 0) {
+        if (!kOnes && mode == kFast && job.p.next >= 0) {
           next = job_of(work, at, job.p.next);
           some = tiles_of(next, at, t) > 0;
           if (some) read_q(next, x);
