@@ -223,7 +223,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     named_barrier(10, Shape::kThreads);
     if (*reinterpret_cast<volatile int*>(&bars->any_again) == 0) return;
     for (int id = (int)blockIdx.x; id >= 0; id = work.pieces[id].next)
-      if (__ldcg(work.again + id) != 0) {
+      if (*reinterpret_cast<volatile int*>(work.again + id) != 0) {
         run(id, kMaxima);
         __syncwarp();
         run(id, kCareful);

@@ -14,10 +14,6 @@ namespace lv {
 
 namespace {
 
-#ifndef LV_MINU
-#define LV_MINU 2
-#define LV_OVH 1.5
-#endif
 constexpr int kMoveThreads = 256;
 
 
@@ -291,8 +287,21 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
   b->few_rows = most;
   const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype == LITEVGGT_KV_E4M3);
   b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
-                  KvCut{kKvFewRows, kKvFewUnit, std::min(c->num_sms * per_sm, kKvFewWorkers), LV_MINU, INT32_MAX, LV_OVH});
-  b->tiles = kv_cut(b->seqs, many, b->group, c->cfg.kv_heads, causal_block, KvCut{kKvTileRows, kKvTileUnit, c->num_sms, 4, 512, 4.0});
+                  KvCut{kKvFewRows, kKvFewUnit, std::min(c->num_sms * per_sm, kKvFewWorkers), kKvFewLeast, INT32_MAX, kKvFewPiece});
+  // In units of 128 keys against 256 rows.  CTAs of one row tile take more time for the same work, but there are twice as many:
+  // where the pieces are few it can be better to have them than to cut keys, since parts have to be joined.
+  const double piece = c->cfg.head_dim == 64 ? kKvTilePiece64 : kKvTilePiece128;
+  auto cut_tiles = [&](int rows, double unit) {
+    KvWork w = kv_cut(b->seqs, many, b->group, c->cfg.kv_heads, causal_block,
+                      KvCut{rows, kKvTileUnit, c->num_sms, kKvTileLeast, kKvTileMost, piece / unit});
+    w.cost = w.cost * unit + (w.joins > 0 ? kKvJoinCost : 0.0);
+    return w;
+  };
+  b->tiles = cut_tiles(kKvTileRows, 1.0);
+  if (b->tiles.cost < kKvShortCost) {  // (elsewhere it cannot win, and need not be counted)
+    KvWork narrow = cut_tiles(kKvTileRows / 2, kKvHalfTiles);
+    if (narrow.cost < b->tiles.cost) b->tiles = narrow;
+  }
   lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
   return LITEVGGT_OK;
 }

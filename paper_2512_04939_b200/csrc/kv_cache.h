@@ -98,12 +98,23 @@ cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch
 constexpr int kKvFewRows = 16;    // rows of a piece at most
 constexpr int kKvFewWarps = 8;
 constexpr int kKvFewUnit = 128;   // keys
+// A piece of so many units at least where keys are cut, and what a piece costs beside its keys: a token over 262 keys takes
+// 8.2 us in one CTA a head, 4.9 in two, over 1,041 9.0 and 8.5, over 4,164 11.6 and 9.0 (least 4 and 2; eight are worse everywhere).
+constexpr int kKvFewLeast = 2;
+constexpr double kKvFewPiece = 1.5;
 constexpr int kKvFewWorkers = 512;  // CTAs of a launch at most: the weights of a row's parts lie in shared memory
 int kv_few_ctas(int head_dim, bool narrow);  // on an SM
 cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
 // kv_attn_tiles.cu
 constexpr int kKvTileRows = 256;
 constexpr int kKvTileUnit = 128;
+// Units of a piece: at least, where keys are cut; at most, so that no accumulator is carried through more than 512 tiles
+// (the tensor core's chain of additions loses bits that sums in 32 bits between pieces keep).
+constexpr int kKvTileLeast = 4, kKvTileMost = 512;
+// What a piece costs beside its keys, joining its parts, a unit of half the rows, in units (measured on 261 rows over 522 keys up to
+// 2,748 over 21,984): 1,041 rows over 5,205 keys 48.1 us with 4 for a piece, 45.5 with 2; chunks of head dim 128 the other
+// way about, 278 and 256 us, their rows being twice as long.  261 rows over 522 keys: 15.0 us in tiles of two, 14.0 in single ones.
+constexpr double kKvTilePiece64 = 2.0, kKvTilePiece128 = 4.0, kKvJoinCost = 8.0, kKvHalfTiles = 0.8, kKvShortCost = 200.0;
 cudaError_t launch_kv_attn_tiles(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
 
 }  // namespace lv

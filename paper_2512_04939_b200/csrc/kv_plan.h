@@ -45,6 +45,7 @@ struct KvWork {
   std::vector<KvPiece> pieces;
   std::vector<int> first;  // [workers + 1] a worker's pieces; every worker that is launched has one
   int slots = 0, joins = 0;
+  double cost = 0.0;       // of the worker with the most to do, in units
   int workers() const { return first.empty() ? 0 : (int)first.size() - 1; }
 };
 
@@ -94,6 +95,7 @@ inline double kv_cut_by(double share, const std::vector<KvSeq>& seqs, const std:
     if (worker + 1 >= cut.workers || (size_t)work.first.back() == work.pieces.size()) return false;
     work.first.push_back((int)work.pieces.size());
     ++worker;
+    work.cost = std::max(work.cost, spent - begun);
     begun = spent;
     return true;
   };
@@ -138,6 +140,7 @@ inline double kv_cut_by(double share, const std::vector<KvSeq>& seqs, const std:
       }
   }
   work.first.push_back((int)work.pieces.size());
+  work.cost = std::max(work.cost, spent - begun);
   return spent - begun;
 }
 

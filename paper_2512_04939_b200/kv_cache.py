@@ -21,11 +21,6 @@ from .binding import KVConfig, _check, load_library
 _DTYPES = {"bf16": (0, torch.bfloat16), "e4m3": (1, torch.float8_e4m3fn)}
 
 
-def _strides(t: torch.Tensor) -> tuple[int, int]:
-    """Elements from row to row and from head to head; the stride of a dimension of one says nothing."""
-    return (t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
-
-
 class KVBatch:
     """Rows, lengths and pages of a step's sequences, planned for one cache (see :meth:`KVCache.batch`)."""
 
@@ -35,6 +30,8 @@ class KVBatch:
         self.memory = memory
         self.rows = rows
         self.q_heads = q_heads
+        self.kv_shape = (rows, owner.kv_heads, owner.head_dim)
+        self.q_shape = (rows, q_heads, owner.head_dim)
         self._stream = stream
 
     def __del__(self):
@@ -68,8 +65,10 @@ class KVCache:
             if not t.is_cuda or t.device != k.device:
                 raise ValueError("every pool must live on the same CUDA device")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        self.device = k.device
+        self.device, self._index = k.device, k.get_device()
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self._scale = 1.0 / math.sqrt(self.head_dim)
+        self._append, self._attend = self.lib.litevggt_kv_append, self.lib.litevggt_kv_attend
         self.status = torch.zeros(64, dtype=torch.int32, device=k.device)
         cfg = KVConfig(self.pages, self.page_size, self.kv_heads, self.head_dim, 1 if narrow else 0)
         self.handle = C.c_void_p()
@@ -134,14 +133,14 @@ class KVCache:
     def append(self, batch: KVBatch, k: torch.Tensor, v: torch.Tensor) -> None:
         """Writes ``k``, ``v`` [batch.rows, kv_heads, head_dim] (bfloat16; slices of a fused projection will do) into the
         batch's sequences as their last tokens."""
-        for name, t in (("k", k), ("v", v)):
-            self._check_rows(name, t, batch.rows, self.kv_heads)
-        _check(self.lib.litevggt_kv_append(self.handle, batch.handle, k.data_ptr(), *_strides(k), v.data_ptr(), *_strides(v),
-                                           self._use(batch)), "kv_append")
+        code = self._append(self.handle, batch.handle, *self._rows("k", k, batch.kv_shape), *self._rows("v", v, batch.kv_shape),
+                            self._use(batch))
+        if code:
+            _check(code, "kv_append")
 
     def gather(self, batch: KVBatch) -> tuple[torch.Tensor, torch.Tensor]:
         """K and V of the batch's rows, bfloat16 [batch.rows, kv_heads, head_dim]."""
-        k = torch.empty(batch.rows, self.kv_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+        k = torch.empty(batch.kv_shape, dtype=torch.bfloat16, device=self.device)
         v = torch.empty_like(k)
         _check(self.lib.litevggt_kv_gather(self.handle, batch.handle, k.data_ptr(), v.data_ptr(), self._use(batch)), "kv_gather")
         return k, v
@@ -149,16 +148,16 @@ class KVCache:
     def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
         """softmax(scale q K^T) V of the batch's rows over the tokens that they see; ``q`` bfloat16 [batch.rows, q_heads, head_dim].
         ``scale`` is 1 / sqrt(head_dim) unless given.  A row that sees no token comes out as zero."""
-        self._check_rows("q", q, batch.rows, batch.q_heads)
+        q_rows = self._rows("q", q, batch.q_shape)
         if out is None:
-            out = torch.empty(batch.rows, batch.q_heads, self.head_dim, dtype=torch.bfloat16, device=self.device)
+            out = q.new_empty(batch.q_shape)
         else:
-            self._check_rows("out", out, batch.rows, batch.q_heads)
+            self._rows("out", out, batch.q_shape)
             if not out.is_contiguous():
                 raise ValueError("out must be contiguous")
-        scale = 1.0 / math.sqrt(self.head_dim) if scale is None else scale
-        _check(self.lib.litevggt_kv_attend(self.handle, batch.handle, q.data_ptr(), *_strides(q), scale, out.data_ptr(),
-                                           self._use(batch)), "kv_attend")
+        code = self._attend(self.handle, batch.handle, *q_rows, self._scale if scale is None else scale, out.data_ptr(), self._use(batch))
+        if code:
+            _check(code, "kv_attend")
         return out
 
     # ------------------------------------------------------------------ checks
@@ -172,7 +171,7 @@ class KVCache:
         return n.value
 
     def _stream(self) -> int:
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
+        return torch._C._cuda_getCurrentRawStream(self._index)  # (a Stream object costs 3 us)
 
     def _use(self, batch: KVBatch) -> int:
         """The current stream, to which the batch's memory now belongs as well."""
@@ -182,10 +181,14 @@ class KVCache:
             self.status.record_stream(torch.cuda.current_stream(self.device))
         return stream
 
-    def _check_rows(self, name: str, t: torch.Tensor, rows: int, heads: int):
-        if t.shape != (rows, heads, self.head_dim):
-            raise ValueError(f"{name} must be [{rows}, {heads}, {self.head_dim}], got {tuple(t.shape)}")
-        if t.dtype != torch.bfloat16 or t.device != self.device:
+    def _rows(self, name: str, t: torch.Tensor, shape: tuple) -> tuple[int, int, int]:
+        """A checked tensor's address and its strides from row to row and head to head (that of a dimension of one says nothing)."""
+        if t.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}, got {tuple(t.shape)}")
+        if t.dtype != torch.bfloat16 or t.get_device() != self._index:
             raise ValueError(f"{name} must be bfloat16 on {self.device}, got {t.dtype} on {t.device}")
-        if t.stride(2) != 1 or any(n % 8 for n in _strides(t)) or t.data_ptr() % 16:
+        row, head, channel = t.stride()
+        row, head, address = row if shape[0] > 1 else 0, head if shape[1] > 1 else 0, t.data_ptr()
+        if channel != 1 or row % 8 or head % 8 or address % 16:
             raise ValueError(f"{name}'s head_dim must be contiguous, its rows and heads 16-byte aligned, got strides {t.stride()}")
+        return address, row, head
