@@ -19,3 +19,4 @@ from .binding import (  # noqa: F401
     load_library,
 )
 from .kv_cache import KVBatch, KVCache  # noqa: E402,F401
+from .streaming import StreamingGlobalAttention  # noqa: E402,F401

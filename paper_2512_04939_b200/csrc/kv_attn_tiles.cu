@@ -212,9 +212,15 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
   if (threadIdx.x == 0) asm volatile("prefetch.global.L1 [%0];" ::"l"(work.pieces + blockIdx.x));
   wait_for_previous_kernel();
 
+  enum Mode { kFast = 0, kMaxima = 1, kCareful = 2 };
+  // Steps of a row tile in which some rows do not see all keys, and all of a piece that is done again: those that reach past
+  // edge_from.  Rows may see few keys there, so their probabilities go in as two bf16 numbers each, in two products; elsewhere
+  // what one of them rounds averages out.
+  auto edge_from = [&](const Job& job, int mode, int t) {
+    return mode == kCareful ? 0 : kv_seen(job.q.len, job.q.rows, at.causal_block, (job.p.row0 + t * 128) / at.group);
+  };
   // Every role goes over the CTA's pieces; and a second time over those whose reference did not do, twice each: once for the
   // maxima, once for the rows.
-  enum Mode { kFast = 0, kMaxima = 1, kCareful = 2 };
   auto pieces = [&](auto run) {
     for (int id = (int)blockIdx.x; id >= 0;) {
       id = run(id, kFast);
@@ -315,7 +321,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     pieces([&](int id, int mode) -> int {
       if (elect_one()) {  // the same lane every time
         const Job job = job_of(work, at, id);
-        const int mine = tiles_of(job, at, t);
+        const int mine = tiles_of(job, at, t), all_see = edge_from(job, mode, t);
         if (ok && mine > 0) {
           ok = mbar_wait(&bars->q_ready[t], round & 1u, ctl) && mbar_wait(&bars->k_full[ring.slot], ring.phase, ctl);
           if (ok) {
@@ -340,6 +346,12 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
                 for (int k = 0; k < kKeys / 16; ++k)
                   umma_ts(o_col, s_col + c * 64 + k * 8, v_desc_at((uint32_t)((ring.slot * kTileBytes + (c * 64 + k * 16) * 128) >> 4)),
                           idesc_pv, (j | c | k) != 0 ? 1u : 0u);
+                if ((job.tile0 + j) * kTileKeys + c * 64 + kKeys > all_see) {  // what the rounding left over
+#pragma unroll
+                  for (int k = 0; k < kKeys / 16; ++k)
+                    umma_ts(o_col, s_col + c * 64 + 32 + k * 8, v_desc_at((uint32_t)((ring.slot * kTileBytes + (c * 64 + k * 16) * 128) >> 4)),
+                            idesc_pv, 1u);
+                }
               }
               if (j + 1 < mine) {
                 if (c == 0 && !(ok = mbar_wait(&bars->k_full[next.slot], next.phase, ctl))) break;
@@ -527,7 +539,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     pieces([&](int id, int mode) -> int {
       const uint32_t parity = turn++ & 1u;
       // What the sweep needs of the piece; the rest is read again behind it, where it does not hold registers.
-      int mine, key_base, seen;
+      int mine, key_base, seen, all_see;
       bool live;
       {
         const Job job = job_of(work, at, id);
@@ -535,6 +547,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         key_base = job.tile0 * kTileKeys + c * 64;
         live = t * 128 + r < job.p.rows;
         seen = kv_seen(job.q.len, job.q.rows, at.causal_block, (job.p.row0 + (live ? t * 128 + r : 0)) / at.group);
+        all_see = edge_from(job, mode, t);
         if (mine > 0 && given != id) {
           uint4 x[kChunks];
           read_q(job, x);
@@ -542,7 +555,6 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
         given = -1;
       }
-      const int first_seen = __shfl_sync(0xffffffffu, live ? seen : 0x7fffffff, 0);  // rows of a warp see ever more
       float top = -INFINITY, ref = 0.0f;  // the row's reference; ref: what is subtracted, top where that is finite
       float2 sum = make_float2(0.0f, 0.0f);
 
@@ -558,7 +570,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars->p_ready[t][c]);
       };
-      // This thread's 64 scores of a step.  With kEdge some rows of the warp may not see all of its keys.
+      // This thread's 64 scores of a step.  With kEdge some rows may not see all of its keys.
       uint32_t s[2][32];
       auto load = [&](bool edge, int key) {
         tmem_ld32(s_addr, s[0]);
@@ -578,23 +590,29 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         const float2 scale2 = make_float2(at.scale_log2, at.scale_log2), ref2 = make_float2(-ref, -ref);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          uint32_t p[16];
+          uint32_t p[16], rest[kEdge ? 16 : 1];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float2 x = __ffma2_rn(make_float2(__uint_as_float(s[g][2 * i]), __uint_as_float(s[g][2 * i + 1])), scale2, ref2);
             if (!kEdge && i < kPolyPairs) x = poly_exp2_clamped(x);
             else x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
-            p[i] = pack_bf16(x.x, x.y);
-            // Where a row may see few keys, the sum is that of the rounded probabilities, so that their rounding changes only
-            // what a key weighs among the others; elsewhere it averages out.
-            if constexpr (!kOnes) sum = __fadd2_rn(sum, kEdge ? make_float2(bf16_lo(p[i]), bf16_hi(p[i])) : x);
+            if constexpr (kEdge) {
+              // The upper half as it is, and the rest; never a rest of zero or less beside a probability, which an infinite value
+              // would make a NaN of.
+              p[i] = __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632);
+              rest[i] = pack_bf16(fmaf(x.x, 9.3e-10f, x.x - bf16_lo(p[i])), fmaf(x.y, 9.3e-10f, x.y - bf16_hi(p[i])));
+            } else {
+              p[i] = pack_bf16(x.x, x.y);
+            }
+            if constexpr (!kOnes) sum = __fadd2_rn(sum, x);
           }
+          if constexpr (kEdge) tmem_st16(s_addr + 32 + g * 16, rest);
           tmem_st16(s_addr + g * 16, p);
         }
       };
       float most = -INFINITY;
       auto add_maximum = [&](int key) {
-        load(key + 64 > first_seen, key);
+        load(key + kKeys > all_see, key);
         most = fmaxf(most, fmaxf(largest(s[0]), largest(s[1])));
       };
       // The two threads of a row tell each other a number, by way of two columns of tensor memory that nothing else uses just
@@ -638,7 +656,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           for (int j = 0; j < mine && ok; ++j, ++step) {
             ok = scores_in();
             if (!ok) break;
-            if (mode == kCareful || key_of(j) + 64 > first_seen) take_half(std::true_type{}, key_of(j));
+            if (key_of(j) + kKeys > all_see) take_half(std::true_type{}, key_of(j));
             else take_half(std::false_type{}, key_of(j));
             give_p();
           }

@@ -225,6 +225,36 @@ def test_scores_that_grow_along_the_keys(dtype, rows):
     scene.check([rows], -q, scene.cache.attend(batch, -q.cuda()))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_pieces_that_are_done_again(dtype, head_dim):
+    """Many pieces a CTA, whole ones and parts, and in some heads scores that leave the first keys' maximum far behind (by more
+    than 2^60): those pieces are done again, the others are not, and nothing of it is left for the next call."""
+    heads, lengths, rows = 6, [3000, 401, 64], [300, 200, 40]
+    scene = Scene(lengths, heads, head_dim, dtype, 64, seed=14)
+    line = torch.randn(head_dim, generator=scene.g)
+    line /= line.norm()
+    at = 0
+    for n in lengths:
+        for h in (1, 4):
+            scene.k_new[at:at + n, h] += (line * torch.linspace(-45, 45, n)[:, None]).bfloat16()
+        at += n
+    scene.store()
+    batch = scene.cache.batch(rows, lengths, scene.pages, causal_block=1)
+    q = (line * 8.0 * (head_dim / 64) ** 0.5 + 0.3 * torch.randn(sum(rows), heads, head_dim, generator=scene.g)).bfloat16()
+    out = scene.cache.attend(batch, q.cuda())
+    scene.check(rows, q, out, 1)
+    assert torch.equal(out, scene.cache.attend(batch, q.cuda()))
+    calm = scene.queries(rows, heads, 0.1)
+    scene.check(rows, calm, scene.cache.attend(batch, calm.cuda()), 1)
+    scene.cache.poll()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_more_keys_than_a_piece_takes(dtype):
+    attend(Scene([70001], 1, 64, dtype, 128, seed=15), [70], 1)
+
+
 # ------------------------------------------------------------------ edges
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("head_dim", [64, 128])
