@@ -203,6 +203,24 @@ cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch
 
 namespace {
 
+// DeviceGuard for calls whose launch is most of their time: nothing is set where the device is the current one already.
+struct OnDevice {
+  int prev = -1;
+  bool ok = false;
+  explicit OnDevice(int device) {
+    if (cudaGetDevice(&prev) != cudaSuccess) return;
+    if (prev == device) {
+      prev = -1;
+      ok = true;
+    } else {
+      ok = cudaSetDevice(device) == cudaSuccess;
+    }
+  }
+  ~OnDevice() {
+    if (prev >= 0) cudaSetDevice(prev);
+  }
+};
+
 bool cache_ok(const litevggt_kv_cache* c) { return c != nullptr && c->magic == kKvCacheMagic; }
 bool batch_ok(const litevggt_kv_batch* b) { return b != nullptr && b->magic == kKvBatchMagic; }
 
@@ -426,7 +444,7 @@ litevggt_status litevggt_kv_append(litevggt_kv_cache* cache, const litevggt_kv_b
   if (!aligned16(k) || !aligned16(v)) return LITEVGGT_ERR_ALIGN;
   if ((st = stride_ok(k_row_stride, k_head_stride)) != LITEVGGT_OK) return st;
   if ((st = stride_ok(v_row_stride, v_head_stride)) != LITEVGGT_OK) return st;
-  DeviceGuard g(cache->device);
+  const OnDevice g(cache->device);
   if (!g.ok) return LITEVGGT_ERR_CUDA;
   int n = 0;
   const cudaError_t e = launch_kv_append(*cache, *batch, static_cast<const __nv_bfloat16*>(k), KvStride{k_row_stride, k_head_stride},
@@ -443,7 +461,7 @@ litevggt_status litevggt_kv_gather(litevggt_kv_cache* cache, const litevggt_kv_b
   if (batch->rows == 0) return LITEVGGT_OK;
   if (k == nullptr || v == nullptr) return LITEVGGT_ERR_NULL;
   if (!aligned16(k) || !aligned16(v)) return LITEVGGT_ERR_ALIGN;
-  DeviceGuard g(cache->device);
+  const OnDevice g(cache->device);
   if (!g.ok) return LITEVGGT_ERR_CUDA;
   int n = 0;
   const cudaError_t e =
@@ -461,7 +479,7 @@ litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_b
   if (q == nullptr || out == nullptr) return LITEVGGT_ERR_NULL;
   if (!aligned16(q) || !aligned16(out)) return LITEVGGT_ERR_ALIGN;
   if ((st = stride_ok(q_row_stride, q_head_stride)) != LITEVGGT_OK) return st;
-  DeviceGuard g(cache->device);
+  const OnDevice g(cache->device);
   if (!g.ok) return LITEVGGT_ERR_CUDA;
   const KvAttend a{static_cast<const __nv_bfloat16*>(q), KvStride{q_row_stride, q_head_stride}, static_cast<__nv_bfloat16*>(out),
                    batch->q_heads, batch->group, batch->causal_block, scale * 1.4426950408889634f};
