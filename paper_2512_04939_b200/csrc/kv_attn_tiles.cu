@@ -31,11 +31,6 @@ namespace lv {
 namespace {
 
 constexpr int kTileKeys = 128;
-// Head dim 64: of the 16 pairs of 32 scores, this many take their exponentials on the FMA pipes.
-#ifndef LV_KV_POLY
-#define LV_KV_POLY 4
-#endif
-constexpr int kPolyPairs = LV_KV_POLY;
 constexpr int kStreams = 2;                  // of a tile: a row's two threads
 constexpr int kSoftmaxWarps = 8 * kStreams;
 constexpr int kKeys = kTileKeys / kStreams;  // of a stream's step
@@ -43,6 +38,11 @@ constexpr int kKeys = kTileKeys / kStreams;  // of a stream's step
 template <int kHd, bool kNarrow>
 struct TiShape {
   static constexpr bool kOnes = kHd == 64;    // the tensor core adds up the rows, and Q is in its memory
+  // Of the 16 pairs of 32 scores, this many take their exponentials on the FMA pipes: 14 issue slots and more for 16 clocks of the
+  // special-function unit.  Where codes are widened beside them there are few slots to spare.  2048 rows over 83,280 keys, none /
+  // 1 / 2 / 4 pairs: head dim 64 800 / 787 / 776 / 779 us, E4M3 929 / 926 / 938 / 966; head dim 128 644 / 647 / 643 / 642, E4M3
+  // 752 / 762 / 771 / 788.
+  static constexpr int kPolyPairs = kNarrow ? (kHd == 64 ? 1 : 0) : 2;
   static constexpr int kHelpers = kNarrow ? 8 : 1;
   static constexpr int kThreads = (kSoftmaxWarps + 4 + (kNarrow ? 8 : 0)) * 32;
   static constexpr int kStages = kHd == 64 ? (kNarrow ? 3 : 4) : 2;
@@ -594,7 +594,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float2 x = __ffma2_rn(make_float2(__uint_as_float(s[g][2 * i]), __uint_as_float(s[g][2 * i + 1])), scale2, ref2);
-            if (!kEdge && i < kPolyPairs) x = poly_exp2_clamped(x);
+            if (!kEdge && i < Shape::kPolyPairs) x = poly_exp2_clamped(x);
             else x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
             if constexpr (kEdge) {
               // The upper half as it is, and the rest; never a rest of zero or less beside a probability, which an infinite value
