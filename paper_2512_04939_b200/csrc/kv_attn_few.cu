@@ -250,7 +250,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     // One stage; with `edge` some rows do not see all of its keys, or not all of its keys are there.
     auto take = [&](auto edge_constant, int key, uint32_t base) {
       constexpr bool edge = decltype(edge_constant)::value;
-      const uint32_t exps = base + 2 * kSubs * Shape::kSubBytes;
+      [[maybe_unused]] const uint32_t exps = base + 2 * kSubs * Shape::kSubBytes;
       // scores
       float sc[kSubs][2][4];
 #pragma unroll
@@ -288,7 +288,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       for (int s = 0; s < kSubs; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          float k_scale[2] = {1.0f, 1.0f};
+          [[maybe_unused]] float k_scale[2] = {1.0f, 1.0f};
           if constexpr (kNarrow) power_pair(exps + s * 16 + 8 * t + 2 * q4, k_scale);
 #pragma unroll
           for (int e = 0; e < 2 * kHalves; ++e) {
@@ -317,7 +317,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       }
       // probabilities, and the weights that the values get
       uint32_t p[kSubs][2][kHalves];
-      float v_power[kSubs][2][2];
+      [[maybe_unused]] float v_power[kSubs][2][2];
       if constexpr (kNarrow) {
         float most_power = 0.0f;  // (positive floats order like their bits)
 #pragma unroll

@@ -34,10 +34,13 @@ class KVBatch:
         self.q_shape = (rows, q_heads, owner.head_dim)
         self._stream = stream
 
-    def __del__(self):
-        if self.handle is not None:
-            self.owner.lib.litevggt_kv_batch_destroy(self.handle)
-            self.handle = None
+    def __del__(self):  # pragma: no cover
+        try:
+            if self.handle is not None:
+                self.owner.lib.litevggt_kv_batch_destroy(self.handle)
+                self.handle = None
+        except Exception:
+            pass
 
 
 class KVCache:
@@ -70,6 +73,7 @@ class KVCache:
         self._scale = 1.0 / math.sqrt(self.head_dim)
         self._append, self._attend = self.lib.litevggt_kv_append, self.lib.litevggt_kv_attend
         self.status = torch.zeros(64, dtype=torch.int32, device=k.device)
+        self._home = self._stream()
         cfg = KVConfig(self.pages, self.page_size, self.kv_heads, self.head_dim, 1 if narrow else 0)
         self.handle = C.c_void_p()
         _check(self.lib.litevggt_kv_create(C.byref(cfg), self.device.index, *(C.c_void_p(t.data_ptr()) if t is not None else None
@@ -174,11 +178,15 @@ class KVCache:
         return torch._C._cuda_getCurrentRawStream(self._index)  # (a Stream object costs 3 us)
 
     def _use(self, batch: KVBatch) -> int:
-        """The current stream, to which the batch's memory now belongs as well."""
+        """The current stream.  Where the batch or the pools come from another one, their memory is in use on this one as well, and
+        is not given away before its work here is done."""
         stream = self._stream()
-        if stream != batch._stream:
-            batch.memory.record_stream(torch.cuda.current_stream(self.device))
-            self.status.record_stream(torch.cuda.current_stream(self.device))
+        if stream != batch._stream or stream != self._home:
+            here = torch.cuda.current_stream(self.device)
+            batch.memory.record_stream(here)
+            for t in (self.k, self.v, self.k_exp, self.v_exp, self.status):
+                if t is not None:
+                    t.record_stream(here)
         return stream
 
     def _rows(self, name: str, t: torch.Tensor, shape: tuple) -> tuple[int, int, int]:
