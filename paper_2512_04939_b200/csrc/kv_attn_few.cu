@@ -16,6 +16,12 @@
 // scores, a value's its probability, relative to the largest that the warp has met.  Q goes to f16 under a power of two of its
 // row (exact but for elements 2^-38 under the row's largest); P has 11 bits there, not 8, down to 2^-14 of a row's largest
 // weight, and fixed steps of 2^-31 below.
+//
+// One token of 16 heads of 64 over 260,250 keys in bf16: 174 us, 6.1 TB/s, the rate of a copy; 48 tokens of 16 heads of 128 over 1,100
+// to 4,164 keys 166 us, 6.2 TB/s.  Codes are bound by the work of widening them (a conversion takes as long as four of the other
+// instructions; the ALU is 60 % busy): over 520,500 keys 205 us, 5.3 TB/s.  (Straight from global memory into the
+// fragments, without rings: 189, 307 and 404 us.)  Few keys: 4.8 us for 262, of which the latency of three dependent loads and the
+// meeting of the parts are most.
 #include "exp2.cuh"
 #include "kv_cache.h"
 #include "kv_quant.cuh"

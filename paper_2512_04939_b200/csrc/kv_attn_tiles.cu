@@ -22,6 +22,17 @@
 //         the piece come again, and then they are taken out here and added to the rows that see them.
 //   E4M3  codes and exponents come by bulk copies into a ring of their own; the eight warps widen them to the same tiles,
 //         exactly, and look after V on the way.
+//
+// 2048 rows over 83,280 keys, 699 GFLOP: head dim 64 (16 heads) 776 us, 900 TFLOP/s; head dim 128 (8 heads) 643 us, 1087; over E4M3
+// 926 us and 752.  In bursts; under the 1 kW cap, which all of them reach, head dim 64 makes 765.  What bounds them (2048 rows over 10,410
+// keys): head dim 64 the special-function unit, 67 % of it with set-up and all, beside 44 % of the issue slots and 43 % of the
+// tensor cores; head dim 128 nothing alone (tensor cores 51 %): a stream waits for its own products, and Q's share of
+// shared memory's bandwidth is taken twice a key tile; codes the issue slots (63 % and 55 %).
+// Tried and left: one product of 128 columns for both streams' scores at head dim 128 (643 -> 649 us, 98 -> 109 at 10,410 keys: the
+// streams then wait for each other); the first 32 keys' probabilities handed over ahead of the others (no change); registers
+// moved between warps by setmaxnreg (no function may be called then, and the waits in line cost more than the registers
+// gave); rows by way of shared memory and the end of a piece as a function (3 % each: registers of the sweep); V looked
+// through by the producer, without a warp of its own (1 % at head dim 64, 5 % over codes).
 #include "exp2.cuh"
 #include "kv_cache.h"
 #include "kv_quant.cuh"

@@ -2,7 +2,8 @@
 //
 // Writing and reading move every byte once and compute next to nothing, so HBM bounds both.  A unit of work is one
 // row of one K/V head, K and V alike: 16 bytes of bf16 a lane, the 8 (or 16) lanes of a row side by side in the warp, so
-// that a row's largest magnitude takes three (four) shuffles and its codes leave as 64 (128) bytes in a row.
+// that a row's largest magnitude takes three (four) shuffles and its codes leave as 64 (128) bytes in a row.  83,280 rows of 16
+// heads of 64: written as bf16 110 us, 6.2 TB/s, as E4M3 85 us, 6.0; read back 106 us, 6.4, and 82 us, 6.3 (a copy makes 6.46).
 #include <string.h>
 
 #include <new>
