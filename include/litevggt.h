@@ -337,11 +337,12 @@ litevggt_status litevggt_launch_count(const litevggt_ctx* ctx, int64_t* launches
  * A batch is what the calls of one step have in common: for each sequence how many rows of the packed tensors belong to
  * it, how many tokens it holds, in which pages.  A sequence's rows are its last tokens: the call that appends a chunk
  * and those that attend from it take the same batch, whose lengths already count the chunk; a reader that wants a whole
- * sequence names as many rows as it has tokens.  Batches are made on the host and serve every layer of a step. */
+ * sequence names as many rows as it has tokens, 2^30 at most.  Batches are made on the host and serve every layer of a step. */
 enum {
   LITEVGGT_KV_BF16 = 0,
   LITEVGGT_KV_E4M3 = 1 /* a row of a head as E4M3 codes x and an exponent byte e + 127, standing for x 2^e: the least
-                          e >= -118 with max|row| <= 448 * 2^e; a row that is not finite is held as byte 255 and reads as NaN */
+                          e >= -118 with max|row| <= 448 * 2^e; a row that is not finite is held as byte 255 beside
+                          codes of zero, and reads as NaN */
 };
 typedef struct {
   int32_t pages;     /* in the pool */

@@ -51,9 +51,9 @@ struct TiShape {
   static constexpr bool kOnes = kHd == 64;    // the tensor core adds up the rows, and Q is in its memory
   // Of the 16 pairs of 32 scores, this many take their exponentials on the FMA pipes: 14 issue slots and more for 16 clocks of the
   // special-function unit.  Where codes are widened beside them there are few slots to spare.  2048 rows over 83,280 keys, none /
-  // 1 / 2 / 4 pairs: head dim 64 800 / 787 / 776 / 779 us, E4M3 929 / 926 / 938 / 966; head dim 128 644 / 647 / 643 / 642, E4M3
+  // 1 / 2 / 4 pairs: head dim 64 800 / 787 / 776 / 779 us, E4M3 935 / 950 / 938 / 966; head dim 128 644 / 647 / 643 / 642, E4M3
   // 752 / 762 / 771 / 788.
-  static constexpr int kPolyPairs = kNarrow ? (kHd == 64 ? 1 : 0) : 2;
+  static constexpr int kPolyPairs = kNarrow ? 0 : 2;
   static constexpr int kHelpers = kNarrow ? 8 : 1;
   static constexpr int kThreads = (kSoftmaxWarps + 4 + (kNarrow ? 8 : 0)) * 32;
   static constexpr int kStages = kHd == 64 ? (kNarrow ? 3 : 4) : 2;
@@ -73,10 +73,13 @@ struct TiBarriers {
   uint64_t raw_full[2][kRaw > 0 ? kRaw : 1], raw_empty[2][kRaw > 0 ? kRaw : 1];  // [K, V]
   uint64_t q_ready[2], s_full[2][2], p_ready[2][2], o_done[2], teardown[2];
   uint32_t tmem_base, abort_flag;
-  int taken_out[2];  // a piece (its number + 1, by the turn's parity) whose V held values that are not finite where not all rows see them
-  int again[2];      // a piece (likewise) that has to be done again
   int any_again, last_of_join;
 };
+// Marks of a piece, in device memory: the row tiles and the warps that look after V may be several short pieces apart.
+constexpr int kAgain = 1;     // it has to be done again
+constexpr int kTakenOut = 2;  // its V held values that are not finite where not all rows see them
+__device__ __forceinline__ void set_mark(int* mark, int value) { *reinterpret_cast<volatile int*>(mark) = value; }
+__device__ __forceinline__ int get_mark(const int* mark) { return *reinterpret_cast<const volatile int*>(mark); }
 
 // 2^x for a pair of arguments on the FMA pipes: the nearest whole number n goes into the exponent field, a cubic gives the
 // power of the rest (relative error 7.5e-5, far below the rounding to bf16).  n is held to [-125, 125] by one integer
@@ -192,8 +195,6 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       mbar_init(&bars->p_ready[t][1], 4);
       mbar_init(&bars->o_done[t], 1);
       mbar_init(&bars->teardown[t], 1);
-      bars->taken_out[t] = 0;
-      bars->again[t] = 0;
     }
     mbar_fence_init();
     bars->abort_flag = 0;
@@ -240,7 +241,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     named_barrier(10, Shape::kThreads);
     if (*reinterpret_cast<volatile int*>(&bars->any_again) == 0) return;
     for (int id = (int)blockIdx.x; id >= 0; id = work.pieces[id].next)
-      if (*reinterpret_cast<volatile int*>(work.again + id) != 0) {
+      if (get_mark(work.again + id) != 0) {
         run(id, kMaxima);
         __syncwarp();
         run(id, kCareful);
@@ -399,10 +400,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
   } else if (warp >= kHelper) {
     // ------------------------------------------------------------------ V (and what is held in codes)
     Ring ring, raw;
-    uint32_t turn = 0;
     bool ok = true;
     pieces([&](int id, int mode) -> int {
-      const uint32_t parity = turn++ & 1u;
       const Job job = job_of(work, at, id);
       for (int j = 0; j < job.tiles && ok; ++j) {
         const int key = (job.tile0 + j) * kTileKeys;
@@ -452,7 +451,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
               *reinterpret_cast<uint4*>(row + (((2 * ch) & 7) ^ (r & 7)) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
               *reinterpret_cast<uint4*>(row + (((2 * ch + 1) & 7) ^ (r & 7)) * 16) = make_uint4(v[4], v[5], v[6], v[7]);
             }
-            if (bad) *reinterpret_cast<volatile int*>(&bars->taken_out[parity]) = id + 1;
+            if (bad) set_mark(work.again + id, kAgain | kTakenOut);
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) {
@@ -485,7 +484,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
                 if (here) *at_row = make_uint4(v[0], v[1], v[2], v[3]);
                 bad = bad || here;
               }
-            if (bad) *reinterpret_cast<volatile int*>(&bars->taken_out[parity]) = id + 1;
+            if (bad) set_mark(work.again + id, kAgain | kTakenOut);
             fence_proxy_async_shared();
           }
           __syncwarp();
@@ -504,7 +503,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
     const uint32_t s_addr = tmem_base + lane_base + t * 128 + c * 64;
     const uint32_t o_addr = tmem_base + lane_base + Shape::kColO + t * Shape::kOCols;
-    uint32_t step = 0, round = 0, turn = 0;
+    uint32_t step = 0, round = 0;
     bool ok = true;
     float kept = -INFINITY;  // the row's maximum, from one sweep to the next
     // The queries, this thread's half row.  Those before have been read where o_done has come: it follows their last product.
@@ -548,7 +547,6 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       return fmaxf(fmax3(m[0], m[1], m[2]), m[3]);
     };
     pieces([&](int id, int mode) -> int {
-      const uint32_t parity = turn++ & 1u;
       // What the sweep needs of the piece; the rest is read again behind it, where it does not hold registers.
       int mine, key_base, seen, all_see;
       bool live;
@@ -711,7 +709,6 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         tmem_ld_wait();
         row_sum = has ? __uint_as_float(l) : 0.0f;
       }
-      const bool bad = *reinterpret_cast<volatile int*>(&bars->taken_out[parity]) == id + 1;
       const bool whole = job.p.slot < 0;
       const float inverse = whole && seen > 0 ? 1.0f / row_sum : 1.0f;
       constexpr int kMine = kHd / kStreams / 32;  // groups of 32 channels of this thread
@@ -734,12 +731,11 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
 #pragma unroll
           for (int i = 0; i < 32; ++i) zero = fmaf(acc[i], 0.0f, zero);
           if (!(row_sum > 0.0f && row_sum < kSumLimit && zero == 0.0f)) {
-            *reinterpret_cast<volatile int*>(work.again + id) = 1;
-            *reinterpret_cast<volatile int*>(&bars->again[parity]) = id + 1;
-            *reinterpret_cast<volatile int*>(&bars->any_again) = 1;
+            set_mark(work.again + id, kAgain);
+            set_mark(&bars->any_again, 1);
           }
         }
-        if (bad && live) {
+        if (mode == kCareful && live && (get_mark(work.again + id) & kTakenOut) != 0) {
           // values that were taken out of V, for the rows that see them
           for (int key = max(job.p.key0, job.min_seen); key < min(job.p.key1, seen); ++key) {
             const long long page = arrays.pages[job.q.page0 + (key >> pool.page_shift)];
@@ -789,7 +785,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         named_barrier(9, kSoftmaxWarps * 32);
         if (threadIdx.x == 0) {
           int last = 0;
-          if (mode == kCareful || *reinterpret_cast<volatile int*>(&bars->again[parity]) != id + 1) {
+          if (mode == kCareful || *reinterpret_cast<volatile int*>(&bars->any_again) == 0 || get_mark(work.again + id) == 0) {
             last = atomicAdd(work.joins + job.p.join, 1) == job.p.parts - 1 ? 1 : 0;
             if (last) work.joins[job.p.join] = 0;
           }

@@ -280,7 +280,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
   long long row0 = 0, page0 = 0;
   b->rows_held = true;
   for (int i = 0; i < n_seq; ++i) {
-    if (rows[i] < 0 || lengths[i] < 0) return LITEVGGT_ERR_SHAPE;
+    if (rows[i] < 0 || lengths[i] < 0 || lengths[i] > kKvLongest) return LITEVGGT_ERR_SHAPE;
     if (rows[i] > lengths[i]) b->rows_held = false;
     b->seqs.push_back(KvSeq{(int)row0, rows[i], lengths[i], (int)page0});
     row0 += rows[i];

@@ -10,6 +10,7 @@ namespace lv {
 
 constexpr uint32_t kKvCacheMagic = 0x4c564b43u;
 constexpr uint32_t kKvBatchMagic = 0x4c564b42u;
+constexpr int kKvLongest = 1 << 30;  // tokens of a sequence: sums of positions and steps stay inside 31 bits
 
 // The pools as a kernel sees them: [pages, kv_heads, page_size, head_dim] of bf16 or E4M3 codes, the codes' exponents
 // [pages, kv_heads, page_size].

@@ -287,6 +287,21 @@ def test_what_a_row_does_not_see_has_no_influence(dtype, head_dim, rows):
     attend(scene, [rows], 1, causal_block=1)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_many_short_pieces_that_are_done_again(dtype, head_dim):
+    """A CTA's pieces are one key tile each and nearly all of them hold values that are not finite where not all rows see them, in
+    other places each, so whatever looks after V may be ahead of the rows by several pieces."""
+    rows = [18 + i % 23 for i in range(400)]
+    scene = Scene([r + 3 for r in rows], 2, head_dim, dtype, 16, seed=16)
+    at = 0
+    for i, r in enumerate(rows):
+        if i % 5:
+            scene.v_new[at + 3 + (7 * i) % r, i % 2, i % head_dim] = float("nan") if i % 3 else float("inf")
+        at += r + 3
+    attend(scene, rows, 2, causal_block=1)
+
+
 @pytest.mark.parametrize("rows", [1, 200])
 def test_not_finite_where_it_is_seen(rows):
     scene = Scene([300], 1, 64, "bf16", 16, seed=9)
@@ -391,6 +406,8 @@ def test_refusals():
             cache.batch([3], [20], [[2, 0]], **extra)
     with pytest.raises(pkg.LiteVGGTError):
         cache.batch([2 ** 30], [20], [[2, 0]], q_heads=4)  # rows times heads
+    with pytest.raises(pkg.LiteVGGTError):
+        cache.batch([1], [2 ** 30 + 1], [np.zeros(2 ** 26 + 1, np.int32)])  # tokens
     other = pkg.KVCache.empty(4, 16, 2, 64)
     with pytest.raises(pkg.LiteVGGTError, match="stale or foreign"):
         other.attend(batch, ok)
