@@ -23,8 +23,8 @@
 //   E4M3  codes and exponents come by bulk copies into a ring of their own; the eight warps widen them to the same tiles,
 //         exactly, and look after V on the way.
 //
-// 2048 rows over 83,280 keys, 699 GFLOP: head dim 64 (16 heads) 776 us, 900 TFLOP/s; head dim 128 (8 heads) 643 us, 1087; over E4M3
-// 926 us and 752.  In bursts; under the 1 kW cap, which all of them reach, head dim 64 makes 765.  What bounds them (2048 rows over 10,410
+// 2048 rows over 83,280 keys, 699 GFLOP: head dim 64 (16 heads) 771 us, 907 TFLOP/s; head dim 128 (8 heads) 633 us, 1104; over E4M3
+// 935 us and 751.  In bursts; under the 1 kW cap, which all of them reach, head dim 64 makes 765.  What bounds them (2048 rows over 10,410
 // keys): head dim 64 the special-function unit, 67 % of it with set-up and all, beside 44 % of the issue slots and 43 % of the
 // tensor cores; head dim 128 nothing alone (tensor cores 51 %): a stream waits for its own products, and Q's share of
 // shared memory's bandwidth is taken twice a key tile; codes the issue slots (63 % and 55 %).
