@@ -13,9 +13,9 @@
 //               channels of those four keys and pairs them up with byte permutations; its accumulators' keys in S are the same
 //               ones, so P goes from accumulator to operand without leaving the lane
 // Codes are widened to f16, which takes one conversion for two of them.  Their powers of two stay outside: a key's scales its
-// scores, a value's its probability, relative to the largest that the warp has met.  Q goes to f16 under a power of two of its
-// row (exact but for elements 2^-38 under the row's largest); P has 11 bits there, not 8, down to 2^-14 of a row's largest
-// weight, and fixed steps of 2^-31 below.
+// scores, a value's its probability; that product is the value's weight, relative to the row's largest.  Q goes to f16 under a
+// power of two of its row (exact but for elements 2^-38 under the row's largest); weights have 11 bits there, not 8, down to 2^-21
+// of the row's largest or less, and fixed steps of 2^-31 of it or less below.
 //
 // One token of 16 heads of 64 over 260,250 keys in bf16: 174 us, 6.1 TB/s, the rate of a copy; 48 tokens of 16 heads of 128 over 1,100
 // to 4,164 keys 166 us, 6.2 TB/s.  Codes are bound by the work of widening them (a conversion takes as long as four of the other
@@ -85,8 +85,14 @@ __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, ui
 }
 
 // The reference may lag this far behind a row's maximum (base-2 units) before the row is scaled anew.
-constexpr float kFewSlack = 8.0f;
-constexpr int kFewShift = 7;  // probabilities in f16 are taken 2^7 times as large: with the slack they stay below 2^15
+constexpr float kFewSlack = 7.0f;
+// Codes: a probability times its value's power of two is a weight, at most 2^127 with this slack, and the product's operand is the
+// weight times a power of two 2^k of its row.  That brings the largest weight to [2^7, 2^8) when it is set, and is set anew where
+// one comes to more than 2^15 (f16 ends at 2^16).
+constexpr int kFewWeight = 7, kFewMostShift = 118;
+constexpr float kFewMostWeight = 32768.0f;
+__device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k + 127) << 23); }
+__device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }
 
 template <int kHd, bool kNarrow, bool kHalf>
 struct FewShape {
@@ -249,9 +255,9 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
 #pragma unroll
       for (int j = 0; j < 2 * kHalves; ++j) o[i][j] = 0.0f;
     float top[2] = {-INFINITY, -INFINITY}, ref[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};  // ref: top where that is finite yet
-    // Codes: the largest power of two of a value so far, which the output is relative to, and the factor that makes weights of
-    // the others'; a power of infinity stands for a row that is not finite, whose codes are zero (0 * infinity = NaN).
-    float v_top = 0.0f, to_v_top = 0.0f;
+    // Codes: the rows' factors of the weights, which the output has in it.  (A power of infinity stands for a value that is not
+    // finite, whose codes are zero: 0 * infinity = NaN.)
+    [[maybe_unused]] float to[2] = {power_of_two(kFewMostShift), power_of_two(kFewMostShift)};
 
     // ---------------------------------------------------------------- sweep
     // One stage; with `edge` some rows do not see all of its keys, or not all of its keys are there.
@@ -313,10 +319,19 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
           if (m > top[half]) {
-            const float factor = top[half] == -INFINITY ? 0.0f : fast_exp2(ref[half] - m);
+            const bool first = top[half] == -INFINITY;
+            const float apart = m - ref[half];
+            float factor = first ? 0.0f : fast_exp2(-apart);
             top[half] = m;
             ref[half] = m;
             sum[half] *= factor;
+            if constexpr (kNarrow) {  // what was the largest weight may be next to nothing now
+              const int k = exponent_of(to[half]), next = min(k + (int)fminf(apart, 512.0f), kFewMostShift);
+              if (!first) {
+                factor = fast_exp2((float)(next - k) - apart);
+                to[half] = power_of_two(next);
+              }
+            }
 #pragma unroll
             for (int i = 0; i < Shape::kOutTiles; ++i) o[i][2 * half] *= factor, o[i][2 * half + 1] *= factor;
           }
@@ -324,38 +339,45 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       }
       // probabilities, and the weights that the values get
       uint32_t p[kSubs][2][kHalves];
-      [[maybe_unused]] float v_power[kSubs][2][2];
       if constexpr (kNarrow) {
-        float most_power = 0.0f;  // (positive floats order like their bits)
+        float heaviest[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int s = 0; s < kSubs; ++s)
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            power_pair(exps + (kSubs + s) * 16 + 8 * t + 2 * q4, v_power[s][t]);
+            float v_power[2];
+            power_pair(exps + (kSubs + s) * 16 + 8 * t + 2 * q4, v_power);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              if (edge && key + 16 * s + 8 * t + 2 * q4 + e >= piece.key1) v_power[s][t][e] = 0.0f;
-              most_power = fmaxf(most_power, v_power[s][t][e]);
+            for (int e = 0; e < 2 * kHalves; ++e) {
+              const float a = fast_exp2(sc[s][t][e] - ref[e >> 1]);
+              sum[e >> 1] += a;
+              float weight = a * v_power[e & 1];
+              // what is not seen has no weight, whatever it holds
+              if (edge && key + 16 * s + 8 * t + 2 * q4 + (e & 1) >= seen[e >> 1]) weight = 0.0f;
+              sc[s][t][e] = weight;
+              heaviest[e >> 1] = fmaxf(heaviest[e >> 1], weight);
             }
           }
-        if (__any_sync(0xffffffffu, most_power > v_top)) {
-          most_power = 0.0f;
+        if (__any_sync(0xffffffffu, heaviest[0] * to[0] > kFewMostWeight || (!kHalf && heaviest[1] * to[1] > kFewMostWeight))) {
 #pragma unroll
-          for (int s = 0; s < kSubs; ++s)
+          for (int half = 0; half < kHalves; ++half) {
+            float m = 0.0f;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int s = 0; s < kSubs; ++s)
 #pragma unroll
-              for (int e = 0; e < 2; ++e)
-                if (v_power[s][t][e] < INFINITY) most_power = fmaxf(most_power, v_power[s][t][e]);
-          most_power = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most_power)));
-          if (most_power > v_top) {
-            const float factor = v_top / most_power;  // powers of two: exact, or zero where it is next to nothing
-            v_top = most_power;
-            to_v_top = 1.0f / most_power * (float)(1 << kFewShift);
+              for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < Shape::kOutTiles; ++i)
+                for (int e = 2 * half; e < 2 * half + 2; ++e)
+                  if (sc[s][t][e] < INFINITY) m = fmaxf(m, sc[s][t][e]);
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+            if (m * to[half] > kFewMostWeight) {
+              const int next = kFewWeight - exponent_of(m);
+              const float factor = fast_exp2((float)(next - exponent_of(to[half])));
+              to[half] = power_of_two(next);
 #pragma unroll
-              for (int j = 0; j < 2 * kHalves; ++j) o[i][j] *= factor;
+              for (int i = 0; i < Shape::kOutTiles; ++i) o[i][2 * half] *= factor, o[i][2 * half + 1] *= factor;
+            }
           }
         }
       }
@@ -365,21 +387,12 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int half = 0; half < kHalves; ++half) {
-            float a = fast_exp2(sc[s][t][2 * half] - ref[half]), b = fast_exp2(sc[s][t][2 * half + 1] - ref[half]);
             if constexpr (kNarrow) {
-              sum[half] += a + b;
-              float f[2];
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                f[e] = v_power[s][t][e] * to_v_top;
-                // what is not seen has no weight, whatever it holds
-                if (edge && key + 16 * s + 8 * t + 2 * q4 + e >= seen[half]) f[e] = 0.0f;
-              }
-              p[s][t][half] = pack_f16(a * f[0], b * f[1]);
+              p[s][t][half] = pack_f16(sc[s][t][2 * half] * to[half], sc[s][t][2 * half + 1] * to[half]);
             } else {
               // operands of the second product, each off by up to 2^-8; the sum is that of the rounded ones, so what the rounding
               // changes is how much a key weighs among the others and not the whole row's size
-              p[s][t][half] = pack_bf16(a, b);
+              p[s][t][half] = pack_bf16(fast_exp2(sc[s][t][2 * half] - ref[half]), fast_exp2(sc[s][t][2 * half + 1] - ref[half]));
               sum[half] += bf16_lo(p[s][t][half]) + bf16_hi(p[s][t][half]);
             }
           }
@@ -486,10 +499,9 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       constexpr int kRun = kNarrow ? kHd / 8 : 8;
       return (tile / kRun) * (8 * kRun) + n * kRun + tile % kRun;
     };
-    // codes: back from "relative to the largest value's power of two"
-    const float v_scale = kNarrow ? v_top * (1.0f / (1 << kFewShift)) : 1.0f;
 #pragma unroll
     for (int half = 0; half < kHalves; ++half) {
+      const float v_scale = kNarrow ? power_of_two(-exponent_of(to[half])) : 1.0f;
       float l = sum[half];
       l += __shfl_xor_sync(0xffffffffu, l, 1);
       l += __shfl_xor_sync(0xffffffffu, l, 2);

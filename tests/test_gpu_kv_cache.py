@@ -287,6 +287,26 @@ def test_what_a_row_does_not_see_has_no_influence(dtype, head_dim, rows):
     attend(scene, [rows], 1, causal_block=1)
 
 
+@pytest.mark.parametrize("rows", [3, 14, 40])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_values_of_very_different_size(dtype, head_dim, rows):
+    """Large values that a row does not see, or that hardly weigh for it, take nothing from the small ones that do."""
+    scene = Scene([200, 500, 300], 1, head_dim, dtype, 16, seed=17)
+    scene.v_new[200 - rows // 2:200] *= 2.0 ** 60  # unseen by the sequence's rows before them
+    scene.v_new[200:700] *= torch.exp2(torch.randint(-20, 20, (500, 1, 1), generator=scene.g).float()).bfloat16()
+    scene.k_new[700:] += 8.0
+    scene.k_new[::150][5:6] = -24.0  # the third sequence's queries lean this way: about 2^-300 of their weight
+    scene.v_new[::150][5:6] *= 2.0 ** 60
+    scene.store()
+    batch = scene.cache.batch([rows] * 3, scene.lengths, scene.pages, causal_block=1)
+    q = scene.queries([rows] * 3, 1)
+    q[2 * rows:] = (0.25 * q[2 * rows:] + 0.75 * 8.0 / head_dim ** 0.5 * 1.0).bfloat16()
+    out = scene.cache.attend(batch, q.cuda())
+    scene.cache.poll()
+    scene.check([rows] * 3, q, out, 1)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("head_dim", [64, 128])
 def test_many_short_pieces_that_are_done_again(dtype, head_dim):
