@@ -19,7 +19,7 @@
 //
 // One token of 16 heads of 64 over 260,250 keys in bf16: 174 us, 6.1 TB/s, the rate of a copy; 48 tokens of 16 heads of 128 over 1,100
 // to 4,164 keys 166 us, 6.2 TB/s.  Codes are bound by the work of widening them (a conversion takes as long as four of the other
-// instructions; the ALU is 60 % busy): over 520,500 keys 205 us, 5.3 TB/s.  (Straight from global memory into the
+// instructions; the ALU is 60 % busy): over 520,500 keys 209 us, 5.2 TB/s.  (Straight from global memory into the
 // fragments, without rings: 189, 307 and 404 us.  The scores by products of 8-bit operands, Q in two of them, which need no
 // conversion of K in the source: 202 -> 220 us, sixteen tokens that share heads by eight 32.9 -> 33.2.)  Few keys: 4.8 us for 262, of which the latency of three dependent loads and the
 // meeting of the parts are most.
