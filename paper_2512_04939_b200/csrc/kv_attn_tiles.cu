@@ -35,6 +35,7 @@
 // through by the producer, without a warp of its own (1 % at head dim 64, 5 % over codes).
 #include "exp2.cuh"
 #include "kv_cache.h"
+#include "kv_handoff.h"
 #include "kv_quant.cuh"
 
 namespace lv {
@@ -350,7 +351,9 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             ok = mbar_wait(&bars->v_full[ring.slot], ring.phase, ctl);
 #pragma unroll
             for (int c = 0; c < kStreams; ++c) {
-              ok = ok && mbar_wait(&bars->p_ready[t][c], step & 1u, ctl);
+#pragma unroll
+              for (int other = 0; other < kStreams; ++other)
+                if (kv_awaits(j, c, other)) ok = ok && mbar_wait(&bars->p_ready[t][other], step & 1u, ctl);
               if (!ok) break;
               tc_fence_after();
               if (mode != kMaxima) {
@@ -624,8 +627,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         load(key + kKeys > all_see, key);
         most = fmaxf(most, fmaxf(largest(s[0]), largest(s[1])));
       };
-      // The two threads of a row tell each other a number, by way of two columns of tensor memory that nothing else uses just
-      // now.  Both come here whatever became of their waits.
+      // The two threads of a row tell each other a number, by way of two columns of tensor memory that nothing else writes before
+      // both have read them.  Both come here whatever became of their waits.
       auto exchange = [&](uint32_t column, uint32_t apart, float own) {
         tmem_st1(column + c * apart, __float_as_uint(own));
         tmem_st_wait();
@@ -638,7 +641,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         tmem_ld_wait();
         return make_float2(__uint_as_float(both[0]), __uint_as_float(both[1]));  // in the same order for both
       };
-      // They agree on its maximum: each where its part of the output before has been read, and the next has not begun.
+      // They agree on its maximum: each where its part of the output before has been read; the next begins when both have handed over
+      // probabilities (kv_awaits), and so have read what the other one left there.
       auto agree = [&]() {
         const float2 both = exchange(o_addr, kHd / 2, most);
         top = fmaxf(both.x, both.y) * at.scale_log2;
