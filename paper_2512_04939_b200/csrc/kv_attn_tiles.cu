@@ -83,22 +83,15 @@ __device__ __forceinline__ void set_mark(int* mark, int value) { *reinterpret_ca
 __device__ __forceinline__ int get_mark(const int* mark) { return *reinterpret_cast<const volatile int*>(mark); }
 
 // 2^x for a pair of arguments on the FMA pipes: the nearest whole number n goes into the exponent field, a cubic gives the
-// power of the rest (relative error 7.5e-5, far below the rounding to bf16).  n is held to [-125, 125] by one integer
-// instruction, so what lies far outside comes out as next to nothing or as a number that no row's sum overlooks; the
-// polynomial carries the factor 2^-125 that the exponent is counted from.  x = -infinity does not come here (NaN).
-__device__ __forceinline__ float2 poly_exp2_clamped(float2 x) {
-  const float2 t = __fadd2_rn(x, make_float2(12582912.0f, 12582912.0f));
-  const float2 n = __fadd2_rn(t, make_float2(-12582912.0f, -12582912.0f));
-  const float2 f = __ffma2_rn(n, make_float2(-1.0f, -1.0f), x);
-  constexpr float k = 2.350988701644575e-38f;  // 2^-125
-  auto horner = [&](float2 p, float c) { return __ffma2_rn(p, f, make_float2(c, c)); };
-  float2 p = horner(make_float2(0.0551716648f * k, 0.0551716648f * k), 0.2426111251f * k);
-  p = horner(p, 0.6932609677f * k);
-  p = horner(p, 0.9999280572f * k);
-  constexpr int kBias = 0x4b400000 - 125;  // of t's bits
-  const int nx = __viaddmin_s32_relu(__float_as_int(t.x), -kBias, 250), ny = __viaddmin_s32_relu(__float_as_int(t.y), -kBias, 250);
-  return make_float2(__int_as_float(__float_as_int(p.x) + (nx << 23)), __int_as_float(__float_as_int(p.y) + (ny << 23)));
+// power of the rest (relative error 7.5e-5, far below the rounding to bf16).  The arguments are held to [-125, 125] first, where
+// rounding to n leaves a rest of at most a half: what lies below comes out as next to nothing, what lies above as a number that no row's
+// sum overlooks.  So does a NaN, which passes these bounds: the integer sum makes the largest finite number of it.
+__device__ __forceinline__ float hold(float x) {
+  float y;
+  asm("{\n\t.reg .f32 t;\n\tmin.NaN.f32 t, %1, 0f42FA0000;\n\tmax.NaN.f32 %0, t, 0fC2FA0000;\n\t}" : "=f"(y) : "f"(x));
+  return y;
 }
+__device__ __forceinline__ float2 poly_exp2_held(float2 x) { return poly_exp2_pair(make_float2(hold(x.x), hold(x.y))); }
 // What a row's sum has to stay below.
 constexpr float kSumLimit = 1.152921504606847e18f;  // 2^60
 
@@ -606,7 +599,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float2 x = __ffma2_rn(make_float2(__uint_as_float(s[g][2 * i]), __uint_as_float(s[g][2 * i + 1])), scale2, ref2);
-            if (!kEdge && i < Shape::kPolyPairs) x = poly_exp2_clamped(x);
+            if (!kEdge && i < Shape::kPolyPairs) x = poly_exp2_held(x);
             else x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
             if constexpr (kEdge) {
               // The upper half as it is, and the rest; never a rest of zero or less beside a probability, which an infinite value
@@ -734,7 +727,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           float zero = 0.0f;  // NaN where something is not finite
 #pragma unroll
           for (int i = 0; i < 32; ++i) zero = fmaf(acc[i], 0.0f, zero);
-          if (!(row_sum > 0.0f && row_sum < kSumLimit && zero == 0.0f)) {
+          // (a row whose first key tile left it without a reference has none that other parts could be weighed against)
+          if (!(top > -INFINITY && row_sum > 0.0f && row_sum < kSumLimit && zero == 0.0f)) {
             set_mark(work.again + id, kAgain);
             set_mark(&bars->any_again, 1);
           }

@@ -1,0 +1,50 @@
+"""Scores, probabilities and values far from the ordinary, every operator of the paged K/V cache against its definition in float64.
+Tolerances are those of test_gpu_kv_cache."""
+import pytest
+import torch
+
+from test_gpu_kv_cache import Scene
+
+pytestmark = pytest.mark.gpu
+
+
+def run(scene, rows, q, causal_block=0, scale=None):
+    scene.store()
+    batch = scene.cache.batch(rows, scene.lengths, scene.pages, q_heads=q.shape[1], causal_block=causal_block)
+    out = scene.cache.attend(batch, q.cuda(), scale=scale)
+    scene.cache.poll()
+    scene.check(rows, q, out, causal_block, scale)
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("power", [20, 23, 25, 26, 27, 28, 29])
+def test_one_score_far_above_the_first_keys(power, head_dim):
+    """One key a head, behind the first tile of keys, whose score is about 2^power for all rows and the others' zero: it takes all of their
+    weight.  Scores beyond 2^22 have no fraction left that a polynomial could take its power of, and some of them, from
+    2^26 on, made one whose exponent ran over: next to no weight, and a row's sum that looked fine."""
+    heads, rows = 16, 17
+    for seed in range(12):
+        scene = Scene([384], heads, head_dim, "bf16", 32, seed=100 + seed)
+        scene.k_new.zero_()
+        q = torch.zeros(rows, heads, head_dim)
+        for h in range(heads):
+            a, b = (1 + torch.rand(2, generator=scene.g)).tolist()
+            scene.k_new[128 + 32 * (h % 8) + h % 4, h, 3] = a * 2.0 ** (power - power // 2 + 2)
+            q[:, h, 3] = b * 2.0 ** (power // 2)
+        run(scene, [rows], q.bfloat16())
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("rows", [1, 14, 40, 300])
+@pytest.mark.parametrize("low", [60, 121, 124])
+def test_scores_of_minus_infinity_in_front(low, rows, head_dim):
+    """The first 150 keys have scores of minus infinity, all others scores of -low in base-2 units: only those count, and alike."""
+    scene = Scene([900], 2, head_dim, "bf16", 64, seed=33)
+    scene.k_new.zero_()
+    scene.k_new[:, :, 0] = -8.0
+    scene.k_new[:150, :, 1] = float("-inf")
+    scene.v_new *= 2.0 ** -12
+    q = torch.zeros(rows, 2, head_dim)
+    q[:, :, 0] = 8.0
+    q[:, :, 1] = 1.0
+    run(scene, [rows], q.bfloat16(), scale=low / (64.0 * 1.4426950408889634))
