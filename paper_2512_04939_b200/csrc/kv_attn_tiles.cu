@@ -501,7 +501,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
     const uint32_t o_addr = tmem_base + lane_base + Shape::kColO + t * Shape::kOCols;
     uint32_t step = 0, round = 0;
     bool ok = true;
-    float kept = -INFINITY;  // the row's maximum, from one sweep to the next
+    float kept = -INFINITY;  // the row's largest score, from one sweep to the next
     // The queries, this thread's half row.  Those before have been read where o_done has come: it follows their last product.
     constexpr int kChunks = kHd / 16;  // of 16 bytes
     int given = -1;                    // the piece whose queries are there already
@@ -560,7 +560,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
         }
         given = -1;
       }
-      float top = -INFINITY, ref = 0.0f;  // the row's reference; ref: what is subtracted, top where that is finite
+      float top = -INFINITY, ref = 0.0f;  // the row's reference; ref: what is subtracted of scaled scores, top where that is finite
       float2 sum = make_float2(0.0f, 0.0f);
 
       auto key_of = [&](int j) { return key_base + j * kTileKeys; };
@@ -592,13 +592,18 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       auto take_half = [&](auto edge_constant, int key) {
         constexpr bool kEdge = decltype(edge_constant)::value;
         load(kEdge, key);
+        // Done again: less the largest score before anything is rounded, so that the largest probability is 1 whatever the scores' size.
+        // (Scaled first, a maximum of 2^30 is rounded by up to 32, and 2^32 would be no probability.)
+        const float less = kEdge && mode == kCareful && kept != -INFINITY ? -kept : 0.0f;
         const float2 scale2 = make_float2(at.scale_log2, at.scale_log2), ref2 = make_float2(-ref, -ref);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           uint32_t p[16], rest[kEdge ? 16 : 1];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            float2 x = __ffma2_rn(make_float2(__uint_as_float(s[g][2 * i]), __uint_as_float(s[g][2 * i + 1])), scale2, ref2);
+            float2 x = make_float2(__uint_as_float(s[g][2 * i]), __uint_as_float(s[g][2 * i + 1]));
+            if constexpr (kEdge) x = __fadd2_rn(x, make_float2(less, less));
+            x = __ffma2_rn(x, scale2, ref2);
             if (!kEdge && i < Shape::kPolyPairs) x = poly_exp2_held(x);
             else x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
             if constexpr (kEdge) {
@@ -638,13 +643,13 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       // probabilities (kv_awaits), and so have read what the other one left there.
       auto agree = [&]() {
         const float2 both = exchange(o_addr, kHd / 2, most);
-        top = fmaxf(both.x, both.y) * at.scale_log2;
+        return fmaxf(both.x, both.y);
       };
       if (mine > 0) {
         if (mode == kFast) {
           ok = ok && scores_in();
           if (ok) add_maximum(key_of(0));
-          agree();
+          top = agree() * at.scale_log2;
         } else if (mode == kMaxima) {
           for (int j = 0; j < mine && ok; ++j, ++step) {
             ok = scores_in();
@@ -652,12 +657,11 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             add_maximum(key_of(j));
             give_p();
           }
-          agree();
-          kept = top;
+          kept = agree();
         } else {
-          top = kept;
+          top = kept * at.scale_log2;
         }
-        ref = top == -INFINITY ? 0.0f : top;
+        ref = top == -INFINITY || mode == kCareful ? 0.0f : top;
         if (mode != kMaxima) {
           for (int j = 0; j < mine && ok; ++j, ++step) {
             ok = scores_in();

@@ -34,6 +34,27 @@ def test_one_score_far_above_the_first_keys(power, head_dim):
         run(scene, [rows], q.bfloat16())
 
 
+@pytest.mark.parametrize("rows", [5, 40])
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("power", [8, 22, 26, 30, 36, 47, 60, 100])
+def test_scores_of_any_size_above_and_below_the_first_keys(power, head_dim, rows):
+    """One key a head, behind the first tile of keys, whose scores lie about 2^power above the others' zeros for one half of the
+    rows and below them for the other: it takes all of a row's weight, or none however large its value is.  A largest score of 2^30
+    and more is rounded by its scaling to something that is not the largest any more."""
+    heads = 16
+    scene = Scene([640], heads, head_dim, "bf16", 32, seed=30)
+    scene.k_new.zero_()
+    g = scene.g
+    for h in range(heads):
+        at = 128 + 32 * h + h % 4
+        scene.k_new[at, h, 3] = float(2.0 ** (power - power // 2 + 2) * (1 + torch.rand(1, generator=g)))
+        scene.v_new[at, h] *= 2.0 ** 40
+    q = torch.zeros(rows, heads, head_dim)
+    q[:, :, 3] = 2.0 ** (power // 2) * (1 + torch.rand(rows, heads, generator=g))
+    q[1::2] *= -1
+    run(scene, [rows], q.bfloat16())
+
+
 @pytest.mark.parametrize("head_dim", [64, 128])
 @pytest.mark.parametrize("rows", [1, 14, 40, 300])
 @pytest.mark.parametrize("low", [60, 121, 124])
