@@ -614,7 +614,8 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             } else {
               p[i] = pack_bf16(x.x, x.y);
             }
-            if constexpr (!kOnes) sum = __fadd2_rn(sum, x);
+            // the sum of what is multiplied: the rounded ones, or both parts
+            if constexpr (!kOnes) sum = __fadd2_rn(sum, kEdge ? x : make_float2(bf16_lo(p[i]), bf16_hi(p[i])));
           }
           if constexpr (kEdge) tmem_st16(s_addr + 32 + g * 16, rest);
           tmem_st16(s_addr + g * 16, p);

@@ -1,9 +1,11 @@
 """Scores, probabilities and values far from the ordinary, every operator of the paged K/V cache against its definition in float64.
 Tolerances are those of test_gpu_kv_cache."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_kv_cache import Scene
+from test_gpu_kv_cache import DTYPES, Scene
 
 pytestmark = pytest.mark.gpu
 
@@ -53,6 +55,23 @@ def test_scores_of_any_size_above_and_below_the_first_keys(power, head_dim, rows
     q[:, :, 3] = 2.0 ** (power // 2) * (1 + torch.rand(rows, heads, generator=g))
     q[1::2] *= -1
     run(scene, [rows], q.bfloat16())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("rows", [1, 14, 200])
+def test_probabilities_that_all_round_the_same_way(rows, head_dim, dtype):
+    """In front of every 127 keys that are alike one of four times their weight, so that wherever the keys are cut their probabilities
+    lie just above a tie of bfloat16, and one value: what the rounding takes from the product it takes from the sum as well, or
+    the whole row is off by it."""
+    scene = Scene([4096], 2, head_dim, dtype, 128, seed=31)
+    scene.k_new.zero_()
+    scene.k_new[::128, :, 0] = 16.0
+    scene.v_new.fill_(1.125)
+    q = torch.zeros(rows, 2, head_dim)
+    q[:, :, 0] = 8.0
+    apart = 2.0 - math.log2(1 + 2.0 ** -8 + 2.0 ** -12)  # p = 2^-2 (1 + 2^-8 + 2^-12)
+    run(scene, [rows], q.bfloat16(), scale=apart / (16.0 * 8.0 * 1.4426950408889634))
 
 
 @pytest.mark.parametrize("head_dim", [64, 128])
