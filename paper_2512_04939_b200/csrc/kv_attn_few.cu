@@ -84,9 +84,11 @@ __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, ui
                : "memory");
 }
 
-// The reference may lag this far behind a row's maximum (base-2 units) before the row is scaled anew.
-constexpr float kFewSlack = 7.0f;
-// Codes: a probability times its value's power of two is a weight, at most 2^127 with this slack, and the product's operand is the
+// A row's reference is set this far above its maximum so far (base-2 units), and anew where a score exceeds it: probabilities are
+// 2^-7 to 1 for the largest, never more, so that sums of values at the end of the range hold where they would for a reference that
+// is the maximum.
+constexpr float kFewAbove = 7.0f;
+// Codes: a probability times its value's power of two is a weight, at most 2^120, and the product's operand is the
 // weight times a power of two 2^k of its row.  That brings the largest weight to [2^7, 2^8) when it is set, and is set anew where
 // one comes to more than 2^15 (f16 ends at 2^16).
 constexpr int kFewWeight = 7, kFewMostShift = 118;
@@ -254,7 +256,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     for (int i = 0; i < Shape::kOutTiles; ++i)
 #pragma unroll
       for (int j = 0; j < 2 * kHalves; ++j) o[i][j] = 0.0f;
-    float top[2] = {-INFINITY, -INFINITY}, ref[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};  // ref: top where that is finite yet
+    float limit[2] = {-INFINITY, -INFINITY}, ref[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};  // limit: ref, or that there is none yet
     // Codes: the rows' factors of the weights, which the output has in it.  (A power of infinity stands for a value that is not
     // finite, whose codes are zero: 0 * infinity = NaN.)
     [[maybe_unused]] float to[2] = {power_of_two(kFewMostShift), power_of_two(kFewMostShift)};
@@ -295,7 +297,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
           }
         }
-      // in base-2 units; the reference of a row moves only when a score lies far above it
+      // in base-2 units; the reference of a row moves only when a score lies above it
       float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int s = 0; s < kSubs; ++s)
@@ -312,18 +314,17 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             most[e >> 1] = fmaxf(most[e >> 1], x);
           }
         }
-      if (__any_sync(0xffffffffu, most[0] > top[0] + kFewSlack || (!kHalf && most[1] > top[1] + kFewSlack))) {
+      if (__any_sync(0xffffffffu, most[0] > limit[0] || (!kHalf && most[1] > limit[1]))) {
 #pragma unroll
         for (int half = 0; half < kHalves; ++half) {
           float m = most[half];
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
           m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-          if (m > top[half]) {
-            const bool first = top[half] == -INFINITY;
-            const float apart = m - ref[half];
+          if (m > limit[half]) {
+            const bool first = limit[half] == -INFINITY;
+            const float apart = m + kFewAbove - ref[half];
             float factor = first ? 0.0f : fast_exp2(-apart);
-            top[half] = m;
-            ref[half] = m;
+            ref[half] = limit[half] = m + kFewAbove;
             sum[half] *= factor;
             if constexpr (kNarrow) {  // what was the largest weight may be next to nothing now
               const int k = exponent_of(to[half]), next = min(k + (int)fminf(apart, 512.0f), kFewMostShift);
@@ -515,7 +516,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         }
         if (q4 == 0) {
           float* ml = smem_ml + (warp * Shape::kRows + r) * 2;
-          ml[0] = top[half];
+          ml[0] = limit[half];
           ml[1] = l;
         }
       }

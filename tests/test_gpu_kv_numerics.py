@@ -5,7 +5,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_kv_cache import DTYPES, Scene
+import kv_reference as ref
+from test_gpu_kv_cache import DTYPES, Scene, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -74,6 +75,23 @@ def test_probabilities_that_all_round_the_same_way(rows, head_dim, dtype):
     run(scene, [rows], q.bfloat16(), scale=apart / (16.0 * 8.0 * 1.4426950408889634))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("rows", [1, 3, 14, 40])
+def test_values_at_the_end_of_the_range(rows, head_dim, dtype):
+    """A key of 2^5 times the others' weight, anywhere among them, with a value of 2^125: the sums of probabilities of at most 1 hold."""
+    heads = 32
+    scene = Scene([8192], heads, head_dim, dtype, 128, seed=32)
+    scene.k_new.zero_()
+    for h in range(heads):
+        at = 200 + 250 * h
+        scene.k_new[at, h, 0] = 8.0
+        scene.v_new[at, h] = 2.0 ** 125 * torch.sign(scene.v_new[at, h].float()).bfloat16()
+    q = torch.zeros(rows, heads, head_dim)
+    q[:, :, 0] = 8.0
+    run(scene, [rows], q.bfloat16(), scale=5.0 / (64.0 * 1.4426950408889634))
+
+
 @pytest.mark.parametrize("head_dim", [64, 128])
 @pytest.mark.parametrize("rows", [1, 14, 40, 300])
 @pytest.mark.parametrize("low", [60, 121, 124])
@@ -88,3 +106,19 @@ def test_scores_of_minus_infinity_in_front(low, rows, head_dim):
     q[:, :, 0] = 8.0
     q[:, :, 1] = 1.0
     run(scene, [rows], q.bfloat16(), scale=low / (64.0 * 1.4426950408889634))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("rows", [1, 14])
+@pytest.mark.parametrize("length", [1, 700])
+def test_values_at_the_lower_end_of_the_range(length, rows, head_dim, dtype):
+    """Values of 2^-112 and, as bfloat16, of 2^-123: the tolerance of the other tests, and half a step of the output."""
+    scene = Scene([length], 2, head_dim, dtype, 16, seed=34)
+    scene.v_new *= 2.0 ** (-112 if dtype == "e4m3" else -123)
+    scene.store()
+    batch = scene.cache.batch([rows], [length], scene.pages)
+    q = scene.queries([rows], 2)
+    out = f64(scene.cache.attend(batch, q.cuda()))
+    want, spread = ref.attend(f64(q), *scene.held(0), 0, head_dim ** -0.5)
+    assert (abs(out - want) <= 2.0 ** -9 * abs(want) + 2.0 ** -8 * spread + 2.0 ** -134).all()
