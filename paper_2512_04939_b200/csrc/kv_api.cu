@@ -9,7 +9,8 @@ namespace lv {
 
 namespace {
 
-// DeviceGuard for calls whose launch is most of their time: nothing is set where the device is the current one already.
+// DeviceGuard for calls whose launch is most of their time: nothing is set where the device is the current one already.  Every call
+// that is given a stream needs one: the handles of default streams mean the current device's.
 struct OnDevice {
   int prev = -1;
   bool ok = false;
@@ -97,6 +98,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
     if (pages[i] < 0 || pages[i] >= c->cfg.pages) return LITEVGGT_ERR_SHAPE;
   b->magic = kKvBatchMagic;
   b->owner = c;
+  b->device = c->device;
   b->q_heads = q_heads;
   b->group = q_heads / c->cfg.kv_heads;
   b->causal_block = causal_block;
@@ -225,6 +227,8 @@ litevggt_status litevggt_kv_batch_place(litevggt_kv_batch* batch, void* memory, 
   if (!batch_ok(batch) || memory == nullptr) return LITEVGGT_ERR_NULL;
   if (bytes < batch->bytes) return LITEVGGT_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(memory) & 255u) != 0) return LITEVGGT_ERR_ALIGN;
+  const OnDevice g(batch->device);
+  if (!g.ok) return LITEVGGT_ERR_CUDA;
   // (from pageable memory: the call has taken the bytes when it returns)
   const cudaError_t e = cudaMemcpyAsync(memory, batch->image.data(), batch->image.size(), cudaMemcpyHostToDevice, (cudaStream_t)stream);
   if (e != cudaSuccess) return cuda_status(e);
@@ -299,6 +303,8 @@ litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_b
 
 litevggt_status litevggt_kv_poll(litevggt_kv_cache* cache, void* stream) {
   if (!cache_ok(cache)) return LITEVGGT_ERR_NULL;
+  const OnDevice g(cache->device);
+  if (!g.ok) return LITEVGGT_ERR_CUDA;
   cudaStream_t s = (cudaStream_t)stream;
   uint32_t word = 0;
   cudaError_t e = cudaMemcpyAsync(&word, cache->status, sizeof(word), cudaMemcpyDeviceToHost, s);

@@ -63,6 +63,7 @@ struct litevggt_kv_cache {
 struct litevggt_kv_batch {
   uint32_t magic;
   const litevggt_kv_cache* owner;
+  int device;
   int q_heads, group, causal_block;
   long long rows;
   bool rows_held;  // no sequence has more rows than tokens

@@ -1,0 +1,73 @@
+"""The paged K/V cache's entry points (kv_api.cu) linked against stand-ins for the CUDA runtime, two devices of it, and for the kernel
+launchers (kv_host_fakes.cpp).  No GPU."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+from paper_2512_04939_b200.binding import KVConfig
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(os.path.dirname(HERE), "paper_2512_04939_b200", "csrc")
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("host") / "libkvhost.so")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-w", "-Wl,-Bsymbolic", "-I/usr/local/cuda/include", "-x", "c++",
+                    os.path.join(CSRC, "kv_api.cu"), os.path.join(HERE, "kv_host_fakes.cpp"), "-o", so], check=True)
+    return C.CDLL(so)
+
+
+@pytest.fixture(autouse=True)
+def fresh(host):
+    host.fake_current_device(0)
+    host.fake_capture(0)
+    host.fake_forget()
+
+
+_KEPT = []
+
+
+def memory(size):
+    _KEPT.append(C.create_string_buffer(size + 256))
+    return C.c_void_p((C.addressof(_KEPT[-1]) + 255) & ~255)
+
+
+def cache_of(host, device=0, pages=8, page_size=16, kv_heads=2, head_dim=64):
+    cfg, handle, p = KVConfig(pages, page_size, kv_heads, head_dim, 0), C.c_void_p(), memory(64)
+    assert host.litevggt_kv_create(C.byref(cfg), device, p, p, None, None, p, C.byref(handle)) == 0
+    return handle
+
+
+def batch_of(host, cache, rows=3, length=20, pages=(1, 0), q_heads=2, place=True):
+    handle, size = C.c_void_p(), C.c_size_t()
+    assert host.litevggt_kv_batch_create(cache, 1, (C.c_int32 * 1)(rows), (C.c_int32 * 1)(length), (C.c_int32 * len(pages))(*pages), q_heads, 0,
+                                         C.byref(handle), C.byref(size)) == 0
+    if place:
+        assert host.litevggt_kv_batch_place(handle, memory(size.value), size, None) == 0
+    return handle, size
+
+
+def calls(host, cache, batch):
+    """Every call that takes a batch: append, gather, attend."""
+    p, i64 = memory(64), C.c_int64
+    return [host.litevggt_kv_append(cache, batch, p, i64(128), i64(64), p, i64(128), i64(64), None),
+            host.litevggt_kv_gather(cache, batch, p, p, None),
+            host.litevggt_kv_attend(cache, batch, p, i64(128), i64(64), C.c_float(0.125), memory(1 << 14), None)]
+
+
+@pytest.mark.parametrize("device,current", [(1, 0), (0, 1), (1, 1)])
+def test_every_stream_call_is_made_on_the_caches_device(host, device, current):
+    """Streams are named by handles that mean another stream on another device (the default ones do): a batch's arrays have to be
+    on their way in the stream that its kernels follow in, whatever device is current, and that stays current."""
+    cache = cache_of(host, device)
+    host.fake_current_device(current)
+    batch, _ = batch_of(host, cache)
+    assert (host.fake_stream_calls(device), host.fake_stream_calls(1 - device)) == (1, 0)
+    assert calls(host, cache, batch) == [0, 0, 0]
+    host.fake_forget()
+    assert host.litevggt_kv_poll(cache, None) == 0
+    assert host.fake_stream_calls(device) == 3 and host.fake_stream_calls(1 - device) == 0
+    assert host.fake_get_device() == current
