@@ -34,7 +34,7 @@ bool batch_ok(const litevggt_kv_batch* b) { return b != nullptr && b->magic == k
 // A batch of this cache whose arrays are on the device.
 litevggt_status usable(const litevggt_kv_cache* c, const litevggt_kv_batch* b) {
   if (!cache_ok(c) || b == nullptr) return LITEVGGT_ERR_NULL;
-  if (!batch_ok(b) || b->owner != c || b->base == nullptr) return LITEVGGT_ERR_STALE_PLAN;
+  if (!batch_ok(b) || b->owner_id != c->id || b->base == nullptr) return LITEVGGT_ERR_STALE_PLAN;
   return LITEVGGT_OK;
 }
 
@@ -97,7 +97,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
   for (long long i = 0; i < page0; ++i)
     if (pages[i] < 0 || pages[i] >= c->cfg.pages) return LITEVGGT_ERR_SHAPE;
   b->magic = kKvBatchMagic;
-  b->owner = c;
+  b->owner_id = c->id;
   b->device = c->device;
   b->q_heads = q_heads;
   b->group = q_heads / c->cfg.kv_heads;
@@ -166,6 +166,8 @@ litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, vo
   if (c == nullptr) return LITEVGGT_ERR_ALLOC;
   c->magic = kKvCacheMagic;
   c->cfg = *cfg;
+  static std::atomic<unsigned long long> made{0};
+  c->id = ++made;
   c->device = device;
   c->num_sms = sms;
   int shift = 4;

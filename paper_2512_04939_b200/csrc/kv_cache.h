@@ -51,6 +51,7 @@ struct KvAttend {
 
 struct litevggt_kv_cache {
   uint32_t magic;
+  unsigned long long id;  // no two caches of a process have the same (their addresses may come round)
   litevggt_kv_config cfg;
   int device, num_sms;
   lv::KvPool pool;
@@ -62,7 +63,7 @@ struct litevggt_kv_cache {
 
 struct litevggt_kv_batch {
   uint32_t magic;
-  const litevggt_kv_cache* owner;
+  unsigned long long owner_id;  // of the cache whose pool its page numbers were checked against
   int device;
   int q_heads, group, causal_block;
   long long rows;

@@ -71,3 +71,16 @@ def test_every_stream_call_is_made_on_the_caches_device(host, device, current):
     assert host.litevggt_kv_poll(cache, None) == 0
     assert host.fake_stream_calls(device) == 3 and host.fake_stream_calls(1 - device) == 0
     assert host.fake_get_device() == current
+
+
+def test_a_batch_does_not_outlive_its_cache(host):
+    """The next cache may lie where the last one did; a batch whose page numbers were checked against that one is refused."""
+    for _ in range(20):
+        old = cache_of(host, pages=8)
+        batch, _ = batch_of(host, old, pages=(7, 6))
+        assert calls(host, old, batch) == [0, 0, 0]
+        assert host.litevggt_kv_destroy(old) == 0
+        new = cache_of(host, pages=2)
+        host.fake_forget()
+        assert calls(host, new, batch) == [8, 8, 8] and host.fake_launches() == 0
+        assert host.litevggt_kv_batch_destroy(batch) == 0 and host.litevggt_kv_destroy(new) == 0
