@@ -371,7 +371,8 @@ litevggt_status litevggt_kv_batch_create(const litevggt_kv_cache* cache, int32_t
                                          const int32_t* pages, int32_t q_heads, int32_t causal_block, litevggt_kv_batch** out,
                                          size_t* bytes);
 /* Gives the batch its memory (dev, 256-byte aligned; the caller's, in use until the last call with this batch has run) and
- * copies its arrays there on `stream`.  Calls with one batch follow one another in stream order: they share its workspace. */
+ * copies its arrays there on `stream`, which must not be capturing (LITEVGGT_ERR_CUDA; calls with a batch that is in place may be captured).
+ * Calls with one batch follow one another in stream order: they share its workspace. */
 litevggt_status litevggt_kv_batch_place(litevggt_kv_batch* batch, void* memory, size_t bytes, void* stream);
 litevggt_status litevggt_kv_batch_destroy(litevggt_kv_batch* batch);
 

@@ -231,8 +231,13 @@ litevggt_status litevggt_kv_batch_place(litevggt_kv_batch* batch, void* memory, 
   if ((reinterpret_cast<uintptr_t>(memory) & 255u) != 0) return LITEVGGT_ERR_ALIGN;
   const OnDevice g(batch->device);
   if (!g.ok) return LITEVGGT_ERR_CUDA;
-  // (from pageable memory: the call has taken the bytes when it returns)
-  const cudaError_t e = cudaMemcpyAsync(memory, batch->image.data(), batch->image.size(), cudaMemcpyHostToDevice, (cudaStream_t)stream);
+  // From pageable memory: the call has taken the bytes when it returns.  In a capture it would not have: a graph reads its source
+  // again whenever it is replayed, and the batch may be gone by then.
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing((cudaStream_t)stream, &capture);
+  if (e != cudaSuccess) return cuda_status(e);
+  if (capture != cudaStreamCaptureStatusNone) return LITEVGGT_ERR_CUDA;
+  e = cudaMemcpyAsync(memory, batch->image.data(), batch->image.size(), cudaMemcpyHostToDevice, (cudaStream_t)stream);
   if (e != cudaSuccess) return cuda_status(e);
   batch->base = static_cast<uint8_t*>(memory);
   return LITEVGGT_OK;

@@ -84,3 +84,16 @@ def test_a_batch_does_not_outlive_its_cache(host):
         host.fake_forget()
         assert calls(host, new, batch) == [8, 8, 8] and host.fake_launches() == 0
         assert host.litevggt_kv_batch_destroy(batch) == 0 and host.litevggt_kv_destroy(new) == 0
+
+
+def test_a_batch_is_not_placed_while_its_stream_is_captured(host):
+    """The copy would be of the batch's own host memory, again at every replay, when the batch may be gone."""
+    cache = cache_of(host)
+    batch, size = batch_of(host, cache, place=False)
+    host.fake_capture(1)
+    assert host.litevggt_kv_batch_place(batch, memory(size.value), size, None) == 6
+    assert host.fake_stream_calls(0) == 0 and calls(host, cache, batch) == [8, 8, 8]
+    host.fake_capture(0)
+    assert host.litevggt_kv_batch_place(batch, memory(size.value), size, None) == 0
+    host.fake_capture(1)
+    assert calls(host, cache, batch) == [0, 0, 0]  # calls with a batch that is in place may be captured
