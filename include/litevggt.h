@@ -385,7 +385,8 @@ litevggt_status litevggt_kv_append(litevggt_kv_cache* cache, const litevggt_kv_b
 litevggt_status litevggt_kv_gather(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, void* k, void* v, void* stream);
 /* out[i] = sum_j softmax_j(scale q[i] . k[j]) v[j] over the tokens j that row i sees; zero for a row that sees none (a
  * sequence without tokens, or causal rows ahead of its first token).  A token that a row does not see has no influence
- * on it, whatever it holds.  q: dev bf16 [rows, q_heads, head_dim] with strides as above; out: dev bf16, contiguous;
+ * on it, whatever it holds.  q: dev bf16 [rows, q_heads, head_dim] with strides as above; out: dev bf16, contiguous, in
+ * memory of its own (LITEVGGT_ERR_SHAPE where it reaches into the queries: they may be read again after rows have been written);
  * scale: positive, finite. */
 litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
                                    int64_t q_head_stride, float scale, void* out, void* stream);

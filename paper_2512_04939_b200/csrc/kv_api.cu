@@ -44,6 +44,18 @@ litevggt_status stride_ok(int64_t row, int64_t head) {
   return row % 8 != 0 || head % 8 != 0 ? LITEVGGT_ERR_ALIGN : LITEVGGT_OK;
 }
 
+// Whether `n` bytes at `out` reach into one of the rows of queries, each taken from its first head to the end of its last.
+bool meets_queries(const void* out, long long n, const void* q, long long rows, long long row_bytes, long long row_stride_bytes) {
+  const long long begin = (long long)(reinterpret_cast<intptr_t>(out) - reinterpret_cast<intptr_t>(q)), end = begin + n;
+  // the first row that ends behind the output's beginning
+  long long i = 0;
+  if (begin >= row_bytes) {
+    if (row_stride_bytes == 0) return false;
+    i = (begin - row_bytes) / row_stride_bytes + 1;
+  }
+  return i < rows && i * row_stride_bytes < end;
+}
+
 // Lays out a batch's device memory: first what the host writes (`image`), then what only kernels use.
 void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int head_dim) {
   size_t at = 0;
@@ -296,6 +308,8 @@ litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_b
   if (q == nullptr || out == nullptr) return LITEVGGT_ERR_NULL;
   if (!aligned16(q) || !aligned16(out)) return LITEVGGT_ERR_ALIGN;
   if ((st = stride_ok(q_row_stride, q_head_stride)) != LITEVGGT_OK) return st;
+  const long long hd = cache->cfg.head_dim, row_bytes = 2 * ((batch->q_heads - 1) * q_head_stride + hd);
+  if (meets_queries(out, 2 * batch->rows * batch->q_heads * hd, q, batch->rows, row_bytes, 2 * q_row_stride)) return LITEVGGT_ERR_SHAPE;
   const OnDevice g(cache->device);
   if (!g.ok) return LITEVGGT_ERR_CUDA;
   const KvAttend a{static_cast<const __nv_bfloat16*>(q), KvStride{q_row_stride, q_head_stride}, static_cast<__nv_bfloat16*>(out),

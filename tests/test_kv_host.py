@@ -97,3 +97,18 @@ def test_a_batch_is_not_placed_while_its_stream_is_captured(host):
     assert host.litevggt_kv_batch_place(batch, memory(size.value), size, None) == 0
     host.fake_capture(1)
     assert calls(host, cache, batch) == [0, 0, 0]  # calls with a batch that is in place may be captured
+
+
+@pytest.mark.parametrize("at,row_stride,refused", [
+    (0, 128, True), (8, 128, True), (-8, 128, True), (376, 128, True), (-376, 128, True),  # of 3 rows of 2 heads of 64
+    (384, 128, False), (-384, 128, False),
+    (-384, 4096, False), (120, 4096, True), (128, 4096, False), (3712, 4096, False), (3720, 4096, True), (4216, 4096, True), (4224, 4096, False),
+    (8192 + 120, 4096, True), (8192 + 128, 4096, False), (120, 0, True), (128, 0, False)])
+def test_outputs_lie_beside_the_queries(host, at, row_stride, refused):
+    """`at`: where the output begins, in elements behind the queries.  A piece that is done again reads its queries again, so they must not
+    have been written over; an output between rows of queries is none of that."""
+    cache = cache_of(host)
+    batch, _ = batch_of(host, cache)
+    q = memory(1 << 16).value + (1 << 14)
+    st = host.litevggt_kv_attend(cache, batch, C.c_void_p(q), C.c_int64(row_stride), C.c_int64(64), C.c_float(0.125), C.c_void_p(q + 2 * at), None)
+    assert st == (3 if refused else 0)
