@@ -103,8 +103,8 @@ inline double kv_cut_by(double share, const std::vector<KvSeq>& seqs, const std:
     const KvSeq& q = seqs[(size_t)s];
     const int all = q.rows * group;
     for (int h = 0; h < kv_heads; ++h)
-      for (int r = 0; r < all; r += cut.row_block) {
-        const int n = std::min(cut.row_block, all - r);
+      for (long long first = 0; first < all; first += cut.row_block) {  // (the end of the last block may lie beyond 32 bits)
+        const int r = (int)first, n = std::min(cut.row_block, all - r);
         const int seen = std::max(kv_seen(q.len, q.rows, causal_block, (r + n - 1) / group), 0);
         const int units = (int)(((long long)seen + cut.unit - 1) / cut.unit);
         const double cost = kv_unit_cost(cut, n);
@@ -155,8 +155,8 @@ inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& whi
     const KvSeq& q = seqs[(size_t)s];
     const int all = q.rows * group;
     double one_head = 0.0;
-    for (int r = 0; r < all; r += cut.row_block) {
-      const int n = std::min(cut.row_block, all - r);
+    for (long long first = 0; first < all; first += cut.row_block) {
+      const int r = (int)first, n = std::min(cut.row_block, all - r);
       const int seen = std::max(kv_seen(q.len, q.rows, causal_block, (r + n - 1) / group), 0);
       one_head += (double)(((long long)seen + cut.unit - 1) / cut.unit) * kv_unit_cost(cut, n) + cut.overhead;
     }
