@@ -112,7 +112,7 @@ inline double kv_cut_by(double share, const std::vector<KvSeq>& seqs, const std:
         int done = 0;
         do {
           const double left = (worker + 1) * share - spent - cut.overhead;
-          int take = left > 0.0 ? (int)(left / cost) : 0;
+          int take = left > 0.0 ? (int)std::min(left / cost, (double)units) : 0;
           if (worker + 1 >= cut.workers) take = units;
           if (take < std::min(cut.min_units, units - done) && next_worker()) continue;
           if (units - done - take < cut.min_units) take = units - done;  // no crumbs
