@@ -21,6 +21,16 @@ from .binding import KVConfig, _check, load_library
 _DTYPES = {"bf16": (0, torch.bfloat16), "e4m3": (1, torch.float8_e4m3fn)}
 
 
+def _whole(name: str, numbers) -> np.ndarray:
+    """One whole number after another, as 64-bit ones."""
+    given = np.asarray(numbers)
+    with np.errstate(invalid="ignore"):
+        whole = given.astype(np.int64)
+    if given.ndim != 1 or not np.array_equal(given, whole):
+        raise ValueError(f"{name} must be whole numbers in one dimension")
+    return whole
+
+
 class KVBatch:
     """Rows, lengths and pages of a step's sequences, planned for one cache (see :meth:`KVCache.batch`)."""
 
@@ -110,7 +120,7 @@ class KVCache:
         row sees the tokens before its sequence's rows and the blocks of c rows up to its own; 0: all of them."""
         if len(rows) != len(lengths) or len(rows) != len(pages) or len(rows) == 0:
             raise ValueError(f"rows, lengths and pages name {len(rows)}, {len(lengths)} and {len(pages)} sequences")
-        n_rows, n_tokens = np.asarray(rows, np.int64), np.asarray(lengths, np.int64)
+        n_rows, n_tokens = _whole("rows", rows), _whole("lengths", lengths)
         if min(n_rows.min(), n_tokens.min()) < 0 or max(n_rows.max(), n_tokens.max()) >= 2 ** 31:
             raise ValueError("rows and lengths must lie in [0, 2^31)")
         lists = []
@@ -118,12 +128,14 @@ class KVCache:
             need = -(-n // self.page_size)
             if len(ids) < need:
                 raise ValueError(f"a sequence of {n} tokens needs {need} pages, got {len(ids)}")
-            lists.append(np.asarray(ids[:need], np.int64))
-        flat = np.concatenate(lists)
+            lists.append(np.asarray(ids[:need]))
+        flat = _whole("pages", lists[0] if len(lists) == 1 else np.concatenate(lists))
         if flat.size and (flat.min() < 0 or flat.max() >= self.pages):
             raise ValueError(f"pages must lie in [0, {self.pages})")
         r32, n32, p32 = (np.ascontiguousarray(a, np.int32) for a in (n_rows, n_tokens, flat))
         q_heads = self.kv_heads if q_heads is None else q_heads
+        if max(abs(q_heads), abs(causal_block)) >= 2 ** 31:  # (ctypes would pass the lower 32 bits)
+            raise ValueError(f"q_heads and causal_block must be less than 2^31, got {q_heads} and {causal_block}")
         handle, n_bytes = C.c_void_p(), C.c_size_t()
         _check(self.lib.litevggt_kv_batch_create(self.handle, len(rows), r32.ctypes.data, n32.ctypes.data, p32.ctypes.data, q_heads,
                                                  causal_block, C.byref(handle), C.byref(n_bytes)), "kv_batch_create")
