@@ -26,7 +26,8 @@ class StreamingGlobalAttention:
             raise ValueError(f"capacity must be positive and hold the window, got {capacity} and {window}")
         self.ctx = ctx
         self.heads, self.head_dim = ctx.cfg.heads, ctx.dim // ctx.cfg.heads
-        n_pages = -(-capacity // page_size)
+        # (whole pages are given back, so what is kept of a window begins somewhere in its first page: one more than it fills)
+        n_pages = -(-capacity // page_size) + (window is not None)
         self.cache = KVCache.empty(n_pages, page_size, self.heads, self.head_dim, dtype, ctx.device.index)
         self.window = window
         self.free = list(range(n_pages))
