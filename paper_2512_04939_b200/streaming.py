@@ -41,23 +41,23 @@ class StreamingGlobalAttention:
 
     def step(self, x: torch.Tensor, w_qkv, b_qkv, w_o, b_o, frame_rows: int = 0) -> torch.Tensor:
         """The layer's output for the new rows ``x`` [rows, dim], which join the sequence.  ``frame_rows`` > 0: the rows are
-        frames of that many, and a frame does not see those behind it; 0: they all see one another."""
+        frames of that many, and a frame does not see those behind it; 0: they all see one another.  If it raises before the rows'
+        K and V are stored, the layer is as it was; what raises behind that leaves them in the sequence."""
         rows, size = x.shape[0], self.cache.page_size
+        spare = 0
         if self.window is not None:
             # what stays in front of the new rows is the window's, less a page at most
             spare = max(0, self.length + rows - max(self.window, rows)) // size
             spare = min(spare, self.length // size)
-            self.free += self.pages[:spare]
-            del self.pages[:spare]
-            self.length -= spare * size
-        need = -(-(self.length + rows) // size) - len(self.pages)
-        if need > len(self.free):
-            raise ValueError(f"{self.length} tokens held and {rows} new ones need {need} pages, {len(self.free)} are free")
-        self.pages += [self.free.pop() for _ in range(need)]
-        self.length += rows
-        batch = self.cache.batch([rows], [self.length], [self.pages], causal_block=frame_rows)
+        held, free, left = self.pages[spare:], self.free + self.pages[:spare], self.length - spare * size
+        need = -(-(left + rows) // size) - len(held)
+        if need > len(free):
+            raise ValueError(f"{left} tokens held and {rows} new ones need {need} pages, {len(free)} are free")
+        pages, free, length = held + free[len(free) - need:], free[:len(free) - need], left + rows
         qkv = self.ctx.linear(x, w_qkv, b_qkv)
         q, k, v = (t.unflatten(1, (self.heads, self.head_dim)) for t in qkv.split(self.ctx.dim, 1))
+        batch = self.cache.batch([rows], [length], [pages], causal_block=frame_rows)
         self.cache.append(batch, k, v)
+        self.pages, self.free, self.length = pages, free, length
         out = self.cache.attend(batch, q)
         return self.ctx.linear(out.flatten(1), w_o, b_o)

@@ -85,3 +85,37 @@ def test_a_window_that_fits_never_runs_out_of_pages(made, window, capacity, page
         held = min(at, max(window, n))
         assert held <= layer.length < held + page_size and whole(layer)
         assert layer.cache.seen == [i % 256 for i in range(at - layer.length, at)]
+
+
+@pytest.mark.parametrize("window", [None, 100])
+@pytest.mark.parametrize("fail", [("linear", 3 * DIM), "batch", "append", "pages"])
+def test_a_step_that_fails_before_its_rows_are_stored_changes_nothing(made, window, fail):
+    """Whatever raises - a projection, the plan, the store, or the lack of pages - the next step goes on from where the last one ended."""
+    layer = made(200, page_size=16, window=window)
+    for at in range(0, 180, 30):
+        layer.step(tokens(at, 30), *WEIGHTS)
+    before = list(layer.pages), list(layer.free), layer.length
+    with pytest.raises(ValueError if fail == "pages" else RuntimeError):
+        if fail == "pages":
+            layer.step(tokens(180, 300), *WEIGHTS)
+        else:
+            Cache.fail = fail
+            layer.step(tokens(180, 17), *WEIGHTS)
+    Cache.fail = None
+    assert (layer.pages, layer.free, layer.length) == before
+    layer.step(tokens(180, 17), *WEIGHTS)
+    assert layer.cache.seen == [i % 256 for i in range(197 - layer.length, 197)] and whole(layer)
+
+
+@pytest.mark.parametrize("fail", ["attend", ("linear", DIM)])
+def test_rows_that_are_stored_stay(made, fail):
+    """What raises behind the store leaves the new rows in the sequence."""
+    layer = made(200, page_size=16, window=100)
+    layer.step(tokens(0, 90), *WEIGHTS)
+    Cache.fail = fail
+    with pytest.raises(RuntimeError):
+        layer.step(tokens(90, 40), *WEIGHTS)
+    Cache.fail = None
+    assert whole(layer)
+    layer.step(tokens(130, 1), *WEIGHTS)
+    assert layer.cache.seen == [i % 256 for i in range(131 - layer.length, 131)] and layer.length >= 100
