@@ -43,6 +43,7 @@ class StreamingGlobalAttention:
         """The layer's output for the new rows ``x`` [rows, dim], which join the sequence.  ``frame_rows`` > 0: the rows are
         frames of that many, and a frame does not see those behind it; 0: they all see one another.  If it raises before the rows'
         K and V are stored, the layer is as it was; what raises behind that leaves them in the sequence."""
+        self._check(x, w_qkv, b_qkv, w_o, b_o)
         rows, size = x.shape[0], self.cache.page_size
         spare = 0
         if self.window is not None:
@@ -61,3 +62,16 @@ class StreamingGlobalAttention:
         self.pages, self.free, self.length = pages, free, length
         out = self.cache.attend(batch, q)
         return self.ctx.linear(out.flatten(1), w_o, b_o)
+
+    def _check(self, x, w_qkv, b_qkv, w_o, b_o):
+        """The matrix product is told sizes and trusts every extent; all operands are looked at before the sequence changes."""
+        d = self.ctx.dim
+        if x.dim() != 2 or x.shape[0] < 1:
+            raise ValueError(f"x must be [rows, {d}] with at least one row, got {tuple(x.shape)}")
+        for name, t, shape in (("x", x, (x.shape[0], d)), ("w_qkv", w_qkv, (3 * d, d)), ("b_qkv", b_qkv, (3 * d,)), ("w_o", w_o, (d, d)), ("b_o", b_o, (d,))):
+            if t is None and name.startswith("b_"):
+                continue
+            if t is None or t.shape != shape:
+                raise ValueError(f"{name} must be {list(shape)}, got {None if t is None else tuple(t.shape)}")
+            if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.device != self.ctx.device:
+                raise ValueError(f"{name} must be a contiguous bfloat16 tensor on {self.ctx.device}, got {t.dtype} on {t.device}")

@@ -44,8 +44,7 @@ class Cache:
 
 
 class Context:
-    cfg, dim, device = types.SimpleNamespace(heads=HEADS), DIM, torch.device("cuda", 0)
-    calls = 0
+    cfg, dim, device = types.SimpleNamespace(heads=HEADS), DIM, torch.device("cpu")
 
     def linear(self, a, w, bias=None):
         if Cache.fail == ("linear", w.shape[0]):
@@ -119,3 +118,22 @@ def test_rows_that_are_stored_stay(made, fail):
     assert whole(layer)
     layer.step(tokens(130, 1), *WEIGHTS)
     assert layer.cache.seen == [i % 256 for i in range(131 - layer.length, 131)] and layer.length >= 100
+
+
+def bf(*shape):
+    return torch.zeros(*shape, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("which,bad", [
+    (0, bf(3, DIM - 64)), (0, bf(3, 2 * DIM)[:, ::2]), (0, torch.zeros(3, DIM)), (0, bf(3, 1, DIM)), (0, bf(0, DIM)), (0, bf(3, DIM).to("meta")),
+    (1, bf(3 * DIM, DIM - 64)), (1, bf(2 * DIM, DIM)), (1, bf(4 * DIM, DIM)), (1, torch.zeros(3 * DIM, DIM)), (1, bf(DIM, 3 * DIM).t()), (1, None),
+    (2, bf(DIM)), (2, bf(3 * DIM, 1)), (2, torch.zeros(3 * DIM)), (3, bf(DIM, DIM - 1)), (3, bf(2 * DIM, DIM)), (3, bf(DIM, DIM).to("meta")), (3, None), (4, bf(DIM - 1))])
+def test_operands_that_the_projections_cannot_take_are_refused(made, which, bad):
+    """The matrix product is told sizes and trusts every extent: what is smaller than them would be read past its end."""
+    layer = made(100)
+    args = [tokens(0, 3), *WEIGHTS]
+    args[which] = bad
+    with pytest.raises(ValueError):
+        layer.step(*args)
+    assert layer.length == 0
+    layer.step(tokens(0, 3), WEIGHTS[0], bf(3 * DIM), WEIGHTS[2], bf(DIM))
