@@ -335,6 +335,9 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
 #pragma unroll
             for (int c = 0; c < kStreams; ++c) issue_qk(c, ring.slot);
             umma_commit(&bars->k_empty[ring.slot]);
+            // what the first product awaits beside its own stream, here, where it is not in the loop's way
+            static_assert(kStreams == 2 && kv_awaits(0, 0, 1) && !kv_awaits(0, 1, 0) && !kv_awaits(1, 0, 1) && !kv_awaits(1, 1, 0), "");
+            ok = mbar_wait(&bars->p_ready[t][1], step & 1u, ctl);
           }
         }
         for (int j = 0; j < job.tiles && ok; ++j) {
@@ -344,9 +347,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             ok = mbar_wait(&bars->v_full[ring.slot], ring.phase, ctl);
 #pragma unroll
             for (int c = 0; c < kStreams; ++c) {
-#pragma unroll
-              for (int other = 0; other < kStreams; ++other)
-                if (kv_awaits(j, c, other)) ok = ok && mbar_wait(&bars->p_ready[t][other], step & 1u, ctl);
+              ok = ok && mbar_wait(&bars->p_ready[t][c], step & 1u, ctl);
               if (!ok) break;
               tc_fence_after();
               if (mode != kMaxima) {
