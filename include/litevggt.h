@@ -337,7 +337,8 @@ litevggt_status litevggt_launch_count(const litevggt_ctx* ctx, int64_t* launches
  * A batch is what the calls of one step have in common: for each sequence how many rows of the packed tensors belong to
  * it, how many tokens it holds, in which pages.  A sequence's rows are its last tokens: the call that appends a chunk
  * and those that attend from it take the same batch, whose lengths already count the chunk; a reader that wants a whole
- * sequence names as many rows as it has tokens, 2^30 at most.  Batches are made on the host and serve every layer of a step. */
+ * sequence names as many rows as it has tokens, 2^30 at most.  Batches are made on the host, for one cache: they serve every
+ * call on it in a step, and another cache refuses them (LITEVGGT_ERR_STALE_PLAN), its pool being another. */
 enum {
   LITEVGGT_KV_BF16 = 0,
   LITEVGGT_KV_E4M3 = 1 /* a row of a head as E4M3 codes x and an exponent byte e + 127, standing for x 2^e: the least

@@ -1,5 +1,5 @@
 // How the work of a batch over a paged K/V cache is cut: which rows of which sequence meet which keys in which CTA.  Host
-// arithmetic only; the batch's arrays are made here once and serve every layer that works on the same lengths and pages.
+// arithmetic only; the batch's arrays are made here once and serve every call that is made with it.
 #pragma once
 
 #include <stdint.h>

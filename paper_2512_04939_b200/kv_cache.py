@@ -1,11 +1,12 @@
 """A paged K/V cache and the attention that reads it, for frames that keep arriving.
 
     cache = KVCache.empty(pages, page_size, kv_heads, head_dim, dtype="e4m3")
-    batch = cache.batch(rows=[1041], lengths=[52050], pages=[page_ids])    # once per step, for every layer's cache alike
+    batch = cache.batch(rows=[1041], lengths=[52050], pages=[page_ids])    # once per step: the same for every call on this cache
     cache.append(batch, k, v)                                              # the last 1041 tokens of the sequence
     out = cache.attend(batch, q)                                           # over all 52050
 
-Which pages a sequence owns is the caller's business; the library checks that they exist.  Shapes, types, strides and
+Which pages a sequence owns is the caller's business; the library checks that they exist - in the pool of the cache that plans the
+batch, and no other cache takes it.  Shapes, types, strides and
 devices are checked here, everything else in the C library.
 """
 from __future__ import annotations
