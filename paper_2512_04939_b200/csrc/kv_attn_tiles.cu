@@ -50,11 +50,11 @@ constexpr int kKeys = kTileKeys / kStreams;  // of a stream's step
 template <int kHd, bool kNarrow>
 struct TiShape {
   static constexpr bool kOnes = kHd == 64;    // the tensor core adds up the rows, and Q is in its memory
-  // Of the 16 pairs of 32 scores, this many take their exponentials on the FMA pipes: 14 issue slots and more for 16 clocks of the
-  // special-function unit.  Where codes are widened beside them there are few slots to spare.  2048 rows over 83,280 keys, none /
-  // 1 / 2 / 4 pairs: head dim 64 800 / 787 / 776 / 779 us, E4M3 935 / 950 / 938 / 966; head dim 128 644 / 647 / 643 / 642, E4M3
-  // 752 / 762 / 771 / 788.
-  static constexpr int kPolyPairs = kNarrow ? 0 : 2;
+  // Of the 16 pairs of 32 scores, this many take their exponentials on the FMA pipes: 16 issue slots and more for 16 clocks of the
+  // special-function unit.  That pays where this unit is the bound, and not beside codes that are widened.  2048 rows over 83,280
+  // keys, none / 1 / 2 / 4 pairs: head dim 64 802 / 786 / 787 / 797 us, E4M3 946 / 952 / 966 / 1006; head dim 128 629 / 636 / 643 /
+  // 640, E4M3 780 / 785 / 801 / 819.
+  static constexpr int kPolyPairs = kOnes && !kNarrow ? 2 : 0;
   static constexpr int kHelpers = kNarrow ? 8 : 1;
   static constexpr int kThreads = (kSoftmaxWarps + 4 + (kNarrow ? 8 : 0)) * 32;
   static constexpr int kStages = kHd == 64 ? (kNarrow ? 3 : 4) : 2;
