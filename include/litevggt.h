@@ -343,7 +343,7 @@ enum {
   LITEVGGT_KV_BF16 = 0,
   LITEVGGT_KV_E4M3 = 1 /* a row of a head as E4M3 codes x and an exponent byte e + 127, standing for x 2^e: the least
                           e >= -118 with max|row| <= 448 * 2^e; a row that is not finite is held as byte 255 beside
-                          codes of zero, and reads as NaN */
+                          codes of zero, and reads as NaN.  Pools that the caller fills keep to it: e <= 120, no codes of NaN */
 };
 typedef struct {
   int32_t pages;     /* in the pool */
@@ -378,7 +378,7 @@ litevggt_status litevggt_kv_batch_place(litevggt_kv_batch* batch, void* memory, 
 litevggt_status litevggt_kv_batch_destroy(litevggt_kv_batch* batch);
 
 /* Writes K and V of the batch's rows into their sequences' pages.  k, v: dev bf16 [rows, kv_heads, head_dim], 16-byte
- * aligned, head_dim contiguous, the other strides in elements (multiples of 8, not negative).
+ * aligned, head_dim contiguous, the other strides in elements (multiples of 8, from 0 to 2^32 - 1).
  * LITEVGGT_ERR_SHAPE if a sequence has more rows than tokens. */
 litevggt_status litevggt_kv_append(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* k, int64_t k_row_stride,
                                    int64_t k_head_stride, const void* v, int64_t v_row_stride, int64_t v_head_stride, void* stream);
@@ -388,7 +388,7 @@ litevggt_status litevggt_kv_gather(litevggt_kv_cache* cache, const litevggt_kv_b
  * sequence without tokens, or causal rows ahead of its first token).  A token that a row does not see has no influence
  * on it, whatever it holds.  q: dev bf16 [rows, q_heads, head_dim] with strides as above; out: dev bf16, contiguous, in
  * memory of its own (LITEVGGT_ERR_SHAPE where it reaches into the queries: they may be read again after rows have been written);
- * scale: positive, finite. */
+ * scale: positive, less than 1e30. */
 litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
                                    int64_t q_head_stride, float scale, void* out, void* stream);
 /* As litevggt_poll_device_status, and the number of kernels launched on behalf of the cache. */

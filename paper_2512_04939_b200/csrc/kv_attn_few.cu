@@ -14,12 +14,14 @@
 //               ones, so P goes from accumulator to operand without leaving the lane
 // Codes are widened to f16, which takes one conversion for two of them.  Their powers of two stay outside: a key's scales its
 // scores, a value's its probability; that product is the value's weight, relative to the row's largest.  Q goes to f16 under a
-// power of two of its row (exact but for elements 2^-38 under the row's largest); weights have 11 bits there, not 8, down to 2^-21
-// of the row's largest or less, and fixed steps of 2^-31 of it or less below.
+// power of two of its row (exact but for elements under 2^-30 of the row's largest, which keep steps of 2^-37 of it or less); weights
+// have 11 bits there, not 8, down to 2^-21 of the row's largest or less, and fixed steps of 2^-31 of it or less below: where one key's value
+// has a code of zero in a channel, keys of 2^-32 of its weight count as nothing there.
 //
-// One token of 16 heads of 64 over 260,250 keys in bf16: 174 us, 6.1 TB/s, the rate of a copy; 48 tokens of 16 heads of 128 over 1,100
-// to 4,164 keys 166 us, 6.2 TB/s.  Codes are bound by the work of widening them (a conversion takes as long as four of the other
-// instructions; the ALU is 60 % busy): over 520,500 keys 209 us, 5.2 TB/s.  (Straight from global memory into the
+// One token of 16 heads of 64 over 260,250 keys in bf16: 176 us, 6.1 TB/s, the rate of a copy; 48 tokens of 16 heads of 128 over 1,100
+// to 4,164 keys 166 us, 6.2 TB/s.  Codes of head dim 64 are bound by the work of widening them (a conversion takes as long as four of the
+// other instructions; the ALU is 60 % busy): over 520,500 keys 207 us, 5.2 TB/s.  At head dim 128 nothing is over 30 % busy: two warps a
+// scheduler, each with one chain of waits, conversions, products and exponentials (16 tokens, 8 query heads a K/V head, 35 us).  (Straight from global memory into the
 // fragments, without rings: 189, 307 and 404 us.  The scores by products of 8-bit operands, Q in two of them, which need no
 // conversion of K in the source: 202 -> 220 us, sixteen tokens that share heads by eight 32.9 -> 33.2.)  Few keys: 4.8 us for 262, of which the latency of three dependent loads and the
 // meeting of the parts are most.

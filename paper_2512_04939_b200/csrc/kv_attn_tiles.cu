@@ -9,8 +9,9 @@
 // the tensor core adds up the bf16 probabilities that it multiplies.  At head dim 128 the tensor cores are the bound, and their
 // memory is full with S and O: Q comes from shared memory, the threads add up their own probabilities.
 // A row's reference is its maximum in the piece's first key tile, and it stays: p may grow to 2^60 in bf16 and 32-bit sums as
-// well as stay below 1.  Where it grows more (the row's sum tells, at the end of the piece), the piece is done again when
-// all others are through, with one sweep for the maxima first.
+// well as stay below 1.  Where it grows more (the row's sum tells, at the end of the piece), or where the first key tile leaves a row
+// without a reference, the piece is done again when all others are through, with one sweep for the maxima first; then a row's largest
+// score is taken off before the scale, so scores may be as large as 32 bits hold.
 // Tensor memory (512 columns): S of both tiles, 128 columns each; O of both, 80 columns (64 channels, the sum, 15 unused) or 128;
 // at head dim 64 Q of both, 32 columns.  P (bf16 pairs) goes over the start of the stream's own columns of S and is the second
 // product's A operand.  The instructions of a tile retire in order: a stream's next Q K^T is issued behind the P V that reads the
@@ -23,11 +24,13 @@
 //   E4M3  codes and exponents come by bulk copies into a ring of their own; the eight warps widen them to the same tiles,
 //         exactly, and look after V on the way.
 //
-// 2048 rows over 83,280 keys, 699 GFLOP: head dim 64 (16 heads) 771 us, 907 TFLOP/s; head dim 128 (8 heads) 633 us, 1104; over E4M3
-// 935 us and 751.  In bursts; under the 1 kW cap, which all of them reach, head dim 64 makes 765.  What bounds them (2048 rows over 10,410
+// 2048 rows over 83,280 keys, 699 GFLOP: head dim 64 (16 heads) 786 us, 889 TFLOP/s; head dim 128 (8 heads) 630 us, 1110; over E4M3
+// 946 us and 780.  In bursts; under the 1 kW cap, which all of them reach, head dim 64 makes 750.  What bounds them (2048 rows over 10,410
 // keys): head dim 64 the special-function unit, 67 % of it with set-up and all, beside 44 % of the issue slots and 43 % of the
-// tensor cores; head dim 128 nothing alone (tensor cores 51 %): a stream waits for its own products, and Q's share of
-// shared memory's bandwidth is taken twice a key tile; codes the issue slots (63 % and 55 %).
+// tensor cores; head dim 128 nothing alone (tensor cores and special-function unit 52 %): a stream waits for its own products, and Q's
+// share of shared memory's bandwidth is taken twice a key tile; codes the issue slots (60 % and 58 %), at 72 registers a thread, of which
+// 334 and 506 bytes are spilled (bf16 76 and 176, at 96).  A piece of 17 rows, which a frame of 1,041 leaves behind four of 256, runs
+// like one of 128: most of its softmax warps take exponentials of rows that do not exist.
 // Tried and left: one product of 128 columns for both streams' scores at head dim 128 (643 -> 649 us, 98 -> 109 at 10,410 keys: the
 // streams then wait for each other); the first 32 keys' probabilities handed over ahead of the others (no change); registers
 // moved between warps by setmaxnreg (no function may be called then, and the waits in line cost more than the registers
@@ -681,7 +684,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       float row_sum = sum.x + sum.y;
       if (mine > 0) {
         // The next piece's queries are under way while the last products are, and its first scores while the rows leave.  (At
-        // head dim 64 that costs registers which the sweep has not got: 792 -> 812 us at 2048 rows over 83,280 keys.)
+        // head dim 64 that costs registers which the sweep has not got: 2.5 % at 2048 rows over 83,280 keys.)
         Job next = job;
         bool some = false;
         uint4 x[kChunks];

@@ -164,7 +164,7 @@ class KVCache:
 
     def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
         """softmax(scale q K^T) V of the batch's rows over the tokens that they see; ``q`` bfloat16 [batch.rows, q_heads, head_dim].
-        ``scale`` is 1 / sqrt(head_dim) unless given.  ``out``, if given, must not lie where ``q`` does.  A row that sees no token
+        ``scale`` is 1 / sqrt(head_dim) unless given (positive, less than 1e30).  ``out``, if given, must not lie where ``q`` does.  A row that sees no token
         comes out as zero."""
         q_rows = self._rows("q", q, batch.q_shape)
         if out is None:
