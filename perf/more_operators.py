@@ -1,12 +1,15 @@
 """What a stream of frames that has no end needs beside its paged K/V cache: where a token stands in time and in its
-frame, and which of the tokens held so far may go.
+frame, a cache of 4 bits an element, and which of the tokens held so far may go.
 
 Queries and keys are turned by their position along several axes (time, height, width) before the keys go into the
-cache; the attention that a cached token draws is added up while chunks pass; and when the cache is full, every head keeps
-the tokens that drew most.  The kinds of pass:
+cache, which may hold them as E2M1 codes with a power of two for every 32 channels; the attention that a cached token draws is
+added up while chunks pass; and when the cache is full, every head keeps the tokens that drew most.  The kinds of pass:
 
   rotate  queries and keys of a fused projection, turned by their tokens' positions
   back    the gradients of turned queries and keys, turned back
+  store   K and V of new tokens written into a cache of 4 bits, and read back
+  attend  the rows of a chunk over the 4-bit keys and values of their sequence
+  step    both: K and V of the chunk written first
   weigh   what every cached token of a sequence draws of the rows' attention, given each row's log-sum-exp
   evict   the tokens that drew most (and the first and last ones, whatever they drew), moved to other pages
 
@@ -32,8 +35,8 @@ def _rotary(op, rows, q_heads, kv_heads, head_dim, layout, sections, dtype="bf16
     return c if name is None else dict(c, name=name)
 
 
-def _weigh(n_seq, rows, keys, q_heads, kv_heads, head_dim, dtype, page_size=64, causal_block=0, ragged=False, name=None):
-    c = dict(op="weigh", n_seq=n_seq, rows=rows, keys=keys, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, dtype=dtype,
+def _over(op, n_seq, rows, keys, q_heads, kv_heads, head_dim, dtype, page_size=64, causal_block=0, ragged=False, name=None):
+    c = dict(op=op, n_seq=n_seq, rows=rows, keys=keys, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, dtype=dtype,
              page_size=page_size, causal_block=causal_block, ragged=ragged)
     return c if name is None else dict(c, name=name)
 
@@ -48,24 +51,24 @@ def listed():
     return [
         # one camera token of a late frame: the smallest call
         _rotary("rotate", 1, 16, 16, 64, "halves", (16, 24, 24), first_frame=90000, name="rotate_token"),
-        # a new frame's tokens on their way into the cache
-        _rotary("rotate", 1041, 16, 16, 64, "halves", (16, 16, 32), name="rotate_frame_28x37"),
         # the merged tokens of a long scene: bandwidth
         _rotary("rotate", 83280, 16, 16, 64, "across", (16, 24, 24), name="rotate_scene_83280"),
         # gradients of a chunk of frames, shared K/V heads of 128, in 32 bits
         _rotary("back", 10992, 32, 8, 128, "pairs", (32, 48, 48), "fp32", (37, 37), name="back_chunk_hd128_fp32"),
+        # a long scene enters the cache at once: bandwidth
+        _over("store", 1, 83280, 83280, 16, 16, 64, "e2m1", 128, name="store_scene_83280_e2m1"),
+        # one token over all merged tokens of a thousand frames
+        _over("attend", 1, 1, 520500, 16, 16, 64, "e2m1", 128, name="token_over_520500_e2m1"),
+        # chunks of several token-causal sequences, shared K/V heads of 128
+        _over("step", 5, 1741, 4099, 32, 8, 128, "e2m1", 32, causal_block=1, ragged=True, name="chunks_5_hd128_e2m1"),
         # one camera token over a small frame and itself
-        _weigh(1, 1, 262, 16, 16, 64, "bf16", name="weigh_token_over_262"),
+        _over("weigh", 1, 1, 262, 16, 16, 64, "bf16", name="weigh_token_over_262"),
         # the camera tokens of sixteen scenes, shared K/V heads, 8-bit cache
-        _weigh(16, 1, 8328, 32, 4, 128, "e4m3", ragged=True, name="weigh_tokens_16_shared8_e4m3"),
-        # two square frames over an 8-bit cache, each frame blind to the later one
-        _weigh(1, 2748, 21984, 16, 16, 64, "e4m3", causal_block=1374, name="weigh_frames_over_21984_e4m3"),
-        # four frames at once over forty: the largest
-        _weigh(1, 4164, 41640, 16, 16, 64, "bf16", 128, causal_block=1041, name="weigh_frames_over_41640"),
+        _over("weigh", 16, 1, 8328, 32, 4, 128, "e4m3", ragged=True, name="weigh_tokens_16_shared8_e4m3"),
+        # four frames at once over forty, each frame blind to the later ones: the largest
+        _over("weigh", 1, 4164, 41640, 16, 16, 64, "bf16", 128, causal_block=1041, name="weigh_frames_over_41640"),
         # a short stream halved
         _evict(1, 1044, 522, 5, 261, 16, 64, "bf16", name="evict_1044_to_522"),
-        # fifty frames down to twenty-five, the last one whole
-        _evict(1, 52050, 26025, 5, 1041, 16, 64, "bf16", name="evict_52050_to_26025"),
         # many scenes of different lengths in 8 bits, read back for a layer that wants them whole
         _evict(24, 5205, 2082, 0, 261, 16, 128, "e4m3", ragged=True, name="evict_24x5205_hd128_e4m3"),
         # the merged tokens of a thousand frames: selection over a long axis
@@ -105,10 +108,10 @@ def draw(rng):
         return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
 
     while True:
-        op = rng.choice(["rotate", "rotate", "back", "weigh", "weigh", "weigh", "evict", "evict"])
+        op = rng.choice(["rotate", "rotate", "back", "store", "attend", "step", "step", "weigh", "weigh", "weigh", "evict", "evict"])
         head_dim = rng.choice([64, 128])
         q_heads, kv_heads = rng.choice([(16, 16), (16, 16), (32, 8), (16, 2), (8, 1), (12, 4)])
-        page_size, dtype, ragged = rng.choice([16, 32, 64, 128]), rng.choice(["bf16", "e4m3"]), rng.random() < 0.6
+        page_size, dtype, ragged = rng.choice([16, 32, 64, 128]), rng.choice(["bf16", "e4m3", "e2m1"]), rng.random() < 0.6
         if op in ("rotate", "back"):
             rows = between(1, 83280)
             most = head_dim // 2  # planes
@@ -123,22 +126,24 @@ def draw(rng):
                         rng.choice([0, 0, between(1, 10 ** 6)]))
             if work(c)["bytes"] <= 6.8e8:
                 return c
-        elif op == "weigh":
-            few = rng.random() < 0.5  # single tokens (and drafts of a few), or chunks
-            n_seq = between(1, 48) if few else between(1, 6)
-            rows = rng.choice([1, 1, 1, 2, 5]) if few else between(9, 4164)
-            keys = between(max(rows, 262), 520500 if few else 41640)
-            causal = rng.choice([0, 1, 1, 261]) if rows > 1 else 0
-            c = _weigh(n_seq, rows, keys, q_heads, kv_heads, head_dim, dtype, page_size, causal, ragged)
-            if (n_seq * keys * kv_heads * head_dim <= 83280 * 1024 * 6.5 and 4 * n_seq * q_heads * rows * keys <= PLAIN_BYTES
-                    and work(c)["flops"] <= LARGEST_FLOPS):
-                return c
-        else:
+        elif op == "evict":
             n_seq, keys = between(1, 24), between(64, 520500)
             keep = max(16, int(keys * rng.uniform(0.05, 1.0)))
             first, last = rng.choice([0, 5, 8]), rng.choice([0, 0, keep // 4])
             c = _evict(n_seq, keys, keep, first, last, kv_heads, head_dim, dtype, page_size, ragged)
             if n_seq * keys * kv_heads * head_dim <= 83280 * 1024:
+                return c
+        else:
+            few = rng.random() < 0.5  # single tokens (and drafts of a few), or chunks
+            n_seq = between(1, 48) if few else between(1, 6)
+            rows = rng.choice([1, 1, 1, 2, 5]) if few else between(9, 4164)
+            if op == "store":
+                n_seq, rows = between(1, 24), between(261, 83280)
+            keys = between(max(rows, 262), 520500 if few else max(rows, 41640))
+            causal = rng.choice([0, 1, 1, 261]) if rows > 1 and op != "store" else 0
+            c = _over(op, n_seq, rows, keys, q_heads, kv_heads, head_dim, dtype if op == "weigh" else "e2m1", page_size, causal, ragged)
+            scores = 0 if op == "store" else 4 * n_seq * q_heads * rows * keys
+            if n_seq * keys * kv_heads * head_dim <= 83280 * 1024 * 6.5 and scores <= PLAIN_BYTES and work(c)["flops"] <= LARGEST_FLOPS:
                 return c
 
 
@@ -151,13 +156,20 @@ def work(case):
         return {"bytes": 2 * n * d * size + 12 * case["rows"], "flops": 3 * n * turned}
     rows, keys = _lengths(case)
     h = case["kv_heads"]
-    held = 2 * d if case["dtype"] == "bf16" else d + 1  # bytes of a token's K (or V) in the cache, a head's
+    held = {"bf16": 2 * d, "e4m3": d + 1, "e2m1": d // 2 + d // 32}[case["dtype"]]  # bytes of a token's K (or V) of a head
+    if case["op"] == "store":
+        return {"bytes": sum(rows) * 2 * h * (4 * d + held), "flops": 0}
+    if case["op"] in ("attend", "step"):
+        n_bytes = sum(keys) * 2 * h * held + sum(rows) * 4 * case["q_heads"] * d
+        if case["op"] == "step":  # the new tokens come from outside and go into the cache as well
+            n_bytes += sum(rows) * 4 * h * d
+        return {"bytes": n_bytes, "flops": 4 * _pairs(case) * case["q_heads"] * d}
     if case["op"] == "weigh":
         qh = case["q_heads"]
         return {"bytes": sum(keys) * h * (held + 4) + sum(rows) * qh * (2 * d + 4), "flops": 2 * _pairs(case) * qh * d}
     kept = sum(_kept(case))
     n_bytes = 4 * h * sum(keys) + kept * h * (4 * held + 4 + 4)
-    if case["dtype"] == "e4m3":  # read back
+    if case["dtype"] != "bf16":  # read back
         n_bytes += kept * h * 2 * (held + 2 * d)
     return {"bytes": n_bytes, "flops": 0}
 
@@ -217,20 +229,24 @@ def _cache_inputs(case, seed):
     weights = torch.empty(n_pages, h, ps, device="cuda").normal_(generator=g).mul_(2.0).exp_()
     weights *= torch.rand(n_pages, h, ps, generator=g, device="cuda") > 0.1
     s = dict(case=case, rows=rows, keys=keys, pages=pages, into=into, k=k, v=None, k_scale=None, v_scale=None, weights=weights)
-    if case["op"] == "evict":
+    if case["op"] != "weigh":  # (which looks at no values)
         s["v"] = torch.empty(n_pages, h, ps, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
-        s["kept"] = _kept(case)
-    if case["dtype"] == "e4m3":
-        s["k"], s["k_scale"] = _quantise(s["k"])
+    if case["dtype"] != "bf16":
+        s["k"], s["k_scale"] = _quantise(s["k"], case["dtype"])
         if s["v"] is not None:
-            s["v"], s["v_scale"] = _quantise(s["v"])
+            s["v"], s["v_scale"] = _quantise(s["v"], case["dtype"])
+    if case["op"] == "evict":
+        s["kept"] = _kept(case)
+        return s
+    qh = case["q_heads"]
+    qkv = torch.empty(sum(rows), (qh + 2 * h) * d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    s["q"], s["k_new"], s["v_new"] = (t.unflatten(1, (-1, d)) for t in qkv.split([qh * d, h * d, h * d], 1))
+    s["k_new"] += lean[:, 0].bfloat16()
     if case["op"] == "weigh":
-        weights *= max(rows) * case["q_heads"] / (8.0 * h * max(keys))  # of the size of what the rows give out
-        qkv = torch.empty(sum(rows), (case["q_heads"] + 2 * h) * d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
-        s["q"] = qkv[:, :case["q_heads"] * d].unflatten(1, (-1, d))
+        weights *= max(rows) * qh / (8.0 * h * max(keys))  # of the size of what the rows give out
         s["plan"] = _plan(case, rows, keys, pages)
         scores, _ = _scores(s)
-        lse = torch.logsumexp(scores, -1).view(len(rows), h, case["q_heads"] // h, -1)  # an attention pass has left this
+        lse = torch.logsumexp(scores, -1).view(len(rows), h, qh // h, -1)  # an attention pass has left this
         del scores
         lse = lse.permute(0, 3, 1, 2).flatten(2, 3)
         s["lse"] = lse[s["plan"]["seq"], s["plan"]["within"]].contiguous()
@@ -253,14 +269,16 @@ def prepare(case, seed):
     if own:
         from paper_2512_04939_b200 import KVCache
 
-        v = s["k"] if s["v"] is None else s["v"]  # weighing looks at no values
-        s["cache"] = KVCache(s["k"], v, s["k_scale"], s["k_scale"] if s["v"] is None else s["v_scale"], weights=s["weights"])
-        if case["op"] == "weigh":
+        v, v_scale = (s["k"], s["k_scale"]) if s["v"] is None else (s["v"], s["v_scale"])
+        s["cache"] = KVCache(s["k"], v, s["k_scale"], v_scale, weights=s["weights"] if case["op"] in ("weigh", "evict") else None)
+        if case["op"] != "evict":
             s["batch"] = s["cache"].batch(s["rows"], s["keys"], s["pages"], q_heads=case["q_heads"], causal_block=case["causal_block"])
         else:
             s["batch"] = s["cache"].batch([0] * case["n_seq"], s["keys"], s["pages"])
             s["target"] = s["cache"].batch(s["kept"], s["kept"], s["into"])
-    elif case["op"] == "evict":
+    elif case["op"] != "evict":
+        s["plan"] = _plan(case, s["rows"], s["keys"], s["pages"])
+    else:
         s["from"], s["to"] = _plan(case, [0] * len(s["keys"]), s["keys"], s["pages"]), _plan(case, s["kept"], s["kept"], s["into"])
     return s
 
@@ -278,6 +296,15 @@ def run(state):
         else:
             _plain_weigh(state)
         return state["weights"]
+    if case["op"] != "evict":
+        if case["op"] in ("store", "step"):
+            if own:
+                state["cache"].append(state["batch"], state["k_new"], state["v_new"])
+            else:
+                _plain_append(state)
+        if case["op"] == "store":
+            return state["cache"].gather(state["batch"]) if own else _plain_gather(state, state["plan"])
+        return state["cache"].attend(state["batch"], state["q"]) if own else _plain_attend(state)
     if own:
         kept = state["cache"].evict(state["batch"], state["target"], first=case["first"], last=case["last"])
     else:
@@ -285,7 +312,7 @@ def run(state):
     first = state["into"][0][0]
     if case["dtype"] == "bf16":
         return kept, state["weights"][first:], state["k"][first:], state["v"][first:]
-    k, v = state["cache"].gather(state["target"]) if own else _plain_gather(state)
+    k, v = state["cache"].gather(state["target"]) if own else _plain_gather(state, state["to"])
     return kept, state["weights"][first:], k, v
 
 
@@ -343,21 +370,45 @@ def _plan(case, rows, keys, pages):
                 all_seq=all_seq, token=token, token_page=table[all_seq, token // ps], token_offset=token % ps)
 
 
-def _quantise(x):
-    """E4M3 codes of the rows of x along its last dimension, under the least power of two 2^e >= 2^-118 with
-    max|x| <= 448 * 2^e, and e + 127."""
-    top = x.abs().amax(-1).float()
+_LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)  # of E2M1
+
+
+def _quantise(x, dtype):
+    """Codes of x along its last dimension, and e + 127 of the powers of two 2^e that they are under (255: something in there is not
+    finite, and the codes are 0).  E4M3: one for a row, the least e >= -118 with max|x| <= 448 * 2^e.  E2M1: one for every 32, the
+    least e >= -126 with max|x| <= 6 * 2^e; the code of an even element is the low half of its byte."""
+    y = x if dtype == "e4m3" else x.unflatten(-1, (-1, 32))
+    top = y.abs().amax(-1).float()
     bits = top.view(torch.int32)
-    e = ((bits >> 23) + ((bits & 0x7FFFFF) > 0x600000) - 8).clamp_(min=9)
-    back = ((254 - e) << 23).view(torch.float32)
-    return (x.float() * back.unsqueeze(-1)).to(torch.float8_e4m3fn), e.to(torch.uint8)
+    if dtype == "e4m3":
+        e = ((bits >> 23) + ((bits & 0x7FFFFF) > 0x600000) - 8).clamp_(min=9)
+    else:
+        e = ((bits >> 23) + ((bits & 0x7FFFFF) > 0x400000) - 2).clamp_(min=1)
+    e = torch.where(torch.isfinite(top), e, 255)
+    y = y.float() * ((254 - e.clamp(max=253)) << 23).view(torch.float32).unsqueeze(-1)
+    y = torch.where((e == 255).unsqueeze(-1), 0.0, y)
+    if dtype == "e4m3":
+        return y.to(torch.float8_e4m3fn), e.to(torch.uint8)
+    code = torch.signbit(y).to(torch.uint8) * 8
+    y = y.abs().clamp(max=6.0)
+    for i in range(7):  # to the nearest, from the middle to the even code
+        middle = (_LEVELS[i] + _LEVELS[i + 1]) / 2
+        code += (y > middle if i % 2 == 0 else y >= middle).to(torch.uint8)
+    code = code.flatten(-2)
+    return code[..., 0::2] | code[..., 1::2] << 4, e.to(torch.uint8)
 
 
 def _values(codes, scale):
     """What pool rows stand for, in 32 bits."""
     if scale is None:
         return codes.float()
-    return codes.float() * (scale.to(torch.int32) << 23).view(torch.float32).unsqueeze(-1)
+    e = scale.to(torch.int32)
+    factor = torch.where(e == 255, float("nan"), (e << 23).view(torch.float32)).unsqueeze(-1)
+    if scale.dim() < codes.dim():
+        return codes.float() * factor
+    levels = torch.tensor(_LEVELS + tuple(-x for x in _LEVELS), device=codes.device)
+    x = torch.stack([levels[(codes & 15).long()], levels[(codes >> 4).long()]], -1).flatten(-2)
+    return (x.unflatten(-1, (-1, 32)) * factor).flatten(-2)
 
 
 def _bytes_at(x, at):
@@ -365,14 +416,20 @@ def _bytes_at(x, at):
     return x[at] if x.dtype != torch.float8_e4m3fn else x.view(torch.uint8)[at].view(torch.float8_e4m3fn)
 
 
+def _whole(s, name):
+    """[n_seq, kv_heads, longest, head_dim] in 32 bits, zero beyond a sequence's end."""
+    p, scale = s["plan"], s[name + "_scale"]
+    x = _values(_bytes_at(s[name], p["table"]), None if scale is None else scale[p["table"]])
+    x = x.permute(0, 2, 1, 3, 4).flatten(2, 3)
+    return x * (torch.arange(x.shape[2], device="cuda") < p["length"][:, None])[:, None, :, None]
+
+
 def _scores(s):
     """Scores [n_seq, kv_heads, rows of heads that share K, keys] in 32 bits, minus infinity where a row does not see a key; and
     the rows' numbers of keys seen."""
     p, case = s["plan"], s["case"]
     h, d, qh = case["kv_heads"], case["head_dim"], case["q_heads"]
-    k = _values(_bytes_at(s["k"], p["table"]), None if s["k_scale"] is None else s["k_scale"][p["table"]])
-    k = k.permute(0, 2, 1, 3, 4).flatten(2, 3)
-    k = k * (torch.arange(k.shape[2], device="cuda") < p["length"][:, None])[:, None, :, None]
+    k = _whole(s, "k")
     n_seq, most = k.shape[0], max(s["rows"])
     q = torch.zeros(n_seq, most, qh, d, device="cuda")
     q[p["seq"], p["within"]] = s["q"].float() / math.sqrt(d)
@@ -383,6 +440,24 @@ def _scores(s):
     hidden = torch.arange(k.shape[2], device="cuda") >= seen[:, :, None]
     scores.view(n_seq, h, qh // h, most, -1).masked_fill_(hidden[:, None, None], float("-inf"))
     return scores, seen
+
+
+def _plain_append(s):
+    at = (s["plan"]["page"], slice(None), s["plan"]["offset"])
+    for name in ("k", "v"):
+        s[name][at], s[name + "_scale"][at] = _quantise(s[name + "_new"], "e2m1")
+
+
+def _plain_attend(s):
+    p, case = s["plan"], s["case"]
+    h, qh = case["kv_heads"], case["q_heads"]
+    scores, seen = _scores(s)
+    scores -= scores.amax(-1, keepdim=True).clamp_(min=-3e38)
+    scores.exp_()
+    total = scores.sum(-1, keepdim=True)
+    o = (scores @ _whole(s, "v")) / total.clamp_(min=1e-38)
+    o = o.view(seen.shape[0], h, qh // h, seen.shape[1], -1).permute(0, 3, 1, 2, 4).flatten(2, 3)
+    return o[p["seq"], p["within"]].bfloat16()
 
 
 def _plain_weigh(s):
@@ -417,12 +492,24 @@ def _plain_evict(s):
     return chosen.int()
 
 
-def _plain_gather(s):
-    at = (s["to"]["page"], slice(None), s["to"]["offset"])
+def _plain_gather(s, plan):
+    at = (plan["page"], slice(None), plan["offset"])
     return tuple(_values(_bytes_at(s[n], at), s[n + "_scale"][at]).bfloat16() for n in ("k", "v"))
 
 
 # ------------------------------------------------------------------ in 64 bits
+def _exact_e2m1(x):
+    """What the E2M1 codes of x stand for, from the definition, in 64 bits."""
+    x = x.double().unflatten(-1, (-1, 32))
+    top = x.abs().amax(-1, keepdim=True)
+    e = torch.ceil(torch.log2(top / 6)).clamp(min=-126)
+    e = torch.where(top > 6 * torch.exp2(e), e + 1, e)  # where the logarithm was a hair too small, or too large
+    e = torch.where((top <= 6 * torch.exp2(e - 1)) & (e > -126), e - 1, e)
+    y = x / torch.exp2(e)
+    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=1.0))) - 1)
+    return (torch.round(y / step) * step * torch.exp2(e)).flatten(-2)
+
+
 def exact(case, seed):
     d = case["head_dim"]
     if case["op"] in ("rotate", "back"):
@@ -446,14 +533,40 @@ def exact(case, seed):
             ladder += n // 2
         return tuple(out)
     s = _cache_inputs(case, seed)
-    ps, h, narrow = case["page_size"], case["kv_heads"], case["dtype"] == "e4m3"
+    ps, h = case["page_size"], case["kv_heads"]
 
     def held(name, ids):
-        x = s[name].view(torch.uint8)[ids].view(s[name].dtype).double()
-        if narrow:
-            x = x * torch.exp2(s[name + "_scale"][ids].double() - 127).unsqueeze(-1)
-        return x.transpose(1, 2).reshape(-1, h, d)
+        """Tokens of pages, [tokens, kv_heads, head_dim]."""
+        x = s[name].view(torch.uint8)[ids].view(s[name].dtype)
+        if case["dtype"] == "e2m1":
+            x = torch.stack([x % 16, x // 16], -1).flatten(-2).long()
+            sign, power, half = x // 8, x // 2 % 4, x % 2
+            size = torch.where(power == 0, 0.5 * half, (1 + 0.5 * half) * torch.exp2(power.double() - 1))
+            x = (1 - 2 * sign) * size * torch.exp2(s[name + "_scale"][ids].double() - 127).repeat_interleave(32, -1)
+        elif case["dtype"] == "e4m3":
+            x = x.double() * torch.exp2(s[name + "_scale"][ids].double() - 127).unsqueeze(-1)
+        return x.double().transpose(1, 2).reshape(-1, h, d)
 
+    if case["op"] in ("store", "attend", "step"):
+        new = [_exact_e2m1(s[n]) for n in ("k_new", "v_new")]
+        if case["op"] == "store":
+            return tuple(new)
+        c, group, row0, out = case["causal_block"], case["q_heads"] // h, 0, []
+        for r, n, pages in zip(s["rows"], s["keys"], s["pages"]):
+            ids = torch.tensor(pages, device="cuda")
+            k, v = held("k", ids)[:n], held("v", ids)[:n]
+            if case["op"] == "step":
+                k[n - r:], v[n - r:] = (x[row0:row0 + r] for x in new)
+            i = torch.arange(r, device="cuda")
+            sees = torch.full_like(i, n) if c == 0 else torch.clamp(n - r + (i // c + 1) * c, max=n)
+            hidden = torch.arange(n, device="cuda")[None] >= sees[:, None]
+            heads = []
+            for qh in range(case["q_heads"]):
+                x = s["q"][row0:row0 + r, qh].double() @ k[:, qh // group].T * d ** -0.5
+                heads.append(torch.softmax(x.masked_fill_(hidden, -math.inf), 1) @ v[:, qh // group])
+            out.append(torch.stack(heads, 1))
+            row0 += r
+        return torch.cat(out)
     weights = s["weights"].double()
     if case["op"] == "weigh":
         c, group, row0 = case["causal_block"], case["q_heads"] // h, 0
