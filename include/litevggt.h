@@ -395,6 +395,46 @@ litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_b
 litevggt_status litevggt_kv_poll(litevggt_kv_cache* cache, void* stream);
 litevggt_status litevggt_kv_launch_count(const litevggt_kv_cache* cache, int64_t* launches);
 
+/* ------------------------------------------------------------------ rotary positions of several axes
+ * Queries and keys of rows that stand somewhere in time, height and width, as those of an image or of frames that keep arriving
+ * (VGGT's aggregator turns them by height and width, litevggt_attn_ext).  Axis a turns sections[a] channels of every head, in planes
+ * of two:  y_a = x_a cos t - x_b sin t,  y_b = x_a sin t + x_b cos t,  t = position * bases[a]^(-i / n) for the i-th of n planes.
+ *   HALVES  each axis has its sections[a] channels side by side, and n = sections[a] / 2; channel i of them turns with channel n + i
+ *   PAIRS   the same, but channel 2 i turns with channel 2 i + 1
+ *   ACROSS  one ladder of n = (sum of sections) / 2 planes over the head, channel i with channel n + i; the first sections[0] / 2
+ *           planes are axis 0's, the next sections[1] / 2 axis 1's, and so on
+ * Channels behind the sections stay as they are, bit for bit.  Angles are exact to 2^-32 of a turn whatever the position; the rest is in
+ * 32 bits with one rounding at the end.  A value that is not finite makes its plane's two not finite. */
+enum { LITEVGGT_BF16 = 0, LITEVGGT_FP16 = 1, LITEVGGT_FP32 = 2 };
+enum { LITEVGGT_ROTARY_HALVES = 0, LITEVGGT_ROTARY_PAIRS = 1, LITEVGGT_ROTARY_ACROSS = 2 };
+typedef struct {
+  int32_t head_dim;    /* 2 to 256 */
+  int32_t n_axes;      /* 1 to 4 */
+  int32_t sections[4]; /* channels of each axis, even, together 2 to head_dim */
+  double bases[4];     /* greater than 1, less than 1e300 */
+  int32_t layout;
+} litevggt_rotary_config;
+/* Rows of heads: element (row, head, channel) lies at row * row_stride + head * head_stride + channel, strides in elements, not
+ * negative, less than 2^40. */
+typedef struct {
+  const void* in;
+  int64_t in_row_stride, in_head_stride;
+  void* out;           /* may be `in` with the same strides; otherwise no output may reach into an input or another output */
+  int64_t out_row_stride, out_head_stride;
+  int32_t heads;       /* 1 to 65,536 */
+} litevggt_rotary_tensor;
+typedef struct litevggt_rotary litevggt_rotary; /* immutable: one serves calls on any streams, at once too */
+
+litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int device, litevggt_rotary** out);
+litevggt_status litevggt_rotary_destroy(litevggt_rotary* rotary);
+/* Turns one or two tensors of the same rows and type (queries and keys) in one launch.  positions: dev int32, element (axis, row) at
+ * axis * axis_stride + row * row_stride, of any sign.  back != 0: by the negative angles, which is the gradient (from the gradient of the
+ * output to that of the input).  Accesses are as wide as addresses, strides and sections allow, 16 bytes at most; elements must be
+ * aligned to their size (LITEVGGT_ERR_ALIGN). */
+litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32_t* positions, int64_t axis_stride, int64_t row_stride,
+                                      int64_t rows, int32_t dtype, int32_t back, const litevggt_rotary_tensor* tensors, int32_t n_tensors,
+                                      void* stream);
+
 const char* litevggt_status_string(litevggt_status s);
 
 #ifdef __cplusplus

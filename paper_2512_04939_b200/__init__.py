@@ -19,4 +19,5 @@ from .binding import (  # noqa: F401
     load_library,
 )
 from .kv_cache import KVBatch, KVCache  # noqa: E402,F401
+from .rotary import RotaryAxes  # noqa: E402,F401
 from .streaming import StreamingGlobalAttention  # noqa: E402,F401

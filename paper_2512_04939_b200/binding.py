@@ -51,6 +51,17 @@ class KVConfig(C.Structure):
                 ("dtype", C.c_int32)]
 
 
+class RotaryConfig(C.Structure):
+    """Mirror of litevggt_rotary_config."""
+    _fields_ = [("head_dim", C.c_int32), ("n_axes", C.c_int32), ("sections", C.c_int32 * 4), ("bases", C.c_double * 4), ("layout", C.c_int32)]
+
+
+class RotaryTensor(C.Structure):
+    """Mirror of litevggt_rotary_tensor."""
+    _fields_ = [("src", C.c_void_p), ("in_row", C.c_int64), ("in_head", C.c_int64), ("dst", C.c_void_p), ("out_row", C.c_int64),
+                ("out_head", C.c_int64), ("heads", C.c_int32)]
+
+
 def load_library():
     """Load liblitevggt.so (once).  Raises if it has not been built: there is no fallback."""
     global _LIB
@@ -103,6 +114,9 @@ def load_library():
         "litevggt_kv_attend": [vp, vp, vp, i64, i64, C.c_float, vp, vp],
         "litevggt_kv_poll": [vp, vp],
         "litevggt_kv_launch_count": [vp, P(i64)],
+        "litevggt_rotary_create": [P(RotaryConfig), C.c_int, P(vp)],
+        "litevggt_rotary_destroy": [vp],
+        "litevggt_rotary_apply": [vp, vp, i64, i64, i64, i32, i32, P(RotaryTensor), i32, vp],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)

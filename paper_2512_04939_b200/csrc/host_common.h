@@ -18,6 +18,25 @@ struct DeviceGuard {
   }
 };
 
+// DeviceGuard for calls whose launch is most of their time: nothing is set where the device is the current one already.  Every call
+// that is given a stream needs one: the handles of default streams mean the current device's.
+struct OnDevice {
+  int prev = -1;
+  bool ok = false;
+  explicit OnDevice(int device) {
+    if (cudaGetDevice(&prev) != cudaSuccess) return;
+    if (prev == device) {
+      prev = -1;
+      ok = true;
+    } else {
+      ok = cudaSetDevice(device) == cudaSuccess;
+    }
+  }
+  ~OnDevice() {
+    if (prev >= 0) cudaSetDevice(prev);
+  }
+};
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool ctx_ok(const litevggt_ctx* c) { return c != nullptr && c->magic == kCtxMagic; }
 inline bool plan_ok(const litevggt_plan* p) { return p != nullptr && p->magic == kPlanMagic; }

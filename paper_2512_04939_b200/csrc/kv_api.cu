@@ -9,25 +9,6 @@ namespace lv {
 
 namespace {
 
-// DeviceGuard for calls whose launch is most of their time: nothing is set where the device is the current one already.  Every call
-// that is given a stream needs one: the handles of default streams mean the current device's.
-struct OnDevice {
-  int prev = -1;
-  bool ok = false;
-  explicit OnDevice(int device) {
-    if (cudaGetDevice(&prev) != cudaSuccess) return;
-    if (prev == device) {
-      prev = -1;
-      ok = true;
-    } else {
-      ok = cudaSetDevice(device) == cudaSuccess;
-    }
-  }
-  ~OnDevice() {
-    if (prev >= 0) cudaSetDevice(prev);
-  }
-};
-
 bool cache_ok(const litevggt_kv_cache* c) { return c != nullptr && c->magic == kKvCacheMagic; }
 bool batch_ok(const litevggt_kv_batch* b) { return b != nullptr && b->magic == kKvBatchMagic; }
 

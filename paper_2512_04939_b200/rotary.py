@@ -1,0 +1,93 @@
+"""Queries and keys turned by their positions along several axes: time, height and width of a token of a video.
+
+    rotary = RotaryAxes(64, sections=(16, 24, 24), bases=(10000.0, 100.0, 100.0))
+    q, k = rotary.rotate(positions, q, k)              # positions int32 [3, rows]; q, k [rows, heads, 64], slices of a projection will do
+    grad_q, grad_k = rotary.rotate_back(positions, grad_q, grad_k)   # the gradient
+
+Shapes, types and devices are checked here, everything else in the C library.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from .binding import RotaryConfig, RotaryTensor, _check, load_library
+
+_LAYOUTS = {"halves": 0, "pairs": 1, "across": 2}
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class RotaryAxes:
+    """Axis a turns ``sections[a]`` channels of a head (even numbers, together at most ``head_dim``; what lies behind them stays) by
+    position * bases[a]^(-i / n) in the i-th of its n planes.  ``layout``: which channels make a plane - ``halves`` of the axis's own
+    section, neighbouring ``pairs``, or halves ``across`` all sections, with one ladder of frequencies for all axes."""
+
+    def __init__(self, head_dim: int, sections, bases, layout: str = "halves", device: int = 0):
+        sections, bases = tuple(sections), tuple(bases)
+        if layout not in _LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}, got {layout!r}")
+        if not 1 <= len(sections) <= 4 or len(bases) != len(sections):
+            raise ValueError(f"one to four axes with a section and a base each, got {sections} and {bases}")
+        if any(int(n) != n or not 0 <= n < 2 ** 31 for n in (head_dim, *sections)):
+            raise ValueError(f"head_dim and sections must be whole numbers, got {head_dim} and {sections}")
+        self.lib = load_library()
+        self.head_dim, self.sections, self.bases, self.layout = int(head_dim), tuple(int(n) for n in sections), bases, layout
+        self.device = torch.device("cuda", device)
+        self._index = device
+        n = len(sections)
+        cfg = RotaryConfig(self.head_dim, n, (C.c_int32 * 4)(*self.sections), (C.c_double * 4)(*bases), _LAYOUTS[layout])
+        self.handle = C.c_void_p()
+        _check(self.lib.litevggt_rotary_create(C.byref(cfg), device, C.byref(self.handle)), "rotary_create")
+        self._apply = self.lib.litevggt_rotary_apply
+
+    def close(self):
+        if getattr(self, "handle", None) is not None and self.handle.value:
+            self.lib.litevggt_rotary_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def rotate(self, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor | None = None, out=None):
+        """``q`` (and ``k``) turned: [rows, heads, head_dim], bfloat16, float16 or float32, the head's channels contiguous, by ``positions``
+        int32 [axes, rows].  New tensors, or those of ``out`` (one, or a pair beside a ``k``), which may be the inputs themselves."""
+        return self._turn(positions, q, k, out, 0)
+
+    def rotate_back(self, positions: torch.Tensor, q: torch.Tensor, k: torch.Tensor | None = None, out=None):
+        """The reverse, and the gradient of :meth:`rotate`: from the gradients of its outputs to those of its inputs."""
+        return self._turn(positions, q, k, out, 1)
+
+    def _turn(self, positions, q, k, out, back):
+        given = [q] if k is None else [q, k]
+        if out is None:
+            outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in given]
+        else:
+            outs = [out] if k is None else list(out)
+            if len(outs) != len(given):
+                raise ValueError(f"out must hold {len(given)} tensors, got {len(outs)}")
+        rows = q.shape[0] if q.dim() == 3 else -1
+        if positions.shape != (len(self.sections), rows) or positions.dtype != torch.int32 or positions.get_device() != self._index:
+            raise ValueError(f"positions must be int32 [{len(self.sections)}, {rows}] on {self.device}, got {positions.dtype} "
+                             f"{tuple(positions.shape)} on {positions.device}")
+        tensors = (RotaryTensor * len(given))()
+        for name, t, o, made in zip(("q", "k"), given, outs, tensors):
+            if t.dim() != 3 or t.shape[0] != rows or t.shape[1] < 1 or t.shape[2] != self.head_dim or o.shape != t.shape:
+                raise ValueError(f"{name} and its output must be [{rows}, heads, {self.head_dim}], got {tuple(t.shape)} and {tuple(o.shape)}")
+            if t.dtype not in _DTYPES or t.dtype != q.dtype or o.dtype != q.dtype:
+                raise ValueError(f"q, k and their outputs must be of one type, bfloat16, float16 or float32, got {t.dtype} and {o.dtype} for {name}")
+            if t.get_device() != self._index or o.get_device() != self._index:
+                raise ValueError(f"{name} and its output must be on {self.device}, got {t.device} and {o.device}")
+            if (t.stride(2) != 1 or o.stride(2) != 1) and self.head_dim > 1:
+                raise ValueError(f"{name}'s channels must be contiguous, got strides {t.stride()} and {o.stride()}")
+            made.src, made.in_row, made.in_head = t.data_ptr(), t.stride(0), t.stride(1)
+            made.dst, made.out_row, made.out_head = o.data_ptr(), o.stride(0), o.stride(1)
+            made.heads = t.shape[1]
+        code = self._apply(self.handle, positions.data_ptr(), positions.stride(0), positions.stride(1), rows, _DTYPES[q.dtype], back,
+                           tensors, len(given), torch._C._cuda_getCurrentRawStream(self._index))
+        if code:
+            _check(code, "rotary_apply")
+        return outs[0] if k is None else tuple(outs)
