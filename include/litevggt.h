@@ -341,22 +341,26 @@ litevggt_status litevggt_launch_count(const litevggt_ctx* ctx, int64_t* launches
  * call on it in a step, and another cache refuses them (LITEVGGT_ERR_STALE_PLAN), its pool being another. */
 enum {
   LITEVGGT_KV_BF16 = 0,
-  LITEVGGT_KV_E4M3 = 1 /* a row of a head as E4M3 codes x and an exponent byte e + 127, standing for x 2^e: the least
-                          e >= -118 with max|row| <= 448 * 2^e; a row that is not finite is held as byte 255 beside
-                          codes of zero, and reads as NaN.  Pools that the caller fills keep to it: e <= 120, no codes of NaN */
+  LITEVGGT_KV_E4M3 = 1, /* a row of a head as E4M3 codes x and an exponent byte e + 127, standing for x 2^e: the least
+                           e >= -118 with max|row| <= 448 * 2^e; a row that is not finite is held as byte 255 beside
+                           codes of zero, and reads as NaN.  Pools that the caller fills keep to it: e <= 120, no codes of NaN */
+  LITEVGGT_KV_E2M1 = 2  /* 4 bits: E2M1 codes x, two to a byte (an even channel's in the low half), and an exponent byte e + 127 for
+                           every 32 channels, standing for x 2^e: the least e >= -126 with max|block| <= 6 * 2^e; a block that is not
+                           finite is held as byte 255 beside codes of zero, and reads as NaN.  Elements of 3.5 * 2^126 and more read as
+                           infinite.  4.25 bits an element.  Pools that the caller fills: bytes 1 to 253, and 255 beside zeros */
 };
 typedef struct {
   int32_t pages;     /* in the pool */
   int32_t page_size; /* tokens of a page: 16, 32, 64 or 128 */
   int32_t kv_heads;
   int32_t head_dim;  /* 64 or 128 */
-  int32_t dtype;     /* LITEVGGT_KV_BF16, LITEVGGT_KV_E4M3 */
+  int32_t dtype;     /* LITEVGGT_KV_BF16, LITEVGGT_KV_E4M3, LITEVGGT_KV_E2M1 */
 } litevggt_kv_config;  /* pages * kv_heads * page_size < 2^31 */
 typedef struct litevggt_kv_cache litevggt_kv_cache;
 typedef struct litevggt_kv_batch litevggt_kv_batch;
 
-/* A cache over the caller's pool.  k, v: dev [pages, kv_heads, page_size, head_dim], bf16 or codes; k_exp, v_exp: dev bytes
- * [pages, kv_heads, page_size], E4M3 only; status: dev, one 32-bit word that holds zero.  All of it outlives the cache,
+/* A cache over the caller's pool.  k, v: dev [pages, kv_heads, page_size, head_dim], bf16 or codes (E2M1: bytes [.., head_dim / 2]);
+ * k_exp, v_exp: dev bytes [pages, kv_heads, page_size], E4M3, or [pages, kv_heads, page_size, head_dim / 32], E2M1; status: dev, one 32-bit word that holds zero.  All of it outlives the cache,
  * pages need not be initialised. */
 litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, void* k, void* v, uint8_t* k_exp, uint8_t* v_exp,
                                    uint32_t* status, litevggt_kv_cache** out);

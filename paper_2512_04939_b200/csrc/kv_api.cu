@@ -104,7 +104,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
     else if (r > 0) few.push_back(i), most = std::max(most, (int)r);
   }
   b->few_rows = most;
-  const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype == LITEVGGT_KV_E4M3);
+  const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype != LITEVGGT_KV_BF16);
   b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
                   KvCut{kKvFewRows, kKvFewUnit, std::min(c->num_sms * per_sm, kKvFewWorkers), kKvFewLeast, INT32_MAX, kKvFewPiece});
   // In units of 128 keys against 256 rows.  CTAs of one row tile take more time for the same work, but there are twice as many:
@@ -138,12 +138,12 @@ litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, vo
   *out = nullptr;
   if (cfg->head_dim != 64 && cfg->head_dim != 128) return LITEVGGT_ERR_BAD_CONFIG;
   if (cfg->page_size != 16 && cfg->page_size != 32 && cfg->page_size != 64 && cfg->page_size != 128) return LITEVGGT_ERR_BAD_CONFIG;
-  if (cfg->dtype != LITEVGGT_KV_BF16 && cfg->dtype != LITEVGGT_KV_E4M3) return LITEVGGT_ERR_BAD_CONFIG;
+  if (cfg->dtype != LITEVGGT_KV_BF16 && cfg->dtype != LITEVGGT_KV_E4M3 && cfg->dtype != LITEVGGT_KV_E2M1) return LITEVGGT_ERR_BAD_CONFIG;
   if (cfg->kv_heads < 1 || cfg->pages < 1) return LITEVGGT_ERR_BAD_CONFIG;
   // a row of a head is addressed by one 32-bit coordinate
   if ((long long)cfg->pages * cfg->kv_heads > INT32_MAX / cfg->page_size) return LITEVGGT_ERR_BAD_CONFIG;
   if (k == nullptr || v == nullptr || status == nullptr) return LITEVGGT_ERR_NULL;
-  const bool narrow = cfg->dtype == LITEVGGT_KV_E4M3;
+  const bool narrow = cfg->dtype != LITEVGGT_KV_BF16;
   if (narrow && (k_exp == nullptr || v_exp == nullptr)) return LITEVGGT_ERR_NULL;
   if (!aligned16(k) || !aligned16(v) || (narrow && (!aligned16(k_exp) || !aligned16(v_exp)))) return LITEVGGT_ERR_ALIGN;
   int count = 0, major = 0, sms = 0;

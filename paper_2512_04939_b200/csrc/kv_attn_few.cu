@@ -98,29 +98,46 @@ constexpr float kFewMostWeight = 32768.0f;
 __device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k + 127) << 23); }
 __device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }
 
-template <int kHd, bool kNarrow, bool kHalf>
+__device__ __forceinline__ uint32_t lds4(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
+  return v;
+}
+
+template <int kHd, int kKind, bool kHalf>
 struct FewShape {
+  static constexpr bool kNarrow = kKind == LITEVGGT_KV_E4M3, kFour = kKind == LITEVGGT_KV_E2M1;
+  using Row = KvRow<kHd, kKind>;
   // Rings of 17 to 25 KB a warp.  Codes of head dim 64 take so much work for a byte that sixteen warps an SM serve them
   // better than eight with more registers (one token over 520,500: 216 us against 241 to 283); those of head dim 128 spill
   // under 128 registers (sixteen tokens that share heads by eight: 36 us against 49).
-  static constexpr int kCtas = kNarrow && kHd == 64 ? 2 : 1;  // per SM
+  static constexpr int kCtas = kKind != LITEVGGT_KV_BF16 && kHd == 64 ? 2 : 1;  // per SM
   static constexpr int kSubs = kNarrow ? 2 : 128 / kHd;       // of 16 keys, of a stage
-  static constexpr int kStages = kNarrow || (kHd == 128 && !kHalf) ? 2 : 3;
+  static constexpr int kStages = kFour ? 4 : kNarrow || (kHd == 128 && !kHalf) ? 2 : 3;
   static constexpr int kRows = kHalf ? 8 : 16;
   static constexpr int kOutTiles = kHd / 8;
-  static constexpr int kSubBytes = 16 * kHd * (kNarrow ? 1 : 2);           // of K or V
-  static constexpr int kStageBytes = 2 * kSubs * kSubBytes + (kNarrow ? 128 : 0);  // [K, V][sub], exponents [K, V][sub] of 16 bytes
+  static constexpr int kSubBytes = 16 * Row::kBytes;  // of K or V
+  static constexpr int kStageBytes = 2 * kSubs * kSubBytes + (Row::kExps > 0 ? 128 : 0);  // [K, V][sub], exponents [K, V][sub] of 16 rows
+  static_assert(2 * kSubs * 16 * Row::kExps <= 128, "");
   static constexpr int kRingBytes = kKvFewWarps * kStages * kStageBytes;
   static constexpr int kMergeBytes = kKvFewWarps * kRows * (kHd + 2) * 4;
-  static constexpr int kSmemBytes = kRingBytes + kMergeBytes + 1024 + 256;
+  static constexpr int kSmemBytes = kRingBytes + kMergeBytes + 1024 + 320;
+  static_assert(kKvFewWarps * kStages * 8 + 8 <= 320, "");
 };
 
 // kHalf: at most eight rows, so the lower half of every row tile is empty and takes no registers.
-template <int kHd, bool kNarrow, bool kHalf>
-__global__ void __launch_bounds__(kKvFewWarps * 32, FewShape<kHd, kNarrow, kHalf>::kCtas)
+template <int kHd, int kKind, bool kHalf>
+__global__ void __launch_bounds__(kKvFewWarps * 32, FewShape<kHd, kKind, kHalf>::kCtas)
 kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, KvPool pool, KvArrays arrays,
                    KvLaunch work, KvAttend at, uint32_t* status) {
-  using Shape = FewShape<kHd, kNarrow, kHalf>;
+  using Shape = FewShape<kHd, kKind, kHalf>;
+  constexpr bool kNarrow = Shape::kNarrow, kFour = Shape::kFour;
+  constexpr int kRowBytes = Shape::Row::kBytes, kExps = Shape::Row::kExps;
   constexpr int kSubs = Shape::kSubs, kStages = Shape::kStages, kStageKeys = 16 * kSubs, kRound = kKvFewWarps * kStageKeys;
   constexpr int kHalves = kHalf ? 1 : 2;
   extern __shared__ uint8_t smem_raw[];
@@ -144,7 +161,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   // ------------------------------------------------------------------ loads
   // The stage that is fetched next, and its piece; a lane's copy is one of K or V of 16 keys (and 64 channels, or the codes or
   // exponents).  Its page is looked up a stage ahead.
-  constexpr int kParts = kNarrow ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts;
+  constexpr int kParts = kExps > 0 ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts;
   const int my_part = lane % kParts, my_x = (lane / kParts) & 1, my_sub = lane / (2 * kParts);
   int f_id = (int)blockIdx.x, f_key = 0, f_end = 0, f_head = 0, f_page0 = 0, f_page = 0, f_next = -1;
   uint32_t fetched = 0;
@@ -172,15 +189,19 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     const uint32_t stage = fetched % kStages;
     uint64_t* bar = &full[stage];
     const int subs = min(kSubs, (f_end - f_key + 15) >> 4);
-    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(subs * (2 * Shape::kSubBytes + (kNarrow ? 32 : 0))));
+    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(subs * (2 * Shape::kSubBytes + 32 * kExps)));
     __syncwarp();
     if (lane < kCopies && my_sub < subs) {
       const int key = f_key + 16 * my_sub;
       const long long row = ((long long)f_page * pool.kv_heads + f_head) * pool.page_size + (key & (pool.page_size - 1));
       const uint32_t base = ring + stage * Shape::kStageBytes;
-      if constexpr (kNarrow) {
-        if (my_part == 0) bulk_load(base + (my_x * kSubs + my_sub) * Shape::kSubBytes, (my_x == 0 ? pool.k : pool.v) + row * kHd, 16 * kHd, bar);
-        else bulk_load(base + 2 * kSubs * Shape::kSubBytes + (my_x * kSubs + my_sub) * 16, (my_x == 0 ? pool.k_exp : pool.v_exp) + row, 16, bar);
+      if constexpr (kExps > 0) {
+        if (my_part == 0) {
+          bulk_load(base + (my_x * kSubs + my_sub) * Shape::kSubBytes, (my_x == 0 ? pool.k : pool.v) + row * kRowBytes, 16 * kRowBytes, bar);
+        } else {
+          bulk_load(base + 2 * kSubs * Shape::kSubBytes + (my_x * kSubs + my_sub) * 16 * kExps, (my_x == 0 ? pool.k_exp : pool.v_exp) + row * kExps,
+                    16 * kExps, bar);
+        }
       } else {
         const uint32_t dst = base + (my_x * kSubs + my_sub) * Shape::kSubBytes + my_part * 2048;
         asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
@@ -213,8 +234,8 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     float row_scale[kHalves];  // of the scores, in base-2 units
 #pragma unroll
     for (int half = 0; half < kHalves; ++half) {
-      // 16 bytes of a K row hold the channels of two contraction steps of 16 (bf16) or of four (codes)
-      constexpr int kRun = kNarrow ? 16 : 8;  // channels of a lane that lie side by side
+      // 16 bytes of a K row hold the channels of two contraction steps of 16 (bf16) or of four (codes); of 4 bits a lane has a quarter row
+      constexpr int kRun = kFour ? kHd / 4 : kNarrow ? 16 : 8;  // channels of a lane that lie side by side
       const int r = g + 8 * half;
       const bool live = r < piece.rows;
       const int at_row = piece.row0 + (live ? r : 0);
@@ -289,6 +310,15 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
               for (int j = 0; j < 4; ++j) step(4 * i + j, widen_low(w[j]), widen_high(w[j]));
+            }
+          } else if constexpr (kFour) {
+            const uint32_t byte = lds1(exps + (s * 16 + row) * kExps + q4 * kExps / 4);
+#pragma unroll
+            for (int i = 0; i < kHd / 32; ++i) {
+              uint32_t x[4];
+              kv4_widen(lds4(at_sub + row * kRowBytes + q4 * (kRowBytes / 4) + 4 * i), byte, x);
+              step(2 * i, x[0], x[1]);
+              step(2 * i + 1, x[2], x[3]);
             }
           } else {
 #pragma unroll
@@ -405,13 +435,20 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const int left = piece.key1 - (key + 16 * s);  // keys of the sub-step that the piece holds
         const uint32_t at_sub = base + (kSubs + s) * Shape::kSubBytes;
         constexpr int kLoads = kNarrow ? 1 : kHd / 64, kWords = kNarrow && kHd == 64 ? 2 : 4;
+        [[maybe_unused]] uint32_t v_byte[4];
+        if constexpr (kFour) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v_byte[e] = lds1(exps + ((kSubs + s) * 16 + 2 * q4 + (e & 1) + 8 * (e >> 1)) * kExps + g * kExps / 8);
+        }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           uint32_t v[4][kWords];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int row = 2 * q4 + (e & 1) + 8 * (e >> 1);
-            if constexpr (kWords == 2) {
+            if constexpr (kFour) {
+              kv4_widen(lds4(at_sub + row * kRowBytes + g * (kRowBytes / 8) + 4 * i), v_byte[e], v[e]);
+            } else if constexpr (kWords == 2) {
               const uint2 x = lds8(at_sub + row * 64 + g * 8);
               v[e][0] = x.x, v[e][1] = x.y;
             } else {
@@ -499,7 +536,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     // ---------------------------------------------------------------- the warps meet
     // tile -> channel: lane g of V's reads holds a run of channels, tile n its n-th
     auto channel_of = [&](int tile, int n) {
-      constexpr int kRun = kNarrow ? kHd / 8 : 8;
+      constexpr int kRun = kNarrow || kFour ? kHd / 8 : 8;
       return (tile / kRun) * (8 * kRun) + n * kRun + tile % kRun;
     };
 #pragma unroll
@@ -609,11 +646,11 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   }
 }
 
-template <int kHd, bool kNarrow, bool kHalf>
+template <int kHd, int kKind, bool kHalf>
 cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s) {
-  using Shape = FewShape<kHd, kNarrow, kHalf>;
+  using Shape = FewShape<kHd, kKind, kHalf>;
   static_assert(Shape::kCtas * (Shape::kSmemBytes + 1024) <= 228 * 1024, "");
-  auto kernel = kv_attn_few_kernel<kHd, kNarrow, kHalf>;
+  auto kernel = kv_attn_few_kernel<kHd, kKind, kHalf>;
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = set_max_dynamic_smem_once(reinterpret_cast<const void*>(kernel), Shape::kSmemBytes, done);
   if (e != cudaSuccess) return e;
@@ -624,18 +661,22 @@ cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const 
 
 }  // namespace
 
-int kv_few_ctas(int head_dim, bool narrow) { return narrow && head_dim == 64 ? FewShape<64, true, true>::kCtas : 1; }
+int kv_few_ctas(int head_dim, bool narrow) {
+  static_assert(FewShape<64, LITEVGGT_KV_E4M3, true>::kCtas == FewShape<64, LITEVGGT_KV_E2M1, true>::kCtas, "");
+  return narrow && head_dim == 64 ? FewShape<64, LITEVGGT_KV_E4M3, true>::kCtas : 1;
+}
 
 cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches) {
-  const bool half = b.few_rows <= 8, narrow = c.cfg.dtype == LITEVGGT_KV_E4M3, wide = c.cfg.head_dim == 128;
+  const bool half = b.few_rows <= 8, wide = c.cfg.head_dim == 128;
   cudaError_t e;
-  if (wide) {
-    if (narrow) e = half ? start<128, true, true>(c, b, a, s) : start<128, true, false>(c, b, a, s);
-    else e = half ? start<128, false, true>(c, b, a, s) : start<128, false, false>(c, b, a, s);
-  } else {
-    if (narrow) e = half ? start<64, true, true>(c, b, a, s) : start<64, true, false>(c, b, a, s);
-    else e = half ? start<64, false, true>(c, b, a, s) : start<64, false, false>(c, b, a, s);
-  }
+  auto kinds = [&](auto kind) {
+    constexpr int kKind = decltype(kind)::value;
+    if (wide) e = half ? start<128, kKind, true>(c, b, a, s) : start<128, kKind, false>(c, b, a, s);
+    else e = half ? start<64, kKind, true>(c, b, a, s) : start<64, kKind, false>(c, b, a, s);
+  };
+  if (c.cfg.dtype == LITEVGGT_KV_E2M1) kinds(std::integral_constant<int, LITEVGGT_KV_E2M1>{});
+  else if (c.cfg.dtype == LITEVGGT_KV_E4M3) kinds(std::integral_constant<int, LITEVGGT_KV_E4M3>{});
+  else kinds(std::integral_constant<int, LITEVGGT_KV_BF16>{});
   ++*launches;
   return e;
 }

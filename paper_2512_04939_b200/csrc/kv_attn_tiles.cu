@@ -50,8 +50,9 @@ constexpr int kStreams = 2;                  // of a tile: a row's two threads
 constexpr int kSoftmaxWarps = 8 * kStreams;
 constexpr int kKeys = kTileKeys / kStreams;  // of a stream's step
 
-template <int kHd, bool kNarrow>
+template <int kHd, int kKind>
 struct TiShape {
+  static constexpr bool kNarrow = kKind != LITEVGGT_KV_BF16;
   static constexpr bool kOnes = kHd == 64;    // the tensor core adds up the rows, and Q is in its memory
   // Of the 16 pairs of 32 scores, this many take their exponentials on the FMA pipes: 16 issue slots and more for 16 clocks of the
   // special-function unit.  That pays where this unit is the bound, and not beside codes that are widened.  2048 rows over 83,280
@@ -64,7 +65,8 @@ struct TiShape {
   static constexpr int kRaw = kNarrow ? (kHd == 64 ? 3 : 1) : 0;
   static constexpr int kSubBytes = 128 * 128;             // 128 rows of 64 channels
   static constexpr int kTileBytes = kSubBytes * kHd / 64; // of Q, K or V
-  static constexpr int kRawBytes = kTileKeys * kHd + kTileKeys;
+  static constexpr int kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps;  // codes and exponents of a row
+  static constexpr int kRawBytes = kTileKeys * (kRowBytes + kExps);
   static constexpr int kOnesBytes = kOnes ? 16 * 128 : 0;
   static constexpr uint32_t kColO = 256, kOCols = kOnes ? 80 : 128, kColQ = 416;
   static constexpr int kQBytes = kOnes ? 0 : 2 * kTileBytes;
@@ -152,12 +154,13 @@ __device__ __forceinline__ int tiles_of(const Job& j, const KvAttend& at, int t)
   return seen > j.p.key0 ? (seen - j.p.key0 + kTileKeys - 1) / kTileKeys : 0;
 }
 
-template <int kHd, bool kNarrow>
-__global__ void __launch_bounds__(TiShape<kHd, kNarrow>::kThreads, 1)
+template <int kHd, int kKind>
+__global__ void __launch_bounds__(TiShape<kHd, kKind>::kThreads, 1)
 kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, KvPool pool, KvArrays arrays,
                      KvLaunch work, KvAttend at, uint32_t* status) {
-  using Shape = TiShape<kHd, kNarrow>;
-  constexpr bool kOnes = Shape::kOnes;
+  using Shape = TiShape<kHd, kKind>;
+  constexpr bool kOnes = Shape::kOnes, kNarrow = Shape::kNarrow, kFour = kKind == LITEVGGT_KV_E2M1;
+  [[maybe_unused]] constexpr int kRowBytes = Shape::kRowBytes, kExps = Shape::kExps;
   constexpr int kStages = Shape::kStages, kRaw = Shape::kRaw, kRawSlots = kRaw > 0 ? kRaw : 1, kSubs = kHd / 64;
   constexpr int kTileBytes = Shape::kTileBytes, kSubBytes = Shape::kSubBytes;
   extern __shared__ uint8_t smem_raw[];
@@ -268,7 +271,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           uint32_t bytes;
           if constexpr (kNarrow) {
             full = &bars->raw_full[x][ring.slot], empty = &bars->raw_empty[x][ring.slot];
-            bytes = (uint32_t)(n * pool.page_size * (kHd + 1));
+            bytes = (uint32_t)(n * pool.page_size * (kRowBytes + kExps));
           } else {
             full = x == 0 ? &bars->k_full[ring.slot] : &bars->v_land[ring.slot];
             empty = x == 0 ? &bars->k_empty[ring.slot] : &bars->v_empty[ring.slot];
@@ -281,8 +284,9 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
           if (lane < n) {
             if constexpr (kNarrow) {
               uint8_t* dst = smem_codes + (x * kRaw + ring.slot) * Shape::kRawBytes;
-              bulk_load(dst + lane * pool.page_size * kHd, (x == 0 ? pool.k : pool.v) + row * kHd, (uint32_t)(pool.page_size * kHd), full);
-              bulk_load(dst + kTileKeys * kHd + lane * pool.page_size, (x == 0 ? pool.k_exp : pool.v_exp) + row, (uint32_t)pool.page_size, full);
+              bulk_load(dst + lane * pool.page_size * kRowBytes, (x == 0 ? pool.k : pool.v) + row * kRowBytes, (uint32_t)(pool.page_size * kRowBytes), full);
+              bulk_load(dst + kTileKeys * kRowBytes + lane * pool.page_size * kExps, (x == 0 ? pool.k_exp : pool.v_exp) + row * kExps,
+                        (uint32_t)(pool.page_size * kExps), full);
             } else {
               uint8_t* dst = (x == 0 ? smem_k : smem_v) + ring.slot * kTileBytes + lane * pool.page_size * 128;
 #pragma unroll
@@ -416,25 +420,36 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             ok = ok && mbar_wait_warp(x == 0 ? &bars->k_empty[ring.slot] : &bars->v_empty[ring.slot], ring.phase ^ 1u, ctl);
             if (!ok) break;
             const uint8_t* codes = smem_codes + (x * kRaw + raw.slot) * Shape::kRawBytes;
-            const uint8_t* exps = codes + kTileKeys * kHd;
+            const uint8_t* exps = codes + kTileKeys * kRowBytes;
             uint8_t* tile = (x == 0 ? smem_k : smem_v) + ring.slot * kTileBytes;
             bool bad = false;
             constexpr int kPerRow = kHd / 16;  // 16 codes at a time
 #pragma unroll 2
             for (int i = 0; i < kPerRow / 2; ++i) {
               const int piece = i * 256 + tid, r = piece / kPerRow, ch = piece % kPerRow;
-              const uint4 w4 = *reinterpret_cast<const uint4*>(codes + piece * 16);
-              const uint32_t byte = exps[r], w[4] = {w4.x, w4.y, w4.z, w4.w};
-              const KvFactor f = kv_factor(byte);
-              uint32_t v[8];
+              uint32_t v[8], byte;
+              if constexpr (kFour) {
+                const uint2 w2 = *reinterpret_cast<const uint2*>(codes + piece * 8);
+                byte = exps[r * kExps + ch / 2];
+                uint32_t (&low)[4] = *reinterpret_cast<uint32_t (*)[4]>(&v[0]), (&high)[4] = *reinterpret_cast<uint32_t (*)[4]>(&v[4]);
+                kv4_widen(w2.x, byte, low);
+                kv4_widen(w2.y, byte, high);
+              } else {
+                const uint4 w4 = *reinterpret_cast<const uint4*>(codes + piece * 16);
+                byte = exps[r];
+                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+                const KvFactor f = kv_factor(byte);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                v[2 * e] = mul_bf16x2(kv_code_bits(__byte_perm(w[e], 0u, 0x1404)), f.first * 0x10001u);
-                v[2 * e + 1] = mul_bf16x2(kv_code_bits(__byte_perm(w[e], 0u, 0x3424)), f.first * 0x10001u);
+                for (int e = 0; e < 4; ++e) {
+                  v[2 * e] = mul_bf16x2(kv_code_bits(__byte_perm(w[e], 0u, 0x1404)), f.first * 0x10001u);
+                  v[2 * e + 1] = mul_bf16x2(kv_code_bits(__byte_perm(w[e], 0u, 0x3424)), f.first * 0x10001u);
+                }
+                if (kv_needs_second(byte)) {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) v[e] = mul_bf16x2(v[e], f.second * 0x10001u);
+                }
               }
-              if (kv_needs_second(byte)) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = mul_bf16x2(v[e], f.second * 0x10001u);
+              if (kFour ? kv4_needs_second(byte) : kv_needs_second(byte)) {  // (no others are not finite)
                 if (x == 1 && r >= part && mode == kCareful) {
 #pragma unroll
                   for (int e = 0; e < 8; ++e) {
@@ -749,7 +764,12 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             const long long at_row = (page * pool.kv_heads + job.p.kv_head) * pool.page_size + (key & (pool.page_size - 1));
             for (int i = 0; i < 32; ++i) {
               float v;
-              if constexpr (kNarrow) {
+              if constexpr (kFour) {
+                const int ch = ch0 + i;
+                uint32_t w[4];
+                kv4_widen((uint32_t)pool.v[at_row * kRowBytes + ch / 2] >> 4 * (ch & 1) & 15u, pool.v_exp[at_row * kExps + ch / 32], w);
+                v = bf16_lo(w[0]);
+              } else if constexpr (kNarrow) {
                 const uint32_t byte = pool.v_exp[at_row];
                 const KvFactor f = kv_factor(byte);
                 uint32_t w = mul_bf16x2(kv_code_bits((uint32_t)pool.v[at_row * kHd + ch0 + i] << 8), f.first);
@@ -857,10 +877,10 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
   }
 }
 
-template <int kHd, bool kNarrow>
+template <int kHd, int kKind>
 cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s) {
-  using Shape = TiShape<kHd, kNarrow>;
-  auto kernel = kv_attn_tiles_kernel<kHd, kNarrow>;
+  using Shape = TiShape<kHd, kKind>;
+  auto kernel = kv_attn_tiles_kernel<kHd, kKind>;
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = set_max_dynamic_smem_once(reinterpret_cast<const void*>(kernel), Shape::kSmemBytes, done);
   if (e != cudaSuccess) return e;
@@ -872,10 +892,11 @@ cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const 
 }  // namespace
 
 cudaError_t launch_kv_attn_tiles(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches) {
-  const bool narrow = c.cfg.dtype == LITEVGGT_KV_E4M3;
   ++*launches;
-  if (c.cfg.head_dim == 64) return narrow ? start<64, true>(c, b, a, s) : start<64, false>(c, b, a, s);
-  return narrow ? start<128, true>(c, b, a, s) : start<128, false>(c, b, a, s);
+  const bool wide = c.cfg.head_dim == 128;
+  if (c.cfg.dtype == LITEVGGT_KV_E2M1) return wide ? start<128, LITEVGGT_KV_E2M1>(c, b, a, s) : start<64, LITEVGGT_KV_E2M1>(c, b, a, s);
+  if (c.cfg.dtype == LITEVGGT_KV_E4M3) return wide ? start<128, LITEVGGT_KV_E4M3>(c, b, a, s) : start<64, LITEVGGT_KV_E4M3>(c, b, a, s);
+  return wide ? start<128, LITEVGGT_KV_BF16>(c, b, a, s) : start<64, LITEVGGT_KV_BF16>(c, b, a, s);
 }
 
 }  // namespace lv

@@ -36,6 +36,7 @@ __device__ __forceinline__ uint32_t lane_top(const uint4& x) {
   const uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
   return __vmaxu2(m, m >> 16);  // (low half)
 }
+// (of the kLanes lanes that share a power of two)
 template <int kLanes>
 __device__ __forceinline__ uint32_t row_tops(const uint4& k, const uint4& v) {
   uint32_t m = __byte_perm(lane_top(k), lane_top(v), 0x5410);
@@ -48,6 +49,18 @@ __device__ __forceinline__ uint2 row_codes(const uint4& x, uint32_t byte) {
   const float f = kv_inverse_scale(byte);
   return make_uint2(pack_e4m3x4(bf16_lo(x.x) * f, bf16_hi(x.x) * f, bf16_lo(x.y) * f, bf16_hi(x.y) * f),
                     pack_e4m3x4(bf16_lo(x.z) * f, bf16_hi(x.z) * f, bf16_lo(x.w) * f, bf16_hi(x.w) * f));
+}
+__device__ __forceinline__ uint32_t row_codes4(const uint4& x, uint32_t byte) {
+  if (byte == kKvNanByte) return 0u;
+  const float f = kv_inverse_scale(byte);
+  const float y[8] = {bf16_lo(x.x) * f, bf16_hi(x.x) * f, bf16_lo(x.y) * f, bf16_hi(x.y) * f,
+                      bf16_lo(x.z) * f, bf16_hi(x.z) * f, bf16_lo(x.w) * f, bf16_hi(x.w) * f};
+  return pack_e2m1x8(y);
+}
+__device__ __forceinline__ uint4 row_values4(uint32_t codes, uint32_t byte) {
+  uint32_t r[4];
+  kv4_widen(codes, byte, r);
+  return make_uint4(r[0], r[1], r[2], r[3]);
 }
 // Eight codes to eight bf16.
 __device__ __forceinline__ uint4 row_values(const uint2& codes, uint32_t byte) {
@@ -78,7 +91,7 @@ struct MoveUnits {
   __device__ __forceinline__ bool live(int i) const { return unit(i) < units; }
 };
 
-template <int kHd, bool kNarrow, int kUnits>
+template <int kHd, int kKind, int kUnits>
 __global__ void __launch_bounds__(kMoveThreads)
 kv_append_kernel(KvPool pool, KvArrays arrays, const __nv_bfloat16* __restrict__ k, KvStride ks, const __nv_bfloat16* __restrict__ v,
                  KvStride vs, unsigned units) {
@@ -100,7 +113,16 @@ kv_append_kernel(KvPool pool, KvArrays arrays, const __nv_bfloat16* __restrict__
   }
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
-    if constexpr (kNarrow) {
+    if constexpr (kKind == LITEVGGT_KV_E2M1) {
+      constexpr int kExps = kHd / 32;
+      const uint32_t tops = row_tops<4>(xk[i], xv[i]), bk = kv4_exponent_byte(tops & 0xffffu), bv = kv4_exponent_byte(tops >> 16);
+      if (mine.live(i)) {
+        *reinterpret_cast<uint32_t*>(pool.k + at[i] * (kHd / 2) + part * 4) = row_codes4(xk[i], bk);
+        *reinterpret_cast<uint32_t*>(pool.v + at[i] * (kHd / 2) + part * 4) = row_codes4(xv[i], bv);
+        if (part % 4 == 0) pool.k_exp[at[i] * kExps + part / 4] = (uint8_t)bk;
+        if (part % 4 == 1) pool.v_exp[at[i] * kExps + part / 4] = (uint8_t)bv;
+      }
+    } else if constexpr (kKind == LITEVGGT_KV_E4M3) {
       const uint32_t tops = row_tops<kLanes>(xk[i], xv[i]), bk = kv_exponent_byte(tops & 0xffffu), bv = kv_exponent_byte(tops >> 16);
       if (mine.live(i)) {
         *reinterpret_cast<uint2*>(pool.k + at[i] * kHd + part * 8) = row_codes(xk[i], bk);
@@ -115,7 +137,7 @@ kv_append_kernel(KvPool pool, KvArrays arrays, const __nv_bfloat16* __restrict__
   }
 }
 
-template <int kHd, bool kNarrow, int kUnits>
+template <int kHd, int kKind, int kUnits>
 __global__ void __launch_bounds__(kMoveThreads)
 kv_gather_kernel(KvPool pool, KvArrays arrays, __nv_bfloat16* __restrict__ k, __nv_bfloat16* __restrict__ v, unsigned units) {
   wait_for_previous_kernel();
@@ -127,7 +149,12 @@ kv_gather_kernel(KvPool pool, KvArrays arrays, __nv_bfloat16* __restrict__ k, __
   for (int i = 0; i < kUnits; ++i) {
     if (!mine.live(i)) continue;
     const size_t at = pool_row(pool, arrays, (int)(mine.unit(i) / (unsigned)pool.kv_heads), (int)(mine.unit(i) % (unsigned)pool.kv_heads));
-    if constexpr (kNarrow) {
+    if constexpr (kKind == LITEVGGT_KV_E2M1) {
+      xk[i].x = *reinterpret_cast<const uint32_t*>(pool.k + at * (kHd / 2) + part * 4);
+      xv[i].x = *reinterpret_cast<const uint32_t*>(pool.v + at * (kHd / 2) + part * 4);
+      bk[i] = pool.k_exp[at * (kHd / 32) + part / 4];
+      bv[i] = pool.v_exp[at * (kHd / 32) + part / 4];
+    } else if constexpr (kKind == LITEVGGT_KV_E4M3) {
       const uint2 ck = *reinterpret_cast<const uint2*>(pool.k + at * kHd + part * 8);
       const uint2 cv = *reinterpret_cast<const uint2*>(pool.v + at * kHd + part * 8);
       xk[i].x = ck.x, xk[i].y = ck.y, xv[i].x = cv.x, xv[i].y = cv.y;
@@ -141,7 +168,10 @@ kv_gather_kernel(KvPool pool, KvArrays arrays, __nv_bfloat16* __restrict__ k, __
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
     if (!mine.live(i)) continue;
-    if constexpr (kNarrow) {
+    if constexpr (kKind == LITEVGGT_KV_E2M1) {
+      xk[i] = row_values4(xk[i].x, bk[i]);
+      xv[i] = row_values4(xv[i].x, bv[i]);
+    } else if constexpr (kKind == LITEVGGT_KV_E4M3) {
       xk[i] = row_values(make_uint2(xk[i].x, xk[i].y), bk[i]);
       xv[i] = row_values(make_uint2(xv[i].x, xv[i].y), bv[i]);
     }
@@ -156,19 +186,18 @@ kv_gather_kernel(KvPool pool, KvArrays arrays, __nv_bfloat16* __restrict__ k, __
 template <class F>
 void by_kind(const litevggt_kv_cache& c, long long units, const F& f) {
   using std::integral_constant;
-  auto sized = [&](auto hd, auto narrow) {
+  auto sized = [&](auto hd, auto kind) {
     const long long per_block = kMoveThreads / (decltype(hd)::value / 8), blocks = (units + per_block - 1) / per_block;
-    if (blocks <= (long long)c.num_sms * (2048 / kMoveThreads)) f(hd, narrow, integral_constant<int, 1>{}, (unsigned)blocks);
-    else f(hd, narrow, integral_constant<int, 2>{}, (unsigned)((blocks + 1) / 2));
+    if (blocks <= (long long)c.num_sms * (2048 / kMoveThreads)) f(hd, kind, integral_constant<int, 1>{}, (unsigned)blocks);
+    else f(hd, kind, integral_constant<int, 2>{}, (unsigned)((blocks + 1) / 2));
   };
-  const bool narrow = c.cfg.dtype == LITEVGGT_KV_E4M3;
-  if (c.cfg.head_dim == 64) {
-    if (narrow) sized(integral_constant<int, 64>{}, integral_constant<bool, true>{});
-    else sized(integral_constant<int, 64>{}, integral_constant<bool, false>{});
-  } else {
-    if (narrow) sized(integral_constant<int, 128>{}, integral_constant<bool, true>{});
-    else sized(integral_constant<int, 128>{}, integral_constant<bool, false>{});
-  }
+  auto kinds = [&](auto hd) {
+    if (c.cfg.dtype == LITEVGGT_KV_E2M1) sized(hd, integral_constant<int, LITEVGGT_KV_E2M1>{});
+    else if (c.cfg.dtype == LITEVGGT_KV_E4M3) sized(hd, integral_constant<int, LITEVGGT_KV_E4M3>{});
+    else sized(hd, integral_constant<int, LITEVGGT_KV_BF16>{});
+  };
+  if (c.cfg.head_dim == 64) kinds(integral_constant<int, 64>{});
+  else kinds(integral_constant<int, 128>{});
 }
 
 }  // namespace
@@ -177,8 +206,8 @@ cudaError_t launch_kv_append(const litevggt_kv_cache& c, const litevggt_kv_batch
                              const __nv_bfloat16* v, KvStride v_stride, cudaStream_t s, int* launches) {
   const long long units = b.rows * c.cfg.kv_heads;
   cudaError_t e = cudaSuccess;
-  by_kind(c, units, [&](auto hd, auto narrow, auto per, unsigned blocks) {
-    e = launch(kv_append_kernel<decltype(hd)::value, decltype(narrow)::value, decltype(per)::value>, dim3(blocks), kMoveThreads, 0, s, c.pool,
+  by_kind(c, units, [&](auto hd, auto kind, auto per, unsigned blocks) {
+    e = launch(kv_append_kernel<decltype(hd)::value, decltype(kind)::value, decltype(per)::value>, dim3(blocks), kMoveThreads, 0, s, c.pool,
                kv_arrays(b), k, k_stride, v, v_stride, (unsigned)units);
   });
   ++*launches;
@@ -189,8 +218,8 @@ cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch
                              int* launches) {
   const long long units = b.rows * c.cfg.kv_heads;
   cudaError_t e = cudaSuccess;
-  by_kind(c, units, [&](auto hd, auto narrow, auto per, unsigned blocks) {
-    e = launch(kv_gather_kernel<decltype(hd)::value, decltype(narrow)::value, decltype(per)::value>, dim3(blocks), kMoveThreads, 0, s, c.pool,
+  by_kind(c, units, [&](auto hd, auto kind, auto per, unsigned blocks) {
+    e = launch(kv_gather_kernel<decltype(hd)::value, decltype(kind)::value, decltype(per)::value>, dim3(blocks), kMoveThreads, 0, s, c.pool,
                kv_arrays(b), k, v, (unsigned)units);
   });
   ++*launches;

@@ -13,7 +13,7 @@ constexpr uint32_t kKvBatchMagic = 0x4c564b42u;
 constexpr int kKvLongest = 1 << 30;  // tokens of a sequence: sums of positions and steps stay inside 31 bits
 
 // The pools as a kernel sees them: [pages, kv_heads, page_size, head_dim] of bf16 or E4M3 codes, the codes' exponents
-// [pages, kv_heads, page_size].
+// [pages, kv_heads, page_size]; E2M1 codes two to a byte, their exponents [.., head_dim / 32].
 struct KvPool {
   uint8_t *k, *v;
   uint8_t *k_exp, *v_exp;  // null for bf16

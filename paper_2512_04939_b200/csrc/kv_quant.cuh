@@ -44,4 +44,59 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return r;
 }
 
+// The 4-bit form: E2M1 codes x (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) under one power of two 2^e for every 32 channels,
+//   e = the least whole number >= -126 with max |block| <= 6 * 2^e, stored as the byte e + 127 (255: not finite, codes of zero)
+// the code of an even channel in the low half of its byte.  Again every x 2^e is a bf16 number, so that reading is exact; blocks of 32
+// because a code has one bit of mantissa and a range of twelve: what shares a power of two with an element twelve times as large is
+// lost, and in a whole row that is common.
+__device__ __forceinline__ uint32_t kv4_exponent_byte(uint32_t top) {
+  if (top >= 0x7f80u) return kKvNanByte;
+  // top = m 2^x, 1 <= m < 2: 6 = 1.5 * 2^2, so e = x - 2, or one more where m > 1.5
+  const int byte = (int)(top >> 7) - 2 + ((top & 0x7fu) > 0x40u ? 1 : 0);
+  return (uint32_t)max(byte, 1);
+}
+// As kv_factor: the bits of a code moved into a bf16 stand for x 2^-126.
+__device__ __forceinline__ KvFactor kv4_factor(uint32_t byte) {
+  KvFactor f;
+  f.first = byte == kKvNanByte ? 0x7fc0u : min(byte + 126u, 254u) << 7;
+  f.second = byte == kKvNanByte ? 0x3f80u : max((int)byte - 1, 127) << 7;
+  return f;
+}
+__device__ __forceinline__ bool kv4_needs_second(uint32_t byte) { return byte > 128u; }  // (blocks whose largest magnitude is over 12)
+// Eight codes to eight bf16.
+__device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t byte, uint32_t (&out)[4]) {
+  const KvFactor f = kv4_factor(byte);
+  const uint32_t low = w << 4;  // the even channels' codes in the upper halves of the bytes
+  constexpr uint32_t kPick[4] = {0x4000u, 0x5010u, 0x6020u, 0x7030u};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t t = __byte_perm(low, w, kPick[i]);
+    out[i] = mul_bf16x2((t & 0x80008000u) | (t >> 6 & 0x01c001c0u), f.first * 0x10001u);
+  }
+  if (kv4_needs_second(byte)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = mul_bf16x2(out[i], f.second * 0x10001u);
+  }
+}
+// Eight floats, at most 6 in magnitude, to eight codes.
+__device__ __forceinline__ uint32_t pack_e2m1x8(const float (&x)[8]) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+  return r;
+}
+
+// What a pool holds of a row of a head: bytes of values or codes, and of exponents.
+template <int kHd, int kKind>
+struct KvRow {
+  static constexpr int kBytes = kKind == LITEVGGT_KV_BF16 ? 2 * kHd : kKind == LITEVGGT_KV_E4M3 ? kHd : kHd / 2;
+  static constexpr int kExps = kKind == LITEVGGT_KV_BF16 ? 0 : kKind == LITEVGGT_KV_E4M3 ? 1 : kHd / 32;
+};
+
 }  // namespace lv

@@ -19,7 +19,8 @@ import torch
 
 from .binding import KVConfig, _check, load_library
 
-_DTYPES = {"bf16": (0, torch.bfloat16), "e4m3": (1, torch.float8_e4m3fn)}
+# number in the C library, the pools' type, elements in one of it, elements that share an exponent (0: none does)
+_DTYPES = {"bf16": (0, torch.bfloat16, 1, 0), "e4m3": (1, torch.float8_e4m3fn, 1, -1), "e2m1": (2, torch.uint8, 2, 32)}
 
 
 def _whole(name: str, numbers) -> np.ndarray:
@@ -55,21 +56,26 @@ class KVBatch:
 
 
 class KVCache:
-    """A cache over pools of the caller's: ``k``, ``v`` [pages, kv_heads, page_size, head_dim], bfloat16, or float8_e4m3fn
-    with the exponents ``k_exp``, ``v_exp`` uint8 [pages, kv_heads, page_size]."""
+    """A cache over pools of the caller's: ``k``, ``v`` [pages, kv_heads, page_size, head_dim], bfloat16; or float8_e4m3fn with the
+    exponents ``k_exp``, ``v_exp`` uint8 [pages, kv_heads, page_size]; or 4 bits, E2M1 codes two to a byte in uint8
+    [pages, kv_heads, page_size, head_dim / 2] (the even channel's in the low half) with exponents for every 32 channels, uint8
+    [pages, kv_heads, page_size, head_dim / 32]."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None):
         self.lib = load_library()
         if k.dim() != 4 or v.shape != k.shape:
             raise ValueError(f"k and v must both be [pages, kv_heads, page_size, head_dim], got {tuple(k.shape)} and {tuple(v.shape)}")
-        narrow = k.dtype == torch.float8_e4m3fn
-        if not narrow and k.dtype != torch.bfloat16 or v.dtype != k.dtype:
-            raise ValueError(f"k and v must both be bfloat16 or both float8_e4m3fn, got {k.dtype} and {v.dtype}")
+        kinds = {kind[1]: kind for kind in _DTYPES.values()}
+        if k.dtype not in kinds or v.dtype != k.dtype:
+            raise ValueError(f"k and v must both be bfloat16, float8_e4m3fn or uint8 (E2M1), got {k.dtype} and {v.dtype}")
+        number, _, packed, block = kinds[k.dtype]
+        head_dim = k.shape[3] * packed
         tensors = {"k": k, "v": v}
-        if narrow:
+        if block:
+            shape = k.shape[:3] if block < 0 else (*k.shape[:3], head_dim // block)
             for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
-                if t is None or t.dtype != torch.uint8 or t.shape != k.shape[:3]:
-                    raise ValueError(f"{name} must be uint8 {tuple(k.shape[:3])} beside float8_e4m3fn pools")
+                if t is None or t.dtype != torch.uint8 or t.shape != shape:
+                    raise ValueError(f"{name} must be uint8 {tuple(shape)} beside {k.dtype} pools")
                 tensors[name] = t
         elif k_exp is not None or v_exp is not None:
             raise ValueError("bfloat16 pools have no exponents")
@@ -80,12 +86,12 @@ class KVCache:
                 raise ValueError("every pool must live on the same CUDA device")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.device, self._index = k.device, k.get_device()
-        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.pages, self.kv_heads, self.page_size, self.head_dim = *k.shape[:3], head_dim
         self._scale = 1.0 / math.sqrt(self.head_dim)
         self._append, self._attend = self.lib.litevggt_kv_append, self.lib.litevggt_kv_attend
         self.status = torch.zeros(64, dtype=torch.int32, device=k.device)
         self._home = self._stream()
-        cfg = KVConfig(self.pages, self.page_size, self.kv_heads, self.head_dim, 1 if narrow else 0)
+        cfg = KVConfig(self.pages, self.page_size, self.kv_heads, self.head_dim, number)
         self.handle = C.c_void_p()
         _check(self.lib.litevggt_kv_create(C.byref(cfg), self.device.index, *(C.c_void_p(t.data_ptr()) if t is not None else None
                                                                              for t in (k, v, k_exp, v_exp, self.status)),
@@ -97,10 +103,11 @@ class KVCache:
         if dtype not in _DTYPES:
             raise ValueError(f"dtype must be one of {sorted(_DTYPES)}, got {dtype!r}")
         where = torch.device("cuda", device)
-        shape = (pages, kv_heads, page_size, head_dim)
-        pools = [torch.empty(shape, dtype=_DTYPES[dtype][1], device=where) for _ in range(2)]
-        if dtype == "e4m3":
-            pools += [torch.empty(shape[:3], dtype=torch.uint8, device=where) for _ in range(2)]
+        _, kind, packed, block = _DTYPES[dtype]
+        shape = (pages, kv_heads, page_size)
+        pools = [torch.empty((*shape, head_dim // packed), dtype=kind, device=where) for _ in range(2)]
+        if block:
+            pools += [torch.empty(shape if block < 0 else (*shape, head_dim // block), dtype=torch.uint8, device=where) for _ in range(2)]
         return cls(*pools)
 
     def close(self):
