@@ -395,6 +395,31 @@ litevggt_status litevggt_kv_gather(litevggt_kv_cache* cache, const litevggt_kv_b
  * scale: positive, less than 1e30. */
 litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
                                    int64_t q_head_stride, float scale, void* out, void* stream);
+/* The same, and lse[i] = log sum_j exp(scale q[i] . k[j]) over the tokens that row i sees: dev fp32 [rows, q_heads], in memory of its own, or
+ * NULL; minus infinity for a row that sees none.  It is that of the sum that the output was divided by, whose terms are rounded to bf16 where
+ * rows see many tokens: off by less than 2^-8 and 2^-22 of itself, and by far less where many tokens share a row's weight. */
+litevggt_status litevggt_kv_attend_lse(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
+                                       int64_t q_head_stride, float scale, void* out, float* lse, void* stream);
+
+/* What a cached token has drawn of the attention so far decides what stays when a cache is full.  The tallies lie in a pool beside K and
+ * V, weights: dev fp32 [pages, kv_heads, page_size], 16-byte aligned, which outlives the cache (NULL: none).  From then on
+ * litevggt_kv_append sets those of the tokens that it writes to zero.  Not while calls with the cache are under way. */
+litevggt_status litevggt_kv_track(litevggt_kv_cache* cache, float* weights);
+/* w[j] = decay w[j] + sum_i exp(scale q[i] . k[j] - lse[i]) for every token j of the batch's sequences that have rows, over the rows i
+ * that see it and the query heads that share its head; what a token does not draw adds nothing, whatever the row holds.  lse: dev fp32
+ * [rows, q_heads], from litevggt_kv_attend_lse on the same queries.  decay in [0, 1]; 0: the tallies begin anew, whatever they held.
+ * Sums are in 32 bits, in an order that does not change from call to call.  LITEVGGT_ERR_NULL without tallies, LITEVGGT_ERR_SHAPE
+ * where sequences of the batch share pages. */
+litevggt_status litevggt_kv_weigh(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
+                                  int64_t q_head_stride, float scale, const float* lse, float decay, void* stream);
+/* Every head of every sequence keeps as many of its tokens as `into` has: its `first` first ones, its `last` last ones, and of the others
+ * those with the largest tallies, of equal ones the earlier (a NaN counts as less than any number).  They are copied, K, V, exponents and
+ * tallies, to the pages of `into`, in the order that they were in; heads differ in which they keep.  `into` names the same number
+ * of sequences, with as many rows as tokens, at most what `from` holds, and where it is less, at least first + last; its pages are
+ * not those of `from`, which stay as they are, and name none twice (LITEVGGT_ERR_SHAPE).  kept: dev int32 [rows of into, kv_heads], where each
+ * token was in its sequence. */
+litevggt_status litevggt_kv_evict(litevggt_kv_cache* cache, const litevggt_kv_batch* from, const litevggt_kv_batch* into, int32_t first,
+                                  int32_t last, int32_t* kept, void* stream);
 /* As litevggt_poll_device_status, and the number of kernels launched on behalf of the cache. */
 litevggt_status litevggt_kv_poll(litevggt_kv_cache* cache, void* stream);
 litevggt_status litevggt_kv_launch_count(const litevggt_kv_cache* cache, int64_t* launches);

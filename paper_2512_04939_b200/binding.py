@@ -112,6 +112,10 @@ def load_library():
         "litevggt_kv_append": [vp, vp, vp, i64, i64, vp, i64, i64, vp],
         "litevggt_kv_gather": [vp, vp, vp, vp, vp],
         "litevggt_kv_attend": [vp, vp, vp, i64, i64, C.c_float, vp, vp],
+        "litevggt_kv_attend_lse": [vp, vp, vp, i64, i64, C.c_float, vp, vp, vp],
+        "litevggt_kv_track": [vp, vp],
+        "litevggt_kv_weigh": [vp, vp, vp, i64, i64, C.c_float, vp, C.c_float, vp],
+        "litevggt_kv_evict": [vp, vp, vp, i32, i32, vp, vp],
         "litevggt_kv_poll": [vp, vp],
         "litevggt_kv_launch_count": [vp, P(i64)],
         "litevggt_rotary_create": [P(RotaryConfig), C.c_int, P(vp)],

@@ -4,38 +4,11 @@
 #include <new>
 
 #include "kv_cache.h"
+#include "kv_checks.h"
 
 namespace lv {
 
 namespace {
-
-bool cache_ok(const litevggt_kv_cache* c) { return c != nullptr && c->magic == kKvCacheMagic; }
-bool batch_ok(const litevggt_kv_batch* b) { return b != nullptr && b->magic == kKvBatchMagic; }
-
-// A batch of this cache whose arrays are on the device.
-litevggt_status usable(const litevggt_kv_cache* c, const litevggt_kv_batch* b) {
-  if (!cache_ok(c) || b == nullptr) return LITEVGGT_ERR_NULL;
-  if (!batch_ok(b) || b->owner_id != c->id || b->base == nullptr) return LITEVGGT_ERR_STALE_PLAN;
-  return LITEVGGT_OK;
-}
-
-// Rows of heads that may be read 16 bytes at a time.
-litevggt_status stride_ok(int64_t row, int64_t head) {
-  if (row < 0 || head < 0 || row > UINT32_MAX || head > UINT32_MAX) return LITEVGGT_ERR_SHAPE;
-  return row % 8 != 0 || head % 8 != 0 ? LITEVGGT_ERR_ALIGN : LITEVGGT_OK;
-}
-
-// Whether `n` bytes at `out` reach into one of the rows of queries, each taken from its first head to the end of its last.
-bool meets_queries(const void* out, long long n, const void* q, long long rows, long long row_bytes, long long row_stride_bytes) {
-  const long long begin = (long long)(reinterpret_cast<intptr_t>(out) - reinterpret_cast<intptr_t>(q)), end = begin + n;
-  // the first row that ends behind the output's beginning
-  long long i = 0;
-  if (begin >= row_bytes) {
-    if (row_stride_bytes == 0) return false;
-    i = (begin - row_bytes) / row_stride_bytes + 1;
-  }
-  return i < rows && i * row_stride_bytes < end;
-}
 
 // Lays out a batch's device memory: first what the host writes (`image`), then what only kernels use.
 void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int head_dim) {
@@ -54,12 +27,16 @@ void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int hea
   b->o_pages = take(n_pages * sizeof(int));
   take_lists(b->few, &b->at_few);
   take_lists(b->tiles, &b->at_tiles);
+  b->o_few_at = take(b->weigh.few_at.size() * sizeof(long long));
+  b->o_tiles_at = take(b->weigh.tiles_at.size() * sizeof(long long));
+  b->o_weigh_joins = take(b->weigh.parts > 1 ? (size_t)b->weigh.items * sizeof(int) : 0);
   b->image.assign(at, 0);  // counters and marks start at zero
   // the two launches follow one another, and so use the same memory
   const size_t parts[2] = {(size_t)b->few.slots * kKvFewRows, (size_t)b->tiles.slots * kKvTileRows};
   const size_t most = std::max(parts[0], parts[1]);
   b->at_few.rows = b->at_tiles.rows = take(most * head_dim * sizeof(float));
   b->at_few.sums = b->at_tiles.sums = take(most * 2 * sizeof(float));
+  b->o_weigh_sums = take(b->weigh.parts > 1 ? (size_t)b->weigh.items * b->weigh.parts * b->weigh.key_block * sizeof(float) : 0);
   b->bytes = at;
   auto put = [&](size_t to, const void* from, size_t bytes) {
     if (bytes > 0) memcpy(b->image.data() + to, from, bytes);
@@ -70,6 +47,8 @@ void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int hea
     const std::vector<KvPiece> chain = kv_chain(w);
     put(p.pieces, chain.data(), chain.size() * sizeof(KvPiece));
   };
+  put(b->o_few_at, b->weigh.few_at.data(), b->weigh.few_at.size() * sizeof(long long));
+  put(b->o_tiles_at, b->weigh.tiles_at.data(), b->weigh.tiles_at.size() * sizeof(long long));
   put_lists(b->few, b->at_few);
   put_lists(b->tiles, b->at_tiles);
 }
@@ -121,6 +100,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
     KvWork narrow = cut_tiles(kKvTileRows / 2, kKvHalfTiles);
     if (narrow.cost < b->tiles.cost) b->tiles = narrow;
   }
+  b->weigh = kv_weigh_plan(b->seqs, b->group, c->cfg.kv_heads, kKvFewRows, c->num_sms);
   lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
   return LITEVGGT_OK;
 }
@@ -166,7 +146,7 @@ litevggt_status litevggt_kv_create(const litevggt_kv_config* cfg, int device, vo
   int shift = 4;
   while ((1 << shift) < cfg->page_size) ++shift;
   c->pool = KvPool{static_cast<uint8_t*>(k), static_cast<uint8_t*>(v), narrow ? k_exp : nullptr, narrow ? v_exp : nullptr,
-                   cfg->kv_heads, cfg->page_size, shift};
+                   cfg->kv_heads, cfg->page_size, shift, nullptr};
   c->status = status;
   c->launches = 0;
   if (!narrow) {  // rows of heads as one matrix; a box is a page of a head and 64 channels
@@ -282,6 +262,11 @@ litevggt_status litevggt_kv_gather(litevggt_kv_cache* cache, const litevggt_kv_b
 
 litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
                                    int64_t q_head_stride, float scale, void* out, void* stream) {
+  return litevggt_kv_attend_lse(cache, batch, q, q_row_stride, q_head_stride, scale, out, nullptr, stream);
+}
+
+litevggt_status litevggt_kv_attend_lse(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
+                                       int64_t q_head_stride, float scale, void* out, float* lse, void* stream) {
   litevggt_status st = usable(cache, batch);
   if (st != LITEVGGT_OK) return st;
   if (!(scale > 0.0f) || !(scale < 1e30f)) return LITEVGGT_ERR_SHAPE;
@@ -290,11 +275,17 @@ litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_b
   if (!aligned16(q) || !aligned16(out)) return LITEVGGT_ERR_ALIGN;
   if ((st = stride_ok(q_row_stride, q_head_stride)) != LITEVGGT_OK) return st;
   const long long hd = cache->cfg.head_dim, row_bytes = 2 * ((batch->q_heads - 1) * q_head_stride + hd);
-  if (meets_queries(out, 2 * batch->rows * batch->q_heads * hd, q, batch->rows, row_bytes, 2 * q_row_stride)) return LITEVGGT_ERR_SHAPE;
+  const long long out_bytes = 2 * batch->rows * batch->q_heads * hd, lse_bytes = 4 * batch->rows * batch->q_heads;
+  if (meets_queries(out, out_bytes, q, batch->rows, row_bytes, 2 * q_row_stride)) return LITEVGGT_ERR_SHAPE;
+  if (lse != nullptr) {
+    if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return LITEVGGT_ERR_ALIGN;
+    if (meets_queries(lse, lse_bytes, q, batch->rows, row_bytes, 2 * q_row_stride) || meets_queries(lse, lse_bytes, out, 1, out_bytes, 0))
+      return LITEVGGT_ERR_SHAPE;
+  }
   const OnDevice g(cache->device);
   if (!g.ok) return LITEVGGT_ERR_CUDA;
   const KvAttend a{static_cast<const __nv_bfloat16*>(q), KvStride{q_row_stride, q_head_stride}, static_cast<__nv_bfloat16*>(out),
-                   batch->q_heads, batch->group, batch->causal_block, scale * 1.4426950408889634f};
+                   batch->q_heads, batch->group, batch->causal_block, scale * 1.4426950408889634f, lse};
   int n = 0;
   cudaError_t e = cudaSuccess;
   if (!batch->few.pieces.empty()) e = launch_kv_attn_few(*cache, *batch, a, (cudaStream_t)stream, &n);

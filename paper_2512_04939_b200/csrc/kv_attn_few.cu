@@ -27,26 +27,13 @@
 // meeting of the parts are most.
 #include "exp2.cuh"
 #include "kv_cache.h"
+#include "kv_mma.cuh"
 #include "kv_quant.cuh"
 
 namespace lv {
 
 namespace {
 
-template <bool kHalfFloat>
-__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if constexpr (kHalfFloat) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  } else {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-}
 // Two codes (the low or the high half of a word) to two f16 numbers, exactly.
 __device__ __forceinline__ uint32_t widen_low(uint32_t w) {
   uint32_t r;
@@ -561,10 +548,9 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       }
     }
     __syncthreads();
-    auto store = [&](int r, int ch, float value) {
+    auto row_of = [&](int r) {
       const int at_row = piece.row0 + r;
-      const size_t row = (size_t)(seq.row0 + at_row / at.group) * at.q_heads + piece.kv_head * at.group + at_row % at.group;
-      at.out[row * kHd + ch] = __float2bfloat16_rn(value);
+      return (size_t)(seq.row0 + at_row / at.group) * at.q_heads + piece.kv_head * at.group + at_row % at.group;
     };
     // What the warps left in shared memory, weighed against each other; the joint reference is the largest of theirs.  One that
     // has met no key has none (-infinity), and weighs nothing.  `out` gets row, channel, output, reference and sum.
@@ -584,9 +570,14 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         out(r, ch, acc, m, l);
       }
     };
-    auto finish = [&](int r, int ch, float acc, float, float l) { store(r, ch, seen_by(r) > 0 ? acc / l : 0.0f); };
+    auto finish = [&](int r, int ch, float acc, float l) {
+      at.out[row_of(r) * kHd + ch] = __float2bfloat16_rn(seen_by(r) > 0 ? acc / l : 0.0f);
+    };
     if (piece.slot < 0) {
-      meet(finish);
+      meet([&](int r, int ch, float acc, float m, float l) {
+        finish(r, ch, acc, l);
+        if (at.lse != nullptr && ch == 0) at.put_lse((long long)row_of(r), seen_by(r) > 0, m == -INFINITY ? 0.0f : m, l);
+      });
     } else {
       meet([&](int r, int ch, float acc, float m, float l) {
         const size_t row = (size_t)piece.slot * kKvFewRows + r;
@@ -622,7 +613,10 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           }
 #pragma unroll
           for (int d = 1; d < 32; d *= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
-          if (lane == 0) smem_ml[r] = l;
+          if (lane == 0) {
+            smem_ml[r] = l;
+            if (at.lse != nullptr) at.put_lse((long long)row_of(r), seen_by(r) > 0, m_use, l);
+          }
         }
         __syncthreads();
 #pragma unroll 2
@@ -631,7 +625,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           float acc = 0.0f;
 #pragma unroll 8
           for (int w = 0; w < n; ++w) acc += __ldcg(parts + (size_t)w * kKvFewRows * kHd + i) * smem_o[r * n + w];
-          finish(r, i % kHd, acc, 0.0f, smem_ml[r]);
+          finish(r, i % kHd, acc, smem_ml[r]);
         }
       }
     }

@@ -732,6 +732,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
       }
       const bool whole = job.p.slot < 0;
       const float inverse = whole && seen > 0 ? 1.0f / row_sum : 1.0f;
+      if (whole && at.lse != nullptr && c == 0 && live) at.put_lse(out_row, seen > 0, top == -INFINITY ? 0.0f : top, row_sum);
       constexpr int kMine = kHd / kStreams / 32;  // groups of 32 channels of this thread
 #pragma unroll 1
       for (int g = 0; g < kMine; ++g) {
@@ -833,6 +834,7 @@ kv_attn_tiles_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_con
             l += x.y * weight_of(x.x);
           }
           const float inv = 1.0f / l;
+          if (at.lse != nullptr && c == 0) at.put_lse(out_row, seen > 0, use, l);
 #pragma unroll 1
           for (int g = 0; g < kMine; ++g) {
             const int ch0 = (c * kMine + g) * 32;

@@ -113,6 +113,7 @@ kv_append_kernel(KvPool pool, KvArrays arrays, const __nv_bfloat16* __restrict__
   }
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
+    if (pool.weights != nullptr && part == 2 && mine.live(i)) pool.weights[at[i]] = 0.0f;
     if constexpr (kKind == LITEVGGT_KV_E2M1) {
       constexpr int kExps = kHd / 32;
       const uint32_t tops = row_tops<4>(xk[i], xv[i]), bk = kv4_exponent_byte(tops & 0xffffu), bv = kv4_exponent_byte(tops >> 16);

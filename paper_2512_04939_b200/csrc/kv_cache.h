@@ -18,6 +18,7 @@ struct KvPool {
   uint8_t *k, *v;
   uint8_t *k_exp, *v_exp;  // null for bf16
   int kv_heads, page_size, page_shift;
+  float* weights;          // [pages, kv_heads, page_size], what tokens have drawn of the attention; or null
 };
 
 // A batch's arrays on the device.
@@ -46,6 +47,13 @@ struct KvAttend {
   __nv_bfloat16* out;  // [rows, q_heads, head_dim]
   int q_heads, group, causal_block;
   float scale_log2;    // softmax scale in base-2 units
+  float* lse;          // [rows, q_heads] natural logarithms of the rows' sums, or null
+  // the row's, whose sum of 2^(score - reference) is `sum`
+#ifdef __CUDACC__
+  __device__ __forceinline__ void put_lse(long long row, bool sees, float reference, float sum) const {
+    lse[row] = sees ? (reference + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+  }
+#endif
 };
 }  // namespace lv
 
@@ -71,12 +79,15 @@ struct litevggt_kv_batch {
   std::vector<lv::KvSeq> seqs;
   lv::KvWork few, tiles;       // sequences of few rows, and the others
   int few_rows;                // the most of the former
+  lv::KvWeigh weigh;
+  mutable int pages_apart = -1;  // whether no page is named twice; -1: nobody has looked
   std::vector<uint8_t> image;  // what the device gets
   size_t bytes;                // of device memory
   size_t o_seqs, o_pages;
   struct Places {
     size_t pieces, joins, again, rows, sums;
   } at_few, at_tiles;
+  size_t o_few_at, o_tiles_at, o_weigh_joins, o_weigh_sums;
   uint8_t* base = nullptr;     // the caller's device memory
 };
 
@@ -90,6 +101,11 @@ inline KvLaunch kv_launch(const litevggt_kv_batch& b, const KvWork& work, const 
   return KvLaunch{reinterpret_cast<const KvPiece*>(b.base + at.pieces), work.workers(), reinterpret_cast<int*>(b.base + at.joins), reinterpret_cast<int*>(b.base + at.again),
                   reinterpret_cast<float*>(b.base + at.rows), reinterpret_cast<float*>(b.base + at.sums)};
 }
+
+inline long long kv_page_count(const litevggt_kv_batch& b, int page_size) {
+  return b.seqs.back().page0 + ((long long)b.seqs.back().len + page_size - 1) / page_size;
+}
+inline const int* kv_host_pages(const litevggt_kv_batch& b) { return reinterpret_cast<const int*>(b.image.data() + b.o_pages); }
 
 // kv_cache.cu
 cudaError_t launch_kv_append(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const __nv_bfloat16* k, KvStride k_stride,
@@ -119,5 +135,18 @@ constexpr int kKvTileLeast = 4, kKvTileMost = 512;
 // way about, 278 and 256 us, their rows being twice as long.  261 rows over 522 keys: 15.0 us in tiles of two, 14.0 in single ones.
 constexpr double kKvTilePiece64 = 2.0, kKvTilePiece128 = 4.0, kKvJoinCost = 8.0, kKvHalfTiles = 0.8, kKvShortCost = 200.0;
 cudaError_t launch_kv_attn_tiles(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s, int* launches);
+// kv_weigh.cu
+struct KvWeighing {
+  const __nv_bfloat16* q;
+  KvStride q_stride;
+  const float* lse;  // [rows, q_heads]
+  int q_heads, group, causal_block;
+  float scale_log2, decay;
+};
+cudaError_t launch_kv_weigh_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvWeighing& w, cudaStream_t s, int* launches);
+cudaError_t launch_kv_weigh_tiles(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvWeighing& w, cudaStream_t s, int* launches);
+// kv_evict.cu
+cudaError_t launch_kv_evict(const litevggt_kv_cache& c, const litevggt_kv_batch& from, const litevggt_kv_batch& into, int first, int last,
+                            int* kept, cudaStream_t s, int* launches);
 
 }  // namespace lv

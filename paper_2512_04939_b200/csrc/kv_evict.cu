@@ -1,0 +1,269 @@
+// Eviction from the paged K/V cache: every head of every sequence keeps its first and its last tokens and, of the others, those that
+// have drawn most of the attention (of equal tallies the earlier), and all of them move to other pages in the order that they were in.
+//
+// Choosing: one cluster of CTAs for a head of a sequence, each with a run of its tokens.  Tallies become numbers that order as they do,
+// and the least one that stays is found digit by digit (11, 11 and 10 bits): a histogram in each CTA's shared memory, whose bins that
+// are not empty are added up in the first CTA's, which looks for the bin.  Then every warp counts what stays of its own tokens and, when all
+// counts are known, writes their numbers.  Sums are of whole numbers, so nothing depends on an order.
+// Moving: HBM bounds it; 16 bytes of K and of V a lane, a warp's writes side by side in the pages that are filled.
+#include "kv_cache.h"
+#include "kv_quant.cuh"
+
+namespace lv {
+
+namespace {
+
+constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kPickBins = 2048, kPickMostBlocks = 8;
+
+// Orders as the tallies do; zeros are equal, NaN is the least.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  if (x != x) return 0u;
+  const uint32_t bits = __float_as_uint(x + 0.0f);  // -0 + 0 = 0
+  return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
+
+__device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_cluster(uint32_t addr, uint32_t n) {
+  asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(n) : "memory");
+}
+
+struct PickShared {
+  uint32_t bins[kPickBins];   // of this CTA's tokens
+  uint32_t joint[kPickBins];  // of the cluster's, in its first CTA
+  uint32_t warp_sums[kPickWarps][2];
+  uint32_t counts[2];         // of this CTA: above the least that stays, equal to it
+  uint32_t bin, left;         // first CTA: the bin that the least one lies in, how many of it stay
+  uint32_t scan[kPickWarps];
+};
+
+// blockIdx.x = (sequence * heads + head) * blocks of a cluster + block
+__global__ void __launch_bounds__(kPickThreads)
+kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, int blocks, int* kept) {
+  __shared__ PickShared sh;
+  const int rank = blocks > 1 ? (int)cluster_ctarank() : 0, pair = (int)blockIdx.x / blocks;
+  const int head = pair % pool.kv_heads, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  wait_for_previous_kernel();
+  const KvSeq src = from.seqs[pair / pool.kv_heads], dst = into.seqs[pair / pool.kv_heads];
+  const int n = src.len, m = dst.len;
+  int* out = kept + (long long)dst.row0 * pool.kv_heads + head;  // the i-th kept token's number at i * heads
+  auto put = [&](int at, int token) { out[(long long)at * pool.kv_heads] = token; };
+  const int all = blocks * kPickThreads, mine = rank * kPickThreads + threadIdx.x;
+  if (m >= n) {  // (the same for the whole cluster)
+    for (int i = mine; i < m; i += all) put(i, i);
+    return;
+  }
+  for (int i = mine; i < first; i += all) put(i, i);
+  for (int i = mine; i < last; i += all) put(m - last + i, n - last + i);
+  const int choose = m - first - last;  // of the tokens in between
+  if (choose <= 0) return;
+  // this warp's run of them, in whole warps' steps
+  const int span = n - first - last, warps = blocks * kPickWarps;
+  const int run = (int)((((long long)span + warps - 1) / warps + 31) / 32 * 32);
+  const long long begin64 = (long long)(rank * kPickWarps + warp) * run;
+  const int begin = (int)min(begin64, (long long)span), end = (int)min(begin64 + run, (long long)span);
+  auto order_at = [&](int i) {
+    const int token = first + i;
+    const size_t page = (size_t)from.pages[src.page0 + (token >> pool.page_shift)];
+    return order_of(pool.weights[((page * pool.kv_heads + head) << pool.page_shift) + (token & (pool.page_size - 1))]);
+  };
+  auto together = [&]() {
+    if (blocks > 1) cluster_sync();
+    else __syncthreads();
+  };
+  const uint32_t joint0 = blocks > 1 ? mapa_u32(smem_u32(sh.joint), 0) : smem_u32(sh.joint);
+
+  uint32_t prefix = 0, known = 0, left = (uint32_t)choose;  // the upper bits of the least that stays; their mask; how many of those with them stay
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t digits = pass == 2 ? 1023u : 2047u;
+    for (int i = threadIdx.x; i < kPickBins; i += kPickThreads) sh.bins[i] = sh.joint[i] = 0u;
+    together();
+    for (int at = begin; at < end; at += 32) {
+      const int i = at + lane;
+      const uint32_t x = i < end ? order_at(i) : 0u;
+      const bool counts = i < end && (x & known) == prefix;
+      const uint32_t bin = x >> shift & digits, active = __ballot_sync(0xffffffffu, counts);
+      if (active == 0u) continue;
+      // one of all where they agree, as where no tallies have been taken
+      const uint32_t some = __shfl_sync(0xffffffffu, bin, __ffs(active) - 1);
+      if (__all_sync(0xffffffffu, !counts || bin == some)) {
+        if (lane == 0) atomicAdd(&sh.bins[some], (uint32_t)__popc(active));
+      } else if (counts) {
+        atomicAdd(&sh.bins[bin], 1u);
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kPickBins; i += kPickThreads)
+      if (sh.bins[i] != 0u) add_cluster(joint0 + 4 * i, sh.bins[i]);
+    together();
+    if (rank == 0) {
+      // the bin that holds the left-th largest: the first one from above whose sum with those above it reaches that
+      constexpr int kEach = kPickBins / kPickThreads;
+      uint32_t own = 0;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) own += sh.joint[kPickBins - 1 - (threadIdx.x * kEach + e)];
+      uint32_t upto = own;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      if (lane == 31) sh.scan[warp] = upto;
+      __syncthreads();
+      uint32_t above = upto - own;
+      for (int w = 0; w < warp; ++w) above += sh.scan[w];
+      if (above < left && above + own >= left) {
+        for (int e = 0; e < kEach; ++e) {
+          const int bin = kPickBins - 1 - (threadIdx.x * kEach + e);
+          const uint32_t here = sh.joint[bin];
+          if (above < left && above + here >= left) {
+            sh.bin = (uint32_t)bin;
+            sh.left = left - above;
+          }
+          above += here;
+        }
+      }
+    }
+    together();
+    const uint32_t at_bin = blocks > 1 ? mapa_u32(smem_u32(&sh.bin), 0) : smem_u32(&sh.bin);
+    const uint32_t at_left = blocks > 1 ? mapa_u32(smem_u32(&sh.left), 0) : smem_u32(&sh.left);
+    prefix |= ld_cluster(at_bin) << shift;
+    known |= digits << shift;
+    left = ld_cluster(at_left);
+  }
+  // prefix: the least that stays; left: how many of its equals do, from the front
+
+  uint32_t above = 0, equal = 0;  // of this warp
+  for (int at = begin; at < end; at += 32) {
+    const int i = at + lane;
+    const uint32_t x = i < end ? order_at(i) : 0u;
+    above += __popc(__ballot_sync(0xffffffffu, i < end && x > prefix));
+    equal += __popc(__ballot_sync(0xffffffffu, i < end && x == prefix));
+  }
+  if (lane == 0) sh.warp_sums[warp][0] = above, sh.warp_sums[warp][1] = equal;
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    uint32_t sum = 0;
+    for (int w = 0; w < kPickWarps; ++w) sum += sh.warp_sums[w][threadIdx.x];
+    sh.counts[threadIdx.x] = sum;
+  }
+  together();
+  above = equal = 0;  // in front of this warp
+  for (int r = 0; r < rank; ++r) {
+    above += ld_cluster(mapa_u32(smem_u32(&sh.counts[0]), r));
+    equal += ld_cluster(mapa_u32(smem_u32(&sh.counts[1]), r));
+  }
+  for (int w = 0; w < warp; ++w) above += sh.warp_sums[w][0], equal += sh.warp_sums[w][1];
+  const uint32_t before = (1u << lane) - 1u;
+  for (int at = begin; at < end; at += 32) {
+    const int i = at + lane;
+    const uint32_t x = i < end ? order_at(i) : 0u;
+    const uint32_t over = __ballot_sync(0xffffffffu, i < end && x > prefix), same = __ballot_sync(0xffffffffu, i < end && x == prefix);
+    const uint32_t rank_over = above + __popc(over & before), rank_same = equal + __popc(same & before);
+    const bool stays = i < end && (x > prefix || (x == prefix && rank_same < left));
+    if (stays) put(first + (int)(rank_over + min(rank_same, left)), first + i);
+    above += __popc(over);
+    equal += __popc(same);
+  }
+  together();  // nobody's shared memory goes while others read it
+}
+
+constexpr int kMoveThreads = 256;
+
+// Places of the pages that are filled, one after another: (page of the list, head, token in the page).
+template <int kHd, int kKind, int kUnits>
+__global__ void __launch_bounds__(kMoveThreads)
+kv_move_kernel(KvPool pool, KvArrays from, KvArrays into, const int* __restrict__ kept, long long units) {
+  constexpr int kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps, kLanes = kRowBytes / 16, kGroups = kMoveThreads / kLanes;
+  wait_for_previous_kernel();
+  const int part = threadIdx.x % kLanes;
+  const long long unit0 = (long long)blockIdx.x * (kGroups * kUnits) + threadIdx.x / kLanes;
+  size_t to[kUnits], at[kUnits];
+  bool live[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const long long unit = unit0 + i * kGroups;
+    live[i] = unit < units;
+    to[i] = at[i] = 0;
+    if (!live[i]) continue;
+    const int offset = (int)(unit & (pool.page_size - 1));
+    const long long in_pages = unit >> pool.page_shift;
+    const int head = (int)(in_pages % pool.kv_heads), entry = (int)(in_pages / pool.kv_heads);
+    int lo = 0, hi = into.n_seq - 1;
+    while (lo < hi) {  // the last sequence that begins at or before the page; ones without pages share their successor's start
+      const int mid = (lo + hi + 1) >> 1;
+      if (into.seqs[mid].page0 <= entry) lo = mid;
+      else hi = mid - 1;
+    }
+    const KvSeq dst = into.seqs[lo];
+    const int slot = ((entry - dst.page0) << pool.page_shift) + offset;
+    live[i] = slot < dst.len;
+    if (!live[i]) continue;
+    const int token = kept[(long long)(dst.row0 + slot) * pool.kv_heads + head];
+    const size_t source = (size_t)from.pages[from.seqs[lo].page0 + (token >> pool.page_shift)], target = (size_t)into.pages[entry];
+    at[i] = ((source * pool.kv_heads + head) << pool.page_shift) + (token & (pool.page_size - 1));
+    to[i] = ((target * pool.kv_heads + head) << pool.page_shift) + offset;
+  }
+  uint4 xk[kUnits], xv[kUnits];
+  uint32_t ek[kUnits], ev[kUnits];
+  float w[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    if (!live[i]) continue;
+    xk[i] = ldg16(pool.k + at[i] * kRowBytes + part * 16);
+    xv[i] = ldg16(pool.v + at[i] * kRowBytes + part * 16);
+    if (kExps > 0 && part < kExps) {  // (a row of E2M1 codes has as many lanes as exponents)
+      ek[i] = pool.k_exp[at[i] * kExps + part];
+      ev[i] = pool.v_exp[at[i] * kExps + part];
+    }
+    if (part == 0) w[i] = pool.weights[at[i]];
+  }
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    if (!live[i]) continue;
+    stg16(pool.k + to[i] * kRowBytes + part * 16, xk[i]);
+    stg16(pool.v + to[i] * kRowBytes + part * 16, xv[i]);
+    if (kExps > 0 && part < kExps) {
+      pool.k_exp[to[i] * kExps + part] = (uint8_t)ek[i];
+      pool.v_exp[to[i] * kExps + part] = (uint8_t)ev[i];
+    }
+    if (part == 0) pool.weights[to[i]] = w[i];
+  }
+}
+
+template <int kHd, int kKind>
+cudaError_t move(const litevggt_kv_cache& c, const litevggt_kv_batch& from, const litevggt_kv_batch& into, const int* kept, long long pages, cudaStream_t s) {
+  constexpr int kLanes = KvRow<kHd, kKind>::kBytes / 16, kGroups = kMoveThreads / kLanes;
+  static_assert(KvRow<kHd, kKind>::kExps <= kLanes, "");
+  const long long units = pages * c.cfg.kv_heads * c.cfg.page_size, blocks = (units + kGroups - 1) / kGroups;
+  if (blocks <= (long long)c.num_sms * (2048 / kMoveThreads))
+    return launch(kv_move_kernel<kHd, kKind, 1>, dim3((unsigned)blocks), kMoveThreads, 0, s, c.pool, kv_arrays(from), kv_arrays(into), kept, units);
+  return launch(kv_move_kernel<kHd, kKind, 2>, dim3((unsigned)((blocks + 1) / 2)), kMoveThreads, 0, s, c.pool, kv_arrays(from), kv_arrays(into), kept, units);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_evict(const litevggt_kv_cache& c, const litevggt_kv_batch& from, const litevggt_kv_batch& into, int first, int last,
+                            int* kept, cudaStream_t s, int* launches) {
+  const long long pairs = (long long)from.seqs.size() * c.cfg.kv_heads;
+  // CTAs of a head: as many as there is room for, where its tokens are more than a CTA's threads look at a few times
+  int longest = 0, blocks = 1;
+  for (const KvSeq& q : from.seqs) longest = std::max(longest, q.len);
+  while (blocks < kPickMostBlocks && 2 * blocks * pairs <= 2ll * c.num_sms && longest > blocks * 8 * kPickThreads) blocks *= 2;
+  cudaError_t e = launch_clusters(blocks, true, kv_pick_kernel, dim3((unsigned)(pairs * blocks)), kPickThreads, 0, s, c.pool, kv_arrays(from),
+                                  kv_arrays(into), first, last, blocks, kept);
+  ++*launches;
+  const long long pages = kv_page_count(into, c.cfg.page_size);
+  if (e != cudaSuccess || pages == 0) return e;
+  ++*launches;
+  const bool wide = c.cfg.head_dim == 128;
+  if (c.cfg.dtype == LITEVGGT_KV_E2M1) return wide ? move<128, LITEVGGT_KV_E2M1>(c, from, into, kept, pages, s) : move<64, LITEVGGT_KV_E2M1>(c, from, into, kept, pages, s);
+  if (c.cfg.dtype == LITEVGGT_KV_E4M3) return wide ? move<128, LITEVGGT_KV_E4M3>(c, from, into, kept, pages, s) : move<64, LITEVGGT_KV_E4M3>(c, from, into, kept, pages, s);
+  return wide ? move<128, LITEVGGT_KV_BF16>(c, from, into, kept, pages, s) : move<64, LITEVGGT_KV_BF16>(c, from, into, kept, pages, s);
+}
+
+}  // namespace lv

@@ -173,4 +173,51 @@ inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& whi
   return work;
 }
 
+// How tallies are taken (litevggt_kv_weigh).  Sequences of few rows: units of 32 keys of one head, dealt out in runs.  The others: items
+// of `key_block` keys of one head, the rows that see them in `parts` runs of row tiles.  *_at: units or items of a head of all sequences
+// before the i-th.
+struct KvWeigh {
+  std::vector<long long> few_at, tiles_at;
+  int key_block = 256, parts = 1;
+  long long items = 0;  // of all heads
+};
+constexpr int kKvWeighUnit = 32;
+constexpr int kKvWeighRows = 128;  // of a row tile
+
+inline KvWeigh kv_weigh_plan(const std::vector<KvSeq>& seqs, int group, int kv_heads, int few_rows, int sms) {
+  KvWeigh w;
+  long long few = 0, blocks[2] = {0, 0}, row_tiles = 0;
+  for (const KvSeq& q : seqs) {
+    w.few_at.push_back(few);
+    const long long r = (long long)q.rows * group;
+    if (r > 0 && r <= few_rows) few += ((long long)q.len + kKvWeighUnit - 1) / kKvWeighUnit;
+    if (r > few_rows) {
+      for (int i = 0; i < 2; ++i) blocks[i] += ((long long)q.len + 128 * (i + 1) - 1) / (128 * (i + 1));
+      row_tiles = std::max(row_tiles, (r + kKvWeighRows - 1) / kKvWeighRows);
+    }
+  }
+  w.few_at.push_back(few);
+  // What fills the chip best: a CTA's time goes by 128 keys against 128 rows, and beside them it has its keys to fetch.
+  constexpr double kFetch = 1.0;
+  double least = 0.0;
+  for (int i = 0; i < 2; ++i)
+    for (int parts = 1; parts <= 64 && parts <= std::max(row_tiles, 1ll) && (parts == 1 || blocks[i] * kv_heads * parts <= 4ll * sms); ++parts) {
+      const double waves = (double)((blocks[i] * kv_heads * parts + sms - 1) / sms);
+      const double cost = waves * ((i + 1) * (double)((row_tiles + parts - 1) / parts) + kFetch) + (parts > 1 ? kFetch : 0.0);
+      if (least == 0.0 || cost < 0.999 * least) {
+        least = cost;
+        w.key_block = 128 * (i + 1);
+        w.parts = parts;
+      }
+    }
+  long long at = 0;
+  for (const KvSeq& q : seqs) {
+    w.tiles_at.push_back(at);
+    if ((long long)q.rows * group > few_rows) at += ((long long)q.len + w.key_block - 1) / w.key_block;
+  }
+  w.tiles_at.push_back(at);
+  w.items = at * kv_heads;
+  return w;
+}
+
 }  // namespace lv

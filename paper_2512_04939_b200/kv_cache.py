@@ -5,6 +5,14 @@
     cache.append(batch, k, v)                                              # the last 1041 tokens of the sequence
     out = cache.attend(batch, q)                                           # over all 52050
 
+With tallies (``KVCache.empty(..., weights=True)``) the cache knows what its tokens have drawn of the attention, and keeps those that
+drew most when it has to make room:
+
+    out, lse = cache.attend(batch, q, lse=True)
+    cache.weigh(batch, q, lse)
+    into = cache.batch(rows=[20000], lengths=[20000], pages=[other_page_ids])
+    kept = cache.evict(batch, into, first=5, last=1041)                    # [20000, kv_heads]: which tokens these are now
+
 Which pages a sequence owns is the caller's business; the library checks that they exist - in the pool of the cache that plans the
 batch, and no other cache takes it.  Shapes, types, strides and
 devices are checked here, everything else in the C library.
@@ -59,9 +67,11 @@ class KVCache:
     """A cache over pools of the caller's: ``k``, ``v`` [pages, kv_heads, page_size, head_dim], bfloat16; or float8_e4m3fn with the
     exponents ``k_exp``, ``v_exp`` uint8 [pages, kv_heads, page_size]; or 4 bits, E2M1 codes two to a byte in uint8
     [pages, kv_heads, page_size, head_dim / 2] (the even channel's in the low half) with exponents for every 32 channels, uint8
-    [pages, kv_heads, page_size, head_dim / 32]."""
+    [pages, kv_heads, page_size, head_dim / 32].  ``weights`` float32 [pages, kv_heads, page_size]: tallies of the attention that tokens draw
+    (see :meth:`weigh`), zero for those that :meth:`append` writes."""
 
-    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None):
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None,
+                 weights: torch.Tensor | None = None):
         self.lib = load_library()
         if k.dim() != 4 or v.shape != k.shape:
             raise ValueError(f"k and v must both be [pages, kv_heads, page_size, head_dim], got {tuple(k.shape)} and {tuple(v.shape)}")
@@ -79,16 +89,21 @@ class KVCache:
                 tensors[name] = t
         elif k_exp is not None or v_exp is not None:
             raise ValueError("bfloat16 pools have no exponents")
+        if weights is not None:
+            if weights.dtype != torch.float32 or weights.shape != k.shape[:3]:
+                raise ValueError(f"weights must be float32 {tuple(k.shape[:3])}, got {weights.dtype} {tuple(weights.shape)}")
+            tensors["weights"] = weights
         for name, t in tensors.items():
             if not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
             if not t.is_cuda or t.device != k.device:
                 raise ValueError("every pool must live on the same CUDA device")
-        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.k, self.v, self.k_exp, self.v_exp, self.weights = k, v, k_exp, v_exp, weights
         self.device, self._index = k.device, k.get_device()
         self.pages, self.kv_heads, self.page_size, self.head_dim = *k.shape[:3], head_dim
         self._scale = 1.0 / math.sqrt(self.head_dim)
-        self._append, self._attend = self.lib.litevggt_kv_append, self.lib.litevggt_kv_attend
+        self._append, self._attend = self.lib.litevggt_kv_append, self.lib.litevggt_kv_attend_lse
+        self._weigh = self.lib.litevggt_kv_weigh
         self.status = torch.zeros(64, dtype=torch.int32, device=k.device)
         self._home = self._stream()
         cfg = KVConfig(self.pages, self.page_size, self.kv_heads, self.head_dim, number)
@@ -96,10 +111,13 @@ class KVCache:
         _check(self.lib.litevggt_kv_create(C.byref(cfg), self.device.index, *(C.c_void_p(t.data_ptr()) if t is not None else None
                                                                              for t in (k, v, k_exp, v_exp, self.status)),
                                            C.byref(self.handle)), "kv_create")
+        if weights is not None:
+            _check(self.lib.litevggt_kv_track(self.handle, weights.data_ptr()), "kv_track")
 
     @classmethod
-    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype: str = "bf16", device: int = 0) -> "KVCache":
-        """A cache with pools of its own, not initialised."""
+    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype: str = "bf16", device: int = 0,
+              weights: bool = False) -> "KVCache":
+        """A cache with pools of its own, not initialised; with tallies if ``weights``."""
         if dtype not in _DTYPES:
             raise ValueError(f"dtype must be one of {sorted(_DTYPES)}, got {dtype!r}")
         where = torch.device("cuda", device)
@@ -108,7 +126,7 @@ class KVCache:
         pools = [torch.empty((*shape, head_dim // packed), dtype=kind, device=where) for _ in range(2)]
         if block:
             pools += [torch.empty(shape if block < 0 else (*shape, head_dim // block), dtype=torch.uint8, device=where) for _ in range(2)]
-        return cls(*pools)
+        return cls(*pools, weights=torch.empty(shape, device=where) if weights else None)
 
     def close(self):
         if getattr(self, "handle", None) is not None and self.handle.value:
@@ -169,10 +187,11 @@ class KVCache:
         _check(self.lib.litevggt_kv_gather(self.handle, batch.handle, k.data_ptr(), v.data_ptr(), self._use(batch)), "kv_gather")
         return k, v
 
-    def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    def attend(self, batch: KVBatch, q: torch.Tensor, scale: float | None = None, out: torch.Tensor | None = None, lse=False):
         """softmax(scale q K^T) V of the batch's rows over the tokens that they see; ``q`` bfloat16 [batch.rows, q_heads, head_dim].
         ``scale`` is 1 / sqrt(head_dim) unless given (positive, less than 1e30).  ``out``, if given, must not lie where ``q`` does.  A row that sees no token
-        comes out as zero."""
+        comes out as zero.  With ``lse`` (True, or a contiguous float32 tensor [batch.rows, q_heads] to be filled) the result is the pair of
+        the output and log sum_j exp(scale q . k_j), minus infinity for a row that sees no token."""
         q_rows = self._rows("q", q, batch.q_shape)
         if out is None:
             out = q.new_empty(batch.q_shape)
@@ -180,10 +199,43 @@ class KVCache:
             self._rows("out", out, batch.q_shape)
             if not out.is_contiguous():
                 raise ValueError("out must be contiguous")
-        code = self._attend(self.handle, batch.handle, *q_rows, self._scale if scale is None else scale, out.data_ptr(), self._use(batch))
+        if lse is True:
+            lse = torch.empty(batch.q_shape[:2], dtype=torch.float32, device=self.device)
+        elif lse is not False:
+            self._sums(batch, lse)
+        code = self._attend(self.handle, batch.handle, *q_rows, self._scale if scale is None else scale, out.data_ptr(),
+                            None if lse is False else lse.data_ptr(), self._use(batch))
         if code:
             _check(code, "kv_attend")
-        return out
+        return out if lse is False else (out, lse)
+
+    # ------------------------------------------------------------------ what stays
+    def weigh(self, batch: KVBatch, q: torch.Tensor, lse: torch.Tensor, scale: float | None = None, decay: float = 1.0) -> None:
+        """Adds to the tallies of all tokens that the batch's sequences hold (those that have rows in it) what they draw of the rows'
+        attention: w_j = decay w_j + sum_i exp(scale q_i . k_j - lse_i), over the rows that see token j and the query heads that share its
+        head.  ``lse`` is that of :meth:`attend` on the same queries.  ``decay`` in [0, 1]; 0 begins anew, whatever was there."""
+        q_rows = self._rows("q", q, batch.q_shape)
+        self._sums(batch, lse)
+        if self.weights is None:
+            raise ValueError("the cache has no tallies (weights)")
+        code = self._weigh(self.handle, batch.handle, *q_rows, self._scale if scale is None else scale, lse.data_ptr(), decay, self._use(batch))
+        if code:
+            _check(code, "kv_weigh")
+
+    def evict(self, batch: KVBatch, into: KVBatch, first: int = 0, last: int = 0) -> torch.Tensor:
+        """Every head of every sequence of ``batch`` keeps as many tokens as ``into`` has for it (a batch of the same number of sequences,
+        with as many rows as tokens, in pages that ``batch`` does not name): its ``first`` first ones, its ``last`` last ones, and of the
+        others those with the largest tallies, of equal ones the earlier, a NaN being less than any number.  They move to the pages of ``into``
+        in the order that they were in, tallies and all; the pages that they come from stay as they are.  Returns which tokens they were,
+        int32 [into.rows, kv_heads]."""
+        if self.weights is None:
+            raise ValueError("the cache has no tallies (weights)")
+        if max(abs(first), abs(last)) >= 2 ** 31:
+            raise ValueError(f"first and last must be less than 2^31, got {first} and {last}")
+        kept = torch.empty(into.kv_shape[:2], dtype=torch.int32, device=self.device)
+        self._use(into)
+        _check(self.lib.litevggt_kv_evict(self.handle, batch.handle, into.handle, first, last, kept.data_ptr(), self._use(batch)), "kv_evict")
+        return kept
 
     # ------------------------------------------------------------------ checks
     def poll(self):
@@ -205,10 +257,14 @@ class KVCache:
         if stream != batch._stream or stream != self._home:
             here = torch.cuda.current_stream(self.device)
             batch.memory.record_stream(here)
-            for t in (self.k, self.v, self.k_exp, self.v_exp, self.status):
+            for t in (self.k, self.v, self.k_exp, self.v_exp, self.weights, self.status):
                 if t is not None:
                     t.record_stream(here)
         return stream
+
+    def _sums(self, batch: KVBatch, lse: torch.Tensor) -> None:
+        if lse.shape != batch.q_shape[:2] or lse.dtype != torch.float32 or lse.get_device() != self._index or not lse.is_contiguous():
+            raise ValueError(f"lse must be contiguous float32 {list(batch.q_shape[:2])} on {self.device}, got {lse.dtype} {tuple(lse.shape)} on {lse.device}")
 
     def _rows(self, name: str, t: torch.Tensor, shape: tuple) -> tuple[int, int, int]:
         """A checked tensor's address and its strides from row to row and head to head (that of a dimension of one says nothing)."""
