@@ -2,7 +2,7 @@
 // have drawn most of the attention (of equal tallies the earlier), and all of them move to other pages in the order that they were in.
 //
 // Choosing: one cluster of CTAs for a head of a sequence, each with a run of its tokens.  Tallies become numbers that order as they do,
-// and the least one that stays is found digit by digit (11, 11 and 10 bits): a histogram in each CTA's shared memory, whose bins that
+// in shared memory, and the least one that stays is found digit by digit (11, 11 and 10 bits): a histogram in each CTA, whose bins that
 // are not empty are added up in the first CTA's, which looks for the bin.  Then every warp counts what stays of its own tokens and, when all
 // counts are known, writes their numbers.  Sums are of whole numbers, so nothing depends on an order.
 // Moving: HBM bounds it; 16 bytes of K and of V a lane, a warp's writes side by side in the pages that are filled.
@@ -13,7 +13,10 @@ namespace lv {
 
 namespace {
 
-constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kPickBins = 2048, kPickMostBlocks = 8;
+constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kPickBins = 2048;
+constexpr int kPickMostBlocks = 16, kPickPortableBlocks = 8;  // of a cluster
+constexpr int kPickAhead = 8;                                 // loads of a thread that are under way together
+constexpr int kPickMostHeld = 48 * 1024;                      // tallies in a CTA's shared memory; what lies behind them is read again
 
 // Orders as the tallies do; zeros are equal, NaN is the least.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -40,15 +43,17 @@ struct PickShared {
   uint32_t scan[kPickWarps];
 };
 
-// blockIdx.x = (sequence * heads + head) * blocks of a cluster + block
+// blockIdx.x = (sequence * heads + head) * blocks of a cluster + block; `held`: numbers that a warp keeps in shared memory
 __global__ void __launch_bounds__(kPickThreads)
-kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, int blocks, int* kept) {
+kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, int blocks, int held, int* kept) {
   __shared__ PickShared sh;
+  extern __shared__ uint32_t numbers[];  // [warp][held]
   const int rank = blocks > 1 ? (int)cluster_ctarank() : 0, pair = (int)blockIdx.x / blocks;
   const int head = pair % pool.kv_heads, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  wait_for_previous_kernel();
+  // (a batch's arrays were there before whatever kernel is still running)
   const KvSeq src = from.seqs[pair / pool.kv_heads], dst = into.seqs[pair / pool.kv_heads];
   const int n = src.len, m = dst.len;
+  wait_for_previous_kernel();
   int* out = kept + (long long)dst.row0 * pool.kv_heads + head;  // the i-th kept token's number at i * heads
   auto put = [&](int at, int token) { out[(long long)at * pool.kv_heads] = token; };
   const int all = blocks * kPickThreads, mine = rank * kPickThreads + threadIdx.x;
@@ -65,11 +70,27 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
   const int run = (int)((((long long)span + warps - 1) / warps + 31) / 32 * 32);
   const long long begin64 = (long long)(rank * kPickWarps + warp) * run;
   const int begin = (int)min(begin64, (long long)span), end = (int)min(begin64 + run, (long long)span);
-  auto order_at = [&](int i) {
+  auto tally_of = [&](int i) {
     const int token = first + i;
     const size_t page = (size_t)from.pages[src.page0 + (token >> pool.page_shift)];
-    return order_of(pool.weights[((page * pool.kv_heads + head) << pool.page_shift) + (token & (pool.page_size - 1))]);
+    return pool.weights[((page * pool.kv_heads + head) << pool.page_shift) + (token & (pool.page_size - 1))];
   };
+  uint32_t* mine_held = numbers + warp * held;
+  for (int at = begin; at < min(end, begin + held); at += 32 * kPickAhead) {
+    float x[kPickAhead];
+#pragma unroll
+    for (int j = 0; j < kPickAhead; ++j) {
+      const int i = at + 32 * j + lane;
+      if (i < end && i < begin + held) x[j] = tally_of(i);
+    }
+#pragma unroll
+    for (int j = 0; j < kPickAhead; ++j) {
+      const int i = at + 32 * j + lane;
+      if (i < end && i < begin + held) mine_held[i - begin] = order_of(x[j]);
+    }
+  }
+  // (a thread reads what it has written itself: numbers 32 apart)
+  auto order_at = [&](int i) { return i < begin + held ? mine_held[i - begin] : order_of(tally_of(i)); };
   auto together = [&]() {
     if (blocks > 1) cluster_sync();
     else __syncthreads();
@@ -179,20 +200,21 @@ template <int kHd, int kKind, int kUnits>
 __global__ void __launch_bounds__(kMoveThreads)
 kv_move_kernel(KvPool pool, KvArrays from, KvArrays into, const int* __restrict__ kept, long long units) {
   constexpr int kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps, kLanes = kRowBytes / 16, kGroups = kMoveThreads / kLanes;
-  wait_for_previous_kernel();
   const int part = threadIdx.x % kLanes;
   const long long unit0 = (long long)blockIdx.x * (kGroups * kUnits) + threadIdx.x / kLanes;
   size_t to[kUnits], at[kUnits];
+  long long number[kUnits];  // in the list of kept tokens
+  int head[kUnits], page0[kUnits];
   bool live[kUnits];
 #pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
+  for (int i = 0; i < kUnits; ++i) {  // (a batch's arrays were there before whatever kernel is still running)
     const long long unit = unit0 + i * kGroups;
     live[i] = unit < units;
-    to[i] = at[i] = 0;
     if (!live[i]) continue;
     const int offset = (int)(unit & (pool.page_size - 1));
     const long long in_pages = unit >> pool.page_shift;
-    const int head = (int)(in_pages % pool.kv_heads), entry = (int)(in_pages / pool.kv_heads);
+    const int entry = (int)(in_pages / pool.kv_heads);
+    head[i] = (int)(in_pages % pool.kv_heads);
     int lo = 0, hi = into.n_seq - 1;
     while (lo < hi) {  // the last sequence that begins at or before the page; ones without pages share their successor's start
       const int mid = (lo + hi + 1) >> 1;
@@ -202,11 +224,20 @@ kv_move_kernel(KvPool pool, KvArrays from, KvArrays into, const int* __restrict_
     const KvSeq dst = into.seqs[lo];
     const int slot = ((entry - dst.page0) << pool.page_shift) + offset;
     live[i] = slot < dst.len;
+    number[i] = (long long)(dst.row0 + slot) * pool.kv_heads + head[i];
+    page0[i] = from.seqs[lo].page0;
+    to[i] = (((size_t)into.pages[entry] * pool.kv_heads + head[i]) << pool.page_shift) + offset;
+  }
+  wait_for_previous_kernel();
+  int token[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i)
+    if (live[i]) token[i] = kept[number[i]];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
     if (!live[i]) continue;
-    const int token = kept[(long long)(dst.row0 + slot) * pool.kv_heads + head];
-    const size_t source = (size_t)from.pages[from.seqs[lo].page0 + (token >> pool.page_shift)], target = (size_t)into.pages[entry];
-    at[i] = ((source * pool.kv_heads + head) << pool.page_shift) + (token & (pool.page_size - 1));
-    to[i] = ((target * pool.kv_heads + head) << pool.page_shift) + offset;
+    const size_t page = (size_t)from.pages[page0[i] + (token[i] >> pool.page_shift)];
+    at[i] = ((page * pool.kv_heads + head[i]) << pool.page_shift) + (token[i] & (pool.page_size - 1));
   }
   uint4 xk[kUnits], xv[kUnits];
   uint32_t ek[kUnits], ev[kUnits];
@@ -245,17 +276,50 @@ cudaError_t move(const litevggt_kv_cache& c, const litevggt_kv_batch& from, cons
   return launch(kv_move_kernel<kHd, kKind, 2>, dim3((unsigned)((blocks + 1) / 2)), kMoveThreads, 0, s, c.pool, kv_arrays(from), kv_arrays(into), kept, units);
 }
 
+// Blocks of a cluster at most: 16 SMs where the device has that many together (more than the eight that every one has to offer).
+// Looked up once for each device.
+int pick_blocks() {
+  static std::atomic<unsigned long long> asked{0}, fits{0};
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return kPickPortableBlocks;
+  const unsigned long long bit = 1ull << (device & 63);
+  if ((asked.load(std::memory_order_acquire) & bit) == 0) {
+    const void* kernel = reinterpret_cast<const void*>(kv_pick_kernel);
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = kPickMostBlocks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kPickMostBlocks);
+    cfg.blockDim = dim3(kPickThreads);
+    cfg.dynamicSmemBytes = kPickMostHeld * 4;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPickMostHeld * 4) == cudaSuccess &&
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+        cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0)
+      fits.fetch_or(bit);
+    else (void)cudaGetLastError();
+    asked.fetch_or(bit, std::memory_order_release);
+  }
+  return (fits.load(std::memory_order_relaxed) & bit) != 0 ? kPickMostBlocks : kPickPortableBlocks;
+}
+
 }  // namespace
 
 cudaError_t launch_kv_evict(const litevggt_kv_cache& c, const litevggt_kv_batch& from, const litevggt_kv_batch& into, int first, int last,
                             int* kept, cudaStream_t s, int* launches) {
   const long long pairs = (long long)from.seqs.size() * c.cfg.kv_heads;
-  // CTAs of a head: as many as there is room for, where its tokens are more than a CTA's threads look at a few times
+  // CTAs of a head: as many as there is room for, where its tokens are more than four for each of a CTA's threads
   int longest = 0, blocks = 1;
   for (const KvSeq& q : from.seqs) longest = std::max(longest, q.len);
-  while (blocks < kPickMostBlocks && 2 * blocks * pairs <= 2ll * c.num_sms && longest > blocks * 8 * kPickThreads) blocks *= 2;
-  cudaError_t e = launch_clusters(blocks, true, kv_pick_kernel, dim3((unsigned)(pairs * blocks)), kPickThreads, 0, s, c.pool, kv_arrays(from),
-                                  kv_arrays(into), first, last, blocks, kept);
+  const int most = pick_blocks();
+  while (blocks < most && 2 * blocks * pairs <= 2ll * c.num_sms && longest > blocks * 4 * kPickThreads) blocks *= 2;
+  const long long run = round_up(((long long)longest + blocks * kPickWarps - 1) / (blocks * kPickWarps), 32);
+  const int held = (int)std::min(run, (long long)kPickMostHeld / kPickWarps);
+  cudaError_t e = launch_clusters(blocks, true, kv_pick_kernel, dim3((unsigned)(pairs * blocks)), kPickThreads, (size_t)held * kPickWarps * 4, s, c.pool,
+                                  kv_arrays(from), kv_arrays(into), first, last, blocks, held, kept);
   ++*launches;
   const long long pages = kv_page_count(into, c.cfg.page_size);
   if (e != cudaSuccess || pages == 0) return e;

@@ -14,6 +14,14 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// 16 bytes to shared memory, or zeros.
+__device__ __forceinline__ void cp_async16(uint8_t* dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
 // What a launch over either kind of sequence is given.
 struct WeighLists {
   const long long* at;  // units or items of a head before each sequence
@@ -22,15 +30,18 @@ struct WeighLists {
   float* sums;
 };
 
-// The sequence that number n of all heads' units belongs to.
+// The sequence that number n of all heads' units belongs to: the last one that begins at or before it (ones without units share their
+// successor's start).  The whole warp looks, 32 at a time.
 __device__ __forceinline__ int seq_of_unit(const long long* at, int n_seq, int heads, long long n) {
-  int lo = 0, hi = n_seq - 1;
-  while (lo < hi) {  // the last one that begins at or before it; ones without units share their successor's start
-    const int mid = (lo + hi + 1) >> 1;
-    if (at[mid] * heads <= n) lo = mid;
-    else hi = mid - 1;
+  const int lane = threadIdx.x & 31;
+  int found = 0;
+  for (int base = 0; base < n_seq; base += 32) {
+    const bool begun = base + lane < n_seq && at[base + lane] * heads <= n;
+    const uint32_t those = __ballot_sync(0xffffffffu, begun);
+    if (those == 0u) break;
+    found = base + 31 - __clz(those);
   }
-  return lo;
+  return found;
 }
 
 __device__ __forceinline__ float tallied(float decay, float before, float sum) { return decay == 0.0f ? sum : fmaf(decay, before, sum); }
@@ -41,7 +52,7 @@ __device__ __forceinline__ float tallied(float decay, float before, float sum) {
 // HBM bounds it: K once, 4 operations a byte at one row; a unit's 4 KB are all under way at once.
 constexpr int kWeighWarps = 4;
 
-template <int kHd, int kKind, bool kHalf>
+template <int kHd, int kKind>
 struct FewKeys {
   static constexpr int kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps;
   static constexpr int kRun = kKind == LITEVGGT_KV_BF16 ? 8 : kKind == LITEVGGT_KV_E4M3 ? 16 : kHd / 4;  // channels side by side in a lane
@@ -50,38 +61,63 @@ struct FewKeys {
   uint32_t byte[4];
 };
 
+// Where a warp is in its run: a head's unit, and the pages that its first and its second 16 keys lie in.
+struct FewPlace {
+  KvSeq seq;
+  int s, head, key0;
+  int page[2];
+  __device__ __forceinline__ void look_up(const KvPool& pool, const KvArrays& arrays) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)  // (of a second half that is not there the first's)
+      page[h] = arrays.pages[seq.page0 + (min(key0 + 16 * h, seq.len - 1) >> pool.page_shift)];
+  }
+  __device__ __forceinline__ size_t row(const KvPool& pool, int h) const {  // of the pool
+    const int key = min(key0 + 16 * h, seq.len - 1) & ~15;
+    return (((size_t)page[h] * pool.kv_heads + head) << pool.page_shift) + (key & (pool.page_size - 1));
+  }
+  // The next keys, the next head, or the next sequence that has units; there is one.
+  __device__ __forceinline__ void advance(const KvPool& pool, const KvArrays& arrays, const long long* at) {
+    key0 += kKvWeighUnit;
+    if (key0 >= seq.len) {
+      key0 = 0;
+      if (++head == pool.kv_heads) {
+        head = 0;
+        do ++s;
+        while (at[s + 1] == at[s]);
+        seq = arrays.seqs[s];
+      }
+    }
+    look_up(pool, arrays);
+  }
+};
+
 template <int kHd, int kKind, bool kHalf>
 __global__ void __launch_bounds__(kWeighWarps * 32)
 kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists lists, long long per_warp, long long units) {
-  using Keys = FewKeys<kHd, kKind, kHalf>;
+  using Keys = FewKeys<kHd, kKind>;
   constexpr int kHalves = kHalf ? 1 : 2, kRun = Keys::kRun, kSteps = kHd / 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q4 = lane & 3;
   long long unit = ((long long)blockIdx.x * kWeighWarps + warp) * per_warp;
   const long long end = min(unit + per_warp, units);
+  // Three units are under way: one is worked on, of the next the keys are, of the one behind it the pages' numbers.
+  // (a batch's arrays were there before whatever kernel is still running)
+  FewPlace place, ahead;
+  if (unit < end) {
+    place.s = seq_of_unit(lists.at, arrays.n_seq, pool.kv_heads, unit);
+    const long long in_head = lists.at[place.s + 1] - lists.at[place.s], rest = unit - lists.at[place.s] * pool.kv_heads;
+    place.head = (int)(rest / in_head);
+    place.key0 = (int)(rest % in_head) * kKvWeighUnit;
+    place.seq = arrays.seqs[place.s];
+    place.look_up(pool, arrays);
+    ahead = place;
+    if (unit + 1 < end) ahead.advance(pool, arrays, lists.at);
+  }
   wait_for_previous_kernel();
   if (unit >= end) return;
-  int s = seq_of_unit(lists.at, arrays.n_seq, pool.kv_heads, unit);
-  long long in_head = lists.at[s + 1] - lists.at[s];
-  const long long rest = unit - lists.at[s] * pool.kv_heads;
-  int head = (int)(rest / in_head), key0 = (int)(rest % in_head) * kKvWeighUnit;
-  KvSeq seq = arrays.seqs[s];
-  bool fresh = true;
-
-  uint32_t qa[kSteps][2 * kHalves];
-  float less[kHalves];  // the rows' log-sum-exp in base 2
-  int seen[kHalves];
-  for (; unit < end; ++unit) {
-    Keys k;
-    size_t row0[2];  // of the pool, of each 16 keys
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int key = min(key0 + 16 * h, seq.len - 1) & ~15;  // (of a second half that is not there the first's rows)
-      const size_t page = (size_t)arrays.pages[seq.page0 + (key >> pool.page_shift)];
-      row0[h] = ((page * pool.kv_heads + head) << pool.page_shift) + (key & (pool.page_size - 1));
-    }
+  auto load = [&](Keys& k, const FewPlace& p) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const size_t row = row0[t >> 1] + 8 * (t & 1) + g;
+      const size_t row = p.row(pool, t >> 1) + 8 * (t & 1) + g;
       const uint8_t* src = pool.k + row * Keys::kRowBytes;
       if constexpr (Keys::kWords == 2) {
         const uint2 x = *reinterpret_cast<const uint2*>(src + q4 * 8);
@@ -95,14 +131,25 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
       }
       if constexpr (Keys::kExps > 0) k.byte[t] = pool.k_exp[row * Keys::kExps + (kKind == LITEVGGT_KV_E2M1 ? q4 * Keys::kExps / 4 : 0)];
     }
+  };
+  Keys k, k_ahead;
+  load(k, place);
+  bool fresh = true;
+  uint32_t qa[kSteps][2 * kHalves];
+  float less[kHalves];  // the rows' log-sum-exp in base 2
+  int seen[kHalves];
+  for (; unit < end; ++unit) {
+    FewPlace behind = ahead;
+    if (unit + 1 < end) load(k_ahead, ahead);
+    if (unit + 2 < end) behind.advance(pool, arrays, lists.at);
     if (fresh) {  // the rows
-      fresh = false;
+      const KvSeq& seq = place.seq;
       const int rows = seq.rows * in.group;
 #pragma unroll
       for (int half = 0; half < kHalves; ++half) {
         const int r = g + 8 * half;
         const bool live = r < rows;
-        const int token = live ? r / in.group : 0, q_head = head * in.group + (live ? r % in.group : 0);
+        const int token = live ? r / in.group : 0, q_head = place.head * in.group + (live ? r % in.group : 0);
         const __nv_bfloat16* src = in.q + (seq.row0 + token) * in.q_stride.row + q_head * in.q_stride.head;
 #pragma unroll
         for (int i = 0; i < kHd / (4 * kRun); ++i)
@@ -116,6 +163,7 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
         seen[half] = live ? kv_seen(seq.len, seq.rows, in.causal_block, token) : 0;
       }
     }
+    const int key0 = place.key0;
     float drawn[4][2];  // of the keys 2 q4 and 2 q4 + 1 of each tile, over this lane's rows
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -177,79 +225,121 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
     const float own = upper ? one[1] : one[0], other = upper ? one[0] : one[1];
     const float sum = own + __shfl_xor_sync(0xffffffffu, other, 4);
     const int in16 = 8 * (lane >> 4) + 2 * q4 + ((lane >> 3) & 1);
-    if (key0 + 16 * (upper ? 1 : 0) + in16 < seq.len) {
-      float* w = pool.weights + (upper ? row0[1] : row0[0]) + in16;
+    if (key0 + 16 * (upper ? 1 : 0) + in16 < place.seq.len) {
+      float* w = pool.weights + place.row(pool, upper ? 1 : 0) + in16;
       *w = tallied(in.decay, in.decay == 0.0f ? 0.0f : *w, sum);
     }
-    // the next unit: the next keys, the next head, or the next sequence that has units
-    key0 += kKvWeighUnit;
-    if (key0 >= seq.len) {
-      key0 = 0;
-      fresh = true;
-      if (++head == pool.kv_heads && unit + 1 < end) {
-        head = 0;
-        do ++s;
-        while (lists.at[s + 1] == lists.at[s]);
-        seq = arrays.seqs[s];
-      }
-    }
+    fresh = ahead.s != place.s || ahead.head != place.head;
+    place = ahead;
+    ahead = behind;
+    k = k_ahead;
   }
 }
 
 // ------------------------------------------------------------------ chunks
 // Scores on the 5th-generation tensor cores, 128 keys by 128 rows a product, kTiles of them side by side against the same rows.  One
 // exponential a score and 64 (128) multiplications for it, so the special-function unit is the bound, at 16 a clock; the products need
-// an eighth (a quarter) of its time.  Roles: 16 warps take the exponentials, each thread a key against a share of the rows; one issues the
-// products; four fetch K once an item and Q tile by tile into swizzled shared memory (widening codes on the way), with what the
-// exponentials need of a row: its log-sum-exp and how many keys it sees.
-constexpr int kDrawWarps = 16, kFetchWarps = 4, kWeighThreads = (kDrawWarps + 1 + kFetchWarps) * 32;
+// an eighth (a quarter) of its time.  Roles: eight warps take the exponentials, each thread a key against all rows or a share of them; one
+// issues the products; two fetch K once an item, two Q tile by tile, into swizzled shared memory (widening codes on the way), with what
+// the exponentials need of a row: its log-sum-exp and how many keys it sees; and one finds out what the CTA's items are, 32 at a time and
+// ahead of all others: the divisions and searches of that, thousands of clocks in a row, were half of the time of short items.
+constexpr int kDrawWarps = 8, kKeyWarps = 2, kRowWarps = 2;
+constexpr int kIssuer = kDrawWarps, kPlanner = kIssuer + 1, kKeyFetcher = kPlanner + 1, kRowFetcher = kKeyFetcher + kKeyWarps;
+constexpr int kWeighThreads = (kRowFetcher + kRowWarps) * 32;
+// Items that are known ahead.  Rows of up to two of them wait for the next ones' to be asked for before they are handed over, so the
+// items behind those have to be known before they are done with.
+constexpr int kRing = 4;
+// Of 16 pairs of scores so many take their exponentials on the FMA pipes, as exactly as the unit's own, where all rows see all keys.
+#ifndef LITEVGGT_WEIGH_POLY
+#define LITEVGGT_WEIGH_POLY 0
+#endif
+constexpr int kPolyPairs = LITEVGGT_WEIGH_POLY;
+constexpr float kRound = 12582912.0f;            // 1.5 * 2^23: adding it rounds to whole numbers
+constexpr float kHeld = 4.1538374868278621e34f;  // 2^115: sums below it hold no exponential of an argument that was held
+// Arguments are held to [-125, 125]: what lies below is next to nothing anyhow, what lies above shows in the sum, as a NaN does, of which
+// the polynomial makes the largest finite number.
+__device__ __forceinline__ float hold(float x) {
+  float y;
+  asm("{\n\t.reg .f32 t;\n\tmin.NaN.f32 t, %1, 0f42FA0000;\n\tmax.NaN.f32 %0, t, 0fC2FA0000;\n\t}" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// An item's part, as every role sees it.
+struct WeighUnit {
+  KvSeq seq;
+  long long item;    // -1: there are no more
+  int head, key0, part;
+  int tile0, tile1;  // row tiles
+  int all_see[2];    // the first tile from which on every row sees all keys of the first 128, and of the second
+  // Whether some rows of tile t are not there, or do not see all of a product's keys.
+  __device__ __forceinline__ bool edge(int group, int t, int product) const {
+    return t < all_see[product] || (t + 1) * kKvWeighRows > seq.rows * group;
+  }
+};
+template <int kTiles>
+__device__ __forceinline__ WeighUnit weigh_unit(const KvArrays& arrays, const WeighLists& lists, const KvWeighing& in, int heads, long long n) {
+  WeighUnit u;
+  u.item = n / lists.parts;
+  u.part = (int)(n - u.item * lists.parts);
+  int lo = 0, hi = arrays.n_seq - 1;
+  while (lo < hi) {  // the last sequence that begins at or before it; ones without items share their successor's start
+    const int mid = (lo + hi + 1) >> 1;
+    if (lists.at[mid] * heads <= u.item) lo = mid;
+    else hi = mid - 1;
+  }
+  const int in_head = (int)(lists.at[lo + 1] - lists.at[lo]);
+  const long long rest = u.item - lists.at[lo] * heads;
+  u.head = (int)(rest / in_head);
+  u.key0 = (int)(rest - (long long)u.head * in_head) * 128 * kTiles;
+  u.seq = arrays.seqs[lo];
+  const int rows = u.seq.rows * in.group, tiles = (rows + kKvWeighRows - 1) / kKvWeighRows;
+  // the first tile whose last (first) row sees `keys` keys: rows see the more the later they are
+  auto first_tile = [&](int from, bool last_row, int keys) {
+    int low = from, high = tiles;
+    while (low < high) {
+      const int mid = (low + high) >> 1, row = last_row ? min((mid + 1) * kKvWeighRows, rows) - 1 : mid * kKvWeighRows;
+      if (kv_seen(u.seq.len, u.seq.rows, in.causal_block, row / in.group) >= keys) high = mid;
+      else low = mid + 1;
+    }
+    return low;
+  };
+  const int seen_from = first_tile(0, true, u.key0 + 1);
+  u.tile0 = seen_from + (int)((long long)(tiles - seen_from) * u.part / lists.parts);
+  u.tile1 = seen_from + (int)((long long)(tiles - seen_from) * (u.part + 1) / lists.parts);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) u.all_see[t] = t < kTiles ? first_tile(seen_from, false, u.key0 + 128 * (t + 1)) : tiles;
+  return u;
+}
 
 template <int kHd, int kTiles>
 struct WeighShape {
   static constexpr int kStages = kHd == 64 ? 4 : 2;  // of Q
   static constexpr int kSubBytes = 128 * 128, kTileBytes = kSubBytes * kHd / 64;
-  static constexpr int kShares = 4 / kTiles;         // threads that share a key's rows
-  static constexpr int kCols = 128 / kShares;        // rows of a thread in a tile
+  static constexpr int kShares = kDrawWarps / (4 * kTiles);  // threads that share a key's rows
+  static constexpr int kCols = 128 / kShares;                // rows of a thread in a tile
   static constexpr int kRowInfoBytes = kStages * 128 * 8;
   static constexpr int kMeetBytes = (kShares - 1) * kTiles * 128 * 4;
-  static constexpr int kSmemBytes = (2 * kTiles + kStages) * kTileBytes + kRowInfoBytes + kMeetBytes + 512 + 1024;
+  static constexpr int kSmemBytes = (2 * kTiles + kStages) * kTileBytes + kRowInfoBytes + kMeetBytes + 1024 + 1024;
 };
 template <int kStages>
 struct WeighBarriers {
-  uint64_t k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], d_full[2][2], d_empty[2][2], teardown;
+  WeighUnit ring[kRing];
+  uint64_t unit_full[kRing], unit_empty[kRing];
+  uint64_t k_full[2], k_empty[2], q_full[kStages], q_empty[kStages], d_full[2][2], d_empty[2][2], met, teardown;
   uint32_t tmem_base, abort_flag;
   int last_of_join;
 };
-
-// An item's part, as every role sees it.
-struct WeighUnit {
-  KvSeq seq;
-  long long item;
-  int head, key0, part;
-  int tile0, tile1;  // row tiles
-};
-template <int kBlock>
-__device__ __forceinline__ WeighUnit weigh_unit(const KvArrays& arrays, const WeighLists& lists, const KvWeighing& in, int heads, long long n) {
-  WeighUnit u;
-  u.item = n / lists.parts;
-  u.part = (int)(n % lists.parts);
-  const int s = seq_of_unit(lists.at, arrays.n_seq, heads, u.item);
-  const long long in_head = lists.at[s + 1] - lists.at[s], rest = u.item - lists.at[s] * heads;
-  u.head = (int)(rest / in_head);
-  u.key0 = (int)(rest % in_head) * kBlock;
-  u.seq = arrays.seqs[s];
-  const int rows = u.seq.rows * in.group, tiles = (rows + kKvWeighRows - 1) / kKvWeighRows;
-  // the first tile of which a row sees the first key: rows see the more the later they are
-  int lo = 0, hi = tiles;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1, last = min((mid + 1) * kKvWeighRows, rows) - 1;
-    if (kv_seen(u.seq.len, u.seq.rows, in.causal_block, last / in.group) > u.key0) hi = mid;
-    else lo = mid + 1;
+// A row of a sequence and head, and those that follow at the same distance.
+struct WeighRow {
+  int row, token, head;
+  __device__ __forceinline__ WeighRow(int r, int group) : row(r), token(r / group), head(r % group) {}
+  __device__ __forceinline__ void advance(int rows, int tokens, int heads, int group) {  // rows = tokens * group + heads
+    row += rows;
+    token += tokens;
+    head += heads;
+    if (head >= group) head -= group, ++token;
   }
-  u.tile0 = lo + (int)((long long)(tiles - lo) * u.part / lists.parts);
-  u.tile1 = lo + (int)((long long)(tiles - lo) * (u.part + 1) / lists.parts);
-  return u;
-}
+};
 
 template <int kHd, int kKind, int kTiles>
 __global__ void __launch_bounds__(kWeighThreads, 1)
@@ -258,30 +348,34 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
   constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kSubBytes = Shape::kSubBytes, kShares = Shape::kShares;
   constexpr int kCols = Shape::kCols, kBlock = 128 * kTiles;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem_k = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));  // [buffer][tile]
-  uint8_t* smem_q = smem_k + 2 * kTiles * kTileBytes;                                                              // [stage]
-  float* row_less = reinterpret_cast<float*>(smem_q + kStages * kTileBytes);                                       // [stage][row]
-  int* row_seen = reinterpret_cast<int*>(row_less + kStages * 128);                                                // [stage][row]
-  float* meet = reinterpret_cast<float*>(row_seen + kStages * 128);                                                // [share - 1][key]
+  uint8_t* smem_k = smem_raw + (-smem_u32(smem_raw) & 1023u);  // [buffer][tile] (as an offset: the compiler knows that it is shared memory)
+  uint8_t* smem_q = smem_k + 2 * kTiles * kTileBytes;          // [stage]
+  float* row_less = reinterpret_cast<float*>(smem_q + kStages * kTileBytes);  // [stage][row]
+  int* row_seen = reinterpret_cast<int*>(row_less + kStages * 128);           // [stage][row]
+  float* meet = reinterpret_cast<float*>(row_seen + kStages * 128);           // [share - 1][key]
   using Barriers = WeighBarriers<kStages>;
   Barriers* bars = reinterpret_cast<Barriers*>(meet + (kShares - 1) * kBlock);
-  static_assert(sizeof(Barriers) <= 512, "");
+  static_assert(sizeof(Barriers) <= 1024 && sizeof(WeighUnit) % 8 == 0, "");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kIssuer = kDrawWarps, kFetcher = kIssuer + 1;
   if (threadIdx.x == 0) {
+    for (int i = 0; i < kRing; ++i) {
+      mbar_init(&bars->unit_full[i], 1);
+      mbar_init(&bars->unit_empty[i], kDrawWarps + 1 + kKeyWarps + kRowWarps);
+    }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars->k_full[i], kFetchWarps);
+      mbar_init(&bars->k_full[i], kKeyWarps);
       mbar_init(&bars->k_empty[i], 1);
       for (int t = 0; t < 2; ++t) {
-        mbar_init(&bars->d_full[t][i], 1);
+        mbar_init(&bars->d_full[t][i], 2);
         mbar_init(&bars->d_empty[t][i], kDrawWarps / kTiles);
       }
     }
     for (int i = 0; i < kStages; ++i) {
-      mbar_init(&bars->q_full[i], kFetchWarps);
+      mbar_init(&bars->q_full[i], kRowWarps);
       mbar_init(&bars->q_empty[i], 1 + kDrawWarps);
     }
+    mbar_init(&bars->met, kDrawWarps);
     mbar_init(&bars->teardown, 1);
     mbar_fence_init();
     bars->abort_flag = 0;
@@ -295,58 +389,87 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
   tc_fence_after();
   const uint32_t tmem_base = bars->tmem_base;
   const WaitCtl ctl{&bars->abort_flag, status};
-  wait_for_previous_kernel();
-  auto unit_of = [&](long long n) { return weigh_unit<kBlock>(arrays, lists, in, pool.kv_heads, n); };
-
-  if (warp >= kFetcher) {
-    // ------------------------------------------------------------------ K and Q
-    const int tid = threadIdx.x - kFetcher * 32;
-    constexpr int kThreads = kFetchWarps * 32, kAhead = 8;  // accesses of a thread that are under way together
-    bool ok = true;
-    uint32_t k_count = 0, q_count = 0;
-    auto given = [&](uint64_t* bar) {
-      fence_proxy_async_shared();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar);
-    };
-    // where 16 bytes (eight channels, number `chunk`) of a tile's row lie
-    auto place = [&](uint8_t* tile, int row, int chunk) {
-      return reinterpret_cast<uint4*>(tile + (chunk >> 3) * kSubBytes + row * 128 + ((chunk & 7) ^ (row & 7)) * 16);
-    };
-    for (long long n = blockIdx.x; n < units && ok; n += gridDim.x) {
-      const WeighUnit u = unit_of(n);
-      if (u.tile0 >= u.tile1) continue;
-      const uint32_t buffer = k_count & 1u;
-      ok = mbar_wait_warp(&bars->k_empty[buffer], ((k_count >> 1) & 1u) ^ 1u, ctl);
+  bool ok = true;
+  // The CTA's items, one after another, for every role but the planner.
+  auto each_unit = [&](auto run) {
+    for (uint32_t i = 0; ok; ++i) {
+      ok = mbar_wait_warp(&bars->unit_full[i % kRing], (i / kRing) & 1u, ctl);
       if (!ok) break;
-      {  // keys behind the sequence's end are zeros: their scores are nobody's, but they are scores
-        constexpr int kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps, kPerRow = kRowBytes / 16;
-        constexpr int kPasses = kBlock * kPerRow / kThreads, kTogether = kPasses < kAhead ? kPasses : kAhead;
-        uint8_t* tiles = smem_k + buffer * kTiles * kTileBytes;
+      const WeighUnit u = bars->ring[i % kRing];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->unit_empty[i % kRing]);
+      if (u.item < 0) break;
+      run(u);
+      __syncwarp();
+    }
+  };
+  // where 16 bytes (eight channels, number `chunk`) of a tile's row lie
+  auto place = [&](uint8_t* tile, int row, int chunk) { return tile + (chunk >> 3) * kSubBytes + row * 128 + ((chunk & 7) ^ (row & 7)) * 16; };
+
+  if (warp == kPlanner) {
+    // ------------------------------------------------------------------ items (a batch's arrays were there before whatever kernel is still running)
+    uint32_t count = 0;
+    for (long long base = blockIdx.x; ok; base += 32ll * gridDim.x) {
+      const long long n = base + (long long)lane * gridDim.x;
+      WeighUnit u{};
+      u.item = -1;
+      if (n < units) u = weigh_unit<kTiles>(arrays, lists, in, pool.kv_heads, n);
+      const int there = __popc(__ballot_sync(0xffffffffu, n < units));
+      for (int i = 0; i < min(there + 1, 32) && ok; ++i, ++count) {  // and behind the last one that there are no more
+        ok = mbar_wait_warp(&bars->unit_empty[count % kRing], ((count / kRing) & 1u) ^ 1u, ctl);
+        if (ok && lane == i) {
+          bars->ring[count % kRing] = u;
+          mbar_arrive(&bars->unit_full[count % kRing]);
+        }
+        __syncwarp();
+      }
+      if (there < 32) break;
+    }
+  } else if (warp >= kKeyFetcher && warp < kRowFetcher) {
+    // ------------------------------------------------------------------ K
+    // Keys behind the sequence's end are zeros: their scores are nobody's, but they are scores.
+    wait_for_previous_kernel();
+    const int tid = threadIdx.x - kKeyFetcher * 32;
+    constexpr int kThreads = kKeyWarps * 32, kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps, kPerRow = kRowBytes / 16;
+    constexpr int kPasses = kBlock * kPerRow / kThreads, kMost = kKind == LITEVGGT_KV_BF16 ? 16 : 8;
+    constexpr int kTogether = kPasses < kMost ? kPasses : kMost;  // accesses of a thread that are under way together
+    uint32_t count = 0;
+    each_unit([&](const WeighUnit& u) {
+      if (u.tile0 >= u.tile1) return;
+      ok = mbar_wait_warp(&bars->k_empty[count & 1u], ((count >> 1) & 1u) ^ 1u, ctl);
+      if (!ok) return;
+      uint8_t* tiles = smem_k + (count & 1u) * kTiles * kTileBytes;
 #pragma unroll 1
-        for (int pass = 0; pass < kPasses; pass += kTogether) {
-          uint4 x[kTogether];
-          uint32_t byte[kTogether];
+      for (int pass = 0; pass < kPasses; pass += kTogether) {
+        uint4 x[kTogether];
+        uint32_t byte[kTogether];
+        int page[kTogether];
 #pragma unroll
-          for (int i = 0; i < kTogether; ++i) {
-            const int piece = (pass + i) * kThreads + tid, key = u.key0 + piece / kPerRow, part = piece % kPerRow;
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            byte[i] = 127u;
-            if (key < u.seq.len) {
-              const size_t page = (size_t)arrays.pages[u.seq.page0 + (key >> pool.page_shift)];
-              const size_t row = ((page * pool.kv_heads + u.head) << pool.page_shift) + (key & (pool.page_size - 1));
-              x[i] = ldg16(pool.k + row * kRowBytes + part * 16);
-              if constexpr (kExps > 0) byte[i] = pool.k_exp[row * kExps + (kKind == LITEVGGT_KV_E2M1 ? part : 0)];
-            }
+        for (int i = 0; i < kTogether; ++i) {
+          const int key = u.key0 + ((pass + i) * kThreads + tid) / kPerRow;
+          page[i] = key < u.seq.len ? arrays.pages[u.seq.page0 + (key >> pool.page_shift)] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) {
+          const int piece = (pass + i) * kThreads + tid, in_block = piece / kPerRow, key = u.key0 + in_block, part = piece % kPerRow;
+          const bool there = key < u.seq.len;
+          const size_t row = there ? (((size_t)page[i] * pool.kv_heads + u.head) << pool.page_shift) + (key & (pool.page_size - 1)) : 0;
+          const uint8_t* src = pool.k + row * kRowBytes + part * 16;
+          if constexpr (kKind == LITEVGGT_KV_BF16) {
+            cp_async16(place(tiles + (in_block >> 7) * kTileBytes, in_block & 127, part), src, there);
+          } else {
+            x[i] = there ? ldg16(src) : make_uint4(0u, 0u, 0u, 0u);
+            byte[i] = there ? pool.k_exp[row * kExps + (kKind == LITEVGGT_KV_E2M1 ? part : 0)] : 127u;
           }
+        }
+        if constexpr (kKind != LITEVGGT_KV_BF16) {
 #pragma unroll
           for (int i = 0; i < kTogether; ++i) {
             const int piece = (pass + i) * kThreads + tid, row = piece / kPerRow, part = piece % kPerRow;
             uint8_t* tile = tiles + (row >> 7) * kTileBytes;
+            auto put = [&](int chunk, const uint32_t* v) { *reinterpret_cast<uint4*>(place(tile, row & 127, chunk)) = make_uint4(v[0], v[1], v[2], v[3]); };
             const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            if constexpr (kKind == LITEVGGT_KV_BF16) {
-              *place(tile, row & 127, part) = x[i];
-            } else if constexpr (kKind == LITEVGGT_KV_E4M3) {
+            if constexpr (kKind == LITEVGGT_KV_E4M3) {
               const KvFactor f = kv_factor(byte[i]);
               uint32_t v[8];
 #pragma unroll
@@ -358,76 +481,101 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = mul_bf16x2(v[e], f.second * 0x10001u);
               }
-              *place(tile, row & 127, 2 * part) = make_uint4(v[0], v[1], v[2], v[3]);
-              *place(tile, row & 127, 2 * part + 1) = make_uint4(v[4], v[5], v[6], v[7]);
+              put(2 * part, v);
+              put(2 * part + 1, v + 4);
             } else {
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 uint32_t v[4];
                 kv4_widen(w[e], byte[i], v);
-                *place(tile, row & 127, 4 * part + e) = make_uint4(v[0], v[1], v[2], v[3]);
+                put(4 * part + e, v);
               }
             }
           }
         }
       }
-      given(&bars->k_full[buffer]);
-      ++k_count;
-      const int rows = u.seq.rows * in.group;
-      for (int t = u.tile0; t < u.tile1; ++t, ++q_count) {
-        const uint32_t stage = q_count % kStages;
-        ok = mbar_wait_warp(&bars->q_empty[stage], ((q_count / kStages) & 1u) ^ 1u, ctl);
-        if (!ok) break;
-        constexpr int kPerRow = kHd / 8, kPasses = 128 * kPerRow / kThreads, kTogether = kPasses < kAhead ? kPasses : kAhead;
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async_shared();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->k_full[count & 1u]);
+      ++count;
+    });
+  } else if (warp >= kRowFetcher) {
+    // ------------------------------------------------------------------ Q
+    // Copies of the last kLag tiles are under way, a group each; what has arrived is handed over by the threads that asked for it.
+    // A thread meets every kStep-th row of a tile, eight channels of it, and kInfo rows of which it leaves what the exponentials need.
+    wait_for_previous_kernel();
+    const int tid = threadIdx.x - kRowFetcher * 32;
+    constexpr int kThreads = kRowWarps * 32, kPerRow = kHd / 8, kStep = kThreads / kPerRow, kInfo = 128 / kThreads;
+    constexpr uint32_t kLag = kStages > 2 ? 2 : 1;
+    const int group = in.group, step_tokens = kStep / group, step_heads = kStep % group, info_tokens = kThreads / group, info_heads = kThreads % group;
+    const uint32_t row_stride = (uint32_t)in.q_stride.row, head_stride = (uint32_t)in.q_stride.head;  // (elements; less than 2^32)
+    uint32_t count = 0, given = 0;
+    auto hand_over = [&]() {  // the oldest, which has arrived
+      fence_proxy_async_shared();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->q_full[given % kStages]);
+      ++given;
+    };
+    each_unit([&](const WeighUnit& u) {
+      const int rows = u.seq.rows * group;
+      WeighRow mine(u.tile0 * kKvWeighRows + tid / kPerRow, group), info(u.tile0 * kKvWeighRows + tid, group);
+      for (int t = u.tile0; t < u.tile1; ++t) {
+        const uint32_t stage = count % kStages;
+        const bool edge = u.edge(group, t, kTiles - 1);  // (of the first keys only where of the last)
+        float less[kInfo];
+        int seen[kInfo];
+#pragma unroll
+        for (int i = 0; i < kInfo; ++i) {
+          const bool there = info.row < rows;
+          less[i] = there ? in.lse[(long long)(u.seq.row0 + info.token) * in.q_heads + u.head * group + info.head] : 0.0f;
+          seen[i] = edge && there ? kv_seen(u.seq.len, u.seq.rows, in.causal_block, info.token) : 0;  // (looked at where there is an edge)
+          info.advance(kThreads, info_tokens, info_heads, group);
+        }
+        ok = mbar_wait_warp(&bars->q_empty[stage], ((count / kStages) & 1u) ^ 1u, ctl);
+        if (!ok) return;
+        ++count;
         uint8_t* tile = smem_q + stage * kTileBytes;
-        const int base = t * kKvWeighRows;
-        {  // this thread's row
-          const int r = base + tid;
-          const bool live = r < rows;
-          const int token = live ? r / in.group : 0, q_head = u.head * in.group + (live ? r % in.group : 0);
-          row_less[stage * 128 + tid] = live ? -kLog2e * in.lse[(long long)(u.seq.row0 + token) * in.q_heads + q_head] : 0.0f;
-          row_seen[stage * 128 + tid] = live ? kv_seen(u.seq.len, u.seq.rows, in.causal_block, token) : 0;
-        }
-#pragma unroll 1
-        for (int pass = 0; pass < kPasses; pass += kTogether) {
-          uint4 x[kTogether];
 #pragma unroll
-          for (int i = 0; i < kTogether; ++i) {
-            const int piece = (pass + i) * kThreads + tid, r = base + piece / kPerRow, part = piece % kPerRow;
-            x[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows) {
-              const int token = r / in.group, q_head = u.head * in.group + r % in.group;
-              x[i] = ldg16(in.q + (u.seq.row0 + token) * in.q_stride.row + q_head * in.q_stride.head + part * 8);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < kTogether; ++i) {
-            const int piece = (pass + i) * kThreads + tid;
-            *place(tile, piece / kPerRow, piece % kPerRow) = x[i];
-          }
+        for (int i = 0; i < 128 / kStep; ++i) {
+          const bool there = mine.row < rows;
+          const unsigned long long at = (unsigned long long)(uint32_t)(u.seq.row0 + mine.token) * row_stride +
+                                        (unsigned long long)(uint32_t)(u.head * group + mine.head) * head_stride;
+          cp_async16(place(tile, tid / kPerRow + i * kStep, tid % kPerRow), in.q + (there ? at : 0) + (tid % kPerRow) * 8, there);
+          mine.advance(kStep, step_tokens, step_heads, group);
         }
-        given(&bars->q_full[stage]);
+        cp_async_commit();
+#pragma unroll
+        for (int i = 0; i < kInfo; ++i) {
+          row_less[stage * 128 + i * kThreads + tid] = -kLog2e * less[i];
+          row_seen[stage * 128 + i * kThreads + tid] = seen[i];
+        }
+        if (count - given > kLag) {
+          cp_async_wait<kLag>();
+          hand_over();
+        }
       }
-    }
+    });
+    cp_async_wait<0>();  // every copy has landed before the CTA may go
+    while (ok && given != count) hand_over();
   } else if (warp == kIssuer) {
     // ------------------------------------------------------------------ products: one lane
-    bool ok = true;
-    if (elect_one()) {
-      constexpr uint32_t idesc = umma_idesc_bf16(128, 128, false, false);
-      const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem_k), 16, 1024), q_desc0 = smem_desc_sw128(smem_u32(smem_q), 16, 1024);
-      uint32_t k_count = 0, q_count = 0;
-      for (long long n = blockIdx.x; n < units && ok; n += gridDim.x) {
-        const WeighUnit u = unit_of(n);
-        if (u.tile0 >= u.tile1) continue;
+    constexpr uint32_t idesc = umma_idesc_bf16(128, 128, false, false);
+    const uint64_t k_desc0 = smem_desc_sw128(smem_u32(smem_k), 16, 1024), q_desc0 = smem_desc_sw128(smem_u32(smem_q), 16, 1024);
+    uint32_t k_count = 0, q_count = 0;
+    bool issued = true;  // (the issuing lane's: all of it went well)
+    each_unit([&](const WeighUnit& u) {
+      if (elect_one() && u.tile0 < u.tile1) {  // the same lane every time
         const uint32_t buffer = k_count & 1u;
-        ok = mbar_wait(&bars->k_full[buffer], (k_count >> 1) & 1u, ctl);
-        for (int t = u.tile0; t < u.tile1 && ok; ++t, ++q_count) {
+        issued = issued && mbar_wait(&bars->k_full[buffer], (k_count >> 1) & 1u, ctl);
+        for (int t = u.tile0; t < u.tile1 && issued; ++t, ++q_count) {
           const uint32_t stage = q_count % kStages, slot = q_count & 1u;
-          ok = mbar_wait(&bars->q_full[stage], (q_count / kStages) & 1u, ctl);
+          issued = mbar_wait(&bars->q_full[stage], (q_count / kStages) & 1u, ctl);
 #pragma unroll
           for (int kt = 0; kt < kTiles; ++kt) {
-            ok = ok && mbar_wait(&bars->d_empty[kt][slot], ((q_count >> 1) & 1u) ^ 1u, ctl);
-            if (!ok) break;
+            issued = issued && mbar_wait(&bars->d_empty[kt][slot], ((q_count >> 1) & 1u) ^ 1u, ctl);
+            if (!issued) break;
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < kHd / 16; ++k) {
@@ -436,79 +584,98 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
                       q_desc0 + (uint64_t)((stage * kTileBytes) >> 4) + in_tile, idesc, k != 0 ? 1u : 0u);
             }
             umma_commit(&bars->d_full[kt][slot]);
+            mbar_arrive(&bars->d_full[kt][slot]);  // (and with it what the fetchers have left in shared memory)
           }
-          if (ok) umma_commit(&bars->q_empty[stage]);
+          if (issued) umma_commit(&bars->q_empty[stage]);
         }
-        if (ok) umma_commit(&bars->k_empty[buffer]);
+        if (issued) umma_commit(&bars->k_empty[buffer]);
         ++k_count;
       }
-      if (!ok) {  // what is under way must have retired before tensor memory is given up
-        umma_commit(&bars->teardown);
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&bars->teardown, 0)) {
-          if (clock64() - t0 > kTimeoutCycles) break;
-        }
+      __syncwarp();
+    });
+    if (elect_one() && !(issued && ok)) {  // what is under way must have retired before tensor memory is given up
+      umma_commit(&bars->teardown);
+      const long long t0 = clock64();
+      while (!mbar_try_wait(&bars->teardown, 0)) {
+        if (clock64() - t0 > kTimeoutCycles) break;
       }
     }
     __syncwarp();
   } else {
     // ------------------------------------------------------------------ exponentials: a thread is a key against a share of the rows
+    wait_for_previous_kernel();
     const int kt = warp / (4 * kShares), share = (warp >> 2) % kShares, key_in = kt * 128 + (warp & 3) * 32 + lane;
     const uint32_t d_addr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + kt * 256 + share * kCols;
-    auto all_draw = []() { asm volatile("bar.sync 1, %0;" ::"n"(kDrawWarps * 32) : "memory"); };
-    bool ok = true;
-    uint32_t count = 0;
-    for (long long n = blockIdx.x; n < units; n += gridDim.x) {
-      const WeighUnit u = unit_of(n);
-      const int key = u.key0 + key_in, rows = u.seq.rows * in.group;
+    uint32_t count = 0, meetings = 0;
+    auto all_draw = [&]() {  // the eight warps; bounded like every wait
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars->met);
+      ok = mbar_wait_warp(&bars->met, meetings & 1u, ctl) && ok;
+      ++meetings;
+    };
+    const float2 scale2 = make_float2(in.scale_log2, in.scale_log2);
+    each_unit([&](const WeighUnit& u) {
+      const int key = u.key0 + key_in;
       float total = 0.0f;
-      for (int t = u.tile0; t < u.tile1 && ok; ++t, ++count) {
+      for (int t = u.tile0; t < u.tile1; ++t, ++count) {
         const uint32_t stage = count % kStages, slot = count & 1u;
-        // the row's numbers come by way of the fetchers, the scores from the tensor core
-        ok = mbar_wait_warp(&bars->q_full[stage], (count / kStages) & 1u, ctl) && mbar_wait_warp(&bars->d_full[kt][slot], (count >> 1) & 1u, ctl);
-        if (!ok) break;
+        ok = mbar_wait_warp(&bars->d_full[kt][slot], (count >> 1) & 1u, ctl);
+        if (!ok) return;
         tc_fence_after();
         const float* less = row_less + stage * 128 + share * kCols;
         const int* seen = row_seen + stage * 128 + share * kCols;
-        // rows that are not there, or do not see all of the keys
-        const bool edge = (t + 1) * kKvWeighRows > rows ||
-                          kv_seen(u.seq.len, u.seq.rows, in.causal_block, t * kKvWeighRows / in.group) < u.key0 + (kt + 1) * 128;
-        const float2 scale2 = make_float2(in.scale_log2, in.scale_log2);
-        float2 sum = make_float2(0.0f, 0.0f);
+        auto tile_sum = [&](auto poly_constant) {
+          constexpr int kPoly = decltype(poly_constant)::value;
+          constexpr bool kEdge = kPoly < 0;
+          float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+          uint32_t x[2][32];  // the next 32 are on their way while these are worked on
+          tmem_ld32(d_addr + slot * 128, x[0]);
 #pragma unroll
-        for (int c0 = 0; c0 < kCols; c0 += 32) {
-          uint32_t x[32];
-          tmem_ld32(d_addr + slot * 128 + c0, x);
-          tmem_ld_wait();
-          if (c0 + 32 == kCols) {  // all read
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars->d_empty[kt][slot]);
-          }
+          for (int c = 0; c < kCols / 32; ++c) {
+            tmem_ld_wait();
+            if (c + 1 < kCols / 32) tmem_ld32(d_addr + slot * 128 + (c + 1) * 32, x[(c + 1) & 1]);
+            const uint32_t (&now)[32] = x[c & 1];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float2 l = *reinterpret_cast<const float2*>(less + c0 + 2 * i);
-            float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), scale2, l);
-            y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-            if (edge) {
-              const int2 s = *reinterpret_cast<const int2*>(seen + c0 + 2 * i);
-              y = make_float2(key < s.x ? y.x : 0.0f, key < s.y ? y.y : 0.0f);
+            for (int i = 0; i < 16; ++i) {
+              const float4 l4 = *reinterpret_cast<const float4*>(less + c * 32 + (2 * i & ~3));
+              const float2 l = i & 1 ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y);
+              float2 y = __ffma2_rn(make_float2(__uint_as_float(now[2 * i]), __uint_as_float(now[2 * i + 1])), scale2, l);
+              if (i < kPoly) y = poly_exp2_pair<true>(make_float2(hold(y.x), hold(y.y)), make_float2(kRound, kRound), make_float2(-kRound, -kRound));
+              else y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+              if constexpr (kEdge) {
+                const int2 s = *reinterpret_cast<const int2*>(seen + c * 32 + 2 * i);
+                y = make_float2(key < s.x ? y.x : 0.0f, key < s.y ? y.y : 0.0f);
+              }
+              sum[i & 1] = __fadd2_rn(sum[i & 1], y);
             }
-            sum = __fadd2_rn(sum, y);
           }
+          sum[0] = __fadd2_rn(sum[0], sum[1]);
+          return sum[0].x + sum[0].y;
+        };
+        float sum;
+        if (u.edge(in.group, t, kt)) {
+          sum = tile_sum(std::integral_constant<int, -1>{});
+        } else {
+          sum = tile_sum(std::integral_constant<int, kPolyPairs>{});
+          // a score that is not finite, or that no sum of exponentials has
+          if (kPolyPairs > 0 && __any_sync(0xffffffffu, !(sum < kHeld))) sum = tile_sum(std::integral_constant<int, 0>{});
         }
+        tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->q_empty[stage]);
-        total += sum.x + sum.y;  // (a tile's own sum first: no number is added to more than a few dozen times its size in turn)
+        if (lane == 0) {
+          mbar_arrive(&bars->d_empty[kt][slot]);
+          mbar_arrive(&bars->q_empty[stage]);
+        }
+        total += sum;  // (a tile's own sum first: no number is added to more than a few dozen times its size in turn)
       }
       // the threads of a key, in their order
-      if (share > 0) meet[(share - 1) * kBlock + key_in] = total;
-      all_draw();
-      bool mine = share == 0 && key < u.seq.len;
-      if (share == 0) {
+      if constexpr (kShares > 1) {
+        if (share > 0) meet[(share - 1) * kBlock + key_in] = total;
+        all_draw();
 #pragma unroll
-        for (int i = 1; i < kShares; ++i) total += meet[(i - 1) * kBlock + key_in];
+        for (int i = 1; i < kShares; ++i) total += meet[(i - 1) * kBlock + key_in];  // (of the first share)
       }
+      bool mine = share == 0 && key < u.seq.len;
       if (lists.parts > 1) {  // whoever comes last adds the parts up, in their order
         float* parts = lists.sums + u.item * lists.parts * kBlock + key_in;
         if (share == 0) __stcg(parts + (long long)u.part * kBlock, total);
@@ -532,8 +699,8 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
         float* w = pool.weights + ((page * pool.kv_heads + u.head) << pool.page_shift) + (key & (pool.page_size - 1));
         *w = tallied(in.decay, in.decay == 0.0f ? 0.0f : *w, total);
       }
-      all_draw();  // what was met with may be written again
-    }
+      if (kShares > 1) all_draw();  // what was met with may be written again
+    });
   }
   tc_fence_before();
   __syncthreads();

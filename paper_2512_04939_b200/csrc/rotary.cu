@@ -76,7 +76,7 @@ constexpr int kRotaryAhead = 4;  // heads of a thread whose loads are under way 
 template <class T, int kV, bool kNeighbours>
 __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_constant__ RotaryLaunch l) {
   constexpr int kPlanes = kNeighbours ? kV / 2 : kV, kSize = (int)sizeof(T);
-  const int unit = threadIdx.x % l.units, rest = threadIdx.x / l.units, slot = rest % l.slots;
+  const int unit = threadIdx.x % l.units, rest = threadIdx.x / l.units, slot = blockIdx.y * l.slots + rest % l.slots;
   const long long row = (long long)blockIdx.x * l.block_rows + rest / l.slots;
   wait_for_previous_kernel();
   if (rest / l.slots >= l.block_rows || row >= l.n_rows) return;
@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
   auto load = [&](int h0) {
 #pragma unroll
     for (int i = 0; i < kRotaryAhead; ++i) {
-      const int h = h0 + i * l.slots;
+      const int h = h0 + i * l.all_slots;
       if (h >= l.heads) break;
       const uint8_t* p = head_at(h, false);
       xa[i].load(p + a);
@@ -112,11 +112,11 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
       sn[i] *= l.sign;
     }
   }
-  for (int h0 = slot; h0 < l.heads; h0 += kRotaryAhead * l.slots) {
+  for (int h0 = slot; h0 < l.heads; h0 += kRotaryAhead * l.all_slots) {
     if (h0 != slot) load(h0);
 #pragma unroll
     for (int i = 0; i < kRotaryAhead; ++i) {
-      const int h = h0 + i * l.slots;
+      const int h = h0 + i * l.all_slots;
       if (h >= l.heads) break;
       uint8_t* p = head_at(h, true);
       if (!turns) {
@@ -148,8 +148,8 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
 }
 
 template <class T>
-cudaError_t by_width(const RotaryLaunch& l, int v, bool neighbours, unsigned blocks, cudaStream_t s) {
-  auto go = [&](auto kernel) { return launch(kernel, dim3(blocks), kRotaryThreads, 0, s, l); };
+cudaError_t by_width(const RotaryLaunch& l, int v, bool neighbours, dim3 grid, unsigned threads, cudaStream_t s) {
+  auto go = [&](auto kernel) { return launch(kernel, grid, threads, 0, s, l); };
   if constexpr (sizeof(T) == 2)
     if (v == 8) return neighbours ? go(rotary_kernel<T, 8, true>) : go(rotary_kernel<T, 8, false>);
   if (v == 4) return neighbours ? go(rotary_kernel<T, 4, true>) : go(rotary_kernel<T, 4, false>);
@@ -159,10 +159,10 @@ cudaError_t by_width(const RotaryLaunch& l, int v, bool neighbours, unsigned blo
 
 }  // namespace
 
-cudaError_t launch_rotary(const RotaryLaunch& l, int dtype, int width, bool neighbours, unsigned blocks, cudaStream_t s) {
-  if (dtype == LITEVGGT_BF16) return by_width<__nv_bfloat16>(l, width, neighbours, blocks, s);
-  if (dtype == LITEVGGT_FP16) return by_width<__half>(l, width, neighbours, blocks, s);
-  return by_width<float>(l, width, neighbours, blocks, s);
+cudaError_t launch_rotary(const RotaryLaunch& l, int dtype, int width, bool neighbours, dim3 grid, unsigned threads, cudaStream_t s) {
+  if (dtype == LITEVGGT_BF16) return by_width<__nv_bfloat16>(l, width, neighbours, grid, threads, s);
+  if (dtype == LITEVGGT_FP16) return by_width<__half>(l, width, neighbours, grid, threads, s);
+  return by_width<float>(l, width, neighbours, grid, threads, s);
 }
 
 }  // namespace lv

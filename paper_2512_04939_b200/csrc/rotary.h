@@ -37,7 +37,8 @@ struct RotaryLaunch {
   long long n_rows;
   int heads0, heads;  // of the first tensor, of both
   int units, turned;  // of a head, and how many of them turn; the others are copied
-  int slots;          // threads that share a unit's heads in a row
+  int slots;          // threads that share a unit's heads in a row, of one block
+  int all_slots;      // and of all blocks of the row
   int block_rows;
   float sign;
 };
@@ -112,7 +113,7 @@ inline bool rotary_apart(const RotarySpan& a) {
 }
 
 // rotary.cu
-cudaError_t launch_rotary(const RotaryLaunch& l, int dtype, int width, bool neighbours, unsigned blocks, cudaStream_t s);
+cudaError_t launch_rotary(const RotaryLaunch& l, int dtype, int width, bool neighbours, dim3 grid, unsigned threads, cudaStream_t s);
 
 }  // namespace lv
 

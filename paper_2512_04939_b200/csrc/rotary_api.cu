@@ -116,15 +116,20 @@ litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32
   l.sign = back != 0 ? -1.0f : 1.0f;
   // A unit's heads by so many threads in a row: four heads each share one set of angles where that fills the chip all the same.
   const long long full = (long long)rotary->num_sms * 2048;
-  const int most = kRotaryThreads / l.units;  // units are 256 at most
   int slots = (heads + 3) / 4;
   if (rows * l.units * slots < full) slots = heads;
-  l.slots = slots < most ? slots : most;
+  const int across = (slots * l.units + kRotaryThreads - 1) / kRotaryThreads;  // blocks of a row (units are 256 at most)
+  l.slots = (slots + across - 1) / across;
+  if (l.slots * l.units > kRotaryThreads) l.slots = kRotaryThreads / l.units;
+  const int grid_y = (slots + l.slots - 1) / l.slots;
+  l.all_slots = l.slots * grid_y;
   l.block_rows = kRotaryThreads / (l.units * l.slots);
+  if (l.block_rows > rows) l.block_rows = (int)rows;
   const long long blocks = (rows + l.block_rows - 1) / l.block_rows;
+  const unsigned threads = (unsigned)round_up((long long)l.units * l.slots * l.block_rows, 32);
   const OnDevice g(rotary->device);
   if (!g.ok) return LITEVGGT_ERR_CUDA;
-  return cuda_status(launch_rotary(l, dtype, v, neighbours, (unsigned)blocks, (cudaStream_t)stream));
+  return cuda_status(launch_rotary(l, dtype, v, neighbours, dim3((unsigned)blocks, (unsigned)grid_y), threads, (cudaStream_t)stream));
 }
 
 }  // extern "C"

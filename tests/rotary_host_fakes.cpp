@@ -5,7 +5,7 @@ using namespace lv;
 
 static RotaryLaunch g_launch;
 static int g_launches = 0, g_width = 0, g_neighbours = 0, g_device = 0, g_launched_on = -1;
-static unsigned g_blocks = 0;
+static unsigned g_blocks = 0, g_threads = 0, g_across = 0;
 
 extern "C" {
 cudaError_t cudaGetDevice(int* d) { *d = g_device; return cudaSuccess; }
@@ -19,10 +19,11 @@ cudaError_t cudaGetLastError() { return cudaSuccess; }
 int fake_launches() { return g_launches; }
 int fake_get_device() { return g_device; }
 int fake_launched_on() { return g_launched_on; }
-// width, neighbours, units, turned, slots, block_rows, blocks, planes
+// width, neighbours, units, turned, slots, block_rows, blocks, planes, threads, blocks of a row, slots of a row
 void fake_last(int* out) {
-  const int x[8] = {g_width, g_neighbours, g_launch.units, g_launch.turned, g_launch.slots, g_launch.block_rows, (int)g_blocks, g_launch.table.planes};
-  for (int i = 0; i < 8; ++i) out[i] = x[i];
+  const int x[11] = {g_width, g_neighbours, g_launch.units, g_launch.turned, g_launch.slots, g_launch.block_rows, (int)g_blocks, g_launch.table.planes,
+                     (int)g_threads, (int)g_across, g_launch.all_slots};
+  for (int i = 0; i < 11; ++i) out[i] = x[i];
 }
 void fake_plane(int p, int* first, int* second, int* axis, unsigned long long* turn) {
   *first = g_launch.table.first[p];
@@ -33,11 +34,13 @@ void fake_plane(int p, int* first, int* second, int* axis, unsigned long long* t
 }
 
 namespace lv {
-cudaError_t launch_rotary(const RotaryLaunch& l, int, int width, bool neighbours, unsigned blocks, cudaStream_t) {
+cudaError_t launch_rotary(const RotaryLaunch& l, int, int width, bool neighbours, dim3 grid, unsigned threads, cudaStream_t) {
   g_launch = l;
   g_width = width;
   g_neighbours = neighbours;
-  g_blocks = blocks;
+  g_blocks = grid.x;
+  g_across = grid.y;
+  g_threads = threads;
   g_launched_on = g_device;
   ++g_launches;
   return cudaSuccess;

@@ -3,7 +3,8 @@
 Tolerance of a tally w_j = decay w_j + sum_i p_ij, p_ij = exp(x_ij), x_ij = scale q_i . k_j - lse_i: a score's products are added in 32 bits, in
 up to 8 steps of 16, off by 2^-23 each of what they add up to at most, B_ij = scale sum_c |q_c k_c|; scaling it, the constants and the
 exponential's argument take 2^-23 (B_ij + |lse_i|) more, the exponential 2^-22 and a sum of up to 32 rows in turn (and as many tiles) 2^-19.
-Together less than 2^-18 (1 + B_ij + |lse_i|) of each p_ij, and 2^-22 of decay w_j.
+Together less than 2^-18 (1 + B_ij + |lse_i|) of each p_ij, and 2^-22 of decay w_j; and 2^-125 for every row, what an exponential may come
+out as where it is less.
 
 Tolerance of lse: 2^-8 + 2^-20 (B + |lse|), B the row's largest B_ij: its terms may be rounded to bfloat16.  Which tokens are kept, and what is
 moved, is exact.
@@ -111,7 +112,7 @@ def check(scene, rows, q, lse, causal_block, scale, decay, was, start):
         total, allowed = drawn(f64(q[at:at + r]), scene.held(i)[0], lse[at:at + r], causal_block, scale)
         at += r
         want = total if decay == 0 else total + decay * was[i]
-        allowed += 2.0 ** -22 * (np.abs(want) if decay == 0 else np.abs(want) + decay * np.abs(was[i])) + 1e-37
+        allowed += 2.0 ** -22 * (np.abs(want) if decay == 0 else np.abs(want) + decay * np.abs(was[i])) + 1e-37 + r * q.shape[1] * 2.0 ** -125
         assert np.array_equal(np.isnan(want), np.isnan(got)) and np.array_equal(want[np.isinf(want)], got[np.isinf(want)]), f"sequence {i}"
         with np.errstate(invalid="ignore"):
             over = np.where(np.isfinite(want), np.abs(got - want) / allowed, 0.0)

@@ -47,9 +47,10 @@ def apply(host, handle, *tensors, rows=7, dtype=0, positions=4 * BASE, axis_stri
 
 
 def last(host):
-    out = (C.c_int * 8)()
+    out = (C.c_int * 11)()
     host.fake_last(out)
-    return dict(zip(("width", "neighbours", "units", "turned", "slots", "block_rows", "blocks", "planes"), out))
+    return dict(zip(("width", "neighbours", "units", "turned", "slots", "block_rows", "blocks", "planes", "threads", "across",
+                     "all_slots"), out))
 
 
 @pytest.mark.parametrize("bad", [
@@ -121,7 +122,8 @@ def test_every_head_dim_is_cut_into_whole_units(host):
                 assert apply(host, handle, tensor(row=head_dim * 16, head=head_dim), rows=100000) == OK
                 got = last(host)
                 covered = got["turned"] * got["width"] * (1 if got["neighbours"] else 2) + (got["units"] - got["turned"]) * got["width"]
-                assert covered == head_dim and 1 <= got["units"] * got["slots"] * got["block_rows"] <= 256
+                assert covered == head_dim and 1 <= got["units"] * got["slots"] * got["block_rows"] <= got["threads"] <= 256
+                assert got["slots"] * got["across"] == got["all_slots"] <= 16
                 host.litevggt_rotary_destroy(handle)
 
 
