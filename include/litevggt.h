@@ -454,6 +454,7 @@ typedef struct {
 } litevggt_rotary_tensor;
 typedef struct litevggt_rotary litevggt_rotary; /* immutable: one serves calls on any streams, at once too */
 
+/* Allocates 2 KB on the device; synchronous, as the destruction is, which waits for calls under way.  Neither while a stream captures. */
 litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int device, litevggt_rotary** out);
 litevggt_status litevggt_rotary_destroy(litevggt_rotary* rotary);
 /* Turns one or two tensors of the same rows and type (queries and keys) in one launch.  positions: dev int32, element (axis, row) at

@@ -120,7 +120,7 @@ def load_library():
         "litevggt_kv_launch_count": [vp, P(i64)],
         "litevggt_rotary_create": [P(RotaryConfig), C.c_int, P(vp)],
         "litevggt_rotary_destroy": [vp],
-        "litevggt_rotary_apply": [vp, vp, i64, i64, i64, i32, i32, P(RotaryTensor), i32, vp],
+        "litevggt_rotary_apply": [vp, vp, i64, i64, i64, i32, i32, vp, i32, vp],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)

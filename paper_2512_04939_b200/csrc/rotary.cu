@@ -78,12 +78,33 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
   constexpr int kPlanes = kNeighbours ? kV / 2 : kV, kSize = (int)sizeof(T);
   const int unit = threadIdx.x % l.units, rest = threadIdx.x / l.units, slot = blockIdx.y * l.slots + rest % l.slots;
   const long long row = (long long)blockIdx.x * l.block_rows + rest / l.slots;
-  wait_for_previous_kernel();
-  if (rest / l.slots >= l.block_rows || row >= l.n_rows) return;
-  const bool turns = unit < l.turned;
+  const bool here = rest / l.slots < l.block_rows && row < l.n_rows, turns = unit < l.turned;
+  // (the table was there before whatever kernel is still running)
   const int plane0 = unit * kPlanes;
-  const int a = turns ? l.table.first[plane0] * kSize : (2 * l.table.planes + (unit - l.turned) * kV) * kSize;
-  const int b = turns && !kNeighbours ? l.table.second[plane0] * kSize : a;
+  int a = (2 * l.planes + (unit - l.turned) * kV) * kSize, b = a;
+  unsigned long long turn[kPlanes];
+  unsigned long long axes = 0;  // a byte for each plane
+  if (turns) {
+    a = l.table->first[plane0] * kSize;
+    if (!kNeighbours) b = l.table->second[plane0] * kSize;
+    const unsigned long long* turns_at = l.table->turn + plane0;
+    if constexpr (kPlanes == 1) {
+      turn[0] = turns_at[0];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPlanes; i += 2) {
+        const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(turns_at + i);
+        turn[i] = x.x, turn[i + 1] = x.y;
+      }
+    }
+    const uint8_t* axes_at = l.table->axis + plane0;
+    if constexpr (kPlanes == 8) axes = *reinterpret_cast<const unsigned long long*>(axes_at);
+    else if constexpr (kPlanes == 4) axes = *reinterpret_cast<const uint32_t*>(axes_at);
+    else if constexpr (kPlanes == 2) axes = *reinterpret_cast<const uint16_t*>(axes_at);
+    else axes = *axes_at;
+  }
+  wait_for_previous_kernel();
+  if (!here) return;
   auto head_at = [&](int h, bool out) {
     const bool second = h >= l.heads0;
     const RotaryRows& x = l.rows[second ? 1 : 0];
@@ -106,8 +127,8 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const __grid_con
   if (turns) {
 #pragma unroll
     for (int i = 0; i < kPlanes; ++i) {
-      const int position = l.positions[l.table.axis[plane0 + i] * l.position_axis + row * l.position_row];
-      const unsigned long long angle = (unsigned long long)(long long)position * l.table.turn[plane0 + i];
+      const int position = l.positions[(long long)(axes >> 8 * i & 0xff) * l.position_axis + row * l.position_row];
+      const unsigned long long angle = (unsigned long long)(long long)position * turn[i];
       sincospif((float)(int)(angle >> 32) * 4.656612873077392578125e-10f, &sn[i], &cs[i]);  // half turns: 2^-31 of the upper word
       sn[i] *= l.sign;
     }

@@ -16,7 +16,7 @@ constexpr int kRotaryThreads = 256;
 
 // A plane is two channels of a head that turn together.  Numbered axis by axis; `turn` is what one step of position turns it by, in
 // turns times 2^64: position * turn modulo 2^64 is the angle, wrapped exactly, however far the position is.
-struct RotaryTable {
+struct alignas(16) RotaryTable {
   unsigned long long turn[kRotaryPlanes];
   uint8_t axis[kRotaryPlanes], first[kRotaryPlanes], second[kRotaryPlanes];
   int planes, head_dim;  // channels from 2 * planes on stay as they are
@@ -30,12 +30,13 @@ struct RotaryRows {
 };
 
 struct RotaryLaunch {
-  RotaryTable table;
+  const RotaryTable* table;  // on the device
   RotaryRows rows[2];
   const int* positions;
   long long position_axis, position_row;  // elements
   long long n_rows;
   int heads0, heads;  // of the first tensor, of both
+  int planes;         // of a head
   int units, turned;  // of a head, and how many of them turn; the others are copied
   int slots;          // threads that share a unit's heads in a row, of one block
   int all_slots;      // and of all blocks of the row
@@ -122,4 +123,5 @@ struct litevggt_rotary {
   int device, num_sms;
   bool neighbours;
   lv::RotaryTable table;
+  lv::RotaryTable* on_device;
 };

@@ -40,6 +40,20 @@ litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int de
   r->num_sms = sms;
   r->neighbours = cfg->layout == LITEVGGT_ROTARY_PAIRS;
   r->table = table;
+  {
+    const DeviceGuard g(device);
+    void* p = nullptr;
+    e = g.ok ? cudaMalloc(&p, sizeof(RotaryTable)) : cudaErrorInvalidDevice;
+    if (e == cudaSuccess) {
+      e = cudaMemcpy(p, &table, sizeof(RotaryTable), cudaMemcpyHostToDevice);
+      if (e != cudaSuccess) cudaFree(p);
+    }
+    r->on_device = static_cast<RotaryTable*>(p);
+  }
+  if (e != cudaSuccess) {
+    delete r;
+    return cuda_status(e);
+  }
   *out = r;
   return LITEVGGT_OK;
 }
@@ -47,9 +61,14 @@ litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int de
 litevggt_status litevggt_rotary_destroy(litevggt_rotary* rotary) {
   if (rotary == nullptr) return LITEVGGT_OK;
   if (!rotary_ok(rotary)) return LITEVGGT_ERR_NULL;
+  cudaError_t e = cudaErrorInvalidDevice;
+  {
+    const DeviceGuard g(rotary->device);
+    if (g.ok) e = cudaFree(rotary->on_device);  // (waits for what is under way)
+  }
   rotary->magic = 0;
   delete rotary;
-  return LITEVGGT_OK;
+  return cuda_status(e);
 }
 
 litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32_t* positions, int64_t axis_stride, int64_t row_stride,
@@ -104,7 +123,8 @@ litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32
   int v = 16 / size;
   while (v > 1 && (low % (uintptr_t)(v * size) != 0 || !rotary_fits(t, rotary->neighbours, v))) v /= 2;
   const bool neighbours = rotary->neighbours && v > 1;
-  l.table = t;
+  l.table = rotary->on_device;
+  l.planes = t.planes;
   l.positions = positions;
   l.position_axis = axis_stride;
   l.position_row = row_stride;

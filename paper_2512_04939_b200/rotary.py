@@ -9,12 +9,14 @@ Shapes, types and devices are checked here, everything else in the C library.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
-from .binding import RotaryConfig, RotaryTensor, _check, load_library
+from .binding import RotaryConfig, _check, load_library
 
 _LAYOUTS = {"halves": 0, "pairs": 1, "across": 2}
+_PACK = tuple(struct.Struct("@" + "qqqqqqi4x" * n).pack for n in (1, 2))  # litevggt_rotary_tensor, one and two of them
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
@@ -35,7 +37,7 @@ class RotaryAxes:
         self.head_dim, self.sections, self.bases, self.layout = int(head_dim), tuple(int(n) for n in sections), bases, layout
         self.device = torch.device("cuda", device)
         self._index = device
-        n = len(sections)
+        self._axes = n = len(sections)
         cfg = RotaryConfig(self.head_dim, n, (C.c_int32 * 4)(*self.sections), (C.c_double * 4)(*bases), _LAYOUTS[layout])
         self.handle = C.c_void_p()
         _check(self.lib.litevggt_rotary_create(C.byref(cfg), device, C.byref(self.handle)), "rotary_create")
@@ -62,32 +64,45 @@ class RotaryAxes:
         return self._turn(positions, q, k, out, 1)
 
     def _turn(self, positions, q, k, out, back):
-        given = [q] if k is None else [q, k]
-        if out is None:
-            outs = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in given]
+        # (a small call takes as long as its checks do)
+        if k is None:
+            given = (q,)
+            outs = (q.new_empty(q.shape),) if out is None else (out,)
         else:
-            outs = [out] if k is None else list(out)
-            if len(outs) != len(given):
-                raise ValueError(f"out must hold {len(given)} tensors, got {len(outs)}")
-        rows = q.shape[0] if q.dim() == 3 else -1
-        if positions.shape != (len(self.sections), rows) or positions.dtype != torch.int32 or positions.get_device() != self._index:
-            raise ValueError(f"positions must be int32 [{len(self.sections)}, {rows}] on {self.device}, got {positions.dtype} "
-                             f"{tuple(positions.shape)} on {positions.device}")
-        tensors = (RotaryTensor * len(given))()
-        for name, t, o, made in zip(("q", "k"), given, outs, tensors):
+            given = (q, k)
+            outs = (q.new_empty(q.shape), k.new_empty(k.shape)) if out is None else tuple(out)
+        kind, rows, index = _DTYPES.get(q.dtype), q.shape[0] if q.dim() == 3 else -1, self._index
+        fine = (kind is not None and len(outs) == len(given) and positions.shape == (self._axes, rows) and positions.dtype == torch.int32
+                and positions.get_device() == index)
+        numbers = []
+        if fine:
+            for t, o in zip(given, outs):
+                shape, s, z = t.shape, t.stride(), o.stride()
+                fine = (fine and len(shape) == 3 and shape[0] == rows and shape[1] >= 1 and shape[2] == self.head_dim and o.shape == shape
+                        and t.dtype == q.dtype and o.dtype == q.dtype and t.get_device() == index and o.get_device() == index
+                        and s[2] == 1 and z[2] == 1)
+                if not fine:
+                    break
+                numbers += (t.data_ptr(), s[0], s[1], o.data_ptr(), z[0], z[1], shape[1])
+        if not fine:
+            self._refuse(positions, given, outs, rows)
+        axis_stride, row_stride = positions.stride()
+        code = self._apply(self.handle, positions.data_ptr(), axis_stride, row_stride, rows, kind, back, _PACK[len(given) - 1](*numbers),
+                           len(given), torch._C._cuda_getCurrentRawStream(index))
+        if code:
+            _check(code, "rotary_apply")
+        return outs[0] if k is None else outs
+
+    def _refuse(self, positions, given, outs, rows):
+        if len(outs) != len(given):
+            raise ValueError(f"out must hold {len(given)} tensors, got {len(outs)}")
+        for name, t, o in zip(("q", "k"), given, outs):
             if t.dim() != 3 or t.shape[0] != rows or t.shape[1] < 1 or t.shape[2] != self.head_dim or o.shape != t.shape:
                 raise ValueError(f"{name} and its output must be [{rows}, heads, {self.head_dim}], got {tuple(t.shape)} and {tuple(o.shape)}")
-            if t.dtype not in _DTYPES or t.dtype != q.dtype or o.dtype != q.dtype:
+            if t.dtype not in _DTYPES or t.dtype != given[0].dtype or o.dtype != t.dtype:
                 raise ValueError(f"q, k and their outputs must be of one type, bfloat16, float16 or float32, got {t.dtype} and {o.dtype} for {name}")
             if t.get_device() != self._index or o.get_device() != self._index:
                 raise ValueError(f"{name} and its output must be on {self.device}, got {t.device} and {o.device}")
-            if (t.stride(2) != 1 or o.stride(2) != 1) and self.head_dim > 1:
+            if t.stride(2) != 1 or o.stride(2) != 1:
                 raise ValueError(f"{name}'s channels must be contiguous, got strides {t.stride()} and {o.stride()}")
-            made.src, made.in_row, made.in_head = t.data_ptr(), t.stride(0), t.stride(1)
-            made.dst, made.out_row, made.out_head = o.data_ptr(), o.stride(0), o.stride(1)
-            made.heads = t.shape[1]
-        code = self._apply(self.handle, positions.data_ptr(), positions.stride(0), positions.stride(1), rows, _DTYPES[q.dtype], back,
-                           tensors, len(given), torch._C._cuda_getCurrentRawStream(self._index))
-        if code:
-            _check(code, "rotary_apply")
-        return outs[0] if k is None else tuple(outs)
+        raise ValueError(f"positions must be int32 [{self._axes}, {rows}] on {self.device}, got {positions.dtype} {tuple(positions.shape)} on {positions.device}")

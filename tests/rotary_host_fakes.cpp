@@ -1,10 +1,13 @@
 // Stand-ins for the CUDA runtime and the kernel launch behind the rotary entry points (rotary_api.cu): what would be launched is kept.
+#include <stdlib.h>
+#include <string.h>
+
 #include "../paper_2512_04939_b200/csrc/rotary.h"
 
 using namespace lv;
 
 static RotaryLaunch g_launch;
-static int g_launches = 0, g_width = 0, g_neighbours = 0, g_device = 0, g_launched_on = -1;
+static int g_launches = 0, g_width = 0, g_neighbours = 0, g_device = 0, g_launched_on = -1, g_held = 0;
 static unsigned g_blocks = 0, g_threads = 0, g_across = 0;
 
 extern "C" {
@@ -16,20 +19,24 @@ cudaError_t cudaDeviceGetAttribute(int* v, cudaDeviceAttr a, int) {
   return cudaSuccess;
 }
 cudaError_t cudaGetLastError() { return cudaSuccess; }
+cudaError_t cudaMalloc(void** p, size_t n) { ++g_held; *p = malloc(n); return cudaSuccess; }
+cudaError_t cudaFree(void* p) { --g_held; free(p); return cudaSuccess; }
+cudaError_t cudaMemcpy(void* d, const void* s, size_t n, cudaMemcpyKind) { memcpy(d, s, n); return cudaSuccess; }
+int fake_held() { return g_held; }
 int fake_launches() { return g_launches; }
 int fake_get_device() { return g_device; }
 int fake_launched_on() { return g_launched_on; }
 // width, neighbours, units, turned, slots, block_rows, blocks, planes, threads, blocks of a row, slots of a row
 void fake_last(int* out) {
-  const int x[11] = {g_width, g_neighbours, g_launch.units, g_launch.turned, g_launch.slots, g_launch.block_rows, (int)g_blocks, g_launch.table.planes,
+  const int x[11] = {g_width, g_neighbours, g_launch.units, g_launch.turned, g_launch.slots, g_launch.block_rows, (int)g_blocks, g_launch.planes,
                      (int)g_threads, (int)g_across, g_launch.all_slots};
   for (int i = 0; i < 11; ++i) out[i] = x[i];
 }
 void fake_plane(int p, int* first, int* second, int* axis, unsigned long long* turn) {
-  *first = g_launch.table.first[p];
-  *second = g_launch.table.second[p];
-  *axis = g_launch.table.axis[p];
-  *turn = g_launch.table.turn[p];
+  *first = g_launch.table->first[p];
+  *second = g_launch.table->second[p];
+  *axis = g_launch.table->axis[p];
+  *turn = g_launch.table->turn[p];
 }
 }
 

@@ -73,6 +73,9 @@ def test_axes_devices_and_handles_that_are_refused(host):
     assert host.litevggt_rotary_create(None, 0, C.byref(handle)) == NULL
     assert host.litevggt_rotary_create(C.byref(cfg), 0, None) == NULL
     assert host.litevggt_rotary_destroy(None) == OK
+    before = host.fake_held()
+    assert host.litevggt_rotary_create(C.byref(cfg), 1, C.byref(handle)) == OK and host.fake_held() == before + 1 and host.fake_get_device() == 0
+    assert host.litevggt_rotary_destroy(handle) == OK and host.fake_held() == before
     assert apply(host, None, tensor()) == NULL
 
 
