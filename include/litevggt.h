@@ -346,8 +346,8 @@ enum {
                            codes of zero, and reads as NaN.  Pools that the caller fills keep to it: e <= 120, no codes of NaN */
   LITEVGGT_KV_E2M1 = 2  /* 4 bits: E2M1 codes x, two to a byte (an even channel's in the low half), and an exponent byte e + 127 for
                            every 32 channels, standing for x 2^e: the least e >= -126 with max|block| <= 6 * 2^e; a block that is not
-                           finite is held as byte 255 beside codes of zero, and reads as NaN.  Elements of 3.5 * 2^126 and more read as
-                           infinite.  4.25 bits an element.  Pools that the caller fills: bytes 1 to 253, and 255 beside zeros */
+                           finite is held as byte 255 beside codes of zero, and reads as NaN.  Under 2^126 (byte 253) codes end at 3,
+                           the largest that bf16 holds.  4.25 bits an element.  Pools that the caller fills keep to all that */
 };
 typedef struct {
   int32_t pages;     /* in the pool */

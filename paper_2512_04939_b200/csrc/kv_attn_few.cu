@@ -45,6 +45,17 @@ __device__ __forceinline__ uint32_t widen_high(uint32_t w) {
   asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(r) : "r"(w));
   return r;
 }
+// The four bytes of a word, two E2M1 codes each, to pairs of f16 numbers, exactly; the low half's code to the low number.
+__device__ __forceinline__ void widen_codes4(uint32_t w, uint32_t (&out)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(out[0]), "=r"(out[1]), "=r"(out[2]), "=r"(out[3])
+      : "r"(w));
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -66,6 +77,13 @@ __device__ __forceinline__ void power_pair(uint32_t addr, float (&p)[2]) {
   asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v) : "r"(addr));
   p[0] = __uint_as_float(v << 23 & 0x7f800000u);
   p[1] = __uint_as_float(v << 15 & 0x7f800000u);
+}
+// Of four bytes side by side.
+__device__ __forceinline__ void power_word(uint32_t v, float (&p)[4]) {
+  p[0] = __uint_as_float(v << 23 & 0x7f800000u);
+  p[1] = __uint_as_float(v << 15 & 0x7f800000u);
+  p[2] = __uint_as_float(v << 7 & 0x7f800000u);
+  p[3] = __uint_as_float(v >> 1 & 0x7f800000u);
 }
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_dst), "l"(src),
@@ -90,15 +108,13 @@ __device__ __forceinline__ uint32_t lds4(uint32_t addr) {
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr));
   return v;
 }
-__device__ __forceinline__ uint32_t lds1(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(addr));
-  return v;
-}
 
 template <int kHd, int kKind, bool kHalf>
 struct FewShape {
   static constexpr bool kNarrow = kKind == LITEVGGT_KV_E4M3, kFour = kKind == LITEVGGT_KV_E2M1;
+  static constexpr bool kMoves = kHalf && !kFour;             // whether the accumulators' empty halves are left out of the registers
+  static constexpr int kParts = kMoves ? 2 : 4;               // registers of a lane and tile of accumulators
+  static constexpr int kBlocks = kFour ? kHd / 32 : 1;        // of channels that have a power of two of their own
   using Row = KvRow<kHd, kKind>;
   // Rings of 17 to 25 KB a warp.  Codes of head dim 64 take so much work for a byte that sixteen warps an SM serve them
   // better than eight with more registers (one token over 520,500: 216 us against 241 to 283); those of head dim 128 spill
@@ -124,6 +140,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                    KvLaunch work, KvAttend at, uint32_t* status) {
   using Shape = FewShape<kHd, kKind, kHalf>;
   constexpr bool kNarrow = Shape::kNarrow, kFour = Shape::kFour;
+  constexpr int kBlocks = Shape::kBlocks, kParts4 = Shape::kParts;
   constexpr int kRowBytes = Shape::Row::kBytes, kExps = Shape::Row::kExps;
   constexpr int kSubs = Shape::kSubs, kStages = Shape::kStages, kStageKeys = 16 * kSubs, kRound = kKvFewWarps * kStageKeys;
   constexpr int kHalves = kHalf ? 1 : 2;
@@ -221,8 +238,9 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     float row_scale[kHalves];  // of the scores, in base-2 units
 #pragma unroll
     for (int half = 0; half < kHalves; ++half) {
-      // 16 bytes of a K row hold the channels of two contraction steps of 16 (bf16) or of four (codes); of 4 bits a lane has a quarter row
-      constexpr int kRun = kFour ? kHd / 4 : kNarrow ? 16 : 8;  // channels of a lane that lie side by side
+      // 16 bytes of a K row hold the channels of two contraction steps of 16 (bf16) or of four (codes of 8 bits); of 4 bits a lane reads
+      // 4 bytes of every block, two steps, so that a step lies in one block
+      constexpr int kRun = kNarrow ? 16 : 8;  // channels of a lane that lie side by side
       const int r = g + 8 * half;
       const bool live = r < piece.rows;
       const int at_row = piece.row0 + (live ? r : 0);
@@ -240,7 +258,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           top = __vmaxu2(top, __vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu));
         }
       row_scale[half] = at.scale_log2;
-      if constexpr (kNarrow) {
+      if constexpr (kNarrow || kFour) {
         top = max(top & 0xffffu, top >> 16);
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -261,11 +279,11 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     const int all_see = min(seen_by(0), piece.key1);  // keys before this one are seen by every row
     const int seen[2] = {min(seen_by(g), piece.key1), min(seen_by(g + 8), piece.key1)};
 
-    float o[Shape::kOutTiles][2 * kHalves];
+    float o[Shape::kOutTiles][kParts4];
 #pragma unroll
     for (int i = 0; i < Shape::kOutTiles; ++i)
 #pragma unroll
-      for (int j = 0; j < 2 * kHalves; ++j) o[i][j] = 0.0f;
+      for (int j = 0; j < kParts4; ++j) o[i][j] = 0.0f;
     float limit[2] = {-INFINITY, -INFINITY}, ref[2] = {0.0f, 0.0f}, sum[2] = {0.0f, 0.0f};  // limit: ref, or that there is none yet
     // Codes: the rows' factors of the weights, which the output has in it.  (A power of infinity stands for a value that is not
     // finite, whose codes are zero: 0 * infinity = NaN.)
@@ -282,13 +300,15 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
       for (int s = 0; s < kSubs; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          float (&c)[4] = sc[s][t];
-          c[0] = c[1] = c[2] = c[3] = 0.0f;
+          float c_block[kBlocks][4];  // sums of the blocks, or the one sum
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b) c_block[b][0] = c_block[b][1] = c_block[b][2] = c_block[b][3] = 0.0f;
           const int row = g + 8 * t;
           const uint32_t at_sub = base + s * Shape::kSubBytes;
           auto step = [&](int n, uint32_t b0, uint32_t b1) {
-            if constexpr (kHalf) mma_16816<kNarrow>(c, qa[n][0], 0u, qa[n][1], 0u, b0, b1);
-            else mma_16816<kNarrow>(c, qa[n][0], qa[n][1], qa[n][2], qa[n][3], b0, b1);
+            float (&c)[4] = c_block[kFour ? n / 2 : 0];
+            if constexpr (kHalf) mma_16816<kNarrow || kFour>(c, qa[n][0], 0u, qa[n][1], 0u, b0, b1);
+            else mma_16816<kNarrow || kFour>(c, qa[n][0], qa[n][1], qa[n][2], qa[n][3], b0, b1);
           };
           if constexpr (kNarrow) {
 #pragma unroll
@@ -299,13 +319,24 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               for (int j = 0; j < 4; ++j) step(4 * i + j, widen_low(w[j]), widen_high(w[j]));
             }
           } else if constexpr (kFour) {
-            const uint32_t byte = lds1(exps + (s * 16 + row) * kExps + q4 * kExps / 4);
 #pragma unroll
-            for (int i = 0; i < kHd / 32; ++i) {
+            for (int i = 0; i < kBlocks; ++i) {
               uint32_t x[4];
-              kv4_widen(lds4(at_sub + row * kRowBytes + q4 * (kRowBytes / 4) + 4 * i), byte, x);
+              widen_codes4(lds4(at_sub + row * kRowBytes + i * 16 + q4 * 4), x);
               step(2 * i, x[0], x[1]);
               step(2 * i + 1, x[2], x[3]);
+            }
+            // powers of two of the keys 2 q4 and 2 q4 + 1, block by block
+            float k_power[2 * kBlocks];
+            const uint32_t at_exps = exps + (s * 16 + 8 * t + 2 * q4) * kExps;
+#pragma unroll
+            for (int i = 0; i < kBlocks / 2; ++i) power_word(lds4(at_exps + 4 * i), *reinterpret_cast<float (*)[4]>(&k_power[4 * i]));
+#pragma unroll
+            for (int e = 0; e < 2 * kHalves; ++e) {
+              float x = c_block[0][e] * row_scale[e >> 1] * k_power[(e & 1) * kBlocks];
+#pragma unroll
+              for (int b = 1; b < kBlocks; ++b) x = fmaf(c_block[b][e] * row_scale[e >> 1], k_power[(e & 1) * kBlocks + b], x);
+              sc[s][t][e] = x;
             }
           } else {
 #pragma unroll
@@ -314,6 +345,10 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               step(2 * i, x.x, x.y);
               step(2 * i + 1, x.z, x.w);
             }
+          }
+          if constexpr (!kFour) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[s][t][e] = c_block[0][e];
           }
         }
       // in base-2 units; the reference of a row moves only when a score lies above it
@@ -326,7 +361,8 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           if constexpr (kNarrow) power_pair(exps + s * 16 + 8 * t + 2 * q4, k_scale);
 #pragma unroll
           for (int e = 0; e < 2 * kHalves; ++e) {
-            float x = sc[s][t][e] * row_scale[e >> 1];
+            float x = sc[s][t][e];
+            if constexpr (!kFour) x *= row_scale[e >> 1];
             if constexpr (kNarrow) x *= k_scale[e & 1];
             if (edge && key + 16 * s + 8 * t + 2 * q4 + (e & 1) >= seen[e >> 1]) x = -INFINITY;
             sc[s][t][e] = x;
@@ -422,10 +458,41 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         const int left = piece.key1 - (key + 16 * s);  // keys of the sub-step that the piece holds
         const uint32_t at_sub = base + (kSubs + s) * Shape::kSubBytes;
         constexpr int kLoads = kNarrow ? 1 : kHd / 64, kWords = kNarrow && kHd == 64 ? 2 : 4;
-        [[maybe_unused]] uint32_t v_byte[4];
+        [[maybe_unused]] uint32_t v_bytes[2];  // exponents of the operand's two halves, a key's in either half of a word
         if constexpr (kFour) {
+          const uint32_t at_exps = exps + ((kSubs + s) * 16 + 2 * q4) * kExps, block = g * kExps / 8;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v_byte[e] = lds1(exps + ((kSubs + s) * 16 + 2 * q4 + (e & 1) + 8 * (e >> 1)) * kExps + g * kExps / 8);
+          for (int h = 0; h < 2; ++h) {
+            if constexpr (kExps == 2) {
+              v_bytes[h] = __byte_perm(lds4(at_exps + 8 * h * kExps), 0u, 0x4240u + block * 0x101u);
+            } else {
+              const uint2 x = lds8(at_exps + 8 * h * kExps);
+              v_bytes[h] = __byte_perm(x.x, x.y, 0x0400u + block * 0x101u) & 0x00ff00ffu;
+            }
+          }
+          // Blocks whose factor is one bf16 number (and so none that are not finite): two keys' codes of a channel go into one byte,
+          // which is a pair of the operand once it is widened.
+          if (!__any_sync(0xffffffffu, ((v_bytes[0] + 0x007f007fu | v_bytes[1] + 0x007f007fu) & 0x01000100u) != 0u)) {
+            const uint32_t factors[2] = {v_bytes[0] + 0x007e007eu << 7, v_bytes[1] + 0x007e007eu << 7};
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+              uint32_t even[2][4], odd[2][4];  // of the even and the odd channels
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t at_row = at_sub + (2 * q4 + 8 * h) * kRowBytes + g * (kRowBytes / 8) + 4 * i;
+                const uint32_t a = lds4(at_row), b = lds4(at_row + kRowBytes);
+                kv4_widen_by((a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u), factors[h], even[h]);
+                kv4_widen_by((a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), factors[h], odd[h]);
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const uint32_t b0 = j & 1 ? odd[0][j / 2] : even[0][j / 2], b1 = j & 1 ? odd[1][j / 2] : even[1][j / 2];
+                float (&c)[4] = *reinterpret_cast<float (*)[4]>(&o[i * 8 + j][0]);
+                mma_16816<false>(c, p[s][0][0], kHalf ? 0u : p[s][0][kHalves - 1], p[s][1][0], kHalf ? 0u : p[s][1][kHalves - 1], b0, b1);
+              }
+            }
+            continue;
+          }
         }
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -434,7 +501,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           for (int e = 0; e < 4; ++e) {
             const int row = 2 * q4 + (e & 1) + 8 * (e >> 1);
             if constexpr (kFour) {
-              kv4_widen(lds4(at_sub + row * kRowBytes + g * (kRowBytes / 8) + 4 * i), v_byte[e], v[e]);
+              kv4_widen(lds4(at_sub + row * kRowBytes + g * (kRowBytes / 8) + 4 * i), v_bytes[e >> 1] >> 16 * (e & 1) & 0xffu, v[e]);
             } else if constexpr (kWords == 2) {
               const uint2 x = lds8(at_sub + row * 64 + g * 8);
               v[e][0] = x.x, v[e][1] = x.y;
@@ -496,13 +563,13 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                   b[n][0] = b0, b[n][1] = b1;
                 }
               }
-              if constexpr (kHalf) {
+              if constexpr (Shape::kMoves) {
                 float c[4] = {o[tile][0], o[tile][1], 0.0f, 0.0f};
                 mma_16816<kNarrow>(c, p[s][0][0], 0u, p[s][1][0], 0u, b[n][0], b[n][1]);
                 o[tile][0] = c[0], o[tile][1] = c[1];
               } else {
                 float (&c)[4] = *reinterpret_cast<float (*)[4]>(&o[tile][0]);
-                mma_16816<kNarrow>(c, p[s][0][0], p[s][0][kHalves - 1], p[s][1][0], p[s][1][kHalves - 1], b[n][0], b[n][1]);
+                mma_16816<kNarrow>(c, p[s][0][0], kHalf ? 0u : p[s][0][kHalves - 1], p[s][1][0], kHalf ? 0u : p[s][1][kHalves - 1], b[n][0], b[n][1]);
               }
             }
           }

@@ -53,8 +53,12 @@ __device__ __forceinline__ uint2 row_codes(const uint4& x, uint32_t byte) {
 __device__ __forceinline__ uint32_t row_codes4(const uint4& x, uint32_t byte) {
   if (byte == kKvNanByte) return 0u;
   const float f = kv_inverse_scale(byte);
-  const float y[8] = {bf16_lo(x.x) * f, bf16_hi(x.x) * f, bf16_lo(x.y) * f, bf16_hi(x.y) * f,
-                      bf16_lo(x.z) * f, bf16_hi(x.z) * f, bf16_lo(x.w) * f, bf16_hi(x.w) * f};
+  float y[8] = {bf16_lo(x.x) * f, bf16_hi(x.x) * f, bf16_lo(x.y) * f, bf16_hi(x.y) * f,
+                bf16_lo(x.z) * f, bf16_hi(x.z) * f, bf16_lo(x.w) * f, bf16_hi(x.w) * f};
+  if (byte == kKv4LastByte) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(y[i], -3.0f), 3.0f);
+  }
   return pack_e2m1x8(y);
 }
 __device__ __forceinline__ uint4 row_values4(uint32_t codes, uint32_t byte) {

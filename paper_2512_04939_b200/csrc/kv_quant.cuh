@@ -48,7 +48,8 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 //   e = the least whole number >= -126 with max |block| <= 6 * 2^e, stored as the byte e + 127 (255: not finite, codes of zero)
 // the code of an even channel in the low half of its byte.  Again every x 2^e is a bf16 number, so that reading is exact; blocks of 32
 // because a code has one bit of mantissa and a range of twelve: what shares a power of two with an element twelve times as large is
-// lost, and in a whole row that is common.
+// lost, and in a whole row that is common.  Under 2^126 codes end at 3: 4 * 2^126 would be no number.
+constexpr uint32_t kKv4LastByte = 253u;
 __device__ __forceinline__ uint32_t kv4_exponent_byte(uint32_t top) {
   if (top >= 0x7f80u) return kKvNanByte;
   // top = m 2^x, 1 <= m < 2: 6 = 1.5 * 2^2, so e = x - 2, or one more where m > 1.5
@@ -63,16 +64,20 @@ __device__ __forceinline__ KvFactor kv4_factor(uint32_t byte) {
   return f;
 }
 __device__ __forceinline__ bool kv4_needs_second(uint32_t byte) { return byte > 128u; }  // (blocks whose largest magnitude is over 12)
-// Eight codes to eight bf16.
-__device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t byte, uint32_t (&out)[4]) {
-  const KvFactor f = kv4_factor(byte);
-  const uint32_t low = w << 4;  // the even channels' codes in the upper halves of the bytes
+// Four bytes of two codes each to four pairs of bf16, the low half's code to the low number, times a pair of factors.
+__device__ __forceinline__ void kv4_widen_by(uint32_t w, uint32_t factors, uint32_t (&out)[4]) {
+  const uint32_t low = w << 4;  // the low halves' codes in the upper halves of the bytes
   constexpr uint32_t kPick[4] = {0x4000u, 0x5010u, 0x6020u, 0x7030u};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t t = __byte_perm(low, w, kPick[i]);
-    out[i] = mul_bf16x2((t & 0x80008000u) | (t >> 6 & 0x01c001c0u), f.first * 0x10001u);
+    out[i] = mul_bf16x2((t & 0x80008000u) | (t >> 6 & 0x01c001c0u), factors);
   }
+}
+// Eight codes of a block to eight bf16.
+__device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t byte, uint32_t (&out)[4]) {
+  const KvFactor f = kv4_factor(byte);
+  kv4_widen_by(w, f.first * 0x10001u, out);
   if (kv4_needs_second(byte)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = mul_bf16x2(out[i], f.second * 0x10001u);
