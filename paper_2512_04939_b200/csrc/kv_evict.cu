@@ -13,14 +13,15 @@ namespace lv {
 
 namespace {
 
-constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32, kPickBins = 2048;
+constexpr int kPickThreads = 512, kPickMostThreads = 1024, kPickBins = 2048;
 constexpr int kPickMostBlocks = 16, kPickPortableBlocks = 8;  // of a cluster
-constexpr int kPickAhead = 8;                                 // loads of a thread that are under way together
-constexpr int kPickMostHeld = 48 * 1024;                      // tallies in a CTA's shared memory; what lies behind them is read again
+constexpr int kPickAhead = 4;                                 // loads of four tallies that a thread has under way together
+constexpr int kPickStep = 128;                                // tokens of a warp's step
+constexpr int kPickMostHeld = 48 * 1024;                      // numbers in a CTA's shared memory; what lies behind them is read again
 
-// Orders as the tallies do; zeros are equal, NaN is the least.
+// Orders as the tallies do; zeros are equal, NaN is less than any number; 0 is nobody's.
 __device__ __forceinline__ uint32_t order_of(float x) {
-  if (x != x) return 0u;
+  if (x != x) return 1u;
   const uint32_t bits = __float_as_uint(x + 0.0f);  // -0 + 0 = 0
   return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
@@ -37,17 +38,18 @@ __device__ __forceinline__ void add_cluster(uint32_t addr, uint32_t n) {
 struct PickShared {
   uint32_t bins[kPickBins];   // of this CTA's tokens
   uint32_t joint[kPickBins];  // of the cluster's, in its first CTA
-  uint32_t warp_sums[kPickWarps][2];
+  uint32_t warp_sums[kPickMostThreads / 32][2];
   uint32_t counts[2];         // of this CTA: above the least that stays, equal to it
   uint32_t bin, left;         // first CTA: the bin that the least one lies in, how many of it stay
-  uint32_t scan[kPickWarps];
+  uint32_t scan[kPickMostThreads / 32];
 };
 
 // blockIdx.x = (sequence * heads + head) * blocks of a cluster + block; `held`: numbers that a warp keeps in shared memory
-__global__ void __launch_bounds__(kPickThreads)
+__global__ void __launch_bounds__(kPickMostThreads)
 kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, int blocks, int held, int* kept) {
   __shared__ PickShared sh;
-  extern __shared__ uint32_t numbers[];  // [warp][held]
+  extern __shared__ uint4 numbers[];  // [warp][held / 4]
+  const int threads = blockDim.x, n_warps = threads >> 5;
   const int rank = blocks > 1 ? (int)cluster_ctarank() : 0, pair = (int)blockIdx.x / blocks;
   const int head = pair % pool.kv_heads, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // (a batch's arrays were there before whatever kernel is still running)
@@ -56,7 +58,7 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
   wait_for_previous_kernel();
   int* out = kept + (long long)dst.row0 * pool.kv_heads + head;  // the i-th kept token's number at i * heads
   auto put = [&](int at, int token) { out[(long long)at * pool.kv_heads] = token; };
-  const int all = blocks * kPickThreads, mine = rank * kPickThreads + threadIdx.x;
+  const int all = blocks * threads, mine = rank * threads + threadIdx.x;
   if (m >= n) {  // (the same for the whole cluster)
     for (int i = mine; i < m; i += all) put(i, i);
     return;
@@ -65,68 +67,80 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
   for (int i = mine; i < last; i += all) put(m - last + i, n - last + i);
   const int choose = m - first - last;  // of the tokens in between
   if (choose <= 0) return;
-  // this warp's run of them, in whole warps' steps
-  const int span = n - first - last, warps = blocks * kPickWarps;
-  const int run = (int)((((long long)span + warps - 1) / warps + 31) / 32 * 32);
-  const long long begin64 = (long long)(rank * kPickWarps + warp) * run;
-  const int begin = (int)min(begin64, (long long)span), end = (int)min(begin64 + run, (long long)span);
-  auto tally_of = [&](int i) {
-    const int token = first + i;
+  // This warp's run of tokens, in steps of kPickStep, four of each lane: all from the first one that may go on, rounded down to four, which
+  // lie side by side in a page.  Those outside the range are nobody's number.
+  const int low = first & ~3, span = n - last - low, warps = blocks * n_warps;
+  const int run = (int)((((long long)span + warps - 1) / warps + kPickStep - 1) / kPickStep * kPickStep);
+  const long long begin64 = (long long)(rank * n_warps + warp) * run;
+  const int begin = low + (int)min(begin64, (long long)span), end = low + (int)min(begin64 + run, (long long)span);
+  auto tallies_at = [&](int token) {
     const size_t page = (size_t)from.pages[src.page0 + (token >> pool.page_shift)];
-    return pool.weights[((page * pool.kv_heads + head) << pool.page_shift) + (token & (pool.page_size - 1))];
+    return *reinterpret_cast<const float4*>(pool.weights + ((page * pool.kv_heads + head) << pool.page_shift) + (token & (pool.page_size - 1)));
   };
-  uint32_t* mine_held = numbers + warp * held;
-  for (int at = begin; at < min(end, begin + held); at += 32 * kPickAhead) {
-    float x[kPickAhead];
+  auto numbers_of = [&](int token, const float4& x) {
+    auto one = [&](int i, float y) { return token + i >= first && token + i < n - last ? order_of(y) : 0u; };
+    return make_uint4(one(0, x.x), one(1, x.y), one(2, x.z), one(3, x.w));
+  };
+  uint4* mine_held = numbers + (warp * held >> 2);
+  const int end_held = min(end, begin + held);
+  for (int at = begin + 4 * lane; at - 4 * lane < end_held; at += kPickStep * kPickAhead) {
+    float4 x[kPickAhead];
 #pragma unroll
-    for (int j = 0; j < kPickAhead; ++j) {
-      const int i = at + 32 * j + lane;
-      if (i < end && i < begin + held) x[j] = tally_of(i);
-    }
+    for (int j = 0; j < kPickAhead; ++j)
+      if (at + kPickStep * j < end_held) x[j] = tallies_at(at + kPickStep * j);
 #pragma unroll
-    for (int j = 0; j < kPickAhead; ++j) {
-      const int i = at + 32 * j + lane;
-      if (i < end && i < begin + held) mine_held[i - begin] = order_of(x[j]);
-    }
+    for (int j = 0; j < kPickAhead; ++j)
+      if (at + kPickStep * j < end_held) mine_held[(at + kPickStep * j - begin) >> 2] = numbers_of(at + kPickStep * j, x[j]);
   }
-  // (a thread reads what it has written itself: numbers 32 apart)
-  auto order_at = [&](int i) { return i < begin + held ? mine_held[i - begin] : order_of(tally_of(i)); };
+  // (a thread reads what it has written itself)
+  auto numbers_at = [&](int token) {
+    if (token >= end) return make_uint4(0u, 0u, 0u, 0u);
+    return token < end_held ? mine_held[(token - begin) >> 2] : numbers_of(token, tallies_at(token));
+  };
   auto together = [&]() {
     if (blocks > 1) cluster_sync();
     else __syncthreads();
   };
   const uint32_t joint0 = blocks > 1 ? mapa_u32(smem_u32(sh.joint), 0) : smem_u32(sh.joint);
+  const uint32_t* joint = blocks > 1 ? sh.joint : sh.bins;  // in the first CTA
 
   uint32_t prefix = 0, known = 0, left = (uint32_t)choose;  // the upper bits of the least that stays; their mask; how many of those with them stay
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digits = pass == 2 ? 1023u : 2047u;
-    for (int i = threadIdx.x; i < kPickBins; i += kPickThreads) sh.bins[i] = sh.joint[i] = 0u;
+    for (int i = threadIdx.x; i < kPickBins; i += threads) {
+      sh.bins[i] = 0u;
+      if (blocks > 1) sh.joint[i] = 0u;
+    }
     together();
-    for (int at = begin; at < end; at += 32) {
-      const int i = at + lane;
-      const uint32_t x = i < end ? order_at(i) : 0u;
-      const bool counts = i < end && (x & known) == prefix;
-      const uint32_t bin = x >> shift & digits, active = __ballot_sync(0xffffffffu, counts);
-      if (active == 0u) continue;
-      // one of all where they agree, as where no tallies have been taken
-      const uint32_t some = __shfl_sync(0xffffffffu, bin, __ffs(active) - 1);
-      if (__all_sync(0xffffffffu, !counts || bin == some)) {
-        if (lane == 0) atomicAdd(&sh.bins[some], (uint32_t)__popc(active));
-      } else if (counts) {
-        atomicAdd(&sh.bins[bin], 1u);
+    for (int at = begin; at < end; at += kPickStep) {
+      const uint4 x4 = numbers_at(at + 4 * lane);
+      const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool counts = (x[j] & known) == prefix;
+        const uint32_t bin = x[j] >> shift & digits, active = __ballot_sync(0xffffffffu, counts);
+        if (active == 0u) continue;
+        // one of all where they agree, as where no tallies have been taken
+        const uint32_t some = __shfl_sync(0xffffffffu, bin, __ffs(active) - 1);
+        if (__all_sync(0xffffffffu, !counts || bin == some)) {
+          if (lane == 0) atomicAdd(&sh.bins[some], (uint32_t)__popc(active));
+        } else if (counts) {
+          atomicAdd(&sh.bins[bin], 1u);
+        }
       }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < kPickBins; i += kPickThreads)
-      if (sh.bins[i] != 0u) add_cluster(joint0 + 4 * i, sh.bins[i]);
+    if (blocks > 1) {
+      __syncthreads();
+      for (int i = threadIdx.x; i < kPickBins; i += threads)
+        if (sh.bins[i] != 0u) add_cluster(joint0 + 4 * i, sh.bins[i]);
+    }
     together();
     if (rank == 0) {
       // the bin that holds the left-th largest: the first one from above whose sum with those above it reaches that
-      constexpr int kEach = kPickBins / kPickThreads;
+      const int each = kPickBins / threads;
       uint32_t own = 0;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) own += sh.joint[kPickBins - 1 - (threadIdx.x * kEach + e)];
+      for (int e = 0; e < each; ++e) own += joint[kPickBins - 1 - (threadIdx.x * each + e)];
       uint32_t upto = own;
 #pragma unroll
       for (int d = 1; d < 32; d *= 2) {
@@ -135,12 +149,14 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
       }
       if (lane == 31) sh.scan[warp] = upto;
       __syncthreads();
-      uint32_t above = upto - own;
-      for (int w = 0; w < warp; ++w) above += sh.scan[w];
+      uint32_t in_front = lane < warp ? sh.scan[lane] : 0u;  // (at most 32 warps)
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) in_front += __shfl_xor_sync(0xffffffffu, in_front, d);
+      uint32_t above = in_front + upto - own;
       if (above < left && above + own >= left) {
-        for (int e = 0; e < kEach; ++e) {
-          const int bin = kPickBins - 1 - (threadIdx.x * kEach + e);
-          const uint32_t here = sh.joint[bin];
+        for (int e = 0; e < each; ++e) {
+          const int bin = kPickBins - 1 - (threadIdx.x * each + e);
+          const uint32_t here = joint[bin];
           if (above < left && above + here >= left) {
             sh.bin = (uint32_t)bin;
             sh.left = left - above;
@@ -155,40 +171,61 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
     prefix |= ld_cluster(at_bin) << shift;
     known |= digits << shift;
     left = ld_cluster(at_left);
+    if (blocks == 1) __syncthreads();  // (a cluster's next pass begins with a barrier before these are written again)
   }
-  // prefix: the least that stays; left: how many of its equals do, from the front
+  // prefix: the least that stays, which is somebody's; left: how many of its equals do, from the front
 
-  uint32_t above = 0, equal = 0;  // of this warp
-  for (int at = begin; at < end; at += 32) {
-    const int i = at + lane;
-    const uint32_t x = i < end ? order_at(i) : 0u;
-    above += __popc(__ballot_sync(0xffffffffu, i < end && x > prefix));
-    equal += __popc(__ballot_sync(0xffffffffu, i < end && x == prefix));
-  }
-  if (lane == 0) sh.warp_sums[warp][0] = above, sh.warp_sums[warp][1] = equal;
+  // Two counts, of larger ones and of equal ones, side by side in 64 bits.
+  auto counts_of = [&](const uint4& x) {
+    auto one = [&](uint32_t y) { return (unsigned long long)(y > prefix ? 1u : 0u) << 32 | (y == prefix ? 1u : 0u); };
+    return one(x.x) + one(x.y) + one(x.z) + one(x.w);
+  };
+  unsigned long long own = 0;
+  for (int at = begin; at < end; at += kPickStep) own += counts_of(numbers_at(at + 4 * lane));
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) own += __shfl_xor_sync(0xffffffffu, own, d);
+  if (lane == 0) sh.warp_sums[warp][0] = (uint32_t)(own >> 32), sh.warp_sums[warp][1] = (uint32_t)own;
   __syncthreads();
-  if (threadIdx.x < 2) {
-    uint32_t sum = 0;
-    for (int w = 0; w < kPickWarps; ++w) sum += sh.warp_sums[w][threadIdx.x];
-    sh.counts[threadIdx.x] = sum;
+  if (warp < 2) {
+    uint32_t sum = lane < n_warps ? sh.warp_sums[lane][warp] : 0u;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    if (lane == 0) sh.counts[warp] = sum;
   }
   together();
-  above = equal = 0;  // in front of this warp
-  for (int r = 0; r < rank; ++r) {
-    above += ld_cluster(mapa_u32(smem_u32(&sh.counts[0]), r));
-    equal += ld_cluster(mapa_u32(smem_u32(&sh.counts[1]), r));
+  // in front of this warp: the ranks', and the CTA's own warps'
+  uint32_t above = 0, equal = 0;
+  if (lane < rank) {
+    above = ld_cluster(mapa_u32(smem_u32(&sh.counts[0]), lane));
+    equal = ld_cluster(mapa_u32(smem_u32(&sh.counts[1]), lane));
   }
-  for (int w = 0; w < warp; ++w) above += sh.warp_sums[w][0], equal += sh.warp_sums[w][1];
-  const uint32_t before = (1u << lane) - 1u;
-  for (int at = begin; at < end; at += 32) {
-    const int i = at + lane;
-    const uint32_t x = i < end ? order_at(i) : 0u;
-    const uint32_t over = __ballot_sync(0xffffffffu, i < end && x > prefix), same = __ballot_sync(0xffffffffu, i < end && x == prefix);
-    const uint32_t rank_over = above + __popc(over & before), rank_same = equal + __popc(same & before);
-    const bool stays = i < end && (x > prefix || (x == prefix && rank_same < left));
-    if (stays) put(first + (int)(rank_over + min(rank_same, left)), first + i);
-    above += __popc(over);
-    equal += __popc(same);
+  if (lane < warp) above += sh.warp_sums[lane][0], equal += sh.warp_sums[lane][1];
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    above += __shfl_xor_sync(0xffffffffu, above, d);
+    equal += __shfl_xor_sync(0xffffffffu, equal, d);
+  }
+  for (int at = begin; at < end; at += kPickStep) {
+    const int token = at + 4 * lane;
+    const uint4 x4 = numbers_at(token);
+    const unsigned long long here = counts_of(x4);
+    unsigned long long upto = here;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += y;
+    }
+    const unsigned long long step = __shfl_sync(0xffffffffu, upto, 31);
+    uint32_t over = above + (uint32_t)((upto - here) >> 32), same = equal + (uint32_t)(upto - here);
+    const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (x[j] > prefix || (x[j] == prefix && same < left)) put(first + (int)(over + min(same, left)), token + j);
+      over += x[j] > prefix ? 1u : 0u;
+      same += x[j] == prefix ? 1u : 0u;
+    }
+    above += (uint32_t)(step >> 32);
+    equal += (uint32_t)step;
   }
   together();  // nobody's shared memory goes while others read it
 }
@@ -291,7 +328,7 @@ int pick_blocks() {
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kPickMostBlocks);
-    cfg.blockDim = dim3(kPickThreads);
+    cfg.blockDim = dim3(kPickMostThreads);
     cfg.dynamicSmemBytes = kPickMostHeld * 4;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
@@ -311,14 +348,17 @@ int pick_blocks() {
 cudaError_t launch_kv_evict(const litevggt_kv_cache& c, const litevggt_kv_batch& from, const litevggt_kv_batch& into, int first, int last,
                             int* kept, cudaStream_t s, int* launches) {
   const long long pairs = (long long)from.seqs.size() * c.cfg.kv_heads;
-  // CTAs of a head: as many as there is room for, where its tokens are more than four for each of a CTA's threads
+  // CTAs of a head: as many as there is room for, where its tokens are more than eight for each of a CTA's threads; and twice the threads
+  // where that is not enough.
   int longest = 0, blocks = 1;
   for (const KvSeq& q : from.seqs) longest = std::max(longest, q.len);
   const int most = pick_blocks();
-  while (blocks < most && 2 * blocks * pairs <= 2ll * c.num_sms && longest > blocks * 4 * kPickThreads) blocks *= 2;
-  const long long run = round_up(((long long)longest + blocks * kPickWarps - 1) / (blocks * kPickWarps), 32);
-  const int held = (int)std::min(run, (long long)kPickMostHeld / kPickWarps);
-  cudaError_t e = launch_clusters(blocks, true, kv_pick_kernel, dim3((unsigned)(pairs * blocks)), kPickThreads, (size_t)held * kPickWarps * 4, s, c.pool,
+  while (blocks < most && 2 * blocks * pairs <= 2ll * c.num_sms && longest > blocks * 8 * kPickThreads) blocks *= 2;
+  const int threads = longest > blocks * 16 * kPickThreads && blocks * pairs <= 2ll * c.num_sms ? kPickMostThreads : kPickThreads;
+  const int warps = threads / 32;
+  const long long run = round_up(((long long)longest + 3 + blocks * warps - 1) / (blocks * warps), kPickStep);
+  const int held = (int)std::min(run, (long long)kPickMostHeld / warps);
+  cudaError_t e = launch_clusters(blocks, true, kv_pick_kernel, dim3((unsigned)(pairs * blocks)), (unsigned)threads, (size_t)held * warps * 4, s, c.pool,
                                   kv_arrays(from), kv_arrays(into), first, last, blocks, held, kept);
   ++*launches;
   const long long pages = kv_page_count(into, c.cfg.page_size);

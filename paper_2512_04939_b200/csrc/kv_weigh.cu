@@ -57,6 +57,7 @@ struct FewKeys {
   static constexpr int kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps;
   static constexpr int kRun = kKind == LITEVGGT_KV_BF16 ? 8 : kKind == LITEVGGT_KV_E4M3 ? 16 : kHd / 4;  // channels side by side in a lane
   static constexpr int kWords = kRowBytes / 16;  // of a lane: a quarter of the row
+  static constexpr int kBlocks = kWords == 16 ? 2 : 4;  // on an SM: registers
   uint32_t w[4][kWords];                         // of the keys lane / 4 of four tiles of 8
   uint32_t byte[4];
 };
@@ -92,7 +93,7 @@ struct FewPlace {
 };
 
 template <int kHd, int kKind, bool kHalf>
-__global__ void __launch_bounds__(kWeighWarps * 32)
+__global__ void __launch_bounds__(kWeighWarps * 32, (FewKeys<kHd, kKind>::kBlocks))
 kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists lists, long long per_warp, long long units) {
   using Keys = FewKeys<kHd, kKind>;
   constexpr int kHalves = kHalf ? 1 : 2, kRun = Keys::kRun, kSteps = kHd / 16;
@@ -739,13 +740,13 @@ cudaError_t by_kind(const litevggt_kv_cache& c, const F& f) {
 cudaError_t launch_kv_weigh_few(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvWeighing& w, cudaStream_t s, int* launches) {
   const long long units = b.weigh.few_at.back() * c.cfg.kv_heads;
   if (units == 0) return cudaSuccess;
-  // A warp's run: as short as the chip allows, but no shorter than a unit.
-  const long long warps = std::min(units, (long long)c.num_sms * 16), per_warp = (units + warps - 1) / warps;
-  const unsigned blocks = (unsigned)(((units + per_warp - 1) / per_warp + kWeighWarps - 1) / kWeighWarps);
   const WeighLists lists{reinterpret_cast<const long long*>(b.base + b.o_few_at), 1, nullptr, nullptr};
   ++*launches;
   return by_kind(c, [&](auto hd, auto kind) {
     constexpr int kHd = decltype(hd)::value, kKind = decltype(kind)::value;
+    // A warp's run: as short as the chip allows, but no shorter than a unit.
+    const long long warps = std::min(units, (long long)c.num_sms * FewKeys<kHd, kKind>::kBlocks * kWeighWarps), per_warp = (units + warps - 1) / warps;
+    const unsigned blocks = (unsigned)(((units + per_warp - 1) / per_warp + kWeighWarps - 1) / kWeighWarps);
     auto go = [&](auto kernel) { return launch(kernel, dim3(blocks), kWeighWarps * 32, 0, s, c.pool, kv_arrays(b), w, lists, per_warp, units); };
     return b.few_rows <= 8 ? go(kv_weigh_few_kernel<kHd, kKind, true>) : go(kv_weigh_few_kernel<kHd, kKind, false>);
   });
