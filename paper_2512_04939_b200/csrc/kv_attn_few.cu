@@ -34,33 +34,6 @@ namespace lv {
 
 namespace {
 
-// Two codes (the low or the high half of a word) to two f16 numbers, exactly.
-__device__ __forceinline__ uint32_t widen_low(uint32_t w) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(w));
-  return r;
-}
-__device__ __forceinline__ uint32_t widen_high(uint32_t w) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(r) : "r"(w));
-  return r;
-}
-// The four bytes of a word, two E2M1 codes each, to pairs of f16 numbers, exactly; the low half's code to the low number.
-__device__ __forceinline__ void widen_codes4(uint32_t w, uint32_t (&out)[4]) {
-  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-      "mov.b32 {a, b, c, d}, %4;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
-      : "=r"(out[0]), "=r"(out[1]), "=r"(out[2]), "=r"(out[3])
-      : "r"(w));
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 __device__ __forceinline__ uint4 lds16(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
@@ -77,13 +50,6 @@ __device__ __forceinline__ void power_pair(uint32_t addr, float (&p)[2]) {
   asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(v) : "r"(addr));
   p[0] = __uint_as_float(v << 23 & 0x7f800000u);
   p[1] = __uint_as_float(v << 15 & 0x7f800000u);
-}
-// Of four bytes side by side.
-__device__ __forceinline__ void power_word(uint32_t v, float (&p)[4]) {
-  p[0] = __uint_as_float(v << 23 & 0x7f800000u);
-  p[1] = __uint_as_float(v << 15 & 0x7f800000u);
-  p[2] = __uint_as_float(v << 7 & 0x7f800000u);
-  p[3] = __uint_as_float(v >> 1 & 0x7f800000u);
 }
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_dst), "l"(src),
@@ -163,14 +129,17 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   const uint32_t ring = smem_u32(smem) + warp * kStages * Shape::kStageBytes;
 
   // ------------------------------------------------------------------ loads
-  // The stage that is fetched next, and its piece; a lane's copy is one of K or V of 16 keys (and 64 channels, or the codes or
-  // exponents).  Its page is looked up a stage ahead.
-  constexpr int kParts = kExps > 0 ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts;
+  // The stage that is fetched next, and its piece; a lane's copy is one of K or V of 16 keys and 64 channels, or of the codes or
+  // exponents of as many keys of the stage as lie in a page (every copy takes a dozen instructions, and codes are bound by them).  Its
+  // page is looked up a stage ahead.
+  constexpr int kParts = kExps > 0 ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts, kStageShift = kSubs == 2 ? 5 : 4;
+  static_assert(kExps == 0 || 1 << kStageShift == kStageKeys, "");
+  const int run_shift = kExps > 0 ? min(kStageShift, pool.page_shift) : 4;  // of a copy's keys
   const int my_part = lane % kParts, my_x = (lane / kParts) & 1, my_sub = lane / (2 * kParts);
   int f_id = (int)blockIdx.x, f_key = 0, f_end = 0, f_head = 0, f_page0 = 0, f_page = 0, f_next = -1;
   uint32_t fetched = 0;
   auto look_up = [&]() {
-    const int key = f_key + 16 * my_sub;
+    const int key = f_key + (my_sub << run_shift);
     if (lane < kCopies && key < f_end) f_page = arrays.pages[f_page0 + (key >> pool.page_shift)];
   };
   auto enter = [&]() {  // the first piece from f_id on that has keys for this warp
@@ -192,20 +161,17 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
     if (f_id < 0) return;
     const uint32_t stage = fetched % kStages;
     uint64_t* bar = &full[stage];
-    const int subs = min(kSubs, (f_end - f_key + 15) >> 4);
-    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(subs * (2 * Shape::kSubBytes + 32 * kExps)));
+    const int runs = min(kStageKeys >> run_shift, (f_end - f_key + (1 << run_shift) - 1) >> run_shift);
+    if (lane == 0) mbar_expect_tx(bar, (uint32_t)(runs * (2 * (kRowBytes + kExps)) << run_shift));
     __syncwarp();
-    if (lane < kCopies && my_sub < subs) {
-      const int key = f_key + 16 * my_sub;
+    if (lane < kCopies && my_sub < runs) {
+      const int key = f_key + (my_sub << run_shift);
       const long long row = ((long long)f_page * pool.kv_heads + f_head) * pool.page_size + (key & (pool.page_size - 1));
       const uint32_t base = ring + stage * Shape::kStageBytes;
       if constexpr (kExps > 0) {
-        if (my_part == 0) {
-          bulk_load(base + (my_x * kSubs + my_sub) * Shape::kSubBytes, (my_x == 0 ? pool.k : pool.v) + row * kRowBytes, 16 * kRowBytes, bar);
-        } else {
-          bulk_load(base + 2 * kSubs * Shape::kSubBytes + (my_x * kSubs + my_sub) * 16 * kExps, (my_x == 0 ? pool.k_exp : pool.v_exp) + row * kExps,
-                    16 * kExps, bar);
-        }
+        const int at = my_x * kStageKeys + (my_sub << run_shift);  // row of the stage
+        if (my_part == 0) bulk_load(base + at * kRowBytes, (my_x == 0 ? pool.k : pool.v) + row * kRowBytes, kRowBytes << run_shift, bar);
+        else bulk_load(base + 2 * kSubs * Shape::kSubBytes + at * kExps, (my_x == 0 ? pool.k_exp : pool.v_exp) + row * kExps, kExps << run_shift, bar);
       } else {
         const uint32_t dst = base + (my_x * kSubs + my_sub) * Shape::kSubBytes + my_part * 2048;
         asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
@@ -262,10 +228,9 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
         top = max(top & 0xffffu, top >> 16);
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // the row's largest element to [2^13, 2^14); rows of zeros or under 2^-113, and those that are not finite, as near as it goes
-        const int up = min(max(13 - ((int)(top >> 7) - 127), -126), 126);
-        const float factor = top >= 0x7f80u ? 1.0f : __int_as_float((up + 127) << 23);
-        if (top < 0x7f80u) row_scale[half] *= __int_as_float((127 - up) << 23);
+        const float2 factors = f16_factor(top);
+        const float factor = factors.x;
+        row_scale[half] *= factors.y;
 #pragma unroll
         for (int i = 0; i < kHd / 16; ++i)
 #pragma unroll

@@ -55,11 +55,12 @@ constexpr int kWeighWarps = 4;
 template <int kHd, int kKind>
 struct FewKeys {
   static constexpr int kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps;
-  static constexpr int kRun = kKind == LITEVGGT_KV_BF16 ? 8 : kKind == LITEVGGT_KV_E4M3 ? 16 : kHd / 4;  // channels side by side in a lane
+  static constexpr int kRun = kKind == LITEVGGT_KV_E4M3 ? 16 : 8;  // channels side by side in a lane
   static constexpr int kWords = kRowBytes / 16;  // of a lane: a quarter of the row
-  static constexpr int kBlocks = kWords == 16 ? 2 : 4;  // on an SM: registers
+  static constexpr int kBlocks = kWords == 16 ? 2 : kHd == 128 ? 3 : 4;  // on an SM: registers
   uint32_t w[4][kWords];                         // of the keys lane / 4 of four tiles of 8
-  uint32_t byte[4];
+  static constexpr int kExpWords = kExps > 2 ? kExps / 2 : 1;
+  uint32_t exps[4][kExpWords];  // of the keys 2 (lane % 4) and the next one of each tile
 };
 
 // Where a warp is in its run: a head's unit, and the pages that its first and its second 16 keys lie in.
@@ -118,11 +119,11 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
   auto load = [&](Keys& k, const FewPlace& p) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const size_t row = p.row(pool, t >> 1) + 8 * (t & 1) + g;
-      const uint8_t* src = pool.k + row * Keys::kRowBytes;
-      if constexpr (Keys::kWords == 2) {
-        const uint2 x = *reinterpret_cast<const uint2*>(src + q4 * 8);
-        k.w[t][0] = x.x, k.w[t][1] = x.y;
+      const size_t row0 = p.row(pool, t >> 1) + 8 * (t & 1);
+      const uint8_t* src = pool.k + (row0 + g) * Keys::kRowBytes;
+      if constexpr (kKind == LITEVGGT_KV_E2M1) {
+#pragma unroll
+        for (int i = 0; i < Keys::kWords; ++i) k.w[t][i] = *reinterpret_cast<const uint32_t*>(src + i * 16 + q4 * 4);
       } else {
 #pragma unroll
         for (int i = 0; i < Keys::kWords / 4; ++i) {
@@ -130,7 +131,15 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
           k.w[t][4 * i] = x.x, k.w[t][4 * i + 1] = x.y, k.w[t][4 * i + 2] = x.z, k.w[t][4 * i + 3] = x.w;
         }
       }
-      if constexpr (Keys::kExps > 0) k.byte[t] = pool.k_exp[row * Keys::kExps + (kKind == LITEVGGT_KV_E2M1 ? q4 * Keys::kExps / 4 : 0)];
+      if constexpr (Keys::kExps > 0) {
+        const uint8_t* at = pool.k_exp + (row0 + 2 * q4) * Keys::kExps;
+        if constexpr (Keys::kExps == 1) {
+          k.exps[t][0] = *reinterpret_cast<const uint16_t*>(at);
+        } else {
+#pragma unroll
+          for (int i = 0; i < Keys::kExpWords; ++i) k.exps[t][i] = reinterpret_cast<const uint32_t*>(at)[i];
+        }
+      }
     }
   };
   Keys k, k_ahead;
@@ -138,6 +147,9 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
   bool fresh = true;
   uint32_t qa[kSteps][2 * kHalves];
   float less[kHalves];  // the rows' log-sum-exp in base 2
+  float row_scale[kHalves];
+  constexpr bool kCodes = kKind != LITEVGGT_KV_BF16;  // their products are of f16, the powers of two stay outside
+  constexpr int kBlocks = kKind == LITEVGGT_KV_E2M1 ? kHd / 32 : 1;
   int seen[kHalves];
   for (; unit < end; ++unit) {
     FewPlace behind = ahead;
@@ -160,6 +172,24 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
             qa[i * (kRun / 4) + j][half] = x.x;
             qa[i * (kRun / 4) + j][kHalves + half] = x.y;
           }
+        row_scale[half] = in.scale_log2;
+        if constexpr (kCodes) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) top = __vmaxu2(top, __vmaxu2(qa[i][half] & 0x7fff7fffu, qa[i][kHalves + half] & 0x7fff7fffu));
+          top = max(top & 0xffffu, top >> 16);
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const float2 factors = f16_factor(top);
+          row_scale[half] *= factors.y;
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t x = qa[i][j * kHalves + half];
+              qa[i][j * kHalves + half] = pack_f16(bf16_lo(x) * factors.x, bf16_hi(x) * factors.x);
+            }
+        }
         less[half] = live ? -kLog2e * in.lse[(long long)(seq.row0 + token) * in.q_heads + q_head] : 0.0f;
         seen[half] = live ? kv_seen(seq.len, seq.rows, in.causal_block, token) : 0;
       }
@@ -168,31 +198,33 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
     float drawn[4][2];  // of the keys 2 q4 and 2 q4 + 1 of each tile, over this lane's rows
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      float c[kBlocks][4];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) c[b][0] = c[b][1] = c[b][2] = c[b][3] = 0.0f;
       auto step = [&](int n, uint32_t b0, uint32_t b1) {
-        if constexpr (kHalf) mma_16816<false>(c, qa[n][0], 0u, qa[n][1], 0u, b0, b1);
-        else mma_16816<false>(c, qa[n][0], qa[n][kHalves - 1], qa[n][kHalves], qa[n][2 * kHalves - 1], b0, b1);
+        float (&to)[4] = c[kBlocks > 1 ? n / 2 : 0];
+        if constexpr (kHalf) mma_16816<kCodes>(to, qa[n][0], 0u, qa[n][1], 0u, b0, b1);
+        else mma_16816<kCodes>(to, qa[n][0], qa[n][kHalves - 1], qa[n][kHalves], qa[n][2 * kHalves - 1], b0, b1);
       };
+      float power[kCodes ? 4 * Keys::kExpWords : 1];  // of the two keys, block by block
       if constexpr (kKind == LITEVGGT_KV_BF16) {
 #pragma unroll
         for (int n = 0; n < kSteps; ++n) step(n, k.w[t][2 * n], k.w[t][2 * n + 1]);
       } else if constexpr (kKind == LITEVGGT_KV_E4M3) {
-        const KvFactor f = kv_factor(k.byte[t]);
 #pragma unroll
-        for (int n = 0; n < kSteps; ++n) {
-          uint32_t lo = mul_bf16x2(kv_code_bits(__byte_perm(k.w[t][n], 0u, 0x1404)), f.first * 0x10001u);
-          uint32_t hi = mul_bf16x2(kv_code_bits(__byte_perm(k.w[t][n], 0u, 0x3424)), f.first * 0x10001u);
-          if (kv_needs_second(k.byte[t])) lo = mul_bf16x2(lo, f.second * 0x10001u), hi = mul_bf16x2(hi, f.second * 0x10001u);
-          step(n, lo, hi);
-        }
+        for (int n = 0; n < kSteps; ++n) step(n, widen_low(k.w[t][n]), widen_high(k.w[t][n]));
       } else {
 #pragma unroll
-        for (int i = 0; i < kHd / 32; ++i) {
+        for (int i = 0; i < kBlocks; ++i) {
           uint32_t x[4];
-          kv4_widen(k.w[t][i], k.byte[t], x);
+          widen_codes4(k.w[t][i], x);
           step(2 * i, x[0], x[1]);
           step(2 * i + 1, x[2], x[3]);
         }
+      }
+      if constexpr (kCodes) {
+#pragma unroll
+        for (int i = 0; i < Keys::kExpWords; ++i) power_word(k.exps[t][i], *reinterpret_cast<float (*)[4]>(&power[4 * i]));
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -200,7 +232,13 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
         drawn[t][e] = 0.0f;
 #pragma unroll
         for (int half = 0; half < kHalves; ++half) {
-          const float p = fast_exp2(fmaf(c[2 * half + e], in.scale_log2, less[half]));
+          float x = less[half];
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b) {
+            const float y = c[b][2 * half + e];
+            x = kCodes ? fmaf(y * row_scale[half], power[kCodes ? e * kBlocks + b : 0], x) : fmaf(y, row_scale[half], x);
+          }
+          const float p = fast_exp2(x);
           if (key < seen[half]) drawn[t][e] += p;
         }
       }

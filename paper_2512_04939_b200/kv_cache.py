@@ -200,7 +200,7 @@ class KVCache:
             if not out.is_contiguous():
                 raise ValueError("out must be contiguous")
         if lse is True:
-            lse = torch.empty(batch.q_shape[:2], dtype=torch.float32, device=self.device)
+            lse = q.new_empty(batch.q_shape[:2], dtype=torch.float32)
         elif lse is not False:
             self._sums(batch, lse)
         code = self._attend(self.handle, batch.handle, *q_rows, self._scale if scale is None else scale, out.data_ptr(),

@@ -67,10 +67,10 @@ class RotaryAxes:
         # (a small call takes as long as its checks do)
         if k is None:
             given = (q,)
-            outs = (q.new_empty(q.shape),) if out is None else (out,)
+            outs = (torch.empty_like(q),) if out is None else (out,)
         else:
             given = (q, k)
-            outs = (q.new_empty(q.shape), k.new_empty(k.shape)) if out is None else tuple(out)
+            outs = (torch.empty_like(q), torch.empty_like(k)) if out is None else tuple(out)
         kind, rows, index = _DTYPES.get(q.dtype), q.shape[0] if q.dim() == 3 else -1, self._index
         fine = (kind is not None and len(outs) == len(given) and positions.shape == (self._axes, rows) and positions.dtype == torch.int32
                 and positions.get_device() == index)
