@@ -435,8 +435,8 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               v_bytes[h] = __byte_perm(x.x, x.y, 0x0400u + block * 0x101u) & 0x00ff00ffu;
             }
           }
-          // Blocks whose factor is one bf16 number (and so none that are not finite): two keys' codes of a channel go into one byte,
-          // which is a pair of the operand once it is widened.
+          // Blocks whose factor is one bf16 number (and so none that are not finite): two keys' codes of a channel are widened together, into a
+          // pair of the operand.
           if (!__any_sync(0xffffffffu, ((v_bytes[0] + 0x007f007fu | v_bytes[1] + 0x007f007fu) & 0x01000100u) != 0u)) {
             const uint32_t factors[2] = {v_bytes[0] + 0x007e007eu << 7, v_bytes[1] + 0x007e007eu << 7};
 #pragma unroll
@@ -446,8 +446,8 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
               for (int h = 0; h < 2; ++h) {
                 const uint32_t at_row = at_sub + (2 * q4 + 8 * h) * kRowBytes + g * (kRowBytes / 8) + 4 * i;
                 const uint32_t a = lds4(at_row), b = lds4(at_row + kRowBytes);
-                kv4_widen_by((a & 0x0f0f0f0fu) | (b << 4 & 0xf0f0f0f0u), factors[h], even[h]);
-                kv4_widen_by((a >> 4 & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), factors[h], odd[h]);
+                kv4_widen_by(kv4_low(a), kv4_low(b), factors[h], even[h]);
+                kv4_widen_by(kv4_high(a), kv4_high(b), factors[h], odd[h]);
               }
 #pragma unroll
               for (int j = 0; j < 8; ++j) {

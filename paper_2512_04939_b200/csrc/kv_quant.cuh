@@ -64,20 +64,24 @@ __device__ __forceinline__ KvFactor kv4_factor(uint32_t byte) {
   return f;
 }
 __device__ __forceinline__ bool kv4_needs_second(uint32_t byte) { return byte > 128u; }  // (blocks whose largest magnitude is over 12)
-// Four bytes of two codes each to four pairs of bf16, the low half's code to the low number, times a pair of factors.
-__device__ __forceinline__ void kv4_widen_by(uint32_t w, uint32_t factors, uint32_t (&out)[4]) {
-  const uint32_t low = w << 4;  // the low halves' codes in the upper halves of the bytes
-  constexpr uint32_t kPick[4] = {0x4000u, 0x5010u, 0x6020u, 0x7030u};
+// The codes in the low and in the high halves of four bytes, a byte each.
+__device__ __forceinline__ uint32_t kv4_low(uint32_t w) { return w & 0x0f0f0f0fu; }
+__device__ __forceinline__ uint32_t kv4_high(uint32_t w) { return w >> 4 & 0x0f0f0f0fu; }
+// Codes that are bytes of `low` and of `high` to four pairs of bf16, times a pair of factors.  A code's bits times 2^6 + 2^12 are its
+// magnitude's where they belong, and its sign's, and others that a mask takes out: a multiplication, which the FMA pipes have time
+// for, in place of the shifts that the logic unit, which bounds all this, has not.
+__device__ __forceinline__ void kv4_widen_by(uint32_t low, uint32_t high, uint32_t factors, uint32_t (&out)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t t = __byte_perm(low, w, kPick[i]);
-    out[i] = mul_bf16x2((t & 0x80008000u) | (t >> 6 & 0x01c001c0u), factors);
+  for (uint32_t i = 0; i < 4; ++i) {
+    uint32_t t;  // (8: the sign of a byte that has none, a byte of zeros; __byte_perm does not know it)
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(t) : "r"(low), "r"(high), "r"(0x8480u + 0x101u * i));
+    out[i] = mul_bf16x2(t * 0x1040u & 0x81c081c0u, factors);
   }
 }
 // Eight codes of a block to eight bf16.
 __device__ __forceinline__ void kv4_widen(uint32_t w, uint32_t byte, uint32_t (&out)[4]) {
   const KvFactor f = kv4_factor(byte);
-  kv4_widen_by(w, f.first * 0x10001u, out);
+  kv4_widen_by(kv4_low(w), kv4_high(w), f.first * 0x10001u, out);
   if (kv4_needs_second(byte)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = mul_bf16x2(out[i], f.second * 0x10001u);
