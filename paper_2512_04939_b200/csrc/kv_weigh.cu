@@ -279,30 +279,18 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
 // Scores on the 5th-generation tensor cores, 128 keys by 128 rows a product, kTiles of them side by side against the same rows.  One
 // exponential a score and 64 (128) multiplications for it, so the special-function unit is the bound, at 16 a clock; the products need
 // an eighth (a quarter) of its time.  Roles: eight warps take the exponentials, each thread a key against all rows or a share of them; one
-// issues the products; two fetch K once an item, two Q tile by tile, into swizzled shared memory (widening codes on the way), with what
-// the exponentials need of a row: its log-sum-exp and how many keys it sees; and one finds out what the CTA's items are, 32 at a time and
-// ahead of all others: the divisions and searches of that, thousands of clocks in a row, were half of the time of short items.
-constexpr int kDrawWarps = 8, kKeyWarps = 2, kRowWarps = 2;
-constexpr int kIssuer = kDrawWarps, kPlanner = kIssuer + 1, kKeyFetcher = kPlanner + 1, kRowFetcher = kKeyFetcher + kKeyWarps;
-constexpr int kWeighThreads = (kRowFetcher + kRowWarps) * 32;
+// issues the products; one fetches K once an item, by TMA, or two widen its codes; four fetch Q tile by tile into swizzled shared memory,
+// with what the exponentials need of a row, its log-sum-exp and how many keys it sees (two warps: head dim 128 20 % slower); and one
+// finds out what the CTA's items are, 32 at a time and ahead of all others: the divisions and searches of that, thousands of clocks in a
+// row, were half of the time of short items.
+// 4164 rows over 41,640 keys, 16 heads of 64: 806 us, 3.3 10^12 exponentials a second, four fifths of what the unit gives at the clock held
+// (1.76 GHz).  Tried and left: an eighth and a quarter of the exponentials on the FMA pipes (816, 850: the two warps of a scheduler wait for one
+// another's results longer than they gain), sixteen warps with half of the rows each (7 % slower).
+constexpr int kDrawWarps = 8, kRowWarps = 4;
+constexpr int kIssuer = kDrawWarps, kPlanner = kIssuer + 1, kRowFetcher = kPlanner + 1, kKeyFetcher = kRowFetcher + kRowWarps;
 // Items that are known ahead.  Rows of up to two of them wait for the next ones' to be asked for before they are handed over, so the
 // items behind those have to be known before they are done with.
 constexpr int kRing = 4;
-// Of 16 pairs of scores so many take their exponentials on the FMA pipes, as exactly as the unit's own, where all rows see all keys.
-#ifndef LITEVGGT_WEIGH_POLY
-#define LITEVGGT_WEIGH_POLY 0
-#endif
-constexpr int kPolyPairs = LITEVGGT_WEIGH_POLY;
-constexpr float kRound = 12582912.0f;            // 1.5 * 2^23: adding it rounds to whole numbers
-constexpr float kHeld = 4.1538374868278621e34f;  // 2^115: sums below it hold no exponential of an argument that was held
-// Arguments are held to [-125, 125]: what lies below is next to nothing anyhow, what lies above shows in the sum, as a NaN does, of which
-// the polynomial makes the largest finite number.
-__device__ __forceinline__ float hold(float x) {
-  float y;
-  asm("{\n\t.reg .f32 t;\n\tmin.NaN.f32 t, %1, 0f42FA0000;\n\tmax.NaN.f32 %0, t, 0fC2FA0000;\n\t}" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // An item's part, as every role sees it.
 struct WeighUnit {
   KvSeq seq;
@@ -350,9 +338,10 @@ __device__ __forceinline__ WeighUnit weigh_unit(const KvArrays& arrays, const We
   return u;
 }
 
-template <int kHd, int kTiles>
+template <int kHd, int kKind, int kTiles>
 struct WeighShape {
   static constexpr int kStages = kHd == 64 ? 4 : 2;  // of Q
+  static constexpr int kKeyWarps = kKind == LITEVGGT_KV_BF16 ? 1 : 2, kThreads = (kKeyFetcher + kKeyWarps) * 32;
   static constexpr int kSubBytes = 128 * 128, kTileBytes = kSubBytes * kHd / 64;
   static constexpr int kShares = kDrawWarps / (4 * kTiles);  // threads that share a key's rows
   static constexpr int kCols = 128 / kShares;                // rows of a thread in a tile
@@ -381,9 +370,10 @@ struct WeighRow {
 };
 
 template <int kHd, int kKind, int kTiles>
-__global__ void __launch_bounds__(kWeighThreads, 1)
-kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists lists, long long units, uint32_t* status) {
-  using Shape = WeighShape<kHd, kTiles>;
+__global__ void __launch_bounds__((WeighShape<kHd, kKind, kTiles>::kThreads), 1)
+kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, KvArrays arrays, KvWeighing in, WeighLists lists, long long units, uint32_t* status) {
+  using Shape = WeighShape<kHd, kKind, kTiles>;
+  constexpr int kKeyWarps = Shape::kKeyWarps;
   constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kSubBytes = Shape::kSubBytes, kShares = Shape::kShares;
   constexpr int kCols = Shape::kCols, kBlock = 128 * kTiles;
   extern __shared__ uint8_t smem_raw[];
@@ -464,14 +454,48 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
       }
       if (there < 32) break;
     }
-  } else if (warp >= kKeyFetcher && warp < kRowFetcher) {
-    // ------------------------------------------------------------------ K
+  } else if (kKind == LITEVGGT_KV_BF16 && warp >= kKeyFetcher) {
+    // ------------------------------------------------------------------ K by TMA: lane i fetches an item's i-th page
+    // (Keys behind the sequence's last page are what was there before: their scores are nobody's.)
+    wait_for_previous_kernel();
+    uint32_t count = 0;
+    each_unit([&](const WeighUnit& u) {
+      if (u.tile0 >= u.tile1) return;
+      ok = mbar_wait_warp(&bars->k_empty[count & 1u], ((count >> 1) & 1u) ^ 1u, ctl);
+      if (!ok) return;
+      uint64_t* full = &bars->k_full[count & 1u];
+      const int n = min(kBlock >> pool.page_shift, (u.seq.len - u.key0 + pool.page_size - 1) >> pool.page_shift);
+      long long row = 0;
+      if (lane < n) row = ((long long)arrays.pages[u.seq.page0 + (u.key0 >> pool.page_shift) + lane] * pool.kv_heads + u.head) << pool.page_shift;
+      if (lane == 0) mbar_expect_tx(full, (uint32_t)(n * pool.page_size * kHd * 2));
+      __syncwarp();
+      if (lane < n) {
+        const int at = lane << pool.page_shift;  // the page's first row of the block
+        uint8_t* dst = smem_k + ((count & 1u) * kTiles + (at >> 7)) * kTileBytes + (at & 127) * 128;
+#pragma unroll
+        for (int s = 0; s < kHd / 64; ++s) tma_load_2d(dst + s * kSubBytes, &k_map, full, s * 64, (int)row);
+      }
+      __syncwarp();
+      ++count;
+    });
+    if (lane == 0) {  // every load has landed before the CTA may go
+      for (uint32_t i = 0; i < min(count, 2u); ++i) {
+        const uint32_t at = count - 1 - i;
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&bars->k_full[at & 1u], (at >> 1) & 1u)) {
+          if (clock64() - t0 > kTimeoutCycles) { atomicOr(status, kStatusTimeout); break; }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp >= kKeyFetcher) {
+    // ------------------------------------------------------------------ K, widened
     // Keys behind the sequence's end are zeros: their scores are nobody's, but they are scores.
     wait_for_previous_kernel();
     const int tid = threadIdx.x - kKeyFetcher * 32;
     constexpr int kThreads = kKeyWarps * 32, kRowBytes = KvRow<kHd, kKind>::kBytes, kExps = KvRow<kHd, kKind>::kExps, kPerRow = kRowBytes / 16;
-    constexpr int kPasses = kBlock * kPerRow / kThreads, kMost = kKind == LITEVGGT_KV_BF16 ? 16 : 8;
-    constexpr int kTogether = kPasses < kMost ? kPasses : kMost;  // accesses of a thread that are under way together
+    constexpr int kPasses = kBlock * kPerRow / kThreads;
+    constexpr int kTogether = kPasses < 8 ? kPasses : 8;  // accesses of a thread that are under way together
     uint32_t count = 0;
     each_unit([&](const WeighUnit& u) {
       if (u.tile0 >= u.tile1) return;
@@ -490,18 +514,14 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
         }
 #pragma unroll
         for (int i = 0; i < kTogether; ++i) {
-          const int piece = (pass + i) * kThreads + tid, in_block = piece / kPerRow, key = u.key0 + in_block, part = piece % kPerRow;
+          const int piece = (pass + i) * kThreads + tid, key = u.key0 + piece / kPerRow, part = piece % kPerRow;
           const bool there = key < u.seq.len;
           const size_t row = there ? (((size_t)page[i] * pool.kv_heads + u.head) << pool.page_shift) + (key & (pool.page_size - 1)) : 0;
           const uint8_t* src = pool.k + row * kRowBytes + part * 16;
-          if constexpr (kKind == LITEVGGT_KV_BF16) {
-            cp_async16(place(tiles + (in_block >> 7) * kTileBytes, in_block & 127, part), src, there);
-          } else {
-            x[i] = there ? ldg16(src) : make_uint4(0u, 0u, 0u, 0u);
-            byte[i] = there ? pool.k_exp[row * kExps + (kKind == LITEVGGT_KV_E2M1 ? part : 0)] : 127u;
-          }
+          x[i] = there ? ldg16(src) : make_uint4(0u, 0u, 0u, 0u);
+          byte[i] = there ? pool.k_exp[row * kExps + (kKind == LITEVGGT_KV_E2M1 ? part : 0)] : 127u;
         }
-        if constexpr (kKind != LITEVGGT_KV_BF16) {
+        {
 #pragma unroll
           for (int i = 0; i < kTogether; ++i) {
             const int piece = (pass + i) * kThreads + tid, row = piece / kPerRow, part = piece % kPerRow;
@@ -533,14 +553,12 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
           }
         }
       }
-      cp_async_commit();
-      cp_async_wait<0>();
       fence_proxy_async_shared();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars->k_full[count & 1u]);
       ++count;
     });
-  } else if (warp >= kRowFetcher) {
+  } else if (warp >= kRowFetcher && warp < kKeyFetcher) {
     // ------------------------------------------------------------------ Q
     // Copies of the last kLag tiles are under way, a group each; what has arrived is handed over by the threads that asked for it.
     // A thread meets every kStep-th row of a tile, eight channels of it, and kInfo rows of which it leaves what the exponentials need.
@@ -560,6 +578,16 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
     each_unit([&](const WeighUnit& u) {
       const int rows = u.seq.rows * group;
       WeighRow mine(u.tile0 * kKvWeighRows + tid / kPerRow, group), info(u.tile0 * kKvWeighRows + tid, group);
+      float ahead[kInfo];  // the next tile's
+      auto look_ahead = [&]() {
+        WeighRow r = info;
+#pragma unroll
+        for (int i = 0; i < kInfo; ++i) {
+          ahead[i] = r.row < rows ? in.lse[(long long)(u.seq.row0 + r.token) * in.q_heads + u.head * group + r.head] : 0.0f;
+          r.advance(kThreads, info_tokens, info_heads, group);
+        }
+      };
+      look_ahead();
       for (int t = u.tile0; t < u.tile1; ++t) {
         const uint32_t stage = count % kStages;
         const bool edge = u.edge(group, t, kTiles - 1);  // (of the first keys only where of the last)
@@ -567,11 +595,11 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
         int seen[kInfo];
 #pragma unroll
         for (int i = 0; i < kInfo; ++i) {
-          const bool there = info.row < rows;
-          less[i] = there ? in.lse[(long long)(u.seq.row0 + info.token) * in.q_heads + u.head * group + info.head] : 0.0f;
-          seen[i] = edge && there ? kv_seen(u.seq.len, u.seq.rows, in.causal_block, info.token) : 0;  // (looked at where there is an edge)
+          less[i] = ahead[i];
+          seen[i] = edge && info.row < rows ? kv_seen(u.seq.len, u.seq.rows, in.causal_block, info.token) : 0;  // (looked at where there is an edge)
           info.advance(kThreads, info_tokens, info_heads, group);
         }
+        if (t + 1 < u.tile1) look_ahead();
         ok = mbar_wait_warp(&bars->q_empty[stage], ((count / kStages) & 1u) ^ 1u, ctl);
         if (!ok) return;
         ++count;
@@ -663,9 +691,8 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
         tc_fence_after();
         const float* less = row_less + stage * 128 + share * kCols;
         const int* seen = row_seen + stage * 128 + share * kCols;
-        auto tile_sum = [&](auto poly_constant) {
-          constexpr int kPoly = decltype(poly_constant)::value;
-          constexpr bool kEdge = kPoly < 0;
+        auto tile_sum = [&](auto edge_constant) {
+          constexpr bool kEdge = decltype(edge_constant)::value;
           float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
           uint32_t x[2][32];  // the next 32 are on their way while these are worked on
           tmem_ld32(d_addr + slot * 128, x[0]);
@@ -679,8 +706,7 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
               const float4 l4 = *reinterpret_cast<const float4*>(less + c * 32 + (2 * i & ~3));
               const float2 l = i & 1 ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y);
               float2 y = __ffma2_rn(make_float2(__uint_as_float(now[2 * i]), __uint_as_float(now[2 * i + 1])), scale2, l);
-              if (i < kPoly) y = poly_exp2_pair<true>(make_float2(hold(y.x), hold(y.y)), make_float2(kRound, kRound), make_float2(-kRound, -kRound));
-              else y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+              y = make_float2(fast_exp2(y.x), fast_exp2(y.y));
               if constexpr (kEdge) {
                 const int2 s = *reinterpret_cast<const int2*>(seen + c * 32 + 2 * i);
                 y = make_float2(key < s.x ? y.x : 0.0f, key < s.y ? y.y : 0.0f);
@@ -691,14 +717,7 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
           sum[0] = __fadd2_rn(sum[0], sum[1]);
           return sum[0].x + sum[0].y;
         };
-        float sum;
-        if (u.edge(in.group, t, kt)) {
-          sum = tile_sum(std::integral_constant<int, -1>{});
-        } else {
-          sum = tile_sum(std::integral_constant<int, kPolyPairs>{});
-          // a score that is not finite, or that no sum of exponentials has
-          if (kPolyPairs > 0 && __any_sync(0xffffffffu, !(sum < kHeld))) sum = tile_sum(std::integral_constant<int, 0>{});
-        }
+        const float sum = u.edge(in.group, t, kt) ? tile_sum(std::true_type{}) : tile_sum(std::false_type{});
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -749,7 +768,7 @@ kv_weigh_tiles_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists li
 
 template <int kHd, int kKind, int kTiles>
 cudaError_t start_tiles(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvWeighing& w, cudaStream_t s) {
-  using Shape = WeighShape<kHd, kTiles>;
+  using Shape = WeighShape<kHd, kKind, kTiles>;
   static_assert(Shape::kSmemBytes <= 227 * 1024, "");
   auto kernel = kv_weigh_tiles_kernel<kHd, kKind, kTiles>;
   static std::atomic<unsigned long long> done{0};
@@ -758,7 +777,7 @@ cudaError_t start_tiles(const litevggt_kv_cache& c, const litevggt_kv_batch& b, 
   const WeighLists lists{reinterpret_cast<const long long*>(b.base + b.o_tiles_at), b.weigh.parts, reinterpret_cast<int*>(b.base + b.o_weigh_joins),
                          reinterpret_cast<float*>(b.base + b.o_weigh_sums)};
   const long long units = b.weigh.items * b.weigh.parts;
-  return launch(kernel, dim3((unsigned)std::min(units, (long long)c.num_sms)), kWeighThreads, (size_t)Shape::kSmemBytes, s, c.pool, kv_arrays(b), w, lists,
+  return launch(kernel, dim3((unsigned)std::min(units, (long long)c.num_sms)), (unsigned)Shape::kThreads, (size_t)Shape::kSmemBytes, s, c.k_map, c.pool, kv_arrays(b), w, lists,
                 units, c.status);
 }
 
