@@ -17,6 +17,7 @@ constexpr int kPickThreads = 512, kPickMostThreads = 1024, kPickBins = 2048;
 constexpr int kPickMostBlocks = 16, kPickPortableBlocks = 8;  // of a cluster
 constexpr int kPickAhead = 4;                                 // loads of four tallies that a thread has under way together
 constexpr int kPickStep = 128;                                // tokens of a warp's step
+constexpr uint32_t kPickFew = 512;                            // numbers that are compared with one another
 constexpr int kPickMostHeld = 48 * 1024;                      // numbers in a CTA's shared memory; what lies behind them is read again
 
 // Orders as the tallies do; zeros are equal, NaN is less than any number; 0 is nobody's.
@@ -35,21 +36,24 @@ __device__ __forceinline__ void add_cluster(uint32_t addr, uint32_t n) {
   asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(addr), "r"(n) : "memory");
 }
 
-struct PickShared {
+struct alignas(16) PickShared {
   uint32_t bins[kPickBins];   // of this CTA's tokens
-  uint32_t joint[kPickBins];  // of the cluster's, in its first CTA
+  uint32_t joint[kPickBins];  // of the cluster's, in its first CTA; of a CTA by itself the list of those that are few
   uint32_t warp_sums[kPickMostThreads / 32][2];
   uint32_t counts[2];         // of this CTA: above the least that stays, equal to it
-  uint32_t bin, left;         // first CTA: the bin that the least one lies in, how many of it stay
+  uint32_t bin, left, in_bin; // first CTA: the bin that the least one lies in, how many of it stay, and are there
+  uint32_t listed;
   uint32_t scan[kPickMostThreads / 32];
 };
 
 // blockIdx.x = (sequence * heads + head) * blocks of a cluster + block; `held`: numbers that a warp keeps in shared memory
-__global__ void __launch_bounds__(kPickMostThreads)
+// (three blocks of the smaller kind on an SM: 16 heads of 24 sequences are there at once)
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == kPickThreads ? 3 : 1)
 kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, int blocks, int held, int* kept) {
   __shared__ PickShared sh;
   extern __shared__ uint4 numbers[];  // [warp][held / 4]
-  const int threads = blockDim.x, n_warps = threads >> 5;
+  constexpr int threads = kThreads, n_warps = threads / 32;
   const int rank = blocks > 1 ? (int)cluster_ctarank() : 0, pair = (int)blockIdx.x / blocks;
   const int head = pair % pool.kv_heads, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // (a batch's arrays were there before whatever kernel is still running)
@@ -116,18 +120,26 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
     for (int at = begin; at < end; at += kPickStep) {
       const uint4 x4 = numbers_at(at + 4 * lane);
       const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+      bool counts[4], some = false;
+      uint32_t bin[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bool counts = (x[j] & known) == prefix;
-        const uint32_t bin = x[j] >> shift & digits, active = __ballot_sync(0xffffffffu, counts);
-        if (active == 0u) continue;
-        // one of all where they agree, as where no tallies have been taken
-        const uint32_t some = __shfl_sync(0xffffffffu, bin, __ffs(active) - 1);
-        if (__all_sync(0xffffffffu, !counts || bin == some)) {
-          if (lane == 0) atomicAdd(&sh.bins[some], (uint32_t)__popc(active));
-        } else if (counts) {
-          atomicAdd(&sh.bins[bin], 1u);
-        }
+        counts[j] = (x[j] & known) == prefix;
+        bin[j] = x[j] >> shift & digits;
+        some = some || counts[j];
+      }
+      if (!__any_sync(0xffffffffu, some)) continue;
+      // one of all where they agree, as where no tallies have been taken: the unit that adds takes them one by one
+      const uint32_t first_bin = __shfl_sync(0xffffffffu, bin[0], 0);
+      bool alike = true;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) alike = alike && counts[j] && bin[j] == first_bin;
+      if (__all_sync(0xffffffffu, alike)) {
+        if (lane == 0) atomicAdd(&sh.bins[first_bin], 128u);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (counts[j]) atomicAdd(&sh.bins[bin[j]], 1u);
       }
     }
     if (blocks > 1) {
@@ -138,7 +150,7 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
     together();
     if (rank == 0) {
       // the bin that holds the left-th largest: the first one from above whose sum with those above it reaches that
-      const int each = kPickBins / threads;
+      constexpr int each = kPickBins / threads;
       uint32_t own = 0;
       for (int e = 0; e < each; ++e) own += joint[kPickBins - 1 - (threadIdx.x * each + e)];
       uint32_t upto = own;
@@ -160,6 +172,7 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
           if (above < left && above + here >= left) {
             sh.bin = (uint32_t)bin;
             sh.left = left - above;
+            sh.in_bin = here;
           }
           above += here;
         }
@@ -171,7 +184,42 @@ kv_pick_kernel(KvPool pool, KvArrays from, KvArrays into, int first, int last, i
     prefix |= ld_cluster(at_bin) << shift;
     known |= digits << shift;
     left = ld_cluster(at_left);
-    if (blocks == 1) __syncthreads();  // (a cluster's next pass begins with a barrier before these are written again)
+    if (blocks > 1) continue;  // (the next pass begins with a barrier before these are written again)
+    const bool few = sh.in_bin <= kPickFew;
+    if (threadIdx.x == 0) sh.listed = 0u;
+    __syncthreads();
+    if (!few || pass == 2) continue;
+    // Those of the bin are few: each is compared with all of them, which takes the place of the passes that are left (5,205 tokens:
+    // most often 150 to 200 are in the first pass's bin).
+    uint32_t* list = sh.joint;
+    for (int at = begin; at < end; at += kPickStep) {
+      const uint4 x4 = numbers_at(at + 4 * lane);
+      const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if ((x[j] & known) == prefix && x[j] != 0u) list[atomicAdd(&sh.listed, 1u)] = x[j];
+    }
+    __syncthreads();
+    const uint32_t n_listed = sh.listed;
+    for (uint32_t i = n_listed + threadIdx.x; i < ((n_listed + 3) & ~3u); i += threads) list[i] = 0u;
+    __syncthreads();
+    if (threadIdx.x < n_listed) {
+      const uint32_t x = list[threadIdx.x];
+      uint32_t over = 0, same = 0;
+      for (uint32_t i = 0; i < n_listed; i += 4) {
+        const uint4 y = *reinterpret_cast<const uint4*>(list + i);
+        over += (y.x > x ? 1u : 0u) + (y.y > x ? 1u : 0u) + (y.z > x ? 1u : 0u) + (y.w > x ? 1u : 0u);
+        same += (y.x == x ? 1u : 0u) + (y.y == x ? 1u : 0u) + (y.z == x ? 1u : 0u) + (y.w == x ? 1u : 0u);
+      }
+      if (over < left && over + same >= left) {  // (its equals write the same)
+        sh.bin = x;
+        sh.left = left - over;
+      }
+    }
+    __syncthreads();
+    prefix = sh.bin;
+    left = sh.left;
+    break;
   }
   // prefix: the least that stays, which is somebody's; left: how many of its equals do, from the front
 
@@ -321,7 +369,7 @@ int pick_blocks() {
   if (cudaGetDevice(&device) != cudaSuccess) return kPickPortableBlocks;
   const unsigned long long bit = 1ull << (device & 63);
   if ((asked.load(std::memory_order_acquire) & bit) == 0) {
-    const void* kernel = reinterpret_cast<const void*>(kv_pick_kernel);
+    const void* kernel = reinterpret_cast<const void*>(kv_pick_kernel<kPickMostThreads>);
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = kPickMostBlocks;
@@ -333,9 +381,11 @@ int pick_blocks() {
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int clusters = 0;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPickMostHeld * 4) == cudaSuccess &&
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-        cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0)
+    bool set = true;
+    for (const void* k : {kernel, reinterpret_cast<const void*>(kv_pick_kernel<kPickThreads>)})
+      set = set && cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kPickMostHeld * 4) == cudaSuccess &&
+            cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+    if (set && cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0)
       fits.fetch_or(bit);
     else (void)cudaGetLastError();
     asked.fetch_or(bit, std::memory_order_release);
@@ -358,7 +408,8 @@ cudaError_t launch_kv_evict(const litevggt_kv_cache& c, const litevggt_kv_batch&
   const int warps = threads / 32;
   const long long run = round_up(((long long)longest + 3 + blocks * warps - 1) / (blocks * warps), kPickStep);
   const int held = (int)std::min(run, (long long)kPickMostHeld / warps);
-  cudaError_t e = launch_clusters(blocks, true, kv_pick_kernel, dim3((unsigned)(pairs * blocks)), (unsigned)threads, (size_t)held * warps * 4, s, c.pool,
+  auto kernel = threads == kPickMostThreads ? kv_pick_kernel<kPickMostThreads> : kv_pick_kernel<kPickThreads>;
+  cudaError_t e = launch_clusters(blocks, true, kernel, dim3((unsigned)(pairs * blocks)), (unsigned)threads, (size_t)held * warps * 4, s, c.pool,
                                   kv_arrays(from), kv_arrays(into), first, last, blocks, held, kept);
   ++*launches;
   const long long pages = kv_page_count(into, c.cfg.page_size);
