@@ -448,14 +448,17 @@ typedef struct {
 typedef struct {
   const void* in;
   int64_t in_row_stride, in_head_stride;
-  void* out;           /* may be `in` with the same strides; otherwise no output may reach into an input or another output */
+  void* out;           /* may be `in` with the same strides; otherwise no output may reach into an input, positions or another output */
   int64_t out_row_stride, out_head_stride;
-  int32_t heads;       /* 1 to 65,536 */
+  int32_t heads;       /* 1 to 16,384 */
 } litevggt_rotary_tensor;
 typedef struct litevggt_rotary litevggt_rotary; /* immutable: one serves calls on any streams, at once too */
 
-/* Allocates 2 KB on the device; synchronous, as the destruction is, which waits for calls under way.  Neither while a stream captures. */
-litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int device, litevggt_rotary** out);
+/* memory: dev, LITEVGGT_ROTARY_BYTES, 16-byte aligned, the caller's, which outlives the calls with it.  It is filled on `stream`, which
+ * must not be capturing (LITEVGGT_ERR_CUDA), before the call returns. */
+#define LITEVGGT_ROTARY_BYTES 2048
+litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int device, void* memory, size_t bytes, void* stream,
+                                       litevggt_rotary** out);
 litevggt_status litevggt_rotary_destroy(litevggt_rotary* rotary);
 /* Turns one or two tensors of the same rows and type (queries and keys) in one launch.  positions: dev int32, element (axis, row) at
  * axis * axis_stride + row * row_stride, of any sign.  back != 0: by the negative angles, which is the gradient (from the gradient of the

@@ -118,7 +118,7 @@ def load_library():
         "litevggt_kv_evict": [vp, vp, vp, i32, i32, vp, vp],
         "litevggt_kv_poll": [vp, vp],
         "litevggt_kv_launch_count": [vp, P(i64)],
-        "litevggt_rotary_create": [P(RotaryConfig), C.c_int, P(vp)],
+        "litevggt_rotary_create": [P(RotaryConfig), C.c_int, vp, C.c_size_t, vp, P(vp)],
         "litevggt_rotary_destroy": [vp],
         "litevggt_rotary_apply": [vp, vp, i64, i64, i64, i32, i32, vp, i32, vp],
     }

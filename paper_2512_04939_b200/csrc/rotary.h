@@ -22,6 +22,8 @@ struct alignas(16) RotaryTable {
   int planes, head_dim;  // channels from 2 * planes on stay as they are
 };
 
+static_assert(sizeof(RotaryTable) <= LITEVGGT_ROTARY_BYTES, "");
+
 // One of a launch's tensors.
 struct RotaryRows {
   const uint8_t* in;
@@ -120,8 +122,8 @@ cudaError_t launch_rotary(const RotaryLaunch& l, int dtype, int width, bool neig
 
 struct litevggt_rotary {
   uint32_t magic;
-  int device, num_sms;
+  int device, num_sms, n_axes;
   bool neighbours;
   lv::RotaryTable table;
-  lv::RotaryTable* on_device;
+  lv::RotaryTable* on_device;  // the caller's
 };

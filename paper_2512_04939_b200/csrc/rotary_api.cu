@@ -7,6 +7,7 @@ namespace lv {
 namespace {
 
 constexpr long long kRotaryStride = 1ll << 40;  // elements
+constexpr int kRotaryMostHeads = 16384;         // of a tensor: at 256 units a head, blocks of a row are as many as heads, 65,535 at most
 
 bool rotary_ok(const litevggt_rotary* r) { return r != nullptr && r->magic == kRotaryMagic; }
 
@@ -19,7 +20,7 @@ using namespace lv;
 
 extern "C" {
 
-litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int device, litevggt_rotary** out) {
+litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int device, void* memory, size_t bytes, void* stream, litevggt_rotary** out) {
   if (cfg == nullptr || out == nullptr) return LITEVGGT_ERR_NULL;
   *out = nullptr;
   RotaryTable table{};
@@ -33,27 +34,27 @@ litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int de
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (e != cudaSuccess) return cuda_status(e);
   if (major != 10) return LITEVGGT_ERR_ARCH;
+  if (memory == nullptr) return LITEVGGT_ERR_NULL;
+  if (bytes < sizeof(RotaryTable)) return LITEVGGT_ERR_SHAPE;
+  if (!aligned16(memory)) return LITEVGGT_ERR_ALIGN;
+  const OnDevice g(device);
+  if (!g.ok) return LITEVGGT_ERR_CUDA;
+  // In a capture the copy would be made at every replay, and not now.
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  e = cudaStreamIsCapturing((cudaStream_t)stream, &capture);
+  if (e == cudaSuccess && capture != cudaStreamCaptureStatusNone) return LITEVGGT_ERR_CUDA;
+  if (e == cudaSuccess) e = cudaMemcpyAsync(memory, &table, sizeof(RotaryTable), cudaMemcpyHostToDevice, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);  // (whichever stream the first call is on)
+  if (e != cudaSuccess) return cuda_status(e);
   litevggt_rotary* r = new (std::nothrow) litevggt_rotary();
   if (r == nullptr) return LITEVGGT_ERR_ALLOC;
   r->magic = kRotaryMagic;
   r->device = device;
   r->num_sms = sms;
+  r->n_axes = cfg->n_axes;
   r->neighbours = cfg->layout == LITEVGGT_ROTARY_PAIRS;
   r->table = table;
-  {
-    const DeviceGuard g(device);
-    void* p = nullptr;
-    e = g.ok ? cudaMalloc(&p, sizeof(RotaryTable)) : cudaErrorInvalidDevice;
-    if (e == cudaSuccess) {
-      e = cudaMemcpy(p, &table, sizeof(RotaryTable), cudaMemcpyHostToDevice);
-      if (e != cudaSuccess) cudaFree(p);
-    }
-    r->on_device = static_cast<RotaryTable*>(p);
-  }
-  if (e != cudaSuccess) {
-    delete r;
-    return cuda_status(e);
-  }
+  r->on_device = static_cast<RotaryTable*>(memory);
   *out = r;
   return LITEVGGT_OK;
 }
@@ -61,14 +62,9 @@ litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int de
 litevggt_status litevggt_rotary_destroy(litevggt_rotary* rotary) {
   if (rotary == nullptr) return LITEVGGT_OK;
   if (!rotary_ok(rotary)) return LITEVGGT_ERR_NULL;
-  cudaError_t e = cudaErrorInvalidDevice;
-  {
-    const DeviceGuard g(rotary->device);
-    if (g.ok) e = cudaFree(rotary->on_device);  // (waits for what is under way)
-  }
   rotary->magic = 0;
   delete rotary;
-  return cuda_status(e);
+  return LITEVGGT_OK;
 }
 
 litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32_t* positions, int64_t axis_stride, int64_t row_stride,
@@ -87,10 +83,10 @@ litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32
   bool in_place = true;
   for (int i = 0; i < n_tensors; ++i) {
     const litevggt_rotary_tensor& x = tensors[i];
-    if (x.heads < 1 || x.heads > 65536) return LITEVGGT_ERR_SHAPE;
+    if (x.heads < 1 || x.heads > kRotaryMostHeads) return LITEVGGT_ERR_SHAPE;
     if (!stride_ok(x.in_row_stride) || !stride_ok(x.in_head_stride) || !stride_ok(x.out_row_stride) || !stride_ok(x.out_head_stride))
       return LITEVGGT_ERR_SHAPE;
-    for (int64_t stride : {x.in_row_stride, x.out_row_stride})  // (sums of addresses stay inside 64 bits)
+    for (int64_t stride : {x.in_row_stride, x.out_row_stride, row_stride})  // (sums of addresses stay inside 64 bits)
       if (rows > 1 && stride > (1ll << 56) / rows) return LITEVGGT_ERR_SHAPE;
     if (rows > 0 && (x.in == nullptr || x.out == nullptr)) return LITEVGGT_ERR_NULL;
     auto span = [&](const void* p, int64_t row, int64_t head) {
@@ -113,8 +109,10 @@ litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32
   if (positions == nullptr) return LITEVGGT_ERR_NULL;
   if (low % size != 0 || reinterpret_cast<uintptr_t>(positions) % 4 != 0) return LITEVGGT_ERR_ALIGN;
   // A row of a head is read before it is written, by the same thread: that makes turning in place safe, and nothing else.
+  const RotarySpan where{reinterpret_cast<uintptr_t>(positions), (unsigned long long)row_stride * 4, (unsigned long long)axis_stride * 4,
+                         (unsigned long long)rows, (unsigned long long)rotary->n_axes, 4};
   for (int i = 0; i < n_tensors; ++i) {
-    if (!rotary_apart(out[i])) return LITEVGGT_ERR_SHAPE;
+    if (!rotary_apart(out[i]) || rotary_may_meet(out[i], where)) return LITEVGGT_ERR_SHAPE;
     for (int j = 0; j < n_tensors; ++j) {
       if (!(i == j && rotary_same(in[i], out[i])) && rotary_may_meet(out[i], in[j])) return LITEVGGT_ERR_SHAPE;
       if (i < j && rotary_may_meet(out[i], out[j])) return LITEVGGT_ERR_SHAPE;

@@ -122,6 +122,8 @@ class KVCache:
             raise ValueError(f"dtype must be one of {sorted(_DTYPES)}, got {dtype!r}")
         where = torch.device("cuda", device)
         _, kind, packed, block = _DTYPES[dtype]
+        if head_dim % packed or (block > 0 and head_dim % block):
+            raise ValueError(f"head_dim must be a multiple of {max(packed, block)} in {dtype}, got {head_dim}")
         shape = (pages, kv_heads, page_size)
         pools = [torch.empty((*shape, head_dim // packed), dtype=kind, device=where) for _ in range(2)]
         if block:

@@ -33,6 +33,8 @@ class RotaryAxes:
             raise ValueError(f"one to four axes with a section and a base each, got {sections} and {bases}")
         if any(int(n) != n or not 0 <= n < 2 ** 31 for n in (head_dim, *sections)):
             raise ValueError(f"head_dim and sections must be whole numbers, got {head_dim} and {sections}")
+        if not 0 <= device < torch.cuda.device_count():
+            raise ValueError(f"there is no CUDA device {device}")
         self.lib = load_library()
         self.head_dim, self.sections, self.bases, self.layout = int(head_dim), tuple(int(n) for n in sections), bases, layout
         self.device = torch.device("cuda", device)
@@ -40,7 +42,9 @@ class RotaryAxes:
         self._axes = n = len(sections)
         cfg = RotaryConfig(self.head_dim, n, (C.c_int32 * 4)(*self.sections), (C.c_double * 4)(*bases), _LAYOUTS[layout])
         self.handle = C.c_void_p()
-        _check(self.lib.litevggt_rotary_create(C.byref(cfg), device, C.byref(self.handle)), "rotary_create")
+        self._table = torch.empty(2048, dtype=torch.uint8, device=self.device)
+        self._home = torch._C._cuda_getCurrentRawStream(device)
+        _check(self.lib.litevggt_rotary_create(C.byref(cfg), device, self._table.data_ptr(), 2048, self._home, C.byref(self.handle)), "rotary_create")
         self._apply = self.lib.litevggt_rotary_apply
 
     def close(self):
@@ -87,8 +91,11 @@ class RotaryAxes:
         if not fine:
             self._refuse(positions, given, outs, rows)
         axis_stride, row_stride = positions.stride()
+        stream = torch._C._cuda_getCurrentRawStream(index)
+        if stream != self._home:  # the table is in use there as well, and is not given away before that is done
+            self._table.record_stream(torch.cuda.current_stream(index))
         code = self._apply(self.handle, positions.data_ptr(), axis_stride, row_stride, rows, kind, back, _PACK[len(given) - 1](*numbers),
-                           len(given), torch._C._cuda_getCurrentRawStream(index))
+                           len(given), stream)
         if code:
             _check(code, "rotary_apply")
         return outs[0] if k is None else outs

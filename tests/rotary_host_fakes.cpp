@@ -1,5 +1,4 @@
 // Stand-ins for the CUDA runtime and the kernel launch behind the rotary entry points (rotary_api.cu): what would be launched is kept.
-#include <stdlib.h>
 #include <string.h>
 
 #include "../paper_2512_04939_b200/csrc/rotary.h"
@@ -7,7 +6,8 @@
 using namespace lv;
 
 static RotaryLaunch g_launch;
-static int g_launches = 0, g_width = 0, g_neighbours = 0, g_device = 0, g_launched_on = -1, g_held = 0;
+static int g_launches = 0, g_width = 0, g_neighbours = 0, g_device = 0, g_launched_on = -1, g_copied_on = -1;
+static bool g_capturing = false;
 static unsigned g_blocks = 0, g_threads = 0, g_across = 0;
 
 extern "C" {
@@ -19,10 +19,18 @@ cudaError_t cudaDeviceGetAttribute(int* v, cudaDeviceAttr a, int) {
   return cudaSuccess;
 }
 cudaError_t cudaGetLastError() { return cudaSuccess; }
-cudaError_t cudaMalloc(void** p, size_t n) { ++g_held; *p = malloc(n); return cudaSuccess; }
-cudaError_t cudaFree(void* p) { --g_held; free(p); return cudaSuccess; }
-cudaError_t cudaMemcpy(void* d, const void* s, size_t n, cudaMemcpyKind) { memcpy(d, s, n); return cudaSuccess; }
-int fake_held() { return g_held; }
+cudaError_t cudaMemcpyAsync(void* d, const void* s, size_t n, cudaMemcpyKind, cudaStream_t) {
+  g_copied_on = g_device;
+  memcpy(d, s, n);
+  return cudaSuccess;
+}
+cudaError_t cudaStreamSynchronize(cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
+  *s = g_capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
+  return cudaSuccess;
+}
+void fake_capture(int on) { g_capturing = on != 0; }
+int fake_copied_on() { return g_copied_on; }
 int fake_launches() { return g_launches; }
 int fake_get_device() { return g_device; }
 int fake_launched_on() { return g_launched_on; }

@@ -290,5 +290,6 @@ def test_refusals():
             pkg.KVCache(*pools)
     with pytest.raises(pkg.LiteVGGTError):
         pkg.KVCache(k[..., :16].contiguous(), k[..., :16].contiguous(), e[..., :1].contiguous(), e[..., :1].contiguous())  # 32 channels
-    with pytest.raises(ValueError):
-        pkg.KVCache.empty(4, 16, 2, 64, "e3m0")
+    for args in ((64, "e3m0"), (65, "e2m1"), (80, "e2m1")):
+        with pytest.raises(ValueError):
+            pkg.KVCache.empty(4, 16, 2, *args)

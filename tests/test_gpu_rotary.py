@@ -149,6 +149,17 @@ def test_captured_replayed_and_on_another_stream():
     assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
 
 
+def test_made_outside_a_capture():
+    """The table is copied from the call's own memory, which a graph would read again at every replay."""
+    x, graph = torch.zeros(8, device="cuda"), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(pkg.LiteVGGTError):
+            pkg.RotaryAxes(64, (64,), (100.0,))
+    graph.replay()
+    assert x.eq(1).all()
+
+
 def test_no_rows_and_refusals():
     rotary = pkg.RotaryAxes(64, (16, 24, 24), (10000.0, 100.0, 100.0))
     (q, k), positions = inputs(10, (16, 4), 64, torch.bfloat16, 3)

@@ -29,9 +29,22 @@ def config(head_dim=64, sections=(16, 24, 24), bases=None, layout=0):
     return RotaryConfig(head_dim, len(sections), (C.c_int32 * 4)(*sections, *[0] * pad), (C.c_double * 4)(*bases, *[0.0] * pad), layout)
 
 
+_KEPT = []
+
+
+def memory(size=2048):
+    _KEPT.append(C.create_string_buffer(size + 16))
+    return C.c_void_p((C.addressof(_KEPT[-1]) + 15) & ~15)
+
+
+def create(host, cfg, handle, device=0, at="own", size=2048):
+    return host.litevggt_rotary_create(None if cfg is None else C.byref(cfg), device, memory() if at == "own" else at, C.c_size_t(size), None,
+                                       None if handle is None else C.byref(handle))
+
+
 def made(host, device=0, **kw):
-    handle, cfg = C.c_void_p(), config(**kw)
-    assert host.litevggt_rotary_create(C.byref(cfg), device, C.byref(handle)) == OK
+    handle = C.c_void_p()
+    assert create(host, config(**kw), handle, device) == OK
     return handle
 
 
@@ -59,7 +72,7 @@ def last(host):
     dict(layout=3), dict(layout=-1)])
 def test_configurations_that_are_refused(host, bad):
     handle, cfg = C.c_void_p(5), config(**bad)
-    assert host.litevggt_rotary_create(C.byref(cfg), 0, C.byref(handle)) == BAD_CONFIG
+    assert create(host, cfg, handle) == BAD_CONFIG
     assert handle.value is None
 
 
@@ -67,15 +80,16 @@ def test_axes_devices_and_handles_that_are_refused(host):
     handle, cfg = C.c_void_p(), config()
     for n in (0, 5, -1):
         cfg.n_axes = n
-        assert host.litevggt_rotary_create(C.byref(cfg), 0, C.byref(handle)) == BAD_CONFIG
+        assert create(host, cfg, handle) == BAD_CONFIG
     cfg.n_axes = 3
-    assert host.litevggt_rotary_create(C.byref(cfg), 2, C.byref(handle)) == CUDA
-    assert host.litevggt_rotary_create(None, 0, C.byref(handle)) == NULL
-    assert host.litevggt_rotary_create(C.byref(cfg), 0, None) == NULL
-    assert host.litevggt_rotary_destroy(None) == OK
-    before = host.fake_held()
-    assert host.litevggt_rotary_create(C.byref(cfg), 1, C.byref(handle)) == OK and host.fake_held() == before + 1 and host.fake_get_device() == 0
-    assert host.litevggt_rotary_destroy(handle) == OK and host.fake_held() == before
+    assert create(host, cfg, handle, 2) == CUDA
+    assert create(host, None, handle) == NULL and create(host, cfg, None) == NULL and create(host, cfg, handle, at=None) == NULL
+    assert create(host, cfg, handle, size=1000) == SHAPE and create(host, cfg, handle, at=C.c_void_p(memory().value + 8)) == ALIGN
+    host.fake_capture(1)
+    assert create(host, cfg, handle) == CUDA and handle.value is None
+    host.fake_capture(0)
+    assert create(host, cfg, handle, 1) == OK and host.fake_copied_on() == 1 and host.fake_get_device() == 0
+    assert host.litevggt_rotary_destroy(handle) == OK and host.litevggt_rotary_destroy(None) == OK
     assert apply(host, None, tensor()) == NULL
 
 
@@ -140,7 +154,7 @@ def test_calls_that_are_refused(host, kw, code):
 
 
 @pytest.mark.parametrize("t,code", [
-    (dict(src=0), NULL), (dict(dst=0), NULL), (dict(heads=0), SHAPE), (dict(heads=65537), SHAPE), (dict(row=-1), SHAPE), (dict(head=-64), SHAPE),
+    (dict(src=0), NULL), (dict(dst=0), NULL), (dict(heads=0), SHAPE), (dict(heads=16385), SHAPE), (dict(row=-1), SHAPE), (dict(head=-64), SHAPE),
     (dict(row=1 << 40), SHAPE), (dict(src=BASE + 1), ALIGN), (dict(out_head=0), SHAPE), (dict(out_row=0), SHAPE), (dict(out_row=960), SHAPE),
     (dict(out_head=63), SHAPE), (dict(dst=BASE + 2048), SHAPE), (dict(dst=BASE, out_row=2048), SHAPE), (dict(dst=BASE + 128), SHAPE)])
 def test_tensors_that_are_refused(host, t, code):
@@ -162,6 +176,9 @@ def test_what_may_lie_where(host):
     # one tensor's output in another's input, or both outputs in one place
     assert apply(host, handle, tensor(), tensor(src=3 * BASE, dst=BASE)) == SHAPE
     assert apply(host, handle, tensor(), tensor(src=3 * BASE, dst=2 * BASE + 64)) == SHAPE
+    # an output over the positions
+    assert apply(host, handle, tensor(), positions=2 * BASE + 128) == SHAPE and apply(host, handle, tensor(dst=4 * BASE)) == SHAPE
+    assert apply(host, handle, tensor(dst=BASE), positions=BASE) == SHAPE
     # no rows: nothing is looked at
     assert apply(host, handle, tensor(src=0, dst=0), rows=0, positions=0) == OK
 
