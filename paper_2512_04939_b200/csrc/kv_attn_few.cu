@@ -17,12 +17,18 @@
 // power of two of its row (exact but for elements under 2^-30 of the row's largest, which keep steps of 2^-37 of it or less); weights
 // have 11 bits there, not 8, down to 2^-21 of the row's largest or less, and fixed steps of 2^-31 of it or less below: where one key's value
 // has a code of zero in a channel, keys of 2^-32 of its weight count as nothing there.
+// Codes of 4 bits have a power of two for 32 channels.  Scores are sums of a block each in f16, brought together in 32 bits under the
+// blocks' powers.  Values have to meet their powers before the product, which takes them in bf16, where codes and powers are exact: two
+// keys' codes of a channel become a pair of the operand by permutations and one multiplication, without a conversion.
 //
 // One token of 16 heads of 64 over 260,250 keys in bf16: 176 us, 6.1 TB/s, the rate of a copy; 48 tokens of 16 heads of 128 over 1,100
 // to 4,164 keys 166 us, 6.2 TB/s.  Codes of head dim 64 are bound by the work of widening them (a conversion takes as long as four of the
-// other instructions; the ALU is 60 % busy): over 520,500 keys 207 us, 5.2 TB/s.  At head dim 128 nothing is over 30 % busy: two warps a
-// scheduler, each with one chain of waits, conversions, products and exponentials (16 tokens, 8 query heads a K/V head, 35 us).  (Straight from global memory into the
-// fragments, without rings: 189, 307 and 404 us.  The scores by products of 8-bit operands, Q in two of them, which need no
+// other instructions; the ALU is 60 % busy): over 520,500 keys 201 us, 5.4 TB/s.  At head dim 128 nothing is over 30 % busy: two warps a
+// scheduler, each with one chain of waits, conversions, products and exponentials (16 tokens, 8 query heads a K/V head, 35 us).
+// Codes of 4 bits are half the bytes and about the same work, and it is the work that bounds them, issue slots and ALU: one token over
+// 520,500 keys 217 us, 2.6 TB/s (335 with a conversion for every pair; values and weights in f16, under a power of two of the warp's,
+// 209, but then keys of 2^-32 of the heaviest one's weight count as nothing where its code is zero).
+// (Straight from global memory into the fragments, without rings: 189, 307 and 404 us for the first three figures.  The scores by products of 8-bit operands, Q in two of them, which need no
 // conversion of K in the source: 202 -> 220 us, sixteen tokens that share heads by eight 32.9 -> 33.2.)  Few keys: 4.8 us for 262, of which the latency of three dependent loads and the
 // meeting of the parts are most.
 #include "exp2.cuh"
@@ -82,17 +88,18 @@ struct FewShape {
   static constexpr int kParts = kMoves ? 2 : 4;               // registers of a lane and tile of accumulators
   static constexpr int kBlocks = kFour ? kHd / 32 : 1;        // of channels that have a power of two of their own
   using Row = KvRow<kHd, kKind>;
-  // Rings of 17 to 25 KB a warp.  Codes of head dim 64 take so much work for a byte that sixteen warps an SM serve them
+  // Rings of 9 to 25 KB a warp.  Codes of head dim 64 take so much work for a byte that sixteen warps an SM serve them
   // better than eight with more registers (one token over 520,500: 216 us against 241 to 283); those of head dim 128 spill
-  // under 128 registers (sixteen tokens that share heads by eight: 36 us against 49).
+  // under 128 registers (sixteen tokens that share heads by eight: 36 us against 49).  Stages of 32 keys in 4 bits: at head dim 128 what
+  // a stage costs beside its keys is as much again (48 sequences of 8192 keys: 442 us with 16, 367 with 32).
   static constexpr int kCtas = kKind != LITEVGGT_KV_BF16 && kHd == 64 ? 2 : 1;  // per SM
-  static constexpr int kSubs = kNarrow ? 2 : 128 / kHd;       // of 16 keys, of a stage
+  static constexpr int kSubs = kNarrow || kFour ? 2 : 128 / kHd;  // of 16 keys, of a stage
   static constexpr int kStages = kFour ? 4 : kNarrow || (kHd == 128 && !kHalf) ? 2 : 3;
   static constexpr int kRows = kHalf ? 8 : 16;
   static constexpr int kOutTiles = kHd / 8;
   static constexpr int kSubBytes = 16 * Row::kBytes;  // of K or V
-  static constexpr int kStageBytes = 2 * kSubs * kSubBytes + (Row::kExps > 0 ? 128 : 0);  // [K, V][sub], exponents [K, V][sub] of 16 rows
-  static_assert(2 * kSubs * 16 * Row::kExps <= 128, "");
+  static constexpr int kExpBytes = (2 * kSubs * 16 * Row::kExps + 127) / 128 * 128;  // exponents [K, V][sub] of 16 rows
+  static constexpr int kStageBytes = 2 * kSubs * kSubBytes + kExpBytes;              // [K, V][sub], exponents
   static constexpr int kRingBytes = kKvFewWarps * kStages * kStageBytes;
   static constexpr int kMergeBytes = kKvFewWarps * kRows * (kHd + 2) * 4;
   static constexpr int kSmemBytes = kRingBytes + kMergeBytes + 1024 + 320;
