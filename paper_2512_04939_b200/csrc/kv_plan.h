@@ -197,13 +197,16 @@ inline KvWeigh kv_weigh_plan(const std::vector<KvSeq>& seqs, int group, int kv_h
     }
   }
   w.few_at.push_back(few);
-  // What fills the chip best: a CTA's time goes by 128 keys against 128 rows, and beside them it has its keys to fetch.
-  constexpr double kFetch = 1.0;
+  // What fills the chip best.  In times of 128 keys against 128 rows where 256 keys share the rows, 0.67 us: by themselves 128 keys take
+  // 1.25 (every thread's turn is half as long), an item 1.75 beside its products, and 2.25 more where its rows are cut and the parts meet.
+  // (2748 rows over 21,984 keys, 16 heads: 365 us with items of 128 keys, 305 with 256; 1041 over 1041 14.0 and 18.0; 261 over 2610 14.0 with
+  // whole rows, 21.7 in three parts; 2048 rows of eight heads each on 2 over 2048 176 whole, 29.5 in eight parts.)
+  constexpr double kTile[2] = {1.25, 2.0}, kItem = 1.75, kMeet = 2.25;
   double least = 0.0;
   for (int i = 0; i < 2; ++i)
     for (int parts = 1; parts <= 64 && parts <= std::max(row_tiles, 1ll) && (parts == 1 || blocks[i] * kv_heads * parts <= 4ll * sms); ++parts) {
       const double waves = (double)((blocks[i] * kv_heads * parts + sms - 1) / sms);
-      const double cost = waves * ((i + 1) * (double)((row_tiles + parts - 1) / parts) + kFetch) + (parts > 1 ? kFetch : 0.0);
+      const double cost = waves * (kTile[i] * (double)((row_tiles + parts - 1) / parts) + kItem + (parts > 1 ? kMeet : 0.0));
       if (least == 0.0 || cost < 0.999 * least) {
         least = cost;
         w.key_block = 128 * (i + 1);
