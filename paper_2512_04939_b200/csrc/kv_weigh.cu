@@ -280,7 +280,7 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
 // exponential a score and 64 (128) multiplications for it, so the special-function unit is the bound, at 16 a clock; the products need
 // an eighth (a quarter) of its time.  Roles: eight warps take the exponentials, each thread a key against all rows or a share of them; one
 // issues the products; one fetches K once an item, by TMA, or two widen its codes; four fetch Q tile by tile into swizzled shared memory,
-// with what the exponentials need of a row, its log-sum-exp and how many keys it sees (two warps: head dim 128 20 % slower); and one
+// with what the exponentials need of a row, its log-sum-exp and how many keys it sees; and one
 // finds out what the CTA's items are, 32 at a time and ahead of all others: the divisions and searches of that, thousands of clocks in a
 // row, were half of the time of short items.
 // 4164 rows over 41,640 keys, 16 heads of 64: 806 us, 3.3 10^12 exponentials a second, four fifths of what the unit gives at the clock held
@@ -345,7 +345,13 @@ struct WeighShape {
   static constexpr int kSubBytes = 128 * 128, kTileBytes = kSubBytes * kHd / 64;
   static constexpr int kShares = kDrawWarps / (4 * kTiles);  // threads that share a key's rows
   static constexpr int kCols = 128 / kShares;                // rows of a thread in a tile
-  static constexpr int kRowInfoBytes = kStages * 128 * 8;
+  // What is left of rows stays until they have been drawn with, Q only until it has been multiplied.  A tile's place is taken anew by the one
+  // kPlaces on, whose stage is free when the product of the tile kStages before it is done; for that the draws of the tile two before
+  // that one had to be over, as there are two accumulators.  kStages + 2 places do therefore.  (With Q held until it had been drawn with,
+  // two sequences of 1041 rows over 10,410 keys, 16 heads of 128, took 202 us instead of 136.)
+  static constexpr int kPlaces = 2 * kStages;
+  static_assert(kPlaces >= kStages + 2, "");
+  static constexpr int kRowInfoBytes = kPlaces * 128 * 8;
   static constexpr int kMeetBytes = (kShares - 1) * kTiles * 128 * 4;
   static constexpr int kSmemBytes = (2 * kTiles + kStages) * kTileBytes + kRowInfoBytes + kMeetBytes + 1024 + 1024;
 };
@@ -374,14 +380,14 @@ __global__ void __launch_bounds__((WeighShape<kHd, kKind, kTiles>::kThreads), 1)
 kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, KvArrays arrays, KvWeighing in, WeighLists lists, long long units, uint32_t* status) {
   using Shape = WeighShape<kHd, kKind, kTiles>;
   constexpr int kKeyWarps = Shape::kKeyWarps;
-  constexpr int kStages = Shape::kStages, kTileBytes = Shape::kTileBytes, kSubBytes = Shape::kSubBytes, kShares = Shape::kShares;
+  constexpr int kStages = Shape::kStages, kPlaces = Shape::kPlaces, kTileBytes = Shape::kTileBytes, kSubBytes = Shape::kSubBytes, kShares = Shape::kShares;
   constexpr int kCols = Shape::kCols, kBlock = 128 * kTiles;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem_k = smem_raw + (-smem_u32(smem_raw) & 1023u);  // [buffer][tile] (as an offset: the compiler knows that it is shared memory)
   uint8_t* smem_q = smem_k + 2 * kTiles * kTileBytes;          // [stage]
-  float* row_less = reinterpret_cast<float*>(smem_q + kStages * kTileBytes);  // [stage][row]
-  int* row_seen = reinterpret_cast<int*>(row_less + kStages * 128);           // [stage][row]
-  float* meet = reinterpret_cast<float*>(row_seen + kStages * 128);           // [share - 1][key]
+  float* row_less = reinterpret_cast<float*>(smem_q + kStages * kTileBytes);  // [place][row]
+  int* row_seen = reinterpret_cast<int*>(row_less + kPlaces * 128);           // [place][row]
+  float* meet = reinterpret_cast<float*>(row_seen + kPlaces * 128);           // [share - 1][key]
   using Barriers = WeighBarriers<kStages>;
   Barriers* bars = reinterpret_cast<Barriers*>(meet + (kShares - 1) * kBlock);
   static_assert(sizeof(Barriers) <= 1024 && sizeof(WeighUnit) % 8 == 0, "");
@@ -402,7 +408,7 @@ kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, Kv
     }
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&bars->q_full[i], kRowWarps);
-      mbar_init(&bars->q_empty[i], 1 + kDrawWarps);
+      mbar_init(&bars->q_empty[i], 1);
     }
     mbar_init(&bars->met, kDrawWarps);
     mbar_init(&bars->teardown, 1);
@@ -602,6 +608,7 @@ kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, Kv
         if (t + 1 < u.tile1) look_ahead();
         ok = mbar_wait_warp(&bars->q_empty[stage], ((count / kStages) & 1u) ^ 1u, ctl);
         if (!ok) return;
+        const uint32_t place_of_tile = count % kPlaces;
         ++count;
         uint8_t* tile = smem_q + stage * kTileBytes;
 #pragma unroll
@@ -615,8 +622,8 @@ kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, Kv
         cp_async_commit();
 #pragma unroll
         for (int i = 0; i < kInfo; ++i) {
-          row_less[stage * 128 + i * kThreads + tid] = -kLog2e * less[i];
-          row_seen[stage * 128 + i * kThreads + tid] = seen[i];
+          row_less[place_of_tile * 128 + i * kThreads + tid] = -kLog2e * less[i];
+          row_seen[place_of_tile * 128 + i * kThreads + tid] = seen[i];
         }
         if (count - given > kLag) {
           cp_async_wait<kLag>();
@@ -685,12 +692,12 @@ kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, Kv
       const int key = u.key0 + key_in;
       float total = 0.0f;
       for (int t = u.tile0; t < u.tile1; ++t, ++count) {
-        const uint32_t stage = count % kStages, slot = count & 1u;
+        const uint32_t place_of_tile = count % kPlaces, slot = count & 1u;
         ok = mbar_wait_warp(&bars->d_full[kt][slot], (count >> 1) & 1u, ctl);
         if (!ok) return;
         tc_fence_after();
-        const float* less = row_less + stage * 128 + share * kCols;
-        const int* seen = row_seen + stage * 128 + share * kCols;
+        const float* less = row_less + place_of_tile * 128 + share * kCols;
+        const int* seen = row_seen + place_of_tile * 128 + share * kCols;
         auto tile_sum = [&](auto edge_constant) {
           constexpr bool kEdge = decltype(edge_constant)::value;
           float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
@@ -720,10 +727,7 @@ kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, Kv
         const float sum = u.edge(in.group, t, kt) ? tile_sum(std::true_type{}) : tile_sum(std::false_type{});
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&bars->d_empty[kt][slot]);
-          mbar_arrive(&bars->q_empty[stage]);
-        }
+        if (lane == 0) mbar_arrive(&bars->d_empty[kt][slot]);
         total += sum;  // (a tile's own sum first: no number is added to more than a few dozen times its size in turn)
       }
       // the threads of a key, in their order
