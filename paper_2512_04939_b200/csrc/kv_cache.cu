@@ -3,7 +3,8 @@
 // Writing and reading move every byte once and compute next to nothing, so HBM bounds both.  A unit of work is one
 // row of one K/V head, K and V alike: 16 bytes of bf16 a lane, the 8 (or 16) lanes of a row side by side in the warp, so
 // that a row's largest magnitude takes three (four) shuffles and its codes leave as 64 (128) bytes in a row.  83,280 rows of 16
-// heads of 64: written as bf16 110 us, 6.2 TB/s, as E4M3 85 us, 6.0; read back 106 us, 6.4, and 82 us, 6.3 (a copy makes 6.46).
+// heads of 64: written as bf16 110 us, 6.2 TB/s, as E4M3 85 us, 6.0, as E2M1 72 us, 6.0; read back 106 us, 6.4, 82 us, 6.3, and 70 us, 6.2 (a
+// copy makes 6.46).
 #include "kv_cache.h"
 #include "kv_quant.cuh"
 
@@ -84,10 +85,15 @@ __device__ __forceinline__ uint4 row_values(const uint2& codes, uint32_t byte) {
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
-// Where a lane's 16 bytes of a unit lie: kUnits of them to a group of lanes, a block's side by side.  (Rows times heads fit 31 bits.)
-template <int kHd, int kUnits>
+// Runs of 8 channels of a row, side by side, that a lane works on.  Two where rows are written in 4 bits, which is bound by instructions, those
+// for where a row lies and what its powers are among them (83,280 rows of 16 heads of 64: 82.6 us with one, 72.4 with two).  What is read back
+// leaves in accesses that only together fill a sector then (70 us with one, 99 with two).
+template <int kKind>
+constexpr int kAppendRuns = kKind == LITEVGGT_KV_E2M1 ? 2 : 1;
+// Where a lane's runs of a unit lie: kUnits of them to a group of lanes, a block's side by side.  (Rows times heads fit 31 bits.)
+template <int kHd, int kUnits, int kRuns>
 struct MoveUnits {
-  static constexpr int kLanes = kHd / 8, kGroups = kMoveThreads / kLanes;
+  static constexpr int kLanes = kHd / 8 / kRuns, kGroups = kMoveThreads / kLanes;
   unsigned first, units;
   int part;
   __device__ __forceinline__ explicit MoveUnits(unsigned n)
@@ -101,20 +107,22 @@ template <int kHd, int kKind, int kUnits, bool kTallies>
 __global__ void __launch_bounds__(kMoveThreads)
 kv_append_kernel(KvPool pool, KvArrays arrays, const __nv_bfloat16* __restrict__ k, KvStride ks, const __nv_bfloat16* __restrict__ v,
                  KvStride vs, unsigned units) {
-  constexpr int kLanes = kHd / 8;
+  constexpr int kRuns = kAppendRuns<kKind>, kLanes = kHd / 8 / kRuns;
   wait_for_previous_kernel();
-  const MoveUnits<kHd, kUnits> mine(units);
+  const MoveUnits<kHd, kUnits, kRuns> mine(units);
   const int part = mine.part;
-  uint4 xk[kUnits], xv[kUnits];
+  uint4 xk[kUnits][kRuns], xv[kUnits][kRuns];
   size_t at[kUnits];
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
-    xk[i] = xv[i] = make_uint4(0u, 0u, 0u, 0u);
     at[i] = 0;
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r) xk[i][r] = xv[i][r] = make_uint4(0u, 0u, 0u, 0u);
     if (!mine.live(i)) continue;
     const int row = (int)(mine.unit(i) / (unsigned)pool.kv_heads), head = (int)(mine.unit(i) % (unsigned)pool.kv_heads);
-    xk[i] = ldg16(k + row * ks.row + head * ks.head + part * 8);
-    xv[i] = ldg16(v + row * vs.row + head * vs.head + part * 8);
+    const __nv_bfloat16 *from_k = k + row * ks.row + head * ks.head + part * 8 * kRuns, *from_v = v + row * vs.row + head * vs.head + part * 8 * kRuns;
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r) xk[i][r] = ldg16(from_k + 8 * r), xv[i][r] = ldg16(from_v + 8 * r);
     at[i] = pool_row(pool, arrays, row, head);
   }
 #pragma unroll
@@ -122,24 +130,26 @@ kv_append_kernel(KvPool pool, KvArrays arrays, const __nv_bfloat16* __restrict__
     if (kTallies && part == 2 && mine.live(i)) pool.weights[at[i]] = 0.0f;
     if constexpr (kKind == LITEVGGT_KV_E2M1) {
       constexpr int kExps = kHd / 32;
-      const uint32_t tops = row_tops<4>(xk[i], xv[i]), bk = kv4_exponent_byte(tops & 0xffffu), bv = kv4_exponent_byte(tops >> 16);
+      uint32_t tops = __vmaxu2(__byte_perm(lane_top(xk[i][0]), lane_top(xv[i][0]), 0x5410), __byte_perm(lane_top(xk[i][1]), lane_top(xv[i][1]), 0x5410));
+      tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, 1));
+      const uint32_t bk = kv4_exponent_byte(tops & 0xffffu), bv = kv4_exponent_byte(tops >> 16);
       if (mine.live(i)) {
-        *reinterpret_cast<uint32_t*>(pool.k + at[i] * (kHd / 2) + part * 4) = row_codes4(xk[i], bk);
-        *reinterpret_cast<uint32_t*>(pool.v + at[i] * (kHd / 2) + part * 4) = row_codes4(xv[i], bv);
-        if (part % 4 == 0) pool.k_exp[at[i] * kExps + part / 4] = (uint8_t)bk;
-        if (part % 4 == 1) pool.v_exp[at[i] * kExps + part / 4] = (uint8_t)bv;
+        *reinterpret_cast<uint2*>(pool.k + at[i] * (kHd / 2) + part * 8) = make_uint2(row_codes4(xk[i][0], bk), row_codes4(xk[i][1], bk));
+        *reinterpret_cast<uint2*>(pool.v + at[i] * (kHd / 2) + part * 8) = make_uint2(row_codes4(xv[i][0], bv), row_codes4(xv[i][1], bv));
+        if (part % 2 == 0) pool.k_exp[at[i] * kExps + part / 2] = (uint8_t)bk;
+        else pool.v_exp[at[i] * kExps + part / 2] = (uint8_t)bv;
       }
     } else if constexpr (kKind == LITEVGGT_KV_E4M3) {
-      const uint32_t tops = row_tops<kLanes>(xk[i], xv[i]), bk = kv_exponent_byte(tops & 0xffffu), bv = kv_exponent_byte(tops >> 16);
+      const uint32_t tops = row_tops<kLanes>(xk[i][0], xv[i][0]), bk = kv_exponent_byte(tops & 0xffffu), bv = kv_exponent_byte(tops >> 16);
       if (mine.live(i)) {
-        *reinterpret_cast<uint2*>(pool.k + at[i] * kHd + part * 8) = row_codes(xk[i], bk);
-        *reinterpret_cast<uint2*>(pool.v + at[i] * kHd + part * 8) = row_codes(xv[i], bv);
+        *reinterpret_cast<uint2*>(pool.k + at[i] * kHd + part * 8) = row_codes(xk[i][0], bk);
+        *reinterpret_cast<uint2*>(pool.v + at[i] * kHd + part * 8) = row_codes(xv[i][0], bv);
         if (part == 0) pool.k_exp[at[i]] = (uint8_t)bk;
         if (part == 1) pool.v_exp[at[i]] = (uint8_t)bv;
       }
     } else if (mine.live(i)) {
-      stg16(pool.k + (at[i] * kHd + part * 8) * 2, xk[i]);
-      stg16(pool.v + (at[i] * kHd + part * 8) * 2, xv[i]);
+      stg16(pool.k + (at[i] * kHd + part * 8) * 2, xk[i][0]);
+      stg16(pool.v + (at[i] * kHd + part * 8) * 2, xv[i][0]);
     }
   }
 }
@@ -148,7 +158,7 @@ template <int kHd, int kKind, int kUnits>
 __global__ void __launch_bounds__(kMoveThreads)
 kv_gather_kernel(KvPool pool, KvArrays arrays, __nv_bfloat16* __restrict__ k, __nv_bfloat16* __restrict__ v, unsigned units) {
   wait_for_previous_kernel();
-  const MoveUnits<kHd, kUnits> mine(units);
+  const MoveUnits<kHd, kUnits, 1> mine(units);
   const int part = mine.part;
   uint4 xk[kUnits], xv[kUnits];  // as they lie in the pool
   uint32_t bk[kUnits], bv[kUnits];
@@ -190,11 +200,11 @@ kv_gather_kernel(KvPool pool, KvArrays arrays, __nv_bfloat16* __restrict__ k, __
 // Calls f with the head dimension, the pool's type and the units of a lane group as constants, and the blocks that this takes.
 // One unit where all blocks are on the chip at once (1,041 rows of 16 heads in E4M3: 2.9 us written, 2.5 read; two: 3.5 and
 // 2.9), two where that keeps more bytes under way (83,280 rows read back: 82.5 us against 95.6; four are no better).
-template <class F>
+template <bool kAppend, class F>
 void by_kind(const litevggt_kv_cache& c, long long units, const F& f) {
   using std::integral_constant;
   auto sized = [&](auto hd, auto kind) {
-    const long long per_block = kMoveThreads / (decltype(hd)::value / 8), blocks = (units + per_block - 1) / per_block;
+    const long long per_block = kMoveThreads / (decltype(hd)::value / 8 / (kAppend ? kAppendRuns<decltype(kind)::value> : 1)), blocks = (units + per_block - 1) / per_block;
     if (blocks <= (long long)c.num_sms * (2048 / kMoveThreads)) f(hd, kind, integral_constant<int, 1>{}, (unsigned)blocks);
     else f(hd, kind, integral_constant<int, 2>{}, (unsigned)((blocks + 1) / 2));
   };
@@ -213,7 +223,7 @@ cudaError_t launch_kv_append(const litevggt_kv_cache& c, const litevggt_kv_batch
                              const __nv_bfloat16* v, KvStride v_stride, cudaStream_t s, int* launches) {
   const long long units = b.rows * c.cfg.kv_heads;
   cudaError_t e = cudaSuccess;
-  by_kind(c, units, [&](auto hd, auto kind, auto per, unsigned blocks) {
+  by_kind<true>(c, units, [&](auto hd, auto kind, auto per, unsigned blocks) {
     auto go = [&](auto kernel) { e = launch(kernel, dim3(blocks), kMoveThreads, 0, s, c.pool, kv_arrays(b), k, k_stride, v, v_stride, (unsigned)units); };
     constexpr int kHd = decltype(hd)::value, kKind = decltype(kind)::value, kUnits = decltype(per)::value;
     if (c.pool.weights != nullptr) go(kv_append_kernel<kHd, kKind, kUnits, true>);
@@ -227,7 +237,7 @@ cudaError_t launch_kv_gather(const litevggt_kv_cache& c, const litevggt_kv_batch
                              int* launches) {
   const long long units = b.rows * c.cfg.kv_heads;
   cudaError_t e = cudaSuccess;
-  by_kind(c, units, [&](auto hd, auto kind, auto per, unsigned blocks) {
+  by_kind<false>(c, units, [&](auto hd, auto kind, auto per, unsigned blocks) {
     e = launch(kv_gather_kernel<decltype(hd)::value, decltype(kind)::value, decltype(per)::value>, dim3(blocks), kMoveThreads, 0, s, c.pool,
                kv_arrays(b), k, v, (unsigned)units);
   });
