@@ -23,9 +23,10 @@
 //         the piece come again, and then they are taken out here and added to the rows that see them.
 //   E4M3  codes and exponents come by bulk copies into a ring of their own; the eight warps widen them to the same tiles,
 //         exactly, and look after V on the way.
+//   E2M1  the same, with a power of two for 32 channels.
 //
 // 2048 rows over 83,280 keys, 699 GFLOP: head dim 64 (16 heads) 786 us, 889 TFLOP/s; head dim 128 (8 heads) 630 us, 1110; over E4M3
-// 946 us and 780.  In bursts; under the 1 kW cap, which all of them reach, head dim 64 makes 750.  What bounds them (2048 rows over 10,410
+// 946 us and 780; two sequences of 1041 rows over 10,410 keys, 16 heads of 128, over E2M1 311 (issue slots 64 %, ALU 55 %).  In bursts; under the 1 kW cap, which all of them reach, head dim 64 makes 750.  What bounds them (2048 rows over 10,410
 // keys): head dim 64 the special-function unit, 67 % of it with set-up and all, beside 44 % of the issue slots and 43 % of the
 // tensor cores; head dim 128 nothing alone (tensor cores and special-function unit 52 %): a stream waits for its own products, and Q's
 // share of shared memory's bandwidth is taken twice a key tile; codes the issue slots (60 % and 58 %), at 72 registers a thread, of which

