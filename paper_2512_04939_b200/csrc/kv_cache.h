@@ -1,6 +1,7 @@
 // The objects behind the paged K/V cache's entry points, and what its kernels are launched with.
 #pragma once
 
+#include <atomic>
 #include <vector>
 
 #include "host_common.h"
@@ -80,7 +81,7 @@ struct litevggt_kv_batch {
   lv::KvWork few, tiles;       // sequences of few rows, and the others
   int few_rows;                // the most of the former
   lv::KvWeigh weigh;
-  mutable int pages_apart = -1;  // whether no page is named twice; -1: nobody has looked
+  mutable std::atomic<int> pages_apart{-1};  // whether no page is named twice; -1: nobody has looked (calls may do so at once)
   std::vector<uint8_t> image;  // what the device gets
   size_t bytes;                // of device memory
   size_t o_seqs, o_pages;

@@ -8,17 +8,18 @@ namespace {
 
 // Whether no page of the batch's list is named twice.  Looked up once: a batch's pages do not change.
 bool pages_apart(const litevggt_kv_cache& c, const litevggt_kv_batch& b) {
-  if (b.pages_apart < 0) {
+  int apart = b.pages_apart;
+  if (apart < 0) {
     std::vector<bool> seen((size_t)c.cfg.pages, false);
     const int* pages = kv_host_pages(b);
-    int apart = 1;
+    apart = 1;
     for (long long i = 0, n = kv_page_count(b, c.cfg.page_size); i < n && apart; ++i) {
       if (seen[(size_t)pages[i]]) apart = 0;
       seen[(size_t)pages[i]] = true;
     }
     b.pages_apart = apart;
   }
-  return b.pages_apart != 0;
+  return apart != 0;
 }
 
 bool pages_meet(const litevggt_kv_cache& c, const litevggt_kv_batch& a, const litevggt_kv_batch& b) {
