@@ -200,6 +200,18 @@ def test_more_items_than_ctas():
     weigh(Tallied([5000, 300, 4000, 17, 900], 4, 64, "bf16", 64, seed=26), [40, 300, 200, 17, 0], 8, causal_block=1)
 
 
+@pytest.mark.parametrize("head_dim,dtype", [(64, "bf16"), (64, "e2m1"), (128, "bf16"), (128, "e4m3")])
+def test_two_items_of_many_rows_for_a_cta(head_dim, dtype):
+    """More tiles of rows, one after the other and from item to item, than there is memory for at once; frames see their past only."""
+    scene = Tallied([8000], 5, head_dim, dtype, 64, seed=40)
+    batch, q, _, lse, start = weigh(scene, [600], 5, causal_block=150, decay=0.5)
+    once = scene.weights.clone()
+    for _ in range(3):
+        scene.weights.copy_(start)
+        scene.cache.weigh(batch, q.cuda(), lse, decay=0.5)
+        assert torch.equal(once, scene.weights)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows", [3, 30, 200])
 def test_rows_that_see_nothing_and_sequences_without_rows(dtype, rows):
