@@ -86,6 +86,9 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
   const int per_sm = kv_few_ctas(c->cfg.head_dim, c->cfg.dtype != LITEVGGT_KV_BF16);
   b->few = kv_cut(b->seqs, few, b->group, c->cfg.kv_heads, causal_block,
                   KvCut{kKvFewRows, kKvFewUnit, std::min(c->num_sms * per_sm, kKvFewWorkers), kKvFewLeast, INT32_MAX, kKvFewPiece});
+  long long keys = 0;
+  for (const KvPiece& p : b->few.pieces) keys += p.key1 - p.key0;
+  b->few_keys = b->few.pieces.empty() ? 0 : (int)(keys / (long long)b->few.pieces.size());
   // In units of 128 keys against 256 rows.  CTAs of one row tile take more time for the same work, but there are twice as many:
   // where the pieces are few it can be better to have them than to cut keys, since parts have to be joined.
   const double piece = c->cfg.head_dim == 64 ? kKvTilePiece64 : kKvTilePiece128;

@@ -26,8 +26,8 @@
 // other instructions; the ALU is 60 % busy): over 520,500 keys 201 us, 5.4 TB/s.  At head dim 128 nothing is over 30 % busy: two warps a
 // scheduler, each with one chain of waits, conversions, products and exponentials (16 tokens, 8 query heads a K/V head, 35 us).
 // Codes of 4 bits are half the bytes and about the same work, and it is the work that bounds them, issue slots and ALU: one token over
-// 520,500 keys 217 us, 2.6 TB/s (335 with a conversion for every pair; values and weights in f16, under a power of two of the warp's,
-// 209, but then keys of 2^-32 of the heaviest one's weight count as nothing where its code is zero).
+// 520,500 keys 204 us, 2.8 TB/s (335 with a conversion for every pair; values and weights in f16, under a power of two of the warp's,
+// 4 % less, but then keys of 2^-32 of the heaviest one's weight count as nothing where its code is zero).
 // (Straight from global memory into the fragments, without rings: 189, 307 and 404 us for the first three figures.  The scores by products of 8-bit operands, Q in two of them, which need no
 // conversion of K in the source: 202 -> 220 us, sixteen tokens that share heads by eight 32.9 -> 33.2.)  Few keys: 4.8 us for 262, of which the latency of three dependent loads and the
 // meeting of the parts are most.
@@ -72,6 +72,10 @@ constexpr float kFewAbove = 7.0f;
 // one comes to more than 2^15 (f16 ends at 2^16).
 constexpr int kFewWeight = 7, kFewMostShift = 118;
 constexpr float kFewMostWeight = 32768.0f;
+// E2M1, up to eight rows: where pieces have this many keys on average warps take 64 at a time (one token over 520,500 keys 218 -> 204 us, 48 sequences
+// of 8192 with heads of 128 channels 367 -> 348); shorter pieces do not go evenly into warps' turns of 64 (48 tokens over up to 4164: 70 us with 32,
+// 73 with 64; four drafts of two over 5000: 16.5, 17.5).
+constexpr int kFewLongPiece = 4096;
 __device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k + 127) << 23); }
 __device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }
 
@@ -81,7 +85,8 @@ __device__ __forceinline__ uint32_t lds4(uint32_t addr) {
   return v;
 }
 
-template <int kHd, int kKind, bool kHalf>
+// kLong: stages of 64 keys.
+template <int kHd, int kKind, bool kHalf, bool kLong = false>
 struct FewShape {
   static constexpr bool kNarrow = kKind == LITEVGGT_KV_E4M3, kFour = kKind == LITEVGGT_KV_E2M1;
   static constexpr bool kMoves = kHalf && !kFour;             // whether the accumulators' empty halves are left out of the registers
@@ -93,8 +98,8 @@ struct FewShape {
   // under 128 registers (sixteen tokens that share heads by eight: 36 us against 49).  Stages of 32 keys in 4 bits: at head dim 128 what
   // a stage costs beside its keys is as much again (48 sequences of 8192 keys: 442 us with 16, 367 with 32).
   static constexpr int kCtas = kKind != LITEVGGT_KV_BF16 && kHd == 64 ? 2 : 1;  // per SM
-  static constexpr int kSubs = kNarrow || kFour ? 2 : 128 / kHd;  // of 16 keys, of a stage
-  static constexpr int kStages = kFour ? 4 : kNarrow || (kHd == 128 && !kHalf) ? 2 : 3;
+  static constexpr int kSubs = kLong ? 4 : kNarrow || kFour ? 2 : 128 / kHd;  // of 16 keys, of a stage
+  static constexpr int kStages = kFour ? (kLong ? 2 : 4) : kNarrow || (kHd == 128 && !kHalf) ? 2 : 3;
   static constexpr int kRows = kHalf ? 8 : 16;
   static constexpr int kOutTiles = kHd / 8;
   static constexpr int kSubBytes = 16 * Row::kBytes;  // of K or V
@@ -107,11 +112,11 @@ struct FewShape {
 };
 
 // kHalf: at most eight rows, so the lower half of every row tile is empty and takes no registers.
-template <int kHd, int kKind, bool kHalf>
-__global__ void __launch_bounds__(kKvFewWarps * 32, FewShape<kHd, kKind, kHalf>::kCtas)
+template <int kHd, int kKind, bool kHalf, bool kLong>
+__global__ void __launch_bounds__(kKvFewWarps * 32, FewShape<kHd, kKind, kHalf, kLong>::kCtas)
 kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, KvPool pool, KvArrays arrays,
                    KvLaunch work, KvAttend at, uint32_t* status) {
-  using Shape = FewShape<kHd, kKind, kHalf>;
+  using Shape = FewShape<kHd, kKind, kHalf, kLong>;
   constexpr bool kNarrow = Shape::kNarrow, kFour = Shape::kFour;
   constexpr int kBlocks = Shape::kBlocks, kParts4 = Shape::kParts;
   constexpr int kRowBytes = Shape::Row::kBytes, kExps = Shape::Row::kExps;
@@ -139,7 +144,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   // The stage that is fetched next, and its piece; a lane's copy is one of K or V of 16 keys and 64 channels, or of the codes or
   // exponents of as many keys of the stage as lie in a page (every copy takes a dozen instructions, and codes are bound by them).  Its
   // page is looked up a stage ahead.
-  constexpr int kParts = kExps > 0 ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts, kStageShift = kSubs == 2 ? 5 : 4;
+  constexpr int kParts = kExps > 0 ? 2 : kHd / 64, kCopies = kSubs * 2 * kParts, kStageShift = kSubs == 4 ? 6 : kSubs == 2 ? 5 : 4;
   static_assert(kExps == 0 || 1 << kStageShift == kStageKeys, "");
   const int run_shift = kExps > 0 ? min(kStageShift, pool.page_shift) : 4;  // of a copy's keys
   const int my_part = lane % kParts, my_x = (lane / kParts) & 1, my_sub = lane / (2 * kParts);
@@ -679,11 +684,11 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
   }
 }
 
-template <int kHd, int kKind, bool kHalf>
+template <int kHd, int kKind, bool kHalf, bool kLong = false>
 cudaError_t start(const litevggt_kv_cache& c, const litevggt_kv_batch& b, const KvAttend& a, cudaStream_t s) {
-  using Shape = FewShape<kHd, kKind, kHalf>;
+  using Shape = FewShape<kHd, kKind, kHalf, kLong>;
   static_assert(Shape::kCtas * (Shape::kSmemBytes + 1024) <= 228 * 1024, "");
-  auto kernel = kv_attn_few_kernel<kHd, kKind, kHalf>;
+  auto kernel = kv_attn_few_kernel<kHd, kKind, kHalf, kLong>;
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = set_max_dynamic_smem_once(reinterpret_cast<const void*>(kernel), Shape::kSmemBytes, done);
   if (e != cudaSuccess) return e;
@@ -704,6 +709,12 @@ cudaError_t launch_kv_attn_few(const litevggt_kv_cache& c, const litevggt_kv_bat
   cudaError_t e;
   auto kinds = [&](auto kind) {
     constexpr int kKind = decltype(kind)::value;
+    if constexpr (kKind == LITEVGGT_KV_E2M1) {
+      if (half && b.few_keys >= kFewLongPiece) {
+        e = wide ? start<128, kKind, true, true>(c, b, a, s) : start<64, kKind, true, true>(c, b, a, s);
+        return;
+      }
+    }
     if (wide) e = half ? start<128, kKind, true>(c, b, a, s) : start<128, kKind, false>(c, b, a, s);
     else e = half ? start<64, kKind, true>(c, b, a, s) : start<64, kKind, false>(c, b, a, s);
   };

@@ -80,6 +80,7 @@ struct litevggt_kv_batch {
   std::vector<lv::KvSeq> seqs;
   lv::KvWork few, tiles;       // sequences of few rows, and the others
   int few_rows;                // the most of the former
+  int few_keys;                // of a piece of theirs, on average
   lv::KvWeigh weigh;
   mutable std::atomic<int> pages_apart{-1};  // whether no page is named twice; -1: nobody has looked (calls may do so at once)
   std::vector<uint8_t> image;  // what the device gets

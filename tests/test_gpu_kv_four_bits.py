@@ -77,6 +77,47 @@ class Four(Scene):
             assert over.max(initial=0.0) <= 1.0, f"sequence {i}: {over.max()} of the tolerance at {np.unravel_index(over.argmax(), over.shape)}"
 
 
+def exact_rows(n, head_dim, g):
+    """Rows that codes hold exactly: every block's largest magnitude is 6 times a power of two of its own, 2^-2 to 2^1."""
+    levels = torch.tensor(LEVELS, device="cuda")
+    x = levels[torch.randint(0, 8, (n, head_dim // 32, 32), generator=g, device="cuda")]
+    x[..., 0] = 6.0
+    x *= torch.randint(0, 2, x.shape, generator=g, device="cuda") * 2 - 1
+    return (x * torch.exp2(torch.randint(-2, 2, (n, head_dim // 32, 1), generator=g, device="cuda").double())).view(n, 1, head_dim)
+
+
+@pytest.mark.parametrize("head_dim,lengths", [(64, [640_000, 1, 650_003]), (128, [310_000, 33, 330_001])])
+@pytest.mark.parametrize("rows,page_size", [(1, 128), (3, 16), (8, 64)])
+def test_pieces_of_many_keys(head_dim, lengths, rows, page_size):
+    """So many keys that every CTA has thousands in a row."""
+    g = torch.Generator(device="cuda").manual_seed(41)
+    cache = pkg.KVCache.empty(sum(-(-n // page_size) for n in lengths), page_size, 1, head_dim, "e2m1")
+    ids, pages = torch.randperm(cache.pages).tolist(), []
+    for n in lengths:
+        pages.append(ids[:-(-n // page_size)])
+        ids = ids[len(pages[-1]):]
+    k, v = exact_rows(sum(lengths), head_dim, g), exact_rows(sum(lengths), head_dim, g)
+    cache.append(cache.batch(lengths, lengths, pages), k.bfloat16(), v.bfloat16())
+    q = (2.0 * torch.randn(3 * rows, 1, head_dim, generator=g, device="cuda")).bfloat16()
+    out, lse = cache.attend(cache.batch([rows] * 3, lengths, pages, causal_block=1), q, lse=True)
+    at = 0
+    for i, n in enumerate(lengths):
+        for row in range(rows):
+            sees = ref.seen(n, rows, 1, row)
+            got = out[i * rows + row, 0].double()
+            if sees == 0:
+                assert not got.any()
+                continue
+            kh, vh = k[at:at + sees, 0], v[at:at + sees, 0]
+            x = head_dim ** -0.5 * (kh @ q[i * rows + row, 0].double())
+            p = torch.softmax(x, 0)[:, None]
+            want = (p * vh).sum(0)
+            allowed = 1.01 * 2.0 ** -8 * ((p * (vh - want).abs()).sum(0) + want.abs()) + 2.0 ** -12 * (p * vh.abs()).sum(0)
+            assert ((got - want).abs() <= allowed).all(), f"sequence {i}, row {row}: {((got - want).abs() / allowed).max()} of the tolerance"
+            assert abs(lse[i * rows + row, 0].item() - x.logsumexp(0).item()) <= 2.0 ** -8 + 2.0 ** -22 * 100
+        at += n
+
+
 # ------------------------------------------------------------------ store, read back
 @pytest.mark.parametrize("head_dim,page_size,kv_heads", [(64, 16, 16), (64, 128, 1), (128, 32, 3), (128, 64, 8)])
 def test_stored_rows_read_back(head_dim, page_size, kv_heads):
