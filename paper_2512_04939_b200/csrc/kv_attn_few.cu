@@ -26,7 +26,7 @@
 // other instructions; the ALU is 60 % busy): over 520,500 keys 201 us, 5.4 TB/s.  At head dim 128 nothing is over 30 % busy: two warps a
 // scheduler, each with one chain of waits, conversions, products and exponentials (16 tokens, 8 query heads a K/V head, 35 us).
 // Codes of 4 bits are half the bytes and about the same work, and it is the work that bounds them, issue slots and ALU: one token over
-// 520,500 keys 204 us, 2.8 TB/s (335 with a conversion for every pair; values and weights in f16, under a power of two of the warp's,
+// 520,500 keys 197 us, 2.9 TB/s (335 with a conversion for every pair; values and weights in f16, under a power of two of the warp's,
 // 4 % less, but then keys of 2^-32 of the heaviest one's weight count as nothing where its code is zero).
 // (Straight from global memory into the fragments, without rings: 189, 307 and 404 us for the first three figures.  The scores by products of 8-bit operands, Q in two of them, which need no
 // conversion of K in the source: 202 -> 220 us, sixteen tokens that share heads by eight 32.9 -> 33.2.)  Few keys: 4.8 us for 262, of which the latency of three dependent loads and the
@@ -72,9 +72,9 @@ constexpr float kFewAbove = 7.0f;
 // one comes to more than 2^15 (f16 ends at 2^16).
 constexpr int kFewWeight = 7, kFewMostShift = 118;
 constexpr float kFewMostWeight = 32768.0f;
-// E2M1, up to eight rows: where pieces have this many keys on average warps take 64 at a time (one token over 520,500 keys 218 -> 204 us, 48 sequences
-// of 8192 with heads of 128 channels 367 -> 348); shorter pieces do not go evenly into warps' turns of 64 (48 tokens over up to 4164: 70 us with 32,
-// 73 with 64; four drafts of two over 5000: 16.5, 17.5).
+// E2M1, up to eight rows: where pieces have this many keys on average warps take 64 at a time (one token over 520,500 keys 210 -> 197 us, 48 sequences
+// of 8192 with heads of 128 channels 352 -> 320); shorter pieces do not go evenly into warps' turns of 64 (48 tokens over up to 4164: 67 us with 32,
+// 69 with 64; four drafts of two over 5000: 15.6, 17.4).
 constexpr int kFewLongPiece = 4096;
 __device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k + 127) << 23); }
 __device__ __forceinline__ int exponent_of(float x) { return (__float_as_int(x) >> 23) - 127; }
@@ -346,7 +346,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             most[e >> 1] = fmaxf(most[e >> 1], x);
           }
         }
-      if (__any_sync(0xffffffffu, most[0] > limit[0] || (!kHalf && most[1] > limit[1]))) {
+      if (__builtin_expect(__any_sync(0xffffffffu, most[0] > limit[0] || (!kHalf && most[1] > limit[1])), 0)) {
 #pragma unroll
         for (int half = 0; half < kHalves; ++half) {
           float m = most[half];
@@ -430,27 +430,32 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
             }
           }
       // output
+      constexpr int kLoads = kNarrow ? 1 : kHd / 64, kWords = kNarrow && kHd == 64 ? 2 : 4;
+      [[maybe_unused]] uint32_t v_bytes[kSubs][2];  // exponents of the operand's two halves, a key's in either half of a word
+      if constexpr (kFour) {
+        uint32_t apart = 0;
 #pragma unroll
-      for (int s = 0; s < kSubs; ++s) {
-        const int left = piece.key1 - (key + 16 * s);  // keys of the sub-step that the piece holds
-        const uint32_t at_sub = base + (kSubs + s) * Shape::kSubBytes;
-        constexpr int kLoads = kNarrow ? 1 : kHd / 64, kWords = kNarrow && kHd == 64 ? 2 : 4;
-        [[maybe_unused]] uint32_t v_bytes[2];  // exponents of the operand's two halves, a key's in either half of a word
-        if constexpr (kFour) {
+        for (int s = 0; s < kSubs; ++s) {
           const uint32_t at_exps = exps + ((kSubs + s) * 16 + 2 * q4) * kExps, block = g * kExps / 8;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if constexpr (kExps == 2) {
-              v_bytes[h] = __byte_perm(lds4(at_exps + 8 * h * kExps), 0u, 0x4240u + block * 0x101u);
+              v_bytes[s][h] = __byte_perm(lds4(at_exps + 8 * h * kExps), 0u, 0x4240u + block * 0x101u);
             } else {
               const uint2 x = lds8(at_exps + 8 * h * kExps);
-              v_bytes[h] = __byte_perm(x.x, x.y, 0x0400u + block * 0x101u) & 0x00ff00ffu;
+              v_bytes[s][h] = __byte_perm(x.x, x.y, 0x0400u + block * 0x101u) & 0x00ff00ffu;
             }
+            apart |= v_bytes[s][h] + 0x007f007fu;
           }
-          // Blocks whose factor is one bf16 number (and so none that are not finite): two keys' codes of a channel are widened together, into a
-          // pair of the operand.
-          if (!__any_sync(0xffffffffu, ((v_bytes[0] + 0x007f007fu | v_bytes[1] + 0x007f007fu) & 0x01000100u) != 0u)) {
-            const uint32_t factors[2] = {v_bytes[0] + 0x007e007eu << 7, v_bytes[1] + 0x007e007eu << 7};
+        }
+        // (One question for a stage, and what seldom happens out of the way: all that is in line here is too much for the instruction caches as it
+        // is, 204 -> 197 us.)  Blocks whose factor is one bf16 number (and so none that are not finite): two keys' codes of a channel are widened together, into a
+        // pair of the operand.
+        if (__builtin_expect(!__any_sync(0xffffffffu, (apart & 0x01000100u) != 0u), 1)) {
+#pragma unroll
+          for (int s = 0; s < kSubs; ++s) {
+            const uint32_t at_sub = base + (kSubs + s) * Shape::kSubBytes;
+            const uint32_t factors[2] = {v_bytes[s][0] + 0x007e007eu << 7, v_bytes[s][1] + 0x007e007eu << 7};
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
               uint32_t even[2][4], odd[2][4];  // of the even and the odd channels
@@ -468,9 +473,14 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
                 mma_16816<false>(c, p[s][0][0], kHalf ? 0u : p[s][0][kHalves - 1], p[s][1][0], kHalf ? 0u : p[s][1][kHalves - 1], b0, b1);
               }
             }
-            continue;
           }
+          return;
         }
+      }
+#pragma unroll
+      for (int s = 0; s < kSubs; ++s) {
+        const int left = piece.key1 - (key + 16 * s);  // keys of the sub-step that the piece holds
+        const uint32_t at_sub = base + (kSubs + s) * Shape::kSubBytes;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           uint32_t v[4][kWords];
@@ -478,7 +488,7 @@ kv_attn_few_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_const
           for (int e = 0; e < 4; ++e) {
             const int row = 2 * q4 + (e & 1) + 8 * (e >> 1);
             if constexpr (kFour) {
-              kv4_widen(lds4(at_sub + row * kRowBytes + g * (kRowBytes / 8) + 4 * i), v_bytes[e >> 1] >> 16 * (e & 1) & 0xffu, v[e]);
+              kv4_widen(lds4(at_sub + row * kRowBytes + g * (kRowBytes / 8) + 4 * i), v_bytes[s][e >> 1] >> 16 * (e & 1) & 0xffu, v[e]);
             } else if constexpr (kWords == 2) {
               const uint2 x = lds8(at_sub + row * 64 + g * 8);
               v[e][0] = x.x, v[e][1] = x.y;
