@@ -371,7 +371,11 @@ litevggt_status litevggt_kv_destroy(litevggt_kv_cache* cache);
  * that they only read).  q_heads: a multiple of kv_heads; query head h reads K/V head h / (q_heads / kv_heads).
  * causal_block = c > 0: row i of a sequence sees the tokens before its rows, and of its rows those of the blocks of c up
  * to i's own, so c = 1 is causal by tokens, c = tokens of a frame causal by frames; 0: all rows see all tokens.
+ * q_heads = LITEVGGT_KV_NO_QUERIES: a batch that stores, reads back or evicts, as source or target, and is refused by attend and weigh
+ * (LITEVGGT_ERR_SHAPE).  It holds its pages' numbers only; one with queries holds the plan of its attention too, and memory for parts of
+ * rows, which for many rows over as many tokens can be more than the tokens themselves.
  * *bytes receives the device memory that the batch needs. */
+#define LITEVGGT_KV_NO_QUERIES (-1)
 litevggt_status litevggt_kv_batch_create(const litevggt_kv_cache* cache, int32_t n_seq, const int32_t* rows, const int32_t* lengths,
                                          const int32_t* pages, int32_t q_heads, int32_t causal_block, litevggt_kv_batch** out,
                                          size_t* bytes);
@@ -416,7 +420,7 @@ litevggt_status litevggt_kv_weigh(litevggt_kv_cache* cache, const litevggt_kv_ba
  * those with the largest tallies, of equal ones the earlier (a NaN counts as less than any number).  They are copied, K, V, exponents and
  * tallies, to the pages of `into`, in the order that they were in; heads differ in which they keep.  `into` names the same number
  * of sequences, with as many rows as tokens, at most what `from` holds, and where it is less, at least first + last; its pages are
- * not those of `from`, which stay as they are, and name none twice (LITEVGGT_ERR_SHAPE).  kept: dev int32 [rows of into, kv_heads], where each
+ * not those of `from`, which stay as they are, and name none twice (LITEVGGT_ERR_SHAPE).  Neither batch needs queries.  kept: dev int32 [rows of into, kv_heads], where each
  * token was in its sequence. */
 litevggt_status litevggt_kv_evict(litevggt_kv_cache* cache, const litevggt_kv_batch* from, const litevggt_kv_batch* into, int32_t first,
                                   int32_t last, int32_t* kept, void* stream);

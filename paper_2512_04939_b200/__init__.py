@@ -18,6 +18,6 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
-from .kv_cache import KVBatch, KVCache  # noqa: E402,F401
+from .kv_cache import NO_QUERIES, KVBatch, KVCache  # noqa: E402,F401
 from .rotary import RotaryAxes  # noqa: E402,F401
 from .streaming import StreamingGlobalAttention  # noqa: E402,F401

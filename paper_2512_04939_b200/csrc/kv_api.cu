@@ -56,6 +56,8 @@ void lay_out(litevggt_kv_batch* b, const int32_t* pages, size_t n_pages, int hea
 litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int32_t* rows, const int32_t* lengths, const int32_t* pages,
                            int32_t q_heads, int32_t causal_block, litevggt_kv_batch* b) {
   long long row0 = 0, page0 = 0;
+  const bool queries = q_heads != LITEVGGT_KV_NO_QUERIES;
+  const long long heads = queries ? q_heads : c->cfg.kv_heads;
   b->rows_held = true;
   for (int i = 0; i < n_seq; ++i) {
     if (rows[i] < 0 || lengths[i] < 0 || lengths[i] > kKvLongest) return LITEVGGT_ERR_SHAPE;
@@ -63,7 +65,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
     b->seqs.push_back(KvSeq{(int)row0, rows[i], lengths[i], (int)page0});
     row0 += rows[i];
     page0 += ((long long)lengths[i] + c->cfg.page_size - 1) / c->cfg.page_size;
-    if (row0 * q_heads > INT32_MAX || page0 > INT32_MAX) return LITEVGGT_ERR_SHAPE;
+    if (row0 * heads > INT32_MAX || page0 > INT32_MAX) return LITEVGGT_ERR_SHAPE;
   }
   if (page0 > 0 && pages == nullptr) return LITEVGGT_ERR_NULL;
   for (long long i = 0; i < page0; ++i)
@@ -71,10 +73,14 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
   b->magic = kKvBatchMagic;
   b->owner_id = c->id;
   b->device = c->device;
-  b->q_heads = q_heads;
-  b->group = q_heads / c->cfg.kv_heads;
+  b->q_heads = queries ? q_heads : 0;
+  b->group = b->q_heads / c->cfg.kv_heads;
   b->causal_block = causal_block;
   b->rows = row0;
+  if (!queries) {  // nothing is cut, and no memory kept for parts of rows: 131,072 tokens of 16 heads of 64 would take 1.1 GB of it
+    lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
+    return LITEVGGT_OK;
+  }
   std::vector<int> few, many;
   int most = 0;
   for (int i = 0; i < n_seq; ++i) {
@@ -184,7 +190,8 @@ litevggt_status litevggt_kv_batch_create(const litevggt_kv_cache* cache, int32_t
                                          size_t* bytes) {
   if (!cache_ok(cache) || rows == nullptr || lengths == nullptr || out == nullptr || bytes == nullptr) return LITEVGGT_ERR_NULL;
   *out = nullptr;
-  if (n_seq < 1 || q_heads < 1 || q_heads % cache->cfg.kv_heads != 0 || causal_block < 0) return LITEVGGT_ERR_SHAPE;
+  if (n_seq < 1 || causal_block < 0) return LITEVGGT_ERR_SHAPE;
+  if (q_heads != LITEVGGT_KV_NO_QUERIES && (q_heads < 1 || q_heads % cache->cfg.kv_heads != 0)) return LITEVGGT_ERR_SHAPE;
   litevggt_kv_batch* b = new (std::nothrow) litevggt_kv_batch();
   if (b == nullptr) return LITEVGGT_ERR_ALLOC;
   litevggt_status st = LITEVGGT_ERR_ALLOC;
@@ -272,6 +279,7 @@ litevggt_status litevggt_kv_attend_lse(litevggt_kv_cache* cache, const litevggt_
                                        int64_t q_head_stride, float scale, void* out, float* lse, void* stream) {
   litevggt_status st = usable(cache, batch);
   if (st != LITEVGGT_OK) return st;
+  if (batch->q_heads == 0) return LITEVGGT_ERR_SHAPE;
   if (!(scale > 0.0f) || !(scale < 1e30f)) return LITEVGGT_ERR_SHAPE;
   if (batch->rows == 0) return LITEVGGT_OK;
   if (q == nullptr || out == nullptr) return LITEVGGT_ERR_NULL;

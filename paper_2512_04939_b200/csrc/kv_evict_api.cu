@@ -50,6 +50,7 @@ litevggt_status litevggt_kv_weigh(litevggt_kv_cache* cache, const litevggt_kv_ba
   litevggt_status st = usable(cache, batch);
   if (st != LITEVGGT_OK) return st;
   if (cache->pool.weights == nullptr) return LITEVGGT_ERR_NULL;
+  if (batch->q_heads == 0) return LITEVGGT_ERR_SHAPE;
   if (!(scale > 0.0f) || !(scale < 1e30f) || !(decay >= 0.0f) || !(decay <= 1.0f)) return LITEVGGT_ERR_SHAPE;
   if (batch->rows == 0) return LITEVGGT_OK;
   if (q == nullptr || lse == nullptr) return LITEVGGT_ERR_NULL;

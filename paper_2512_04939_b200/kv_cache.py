@@ -10,7 +10,7 @@ drew most when it has to make room:
 
     out, lse = cache.attend(batch, q, lse=True)
     cache.weigh(batch, q, lse)
-    into = cache.batch(rows=[20000], lengths=[20000], pages=[other_page_ids])
+    into = cache.batch(rows=[20000], lengths=[20000], pages=[other_page_ids], q_heads=NO_QUERIES)
     kept = cache.evict(batch, into, first=5, last=1041)                    # [20000, kv_heads]: which tokens these are now
 
 Which pages a sequence owns is the caller's business; the library checks that they exist - in the pool of the cache that plans the
@@ -26,6 +26,8 @@ import numpy as np
 import torch
 
 from .binding import KVConfig, _check, load_library
+
+NO_QUERIES = -1  # of a batch that is never attended with (LITEVGGT_KV_NO_QUERIES)
 
 # number in the C library, the pools' type, elements in one of it, elements that share an exponent (0: none does)
 _DTYPES = {"bf16": (0, torch.bfloat16, 1, 0), "e4m3": (1, torch.float8_e4m3fn, 1, -1), "e2m1": (2, torch.uint8, 2, 32)}
@@ -145,7 +147,9 @@ class KVCache:
     def batch(self, rows, lengths, pages, q_heads: int | None = None, causal_block: int = 0) -> KVBatch:
         """Plans a step: ``rows[i]`` rows of the packed tensors belong to sequence i, which holds ``lengths[i]`` tokens (those
         rows included, as its last) in the pages ``pages[i]`` (more than it needs may be named).  ``causal_block`` = c: a
-        row sees the tokens before its sequence's rows and the blocks of c rows up to its own; 0: all of them."""
+        row sees the tokens before its sequence's rows and the blocks of c rows up to its own; 0: all of them.  ``q_heads`` is that of
+        the cache unless given; ``NO_QUERIES`` makes a batch that only stores, reads back or evicts, and holds no more than its pages' numbers:
+        the plan of an attention of many rows takes memory of its own."""
         if len(rows) != len(lengths) or len(rows) != len(pages) or len(rows) == 0:
             raise ValueError(f"rows, lengths and pages name {len(rows)}, {len(lengths)} and {len(pages)} sequences")
         n_rows, n_tokens = _whole("rows", rows), _whole("lengths", lengths)
@@ -170,7 +174,7 @@ class KVCache:
         with torch.cuda.device(self.device):
             memory = torch.empty(n_bytes.value, dtype=torch.uint8, device=self.device)
         stream = self._stream()
-        made = KVBatch(self, handle, memory, int(n_rows.sum()), q_heads, stream)
+        made = KVBatch(self, handle, memory, int(n_rows.sum()), 0 if q_heads == NO_QUERIES else q_heads, stream)
         _check(self.lib.litevggt_kv_batch_place(handle, memory.data_ptr(), n_bytes.value, stream), "kv_batch_place")
         return made
 
@@ -226,7 +230,7 @@ class KVCache:
 
     def evict(self, batch: KVBatch, into: KVBatch, first: int = 0, last: int = 0) -> torch.Tensor:
         """Every head of every sequence of ``batch`` keeps as many tokens as ``into`` has for it (a batch of the same number of sequences,
-        with as many rows as tokens, in pages that ``batch`` does not name): its ``first`` first ones, its ``last`` last ones, and of the
+        with as many rows as tokens, in pages that ``batch`` does not name; ``NO_QUERIES`` will do): its ``first`` first ones, its ``last`` last ones, and of the
         others those with the largest tallies, of equal ones the earlier, a NaN being less than any number.  They move to the pages of ``into``
         in the order that they were in, tallies and all; the pages that they come from stay as they are.  Returns which tokens they were,
         int32 [into.rows, kv_heads]."""

@@ -9,7 +9,7 @@ from __future__ import annotations
 import torch
 
 from .binding import LiteVGGT
-from .kv_cache import KVCache
+from .kv_cache import NO_QUERIES, KVCache
 from .rotary import RotaryAxes
 
 
@@ -88,7 +88,8 @@ class StreamingGlobalAttention:
         if self.rotary is not None:
             self.rotary.rotate(positions, q, k, out=(q, k))
         if full:  # (the pages that are read are as they were, and the sequence's until the rows are stored)
-            kept = self.cache.evict(self.cache.batch([0], [self.length], [self.pages]), self.cache.batch([left], [left], [held]), self.first, self.recent)
+            source, target = self.cache.batch([0], [self.length], [self.pages]), self.cache.batch([left], [left], [held], NO_QUERIES)
+            kept = self.cache.evict(source, target, self.first, self.recent)
         batch = self.cache.batch([rows], [length], [pages], causal_block=frame_rows)
         self.cache.append(batch, k, v)
         self.pages, self.free, self.length, self.kept = pages, free, length, kept
