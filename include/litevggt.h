@@ -407,7 +407,8 @@ litevggt_status litevggt_kv_attend_lse(litevggt_kv_cache* cache, const litevggt_
 
 /* What a cached token has drawn of the attention so far decides what stays when a cache is full.  The tallies lie in a pool beside K and
  * V, weights: dev fp32 [pages, kv_heads, page_size], 16-byte aligned, which outlives the cache (NULL: none).  From then on
- * litevggt_kv_append sets those of the tokens that it writes to zero.  Not while calls with the cache are under way. */
+ * litevggt_kv_append sets those of the tokens that it writes to zero.  Batches that were planned before can be weighed as well, but keep
+ * their rows whole, which is slower where there are few keys.  Not while calls with the cache are under way. */
 litevggt_status litevggt_kv_track(litevggt_kv_cache* cache, float* weights);
 /* w[j] = decay w[j] + sum_i exp(scale q[i] . k[j] - lse[i]) for every token j of the batch's sequences that have rows, over the rows i
  * that see it and the query heads that share its head; what a token does not draw adds nothing, whatever the row holds.  lse: dev fp32

@@ -109,7 +109,7 @@ litevggt_status plan_batch(const litevggt_kv_cache* c, int32_t n_seq, const int3
     KvWork narrow = cut_tiles(kKvTileRows / 2, kKvHalfTiles);
     if (narrow.cost < b->tiles.cost) b->tiles = narrow;
   }
-  b->weigh = kv_weigh_plan(b->seqs, b->group, c->cfg.kv_heads, kKvFewRows, c->num_sms);
+  b->weigh = kv_weigh_plan(b->seqs, b->group, c->cfg.kv_heads, kKvFewRows, c->num_sms, c->pool.weights != nullptr);
   lay_out(b, pages, (size_t)page0, c->cfg.head_dim);
   return LITEVGGT_OK;
 }

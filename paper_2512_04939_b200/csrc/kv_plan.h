@@ -176,6 +176,8 @@ inline KvWork kv_cut(const std::vector<KvSeq>& seqs, const std::vector<int>& whi
 // How tallies are taken (litevggt_kv_weigh).  Sequences of few rows: units of 32 keys of one head, dealt out in runs.  The others: items
 // of `key_block` keys of one head, the rows that see them in `parts` runs of row tiles.  *_at: units or items of a head of all sequences
 // before the i-th.
+// `tallies`: whether the cache has any when the batch is planned.  Where they come later, rows are not cut: every batch would pay for what
+// hardly one needs (up to 128 trial cuts, and 0.6 MB for the parts' sums).
 struct KvWeigh {
   std::vector<long long> few_at, tiles_at;
   int key_block = 256, parts = 1;
@@ -184,7 +186,7 @@ struct KvWeigh {
 constexpr int kKvWeighUnit = 32;
 constexpr int kKvWeighRows = 128;  // of a row tile
 
-inline KvWeigh kv_weigh_plan(const std::vector<KvSeq>& seqs, int group, int kv_heads, int few_rows, int sms) {
+inline KvWeigh kv_weigh_plan(const std::vector<KvSeq>& seqs, int group, int kv_heads, int few_rows, int sms, bool tallies) {
   KvWeigh w;
   long long few = 0, blocks[2] = {0, 0}, row_tiles = 0;
   for (const KvSeq& q : seqs) {
@@ -203,7 +205,7 @@ inline KvWeigh kv_weigh_plan(const std::vector<KvSeq>& seqs, int group, int kv_h
   // whole rows, 21.7 in three parts; 2048 rows of eight heads each on 2 over 2048 176 whole, 29.5 in eight parts.)
   constexpr double kTile[2] = {1.25, 2.0}, kItem = 1.75, kMeet = 2.25;
   double least = 0.0;
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 2 && tallies; ++i)
     for (int parts = 1; parts <= 64 && parts <= std::max(row_tiles, 1ll) && (parts == 1 || blocks[i] * kv_heads * parts <= 4ll * sms); ++parts) {
       const double waves = (double)((blocks[i] * kv_heads * parts + sms - 1) / sms);
       const double cost = waves * (kTile[i] * (double)((row_tiles + parts - 1) / parts) + kItem + (parts > 1 ? kMeet : 0.0));
