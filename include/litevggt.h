@@ -413,7 +413,7 @@ litevggt_status litevggt_kv_track(litevggt_kv_cache* cache, float* weights);
 /* w[j] = decay w[j] + sum_i exp(scale q[i] . k[j] - lse[i]) for every token j of the batch's sequences that have rows, over the rows i
  * that see it and the query heads that share its head; what a token does not draw adds nothing, whatever the row holds.  lse: dev fp32
  * [rows, q_heads], from litevggt_kv_attend_lse on the same queries.  decay in [0, 1]; 0: the tallies begin anew, whatever they held.
- * Sums are in 32 bits, in an order that does not change from call to call.  LITEVGGT_ERR_NULL without tallies, LITEVGGT_ERR_SHAPE
+ * Sums are in 32 bits, in chains of 32 and of one for every 4,096 rows, in an order that does not change from call to call.  LITEVGGT_ERR_NULL without tallies, LITEVGGT_ERR_SHAPE
  * where sequences of the batch share pages. */
 litevggt_status litevggt_kv_weigh(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
                                   int64_t q_head_stride, float scale, const float* lse, float decay, void* stream);

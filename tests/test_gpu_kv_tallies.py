@@ -29,3 +29,24 @@ def test_tallies_that_come_after_the_batch(rows, length):
         cache.poll()
         got.append(weights.flatten()[:length].double())
     assert ((got[0] - got[1]).abs() <= 2.0 ** -18 * got[0]).all() and got[0].sum() > 3.9 * rows
+
+
+@pytest.mark.parametrize("head_dim,dtype", [(64, "bf16"), (128, "bf16"), (64, "e4m3"), (128, "e2m1")])
+def test_many_tiles_of_rows_in_turn(head_dim, dtype):
+    """256,000 rows a K/V head, 2000 tiles that one thread adds up.  Keys of zeros: every p is exp(-lse), in every head another one, so each
+    addition is rounded the same way.  Allowed are 2^-18 (1 + |lse|) of the sum.  The k-th addition of a chain is off by half a step, from 2^-24
+    of the k numbers' sum down to half of that, so n equal numbers by 3/4 n/2 2^-24 of theirs at most: chains of 32 rows, 32 tiles and 63 such sums
+    by 3/4 (16 + 16 + 32) 2^-24 = 3/4 2^-18; the exponential and its argument by 2^-22 + 2^-23 (1 + |lse|)."""
+    heads, rows, length = 16, 32_000, 4_752
+    cache = pkg.KVCache.empty(38, 128, heads, head_dim, dtype, weights=True)
+    nothing = torch.zeros(1, 1, head_dim, dtype=torch.bfloat16, device="cuda").expand(length, heads, head_dim)
+    cache.append(cache.batch([length], [length], [range(38)]), nothing, nothing)
+    batch = cache.batch([rows], [length], [range(38)], q_heads=8 * heads)
+    q = torch.randn(1, 1, head_dim, device="cuda").bfloat16().expand(rows, 8 * heads, head_dim)
+    lse = 0.03 + torch.arange(heads, device="cuda") / 16
+    cache.weigh(batch, q, lse.repeat_interleave(8).expand(rows, -1).contiguous(), decay=0.0)
+    cache.poll()
+    got = cache.weights.transpose(1, 2).reshape(-1, heads)[:length].double()
+    want = 8 * rows * torch.exp(-lse.double())
+    over = (got - want).abs() / (2.0 ** -18 * (1 + lse.double()) * want)
+    assert (got == got[0]).all() and over.max() <= 1.0, f"{over.max().item()} of the tolerance"
