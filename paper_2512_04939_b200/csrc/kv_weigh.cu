@@ -293,8 +293,10 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
 constexpr int kDrawWarps = 8, kRowWarps = 4;
 constexpr int kIssuer = kDrawWarps, kPlanner = kIssuer + 1, kRowFetcher = kPlanner + 1, kKeyFetcher = kRowFetcher + kRowWarps;
 // Items that are known ahead.  Rows of up to two of them wait for the next ones' to be asked for before they are handed over, so the
-// items behind those have to be known before they are done with.
+// items behind those have to be known before they are done with.  An item without rows (a part of few) hands over what waits, so that
+// is of the last two items at most, and what is drawn with is never further behind, whatever the items and however many a CTA has.
 constexpr int kRing = 4;
+static_assert(kRing > 2, "");
 // An item's part, as every role sees it.
 struct WeighUnit {
   KvSeq seq;
@@ -586,6 +588,11 @@ kv_weigh_tiles_kernel(const __grid_constant__ CUtensorMap k_map, KvPool pool, Kv
       ++given;
     };
     each_unit([&](const WeighUnit& u) {
+      if (u.tile0 >= u.tile1) {  // nothing of this item drives on what is under way, and the next item may never be known without that
+        cp_async_wait<0>();
+        while (given != count) hand_over();
+        return;
+      }
       const int rows = u.seq.rows * group;
       WeighRow mine(u.tile0 * kKvWeighRows + tid / kPerRow, group), info(u.tile0 * kKvWeighRows + tid, group);
       float ahead[kInfo];  // the next tile's

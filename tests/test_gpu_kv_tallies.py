@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2512_04939_b200 as pkg
+from test_gpu_kv_evict import Tallied, weigh
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +51,16 @@ def test_many_tiles_of_rows_in_turn(head_dim, dtype):
     want = 8 * rows * torch.exp(-lse.double())
     over = (got - want).abs() / (2.0 ** -18 * (1 + lse.double()) * want)
     assert (got == got[0]).all() and over.max() <= 1.0, f"{over.max().item()} of the tolerance"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3", "e2m1"])
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_sequences_of_few_rows_beside_one_of_many_leave_most_parts_empty(head_dim, dtype):
+    rows = [4000, 17, 20, 40, 30, 9]
+    scene = Tallied([300, 300, 280, 900, 500, 260], 4, head_dim, dtype, 32, seed=61)
+    batch, q, _, lse, start = weigh(scene, rows, 16, decay=0.5)
+    once = scene.weights.clone()
+    for _ in range(3):
+        scene.weights.copy_(start)
+        scene.cache.weigh(batch, q.cuda(), lse, decay=0.5)
+        assert torch.equal(once, scene.weights)

@@ -21,3 +21,16 @@ def test_a_cache_without_tallies_pays_for_none(host, rows, lengths, q_heads):
     # tallies that come later are taken all the same
     before = host.fake_weighs()
     assert host.litevggt_kv_track(cache, base.base.memory(64)) == OK and weigh(host, cache, b) == OK and host.fake_weighs() > before
+
+
+def test_sequences_of_few_rows_beside_one_of_many_leave_most_parts_empty(host):
+    """(The batch of the GPU test of the same name.)"""
+    rows, lengths = [4000, 17, 20, 40, 30, 9], [300, 300, 280, 900, 500, 260]
+    counts = [-(-n // 32) for n in lengths]
+    cache = base.base.cache_of(host, pages=sum(counts), page_size=32, kv_heads=4)
+    assert host.litevggt_kv_track(cache, base.base.memory(64)) == OK
+    p = plan(host, batch(host, cache, rows, lengths, np.arange(sum(counts)), 16))
+    tiles = [-(-4 * r // 128) for r in rows]
+    units = [4 * -(-n // p["block"]) * p["parts"] for n in lengths]
+    full = [4 * -(-n // p["block"]) * min(t, p["parts"]) for n, t in zip(lengths, tiles)]
+    assert p["parts"] > 2 and sum(units) > 148 and sum(full) < sum(units) / 2
