@@ -4,6 +4,9 @@
     q, k = rotary.rotate(positions, q, k)              # positions int32 [3, rows]; q, k [rows, heads, 64], slices of a projection will do
     grad_q, grad_k = rotary.rotate_back(positions, grad_q, grad_k)   # the gradient
 
+Nothing here enters an autograd graph: tensors that require a gradient are refused unless gradients are off (``torch.no_grad``, or inside the
+``forward`` and ``backward`` of a ``torch.autograd.Function``, which is where ``rotate`` and ``rotate_back`` belong in training).
+
 Shapes, types and devices are checked here, everything else in the C library.
 """
 from __future__ import annotations
@@ -70,11 +73,14 @@ class RotaryAxes:
     def _turn(self, positions, q, k, out, back):
         # (a small call takes as long as its checks do)
         if k is None:
-            given = (q,)
+            given, graph = (q,), q.requires_grad
             outs = (torch.empty_like(q),) if out is None else (out,)
         else:
-            given = (q, k)
+            given, graph = (q, k), q.requires_grad or k.requires_grad
             outs = (torch.empty_like(q), torch.empty_like(k)) if out is None else tuple(out)
+        if (graph or (out is not None and any(o.requires_grad for o in outs))) and torch.is_grad_enabled():
+            raise ValueError("rotations are not recorded by autograd, and their gradient would be lost: call them under torch.no_grad() or in "
+                             "a torch.autograd.Function, with rotate_back for the gradients, or detach the tensors")
         kind, rows, index = _DTYPES.get(q.dtype), q.shape[0] if q.dim() == 3 else -1, self._index
         fine = (kind is not None and len(outs) == len(given) and positions.shape == (self._axes, rows) and positions.dtype == torch.int32
                 and positions.get_device() == index)
