@@ -94,19 +94,25 @@ struct RotarySpan {
   uintptr_t begin;
   unsigned long long row, head, rows, heads, bytes;  // strides and counts; bytes of a head's row
   unsigned long long of_row() const { return (heads - 1) * head + bytes; }
+  unsigned long long of_head() const { return (rows - 1) * row + bytes; }
   unsigned long long of_all() const { return (rows - 1) * row + of_row(); }
 };
 inline bool rotary_same(const RotarySpan& a, const RotarySpan& b) {
   return a.begin == b.begin && (a.row == b.row || a.rows == 1) && (a.head == b.head || a.heads == 1) && a.rows == b.rows && a.heads == b.heads;
 }
-// May answer yes for tensors that interleave in ways other than as columns of one matrix.
+// Pieces of `of_a` bytes and of `of_b` bytes, one of each in every `period`: whether they are apart.
+inline bool rotary_alternate(uintptr_t a, unsigned long long of_a, uintptr_t b, unsigned long long of_b, unsigned long long period) {
+  if (of_a > period || of_b > period) return false;
+  const unsigned long long ahead = b >= a ? (b - a) % period : (period - (a - b) % period) % period;
+  return ahead >= of_a && ahead + of_b <= period;
+}
+// May answer yes for tensors that interleave in ways other than as columns of one matrix, row by row or head by head.
 inline bool rotary_may_meet(const RotarySpan& a, const RotarySpan& b) {
   if (a.begin + a.of_all() <= b.begin || b.begin + b.of_all() <= a.begin) return false;
-  if (a.rows > 1 && b.rows > 1 && a.row == b.row && a.of_row() <= a.row && b.of_row() <= b.row) {
-    const unsigned long long ahead = b.begin >= a.begin ? (b.begin - a.begin) % a.row : (a.row - (a.begin - b.begin) % a.row) % a.row;
-    return ahead < a.of_row() || ahead + b.of_row() > a.row;
-  }
-  return true;
+  if (a.rows > 1 && b.rows > 1 && a.row == b.row && rotary_alternate(a.begin, a.of_row(), b.begin, b.of_row(), a.row)) return false;
+  const unsigned long long head = a.heads > 1 ? a.head : b.head;
+  const bool heads = (a.heads > 1 || b.heads > 1) && (a.heads == 1 || a.head == head) && (b.heads == 1 || b.head == head);
+  return !(heads && rotary_alternate(a.begin, a.of_head(), b.begin, b.of_head(), head));
 }
 // Whether no two elements of it lie on one another.
 inline bool rotary_apart(const RotarySpan& a) {
