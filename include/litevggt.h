@@ -401,7 +401,8 @@ litevggt_status litevggt_kv_attend(litevggt_kv_cache* cache, const litevggt_kv_b
                                    int64_t q_head_stride, float scale, void* out, void* stream);
 /* The same, and lse[i] = log sum_j exp(scale q[i] . k[j]) over the tokens that row i sees: dev fp32 [rows, q_heads], in memory of its own, or
  * NULL; minus infinity for a row that sees none.  It is that of the sum that the output was divided by, whose terms are rounded to bf16 where
- * rows see many tokens: off by less than 2^-8 and 2^-22 of itself, and by far less where many tokens share a row's weight. */
+ * rows see many tokens: off by less than 2^-8, and by far less where many tokens share a row's weight; and by 2^-20 of |lse| + the row's largest
+ * scale sum_c |q_c k_c| for the scores, whose terms may cancel. */
 litevggt_status litevggt_kv_attend_lse(litevggt_kv_cache* cache, const litevggt_kv_batch* batch, const void* q, int64_t q_row_stride,
                                        int64_t q_head_stride, float scale, void* out, float* lse, void* stream);
 

@@ -3,7 +3,8 @@ import pytest
 import torch
 
 import paper_2512_04939_b200 as pkg
-from test_gpu_kv_evict import Tallied, weigh
+from test_gpu_kv_cache import f64
+from test_gpu_kv_evict import Tallied, check_lse, weigh
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +65,16 @@ def test_sequences_of_few_rows_beside_one_of_many_leave_most_parts_empty(head_di
         scene.weights.copy_(start)
         scene.cache.weigh(batch, q.cuda(), lse, decay=0.5)
         assert torch.equal(once, scene.weights)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3", "e2m1"])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_log_sums_of_scores_whose_terms_cancel(dtype, rows):
+    """Products of 2^11 times the score: the bound that include/litevggt.h states, with the scores' own term."""
+    scene = Tallied([500], 1, 64, dtype, 64, seed=62)
+    scene.k_new[..., 32:] = scene.k_new[..., :32]
+    scene.store()
+    q = 48.0 * torch.randn(rows, 1, 64, generator=scene.g).bfloat16()
+    q[..., 32:] = -q[..., :32] + (q[..., :32] * 2.0 ** -7 * torch.randint(-1, 2, (rows, 1, 32), generator=scene.g)).bfloat16()
+    lse = scene.cache.attend(scene.cache.batch([rows], [500], scene.pages), q.cuda(), lse=True)[1]
+    check_lse(scene, [rows], q, f64(lse), 0, 0.125)
