@@ -4,7 +4,7 @@ import torch
 
 import paper_2512_04939_b200 as pkg
 from test_gpu_kv_cache import f64
-from test_gpu_kv_evict import Tallied, check_lse, weigh
+from test_gpu_kv_evict import Tallied, check_lse, evict, scene_of, weigh
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +78,30 @@ def test_log_sums_of_scores_whose_terms_cancel(dtype, rows):
     q[..., 32:] = -q[..., :32] + (q[..., :32] * 2.0 ** -7 * torch.randint(-1, 2, (rows, 1, 32), generator=scene.g)).bfloat16()
     lse = scene.cache.attend(scene.cache.batch([rows], [500], scene.pages), q.cuda(), lse=True)[1]
     check_lse(scene, [rows], q, f64(lse), 0, 0.125)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3", "e2m1"])
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("rows,q_heads", [([1, 1, 1, 1, 1, 0, 1], 12), ([1, 3, 2, 1, 1, 0, 8], 24)])
+def test_warps_that_take_several_units_of_few_rows(head_dim, dtype, rows, q_heads):
+    """More units of 32 keys than there are warps on the chip, three to five for each: runs that go over from keys to keys, from head to head and
+    from sequence to sequence, some of which have no units; at most eight rows of a head, and more."""
+    scene = Tallied([9000, 33, 0, 5000, 1, 250, 64], 12, head_dim, dtype, 64, seed=63)
+    batch, q, _, lse, start = weigh(scene, rows, q_heads, causal_block=1, decay=0.5)
+    once = scene.weights.clone()
+    scene.weights.copy_(start)
+    scene.cache.weigh(batch, q.cuda(), lse, decay=0.5)
+    assert torch.equal(once, scene.weights)
+
+
+@pytest.mark.parametrize("lengths,kv_heads", [([513], 4), ([700], 2), ([2000], 3), ([4096], 4), ([600, 5000, 513, 20000, 40] * 8, 8)])
+def test_many_equal_tallies_in_one_block(lengths, kv_heads):
+    """Tallies that nobody has taken, and others of which more are alike than are compared with one another."""
+    scene = scene_of(lengths, kv_heads, 64, "bf16", 64, sum(-(-n // 64) for n in lengths), 64)
+    keep = [n // 2 for n in lengths]
+    for values in ([0.0], [0.0, 1.0], [3.0, 3.0, 3.0, 0.5, 7.0], [1.0, 1.0 + 2.0 ** -23, 1.0 + 2.0 ** -13, -1.0, float("nan")]):
+        choice = torch.randint(0, len(values), scene.weights.shape, device="cuda")
+        scene.weights.copy_(torch.tensor(values, device="cuda")[choice])
+        evict(scene, keep, 3, 4)
+    evict(scene, [n - 1 for n in lengths])
+    evict(scene, [1 for _ in lengths])
