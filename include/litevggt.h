@@ -468,7 +468,8 @@ litevggt_status litevggt_rotary_create(const litevggt_rotary_config* cfg, int de
 litevggt_status litevggt_rotary_destroy(litevggt_rotary* rotary);
 /* Turns one or two tensors of the same rows and type (queries and keys) in one launch.  positions: dev int32, element (axis, row) at
  * axis * axis_stride + row * row_stride, of any sign.  back != 0: by the negative angles, which is the gradient (from the gradient of the
- * output to that of the input).  Accesses are as wide as addresses, strides and sections allow, 16 bytes at most; elements must be
+ * output to that of the input).  Accesses are as wide as addresses, strides and sections allow, 16 bytes at most (HALVES: as many channels as
+ * divide every half section, so that sections of 24 make 8 bytes in 16-bit types); elements must be
  * aligned to their size (LITEVGGT_ERR_ALIGN). */
 litevggt_status litevggt_rotary_apply(const litevggt_rotary* rotary, const int32_t* positions, int64_t axis_stride, int64_t row_stride,
                                       int64_t rows, int32_t dtype, int32_t back, const litevggt_rotary_tensor* tensors, int32_t n_tensors,

@@ -73,7 +73,7 @@ constexpr float kFewAbove = 7.0f;
 constexpr int kFewWeight = 7, kFewMostShift = 118;
 constexpr float kFewMostWeight = 32768.0f;
 // E2M1, up to eight rows: where pieces have this many keys on average warps take 64 at a time (one token over 520,500 keys 210 -> 197 us, 48 sequences
-// of 8192 with heads of 128 channels 352 -> 320); shorter pieces do not go evenly into warps' turns of 64 (48 tokens over up to 4164: 67 us with 32,
+// of 8192 with heads of 128 channels 352 -> 320); shorter pieces do not go evenly into warps' turns of 64 (48 tokens of 16 heads of 64 over up to 4164: 67 us with 32,
 // 69 with 64; four drafts of two over 5000: 15.6, 17.4).
 constexpr int kFewLongPiece = 4096;
 __device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k + 127) << 23); }

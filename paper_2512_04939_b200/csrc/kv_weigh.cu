@@ -6,7 +6,8 @@
 //
 // Few rows are bound by K's bytes: 16 tokens of 32 heads on 4 over up to 8,328 keys of 128 channels in 8 bits (45 MB) 13 us where the codes
 // are still in L2 and 17 where they come from memory, by the latency of a unit's loads (18.6 us before units were fetched two ahead and codes
-// became f16 operands); one token over 262 4.5 us.  Chunks are bound by exponentials, see there.
+// became f16 operands); one token over 262 4.5 us; one over 520,500 in bf16 182 us, 6.0 TB/s, and 219 where the tallies that are there are read as
+// well (a decay other than zero).  Chunks are bound by exponentials, see there.
 #include "exp2.cuh"
 #include "kv_cache.h"
 #include "kv_mma.cuh"
@@ -287,7 +288,7 @@ kv_weigh_few_kernel(KvPool pool, KvArrays arrays, KvWeighing in, WeighLists list
 // with what the exponentials need of a row, its log-sum-exp and how many keys it sees; and one
 // finds out what the CTA's items are, 32 at a time and ahead of all others: the divisions and searches of that, thousands of clocks in a
 // row, were half of the time of short items.
-// 4164 rows over 41,640 keys, 16 heads of 64: 806 us, 3.3 10^12 exponentials a second, four fifths of what the unit gives at the clock held
+// 4164 rows over 41,640 keys, 16 heads of 64: 798 us, 3.3 10^12 exponentials a second, four fifths of what the unit gives at the clock held
 // (1.76 GHz).  Tried and left: an eighth and a quarter of the exponentials on the FMA pipes (816, 850: the two warps of a scheduler wait for one
 // another's results longer than they gain), sixteen warps with half of the rows each (7 % slower).
 constexpr int kDrawWarps = 8, kRowWarps = 4;

@@ -10,7 +10,9 @@
 // rounding at the end.
 //
 // 83,280 rows, queries and keys of 16 heads of 64 in bf16: 110 us, 6.2 TB/s (a copy makes 6.46), at 67 % of the issue slots; 10,992 rows of 32 and
-// 8 heads of 128 in fp32 72 us, 6.2.  One row: 2.9 us.  (One load under way at a time 115 and 79 us, two 111 and 78.  A plane's
+// 8 heads of 128 in fp32 72 us, 6.2.  One row: 2.9 us.  That is of axes whose planes come in eights side by side; `halves` of sections (16, 24, 24)
+// come in fours, in accesses of 8 bytes: 133 us, 5.1 TB/s, and 137 in place in the columns of a projection (sections (16, 16, 32) 111 either way);
+// `pairs` 123.  (One load under way at a time 115 and 79 us, two 111 and 78.  A plane's
 // frequency from the launch's parameters instead of a table in memory 150: lanes that ask for different words of those wait in turn.)
 #include <cuda_fp16.h>
 
